@@ -363,6 +363,136 @@ ad_status ad_anchordraft_loss(const ad_model* draft, const ad_cross* cross, int3
                               void* stream);
 
 /*
+ * Training the draft block: what carries the objective's gradients (ad_anchordraft_loss:
+ * dL/dlogits, dL/dfeat, dL/dxq) back through LayerNorm, the projections and the
+ * feed-forward sublayer x + W2 GELU(W1 LN(x) + b1) + b2 of the decoder's blocks (paper,
+ * section "Correction and Cost", paragraph "AnchorDraft Training Objective").  These entry
+ * points take matrices, not a model, and follow the conventions above; nothing on the
+ * device is checked (there is no index to check), and NaN and infinities propagate.
+ * Sums run in a fixed order: the same call gives the same bits.
+ *
+ * A matrix is `rows` rows of `cols` elements, row r starting at element r * ld of data,
+ * which is aligned to its element size.  ld >= cols (the rows of an output do not overlap);
+ * elements between cols and ld are not read and not written.  Sizes: 0 <= rows <= 2^24,
+ * 1 <= cols <= 2^20, ld <= 2^22 (AD_ERANGE otherwise).  With rows = 0 the per-row arguments
+ * may be NULL.  Any alignment and any odd size is taken; matrices whose data is 16-byte
+ * aligned and whose ld and cols are multiples of 8 are the fast ones.
+ */
+typedef struct {
+  void* data;       /* device                                                          */
+  int64_t ld;       /* elements from one row to the next                               */
+  int32_t dtype;    /* ad_dtype                                                        */
+} ad_mat;
+
+/*
+ * An activation kept in 8 bits (a checkpoint) of a [rows][cols] matrix.  32 consecutive
+ * columns of a row (the last group of a row may be shorter) share one scale 2^(s - 127),
+ * s the smallest byte >= 1 with max |v| <= 127 * 2^(s - 127); a value is q * 2^(s - 127)
+ * with q = v / 2^(s - 127) rounded to the nearest integer, ties to even.  So the error is at
+ * most half a step, 2^(s - 128) <= max |v| / 127, and every value is exact in bf16: products
+ * read checkpoints without a further rounding.  A group that holds a NaN or an infinity
+ * has s = 255 and reads as NaN throughout.  Rows are padded to ad_ckpt_ld(cols) = cols
+ * rounded up to 128: q is [rows][ld], scale [rows][ld / 32]; padding is written as q = 0,
+ * s = 1.  q is 16-byte aligned and scale 4-byte aligned (AD_EINVAL otherwise).
+ */
+typedef struct {
+  int8_t* q;        /* device [rows][ad_ckpt_ld(cols)]                                 */
+  uint8_t* scale;   /* device [rows][ad_ckpt_ld(cols) / 32]                            */
+} ad_ckpt;
+
+/* Activations of the products below: none, or the decoder's GELU(h) = h Phi(h). */
+typedef enum { AD_ACT_NONE = 0, AD_ACT_GELU = 1 } ad_act;
+
+int32_t ad_ckpt_ld(int32_t cols);
+/* ckpt <- x (float32 or bf16), and out <- act(value of ckpt) (float32, or bf16 with one
+ * rounding).  Errors: AD_EINVAL, AD_ERANGE, AD_EHIP. */
+ad_status ad_ckpt_pack(int32_t rows, int32_t cols, const ad_mat* x, const ad_ckpt* ckpt, void* stream);
+ad_status ad_ckpt_unpack(int32_t rows, int32_t cols, const ad_ckpt* ckpt, int32_t act, const ad_mat* out,
+                         void* stream);
+
+/*
+ * LayerNorm over each row's cols values (the decoder's: biased variance, eps 1e-5):
+ *   xhat = (x - mean) rstd,  rstd = 1 / sqrt(var + eps),  y = xhat gain + bias
+ * x float32 or bf16; gain, bias: device [cols] of param_dtype; y float32 or bf16 (one
+ * rounding).  Optional outputs for the backward pass: mean, rstd [rows] float32, and xhat,
+ * the normalised rows before gain and bias in 8 bits.  y may be x when their types and ld
+ * are the same.  Statistics are float32, in two passes over registers.
+ * Errors: AD_EINVAL (NULL argument, bad dtype, misaligned data, ld < cols), AD_ERANGE,
+ * AD_EUNSUPPORTED (cols > 8192), AD_EHIP.
+ */
+ad_status ad_layer_norm(int32_t rows, int32_t cols, const ad_mat* x, const void* gain, const void* bias,
+                        int32_t param_dtype, const ad_mat* y, float* mean, float* rstd, const ad_ckpt* xhat,
+                        void* stream);
+
+/*
+ * Its backward pass.  With dxhat = dy gain and means over a row's columns,
+ *   dx = rstd (dxhat - mean(dxhat) - xhat mean(dxhat xhat)) + dres,
+ *   dgain = sum over rows of dy xhat,  dbias = sum over rows of dy.
+ * xhat comes from the checkpoint (x and mean are then NULL) or from x (float32 or bf16) and
+ * mean, and rstd is the forward pass's.  dy float32 or bf16; dres (optional, float32 or
+ * bf16) is the gradient that reaches x past the LayerNorm, as the residual path's does; dx
+ * float32 or bf16; dx_copy (optional) a bf16 copy of dx, the operand of the next product.
+ * dx may be dres or dy when their types and ld are the same.  dgain and dbias (float32
+ * [cols], both or neither) are written, or with accumulate != 0 added to.
+ * workspace: device, >= ad_layer_norm_backward_workspace_size() bytes, 256-byte aligned;
+ * its content between calls does not matter.
+ * Errors: as ad_layer_norm; AD_ENOSPACE.
+ */
+ad_status ad_layer_norm_backward_workspace_size(int32_t rows, int32_t cols, size_t* bytes);
+ad_status ad_layer_norm_backward(int32_t rows, int32_t cols, const ad_mat* dy, const ad_mat* x, const float* mean,
+                                 const float* rstd, const ad_ckpt* xhat, const void* gain, int32_t param_dtype,
+                                 const ad_mat* dres, const ad_mat* dx, const ad_mat* dx_copy, float* dgain,
+                                 float* dbias, int32_t accumulate, void* workspace, size_t workspace_bytes,
+                                 void* stream);
+
+/*
+ * A projection with its epilogue:
+ *   h = x w^T + bias,  y = act(h) + residual
+ * x bf16 [rows][k], w bf16 [n][k] (as the model stores its matrices), bias (optional) device
+ * [n] of bias_dtype, residual (optional) [rows][n] float32 or bf16, y [rows][n] float32 or
+ * bf16.  Products accumulate in float32; bias, activation and residual are applied to the
+ * float32 sum, which is rounded once.  Optional outputs for the backward pass: pre, h in bf16,
+ * or pre_ckpt, h in 8 bits.  y may be residual when their types and ld are the same.
+ * workspace as above, of ad_linear_workspace_size() bytes (may be 0: then it may be NULL).
+ * Errors: AD_EINVAL (NULL argument, bad dtype or act, misaligned data, ld too small),
+ * AD_ERANGE, AD_ENOSPACE, AD_EUNSUPPORTED (a float32 x or w), AD_EHIP.
+ */
+ad_status ad_linear_workspace_size(int32_t rows, int32_t n, int32_t k, size_t* bytes);
+ad_status ad_linear(int32_t rows, int32_t n, int32_t k, const ad_mat* x, const ad_mat* w, const void* bias,
+                    int32_t bias_dtype, int32_t act, const ad_mat* residual, const ad_mat* y, const ad_mat* pre,
+                    const ad_ckpt* pre_ckpt, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The projection's gradient for its input, through the activation that made the input:
+ *   dx = (dy w) act'(pre)
+ * dy bf16 [rows][n], w bf16 [n][k], dx [rows][k] float32 or bf16.  With act = AD_ACT_GELU, pre
+ * (bf16 [rows][k]) or pre_ckpt (8 bits) is the value that GELU was applied to, and act_out
+ * (optional, bf16 [rows][k]) receives GELU(pre) again: the down-projection's input, which its
+ * weight gradient reads, need not be kept.  With AD_ACT_NONE all three are NULL.
+ * workspace and errors as for ad_linear.
+ */
+ad_status ad_linear_dgrad_workspace_size(int32_t rows, int32_t n, int32_t k, size_t* bytes);
+ad_status ad_linear_dgrad(int32_t rows, int32_t n, int32_t k, const ad_mat* dy, const ad_mat* w, int32_t act,
+                          const ad_mat* pre, const ad_ckpt* pre_ckpt, const ad_mat* dx, const ad_mat* act_out,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The projection's gradients for its weight and bias:
+ *   dw = dy^T x,  dbias = sum over rows of dy
+ * dy bf16 [rows][n]; x bf16 [rows][k], or x_ckpt in 8 bits (the other NULL).  With gain and
+ * shift (device [k] of param_dtype, both or neither; x_ckpt only) the input is gain x + shift,
+ * the LayerNorm output whose normalised rows x_ckpt holds: dw = (dy^T x) gain + dbias shift^T,
+ * so that output need not be kept either.  dw float32 [n][k]; dbias (optional) float32 [n].
+ * Both are written, or with accumulate != 0 added to.  rows = 0 gives zeros.
+ * workspace and errors as for ad_linear.
+ */
+ad_status ad_linear_wgrad_workspace_size(int32_t rows, int32_t n, int32_t k, size_t* bytes);
+ad_status ad_linear_wgrad(int32_t rows, int32_t n, int32_t k, const ad_mat* dy, const ad_mat* x,
+                          const ad_ckpt* x_ckpt, const void* gain, const void* shift, int32_t param_dtype,
+                          const ad_mat* dw, float* dbias, int32_t accumulate, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+/*
  * Next draft block from linear draft heads on the final hidden state.  For sequence b
  * take the LN_f output h at row row0_b + a_b (row0_b = first row of b in `layout`),
  * d_i = argmax(W_i h) (float32 logits, lowest index on ties), i = 1..n_heads, and write

@@ -21,6 +21,8 @@ AD_ERR_TREE = 32
 STATUS = {0: "AD_OK", -1: "AD_EINVAL", -2: "AD_ERANGE", -3: "AD_ENOSPACE", -4: "AD_EHIP",
           -5: "AD_EUNSUPPORTED"}
 
+ACT_NONE, ACT_GELU = 0, 1
+
 _i32 = ctypes.c_int32
 _ptr = ctypes.c_void_p
 _size = ctypes.c_size_t
@@ -52,10 +54,19 @@ class Step(ctypes.Structure):
                 ("out_xq", _ptr)]
 
 
+class Mat(ctypes.Structure):
+    _fields_ = [("data", _ptr), ("ld", ctypes.c_int64), ("dtype", _i32)]
+
+
+class CkptView(ctypes.Structure):
+    _fields_ = [("q", _ptr), ("scale", _ptr)]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is not built; run paper_2608_12703_amd.build.build()")
     lib = ctypes.CDLL(LIB_PATH)
+    _mat, _ckpt = ctypes.POINTER(Mat), ctypes.POINTER(CkptView)
     sig = {
         "ad_last_error": (ctypes.c_char_p, []),
         "ad_model_param_count": (_i32, [ctypes.POINTER(ModelDesc)]),
@@ -83,6 +94,22 @@ def _load():
                                   _ptr, _i32, _ptr, _ptr, _i32, _ptr, _ptr, _ptr, _i32, _ptr, _ptr,
                                   _ptr, _size, _ptr]),
         "ad_kv_export": (_i32, [_ptr, ctypes.POINTER(KV), _i32, _ptr, _i32, _ptr, _ptr]),
+        "ad_ckpt_ld": (_i32, [_i32]),
+        "ad_ckpt_pack": (_i32, [_i32, _i32, _mat, _ckpt, _ptr]),
+        "ad_ckpt_unpack": (_i32, [_i32, _i32, _ckpt, _i32, _mat, _ptr]),
+        "ad_layer_norm": (_i32, [_i32, _i32, _mat, _ptr, _ptr, _i32, _mat, _ptr, _ptr, _ckpt, _ptr]),
+        "ad_layer_norm_backward_workspace_size": (_i32, [_i32, _i32, ctypes.POINTER(_size)]),
+        "ad_layer_norm_backward": (_i32, [_i32, _i32, _mat, _mat, _ptr, _ptr, _ckpt, _ptr, _i32, _mat, _mat,
+                                          _mat, _ptr, _ptr, _i32, _ptr, _size, _ptr]),
+        "ad_linear_workspace_size": (_i32, [_i32, _i32, _i32, ctypes.POINTER(_size)]),
+        "ad_linear": (_i32, [_i32, _i32, _i32, _mat, _mat, _ptr, _i32, _i32, _mat, _mat, _mat, _ckpt, _ptr,
+                             _size, _ptr]),
+        "ad_linear_dgrad_workspace_size": (_i32, [_i32, _i32, _i32, ctypes.POINTER(_size)]),
+        "ad_linear_dgrad": (_i32, [_i32, _i32, _i32, _mat, _mat, _i32, _mat, _ckpt, _mat, _mat, _ptr, _size,
+                                   _ptr]),
+        "ad_linear_wgrad_workspace_size": (_i32, [_i32, _i32, _i32, ctypes.POINTER(_size)]),
+        "ad_linear_wgrad": (_i32, [_i32, _i32, _i32, _mat, _mat, _ckpt, _ptr, _ptr, _i32, _mat, _ptr, _i32,
+                                   _ptr, _size, _ptr]),
         "ad_profile_enable": (_i32, [_ptr, _i32, _i32]),
         "ad_profile_read": (_i32, [_ptr, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(_i32)]),
     }
@@ -100,6 +127,10 @@ EXPORTS = ("ad_last_error", "ad_model_param_count", "ad_model_create", "ad_model
            "ad_draft_heads_workspace_size", "ad_draft_heads", "ad_kv_import", "ad_kv_export",
            "ad_draft_input_workspace_size", "ad_draft_input",
            "ad_anchordraft_loss_workspace_size", "ad_anchordraft_loss",
+           "ad_ckpt_ld", "ad_ckpt_pack", "ad_ckpt_unpack", "ad_layer_norm",
+           "ad_layer_norm_backward_workspace_size", "ad_layer_norm_backward",
+           "ad_linear_workspace_size", "ad_linear", "ad_linear_dgrad_workspace_size", "ad_linear_dgrad",
+           "ad_linear_wgrad_workspace_size", "ad_linear_wgrad",
            "ad_profile_enable", "ad_profile_read")
 PROF_CROSS_ATTN, PROF_SELF_ATTN, PROF_GEMM, PROF_LM_HEAD, PROF_XQ_CROSS, PROF_XQ, PROF_ANCHOR = 1, 2, 3, 4, 5, 6, 7
 
@@ -256,6 +287,185 @@ def draft_input(model: Model, w_fuse, b_fuse, w_in, b_in, batch: int, taps, hidd
                              ptr(anchor), ptr(enc_len), half_window, ptr(window), ptr(out),
                              ptr(workspace), workspace.numel(), stream_handle(stream)),
           "ad_draft_input")
+
+
+# ------------------------------------------------------------------ training operators
+# Tensors carry their own shapes here, so the binding checks what the C-ABI cannot see: that
+# they agree with each other, lie on the current device and have their columns side by side.
+
+_DTYPE = {torch.float32: AD_F32, torch.bfloat16: AD_BF16}
+
+
+def _on_device(name: str, t):
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, not on the current GPU")
+
+
+def _mat(name: str, t, rows: int, cols: int):
+    """A [rows][cols] float32 or bf16 tensor with adjacent columns as an ad_mat (None for None)."""
+    if t is None:
+        return None
+    _on_device(name, t)
+    if tuple(t.shape) != (rows, cols):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(rows, cols)}")
+    if t.dtype not in _DTYPE:
+        raise ValueError(f"{name} is {t.dtype}, expected float32 or bfloat16")
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: the columns of a row must be adjacent")
+    return ctypes.byref(Mat(t.data_ptr(), cols if rows <= 1 else t.stride(0), _DTYPE[t.dtype]))
+
+
+def _vec(name: str, t, n: int, dtypes=(torch.float32, torch.bfloat16)):
+    """The address of a contiguous [n] tensor (None for None)."""
+    if t is None:
+        return None
+    _on_device(name, t)
+    if tuple(t.shape) != (n,) or t.dtype not in dtypes or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous [{n}] tensor of {' or '.join(map(str, dtypes))}")
+    return t.data_ptr()
+
+
+def _floats(name: str, t, n: int):
+    return _vec(name, t, n, (torch.float32,))
+
+
+def _params(a_name: str, a, b_name: str, b, n: int):
+    """Two parameter vectors of one dtype: their addresses and that dtype."""
+    if a is not None and b is not None and a.dtype != b.dtype:
+        raise ValueError(f"{a_name} and {b_name} must have the same dtype")
+    return _vec(a_name, a, n), _vec(b_name, b, n), AD_F32 if a is None else _DTYPE[a.dtype]
+
+
+def _space(workspace):
+    if workspace is None:
+        return None, 0
+    _on_device("workspace", workspace)
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+class Ckpt:
+    """An activation of `cols` columns kept in 8 bits (ad.h: ad_ckpt): q int8 [rows][ld] and
+    scale uint8 [rows][ld / 32], ld = cols rounded up to 128."""
+
+    def __init__(self, q, scale, cols: int):
+        ld = LIB.ad_ckpt_ld(cols)
+        rows = q.shape[0]
+        for name, t, dtype, width in (("q", q, torch.int8, ld), ("scale", scale, torch.uint8, ld // 32)):
+            if tuple(t.shape) != (rows, width) or t.dtype != dtype or not t.is_contiguous() or not ld:
+                raise ValueError(f"a checkpoint's {name} must be a contiguous [{rows}][{width}] {dtype} tensor")
+        self.q, self.scale, self.rows, self.cols = q, scale, rows, cols
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, device="cuda"):
+        ld = LIB.ad_ckpt_ld(cols)
+        return cls(torch.empty(rows, ld, dtype=torch.int8, device=device),
+                   torch.empty(rows, ld // 32, dtype=torch.uint8, device=device), cols)
+
+
+def _ckpt(name: str, k, rows: int, cols: int):
+    if k is None:
+        return None
+    _on_device(name, k.q)
+    _on_device(name, k.scale)
+    if (k.rows, k.cols) != (rows, cols):
+        raise ValueError(f"{name} holds {(k.rows, k.cols)}, expected {(rows, cols)}")
+    return ctypes.byref(CkptView(k.q.data_ptr(), k.scale.data_ptr()))
+
+
+def ckpt_pack(x, ckpt: Ckpt, stream=None):
+    """ckpt <- the rows of x in 8 bits."""
+    rows, cols = ckpt.rows, ckpt.cols
+    check(LIB.ad_ckpt_pack(rows, cols, _mat("x", x, rows, cols), _ckpt("ckpt", ckpt, rows, cols),
+                           stream_handle(stream)), "ad_ckpt_pack")
+
+
+def ckpt_unpack(ckpt: Ckpt, out, act: int = ACT_NONE, stream=None):
+    """out <- act(the values of ckpt)."""
+    rows, cols = ckpt.rows, ckpt.cols
+    check(LIB.ad_ckpt_unpack(rows, cols, _ckpt("ckpt", ckpt, rows, cols), act, _mat("out", out, rows, cols),
+                             stream_handle(stream)), "ad_ckpt_unpack")
+
+
+def layer_norm(x, gain, bias, y, mean=None, rstd=None, xhat: Ckpt | None = None, stream=None):
+    """LayerNorm of the rows of x into y (ad.h: ad_layer_norm); mean, rstd and xhat (the
+    normalised rows in 8 bits) are kept for the backward pass when given."""
+    rows, cols = x.shape
+    g, b, dt = _params("gain", gain, "bias", bias, cols)
+    check(LIB.ad_layer_norm(rows, cols, _mat("x", x, rows, cols), g, b, dt, _mat("y", y, rows, cols),
+                            _floats("mean", mean, rows), _floats("rstd", rstd, rows),
+                            _ckpt("xhat", xhat, rows, cols), stream_handle(stream)), "ad_layer_norm")
+
+
+def _workspace_size(name: str, *sizes) -> int:
+    n = _size()
+    check(getattr(LIB, name)(*sizes, ctypes.byref(n)), name)
+    return n.value
+
+
+def layer_norm_backward_workspace_size(rows: int, cols: int) -> int:
+    return _workspace_size("ad_layer_norm_backward_workspace_size", rows, cols)
+
+
+def layer_norm_backward(dy, x, mean, rstd, xhat, gain, dres, dx, dx_copy, dgain, dbias, workspace,
+                        accumulate: bool = False, stream=None):
+    """LayerNorm's gradients (ad.h: ad_layer_norm_backward) from x and mean, or from the
+    checkpoint xhat (x and mean None); dres, dx_copy and the pair dgain, dbias may be None."""
+    rows, cols = dy.shape
+    ws, ws_bytes = _space(workspace)
+    g, _, dt = _params("gain", gain, "gain", None, cols)
+    check(LIB.ad_layer_norm_backward(
+        rows, cols, _mat("dy", dy, rows, cols), _mat("x", x, rows, cols), _floats("mean", mean, rows),
+        _floats("rstd", rstd, rows), _ckpt("xhat", xhat, rows, cols), g, dt, _mat("dres", dres, rows, cols),
+        _mat("dx", dx, rows, cols), _mat("dx_copy", dx_copy, rows, cols), _floats("dgain", dgain, cols),
+        _floats("dbias", dbias, cols), int(accumulate), ws, ws_bytes, stream_handle(stream)),
+        "ad_layer_norm_backward")
+
+
+def linear_workspace_size(rows: int, n: int, k: int) -> int:
+    return _workspace_size("ad_linear_workspace_size", rows, n, k)
+
+
+def linear(x, w, bias, act: int, residual, y, pre, pre_ckpt, workspace, stream=None):
+    """y = act(x w^T + bias) + residual (ad.h: ad_linear); bias, residual and the kept
+    pre-activation (pre in bf16, or pre_ckpt in 8 bits) may be None."""
+    (rows, k), n = x.shape, w.shape[0]
+    ws, ws_bytes = _space(workspace)
+    b, _, dt = _params("bias", bias, "bias", None, n)
+    check(LIB.ad_linear(rows, n, k, _mat("x", x, rows, k), _mat("w", w, n, k), b, dt, act,
+                        _mat("residual", residual, rows, n), _mat("y", y, rows, n), _mat("pre", pre, rows, n),
+                        _ckpt("pre_ckpt", pre_ckpt, rows, n), ws, ws_bytes, stream_handle(stream)), "ad_linear")
+
+
+def linear_dgrad_workspace_size(rows: int, n: int, k: int) -> int:
+    return _workspace_size("ad_linear_dgrad_workspace_size", rows, n, k)
+
+
+def linear_dgrad(dy, w, act: int, pre, pre_ckpt, dx, act_out, workspace, stream=None):
+    """dx = (dy w) act'(pre) (ad.h: ad_linear_dgrad); act_out, when given, receives act(pre)."""
+    (rows, n), k = dy.shape, w.shape[1]
+    ws, ws_bytes = _space(workspace)
+    check(LIB.ad_linear_dgrad(rows, n, k, _mat("dy", dy, rows, n), _mat("w", w, n, k), act,
+                              _mat("pre", pre, rows, k), _ckpt("pre_ckpt", pre_ckpt, rows, k),
+                              _mat("dx", dx, rows, k), _mat("act_out", act_out, rows, k), ws, ws_bytes,
+                              stream_handle(stream)), "ad_linear_dgrad")
+
+
+def linear_wgrad_workspace_size(rows: int, n: int, k: int) -> int:
+    return _workspace_size("ad_linear_wgrad_workspace_size", rows, n, k)
+
+
+def linear_wgrad(dy, x, x_ckpt, gain, shift, dw, dbias, workspace, accumulate: bool = False, stream=None):
+    """dw = dy^T x and dbias = the column sums of dy (ad.h: ad_linear_wgrad), x in bf16 or as the
+    checkpoint x_ckpt, of which gain and shift make the input; dbias may be None."""
+    (rows, n), k = dy.shape, dw.shape[1]
+    ws, ws_bytes = _space(workspace)
+    g, s, dt = _params("gain", gain, "shift", shift, k)
+    check(LIB.ad_linear_wgrad(rows, n, k, _mat("dy", dy, rows, n), _mat("x", x, rows, k),
+                              _ckpt("x_ckpt", x_ckpt, rows, k), g, s, dt, _mat("dw", dw, n, k),
+                              _floats("dbias", dbias, n), int(accumulate), ws, ws_bytes, stream_handle(stream)),
+          "ad_linear_wgrad")
 
 
 def kv_import(model: Model, kv: KV, b: int, src, n: int, err_flag, stream=None):

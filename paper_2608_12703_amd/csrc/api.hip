@@ -9,6 +9,7 @@
 #include "../../include/ad.h"
 #include "common.h"
 #include "launch.h"
+#include "status.h"
 
 struct ad_model {
   ad_model_desc desc;
@@ -21,14 +22,27 @@ struct ad_model {
   int prof_used = 0;
 };
 
-namespace {
+static thread_local std::string g_err = "";
 
-thread_local std::string g_err = "";
+namespace ad {
 
 ad_status fail(ad_status s, const std::string& msg) {
   g_err = msg;
   return s;
 }
+
+ad_status check_hip(const char* where) {
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return fail(AD_EHIP, std::string(where) + ": " + hipGetErrorString(e));
+  return AD_OK;
+}
+
+}  // namespace ad
+
+namespace {
+
+using ad::check_hip;
+using ad::fail;
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
@@ -144,12 +158,6 @@ Workspace carve(const ad_model_desc& d, int M, int B, int k_max, char* base) {
   }
   w.bytes = off;
   return w;
-}
-
-ad_status check_hip(const char* where) {
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return fail(AD_EHIP, std::string(where) + ": " + hipGetErrorString(e));
-  return AD_OK;
 }
 
 // Brackets one kernel launch with a profiling event pair when that class is enabled.

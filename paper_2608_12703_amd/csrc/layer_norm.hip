@@ -1,0 +1,290 @@
+// LayerNorm forward and backward, and 8-bit activation checkpoints.
+//
+// All of these stream rows once; the floor is HBM traffic.  A lane holds 8 consecutive columns
+// at a time (16 bytes of bf16), a wave 512, so rows of up to 2048 columns live in one wave's
+// registers (J = 1 .. 4 pieces a lane) and need no LDS for their sums; wider rows, up to 8192
+// columns, are spread over the four waves of a workgroup.
+#include <algorithm>
+
+#include "train.h"
+#include "top2.h"
+
+namespace ad {
+
+namespace {
+
+constexpr float kEps = 1e-5f;
+
+// Sum over the wave: rotations inside 16-lane rows, then the row swaps (no LDS round trip).
+__device__ __forceinline__ float wave_total(float v) {
+  v += __int_as_float(ror16<8>(__float_as_int(v)));
+  v += __int_as_float(ror16<4>(__float_as_int(v)));
+  v += __int_as_float(ror16<2>(__float_as_int(v)));
+  v += __int_as_float(ror16<1>(__float_as_int(v)));
+  return rows4_sum(v);
+}
+
+// Sum over the lanes that share a row: the wave, or the workgroup's four waves.
+template <int W>
+__device__ __forceinline__ float row_total(float v, float* red) {
+  v = wave_total(v);
+  if constexpr (W == 4) {
+    __syncthreads();
+    if (threadIdx.x % kWave == 0) red[threadIdx.x / kWave] = v;
+    __syncthreads();
+    v = (red[0] + red[1]) + (red[2] + red[3]);
+  }
+  return v;
+}
+
+__device__ __forceinline__ void load_vec8(const DVec& g, int c, int cols, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? ld_vec(g, c + i) : 0.f;
+}
+
+// W: waves per row (1 or 4).  The statistics are two passes over the registers: the mean,
+// then the squared deviations from it (no cancellation of large means).
+template <int J, int W>
+__global__ void __launch_bounds__(256) ln_fwd_kernel(LnFwdArgs a) {
+  __shared__ float red[4];
+  const int t = W == 1 ? threadIdx.x % kWave : threadIdx.x;
+  const int first = W == 1 ? blockIdx.x * 4 + threadIdx.x / kWave : blockIdx.x, stride = W == 1 ? gridDim.x * 4 : gridDim.x;
+  constexpr int kStep = 8 * kWave * W;
+  // (with W == 4 every wave of the workgroup has the same rows, so the barriers are met by all)
+  for (int row = first; row < a.rows; row += stride) {
+    float x[J][8];
+#pragma unroll
+    for (int j = 0; j < J; ++j) load8(a.x, row, 8 * t + j * kStep, a.cols, x[j]);
+    float s = 0.f;
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s += x[j][i];
+    const float mean = row_total<W>(s, red) / (float)a.cols;
+    float v = 0.f;
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        x[j][i] -= mean;
+        if (8 * t + j * kStep + i < a.cols) v = fmaf(x[j][i], x[j][i], v);
+      }
+    const float rstd = 1.0f / sqrtf(row_total<W>(v, red) / (float)a.cols + kEps);
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const int c = 8 * t + j * kStep;
+      float g[8], b[8], y[8];
+      load_vec8(a.gain, c, a.cols, g);
+      load_vec8(a.bias, c, a.cols, b);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        x[j][i] = c + i < a.cols ? x[j][i] * rstd : 0.f;
+        y[i] = fmaf(x[j][i], g[i], b[i]);
+      }
+      store8(a.y, row, c, a.cols, y);
+      if (a.xhat.q) ckpt_store8(a.xhat, row, c, x[j]);
+    }
+    if (t == 0) {
+      if (a.mean) a.mean[row] = mean;
+      if (a.rstd) a.rstd[row] = rstd;
+    }
+  }
+}
+
+// A workgroup walks rows g, g + G, ... and keeps the sums for dgain and dbias of its columns
+// in registers; they leave once, as one of G partial rows.  The order of the sums depends
+// on the number of rows and columns only.
+template <int J, int W>
+__global__ void __launch_bounds__(256) ln_bwd_kernel(LnBwdArgs a) {
+  __shared__ float red[4];
+  constexpr int kStep = 8 * kWave * W;
+  const int w = threadIdx.x / kWave, t = W == 1 ? threadIdx.x % kWave : threadIdx.x;
+  const int first = W == 1 ? blockIdx.x * 4 + w : blockIdx.x, stride = W == 1 ? gridDim.x * 4 : gridDim.x;
+  float g[J][8], dg[J][8], db[J][8];
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    load_vec8(a.gain, 8 * t + j * kStep, a.cols, g[j]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) dg[j][i] = db[j][i] = 0.f;
+  }
+  const float inv_n = 1.0f / (float)a.cols;
+  for (int row = first; row < a.rows; row += stride) {
+    float xh[J][8], dy[J][8];
+#pragma unroll
+    for (int j = 0; j < J; ++j) load8(a.dy, row, 8 * t + j * kStep, a.cols, dy[j]);
+    const float rstd = a.rstd[row];
+    if (a.xhat.q) {
+#pragma unroll
+      for (int j = 0; j < J; ++j) ckpt_load8(a.xhat, row, 8 * t + j * kStep, xh[j]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < J; ++j) load8(a.x, row, 8 * t + j * kStep, a.cols, xh[j]);
+      const float mean = a.mean[row];
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) xh[j][i] = (xh[j][i] - mean) * rstd;
+    }
+    float s = 0.f, sx = 0.f;
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        // (a column past the last has dy = 0 and gain 0, and its xhat is not used)
+        const bool in = 8 * t + j * kStep + i < a.cols;
+        xh[j][i] = in ? xh[j][i] : 0.f;
+        dg[j][i] = fmaf(dy[j][i], xh[j][i], dg[j][i]);
+        db[j][i] += dy[j][i];
+        dy[j][i] *= g[j][i];
+        s += dy[j][i];
+        sx = fmaf(dy[j][i], xh[j][i], sx);
+      }
+    const float m = row_total<W>(s, red) * inv_n, mx = row_total<W>(sx, red) * inv_n;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const int c = 8 * t + j * kStep;
+      float d[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) d[i] = rstd * (dy[j][i] - m - xh[j][i] * mx);
+      if (a.dres.p) {
+        float r[8];
+        load8(a.dres, row, c, a.cols, r);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[i] += r[i];
+      }
+      store8(a.dx, row, c, a.cols, d);
+      if (a.copy.p) store8(a.copy, row, c, a.cols, d);
+    }
+  }
+  if (!a.dgain) return;
+  float* part = a.part + (size_t)blockIdx.x * 2 * a.cols;
+  if constexpr (W == 4) {
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int c = 8 * t + j * kStep + i;
+        if (c < a.cols) { part[c] = dg[j][i]; part[a.cols + c] = db[j][i]; }
+      }
+  } else {
+    // the four waves hold the same columns: they add in turn
+    __shared__ float sum[2][J * kStep];
+    for (int v = 0; v < 4; ++v) {
+      if (w == v) {
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int c = 8 * t + j * kStep + i;
+            sum[0][c] = v ? sum[0][c] + dg[j][i] : dg[j][i];
+            sum[1][c] = v ? sum[1][c] + db[j][i] : db[j][i];
+          }
+      }
+      __syncthreads();
+    }
+    for (int c = threadIdx.x; c < a.cols; c += 256) {
+      part[c] = sum[0][c];
+      part[a.cols + c] = sum[1][c];
+    }
+  }
+}
+
+// dgain | dbias: column c of [groups][2 cols] partial rows, 16 columns x 16 row slices a
+// workgroup, the slices joined in order.
+__global__ void __launch_bounds__(256) ln_param_kernel(int groups, int cols, const float* part, float* dgain,
+                                                       float* dbias, int accumulate) {
+  __shared__ float red[16][17];
+  const int x = threadIdx.x % 16, y = threadIdx.x / 16, c = blockIdx.x * 16 + x;
+  float s = 0.f;
+  if (c < 2 * cols)
+    for (int r = y; r < groups; r += 16) s += part[(size_t)r * 2 * cols + c];
+  red[y][x] = s;
+  __syncthreads();
+  if (y == 0 && c < 2 * cols) {
+    for (int r = 1; r < 16; ++r) s += red[r][x];
+    float* o = c < cols ? dgain + c : dbias + (c - cols);
+    *o = accumulate ? *o + s : s;
+  }
+}
+
+// A wave takes 512 columns of one row at a time (unit u: row u / segs, segment u % segs; the
+// launcher's caller has checked rows * segs < 2^31).
+__global__ void __launch_bounds__(256) ckpt_pack_kernel(unsigned units, unsigned segs, int cols, DMat x, DCkpt k) {
+  for (unsigned u = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + threadIdx.x / kWave); u < units; u += gridDim.x * 4) {
+    const int c = (int)(u % segs) * 512 + 8 * (threadIdx.x % kWave);
+    float v[8];
+    load8(x, u / segs, c, cols, v);
+    ckpt_store8(k, u / segs, c, v);
+  }
+}
+
+template <bool GELU>
+__global__ void __launch_bounds__(256) ckpt_unpack_kernel(unsigned units, unsigned segs, int cols, DCkpt k, DMat out) {
+  for (unsigned u = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + threadIdx.x / kWave); u < units; u += gridDim.x * 4) {
+    const int c = (int)(u % segs) * 512 + 8 * (threadIdx.x % kWave);
+    float v[8];
+    ckpt_load8(k, u / segs, c, v);
+    if (GELU)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = gelu_value(v[i]);
+    store8(out, u / segs, c, cols, v);
+  }
+}
+
+constexpr int kMaxGrid = 1 << 22;   // workgroups of 256 threads that a launch may have
+int grid_of(int64_t groups) { return (int)std::min<int64_t>(groups, kMaxGrid); }
+
+// J pieces of 8 columns a lane, one wave a row up to 2048 columns, else four
+template <template <int, int> class F, class... A>
+void by_width(int cols, A&&... args) {
+  if (cols <= 512) F<1, 1>::run(args...);
+  else if (cols <= 1024) F<2, 1>::run(args...);
+  else if (cols <= 1536) F<3, 1>::run(args...);
+  else if (cols <= 2048) F<4, 1>::run(args...);
+  else if (cols <= 4096) F<2, 4>::run(args...);
+  else F<4, 4>::run(args...);
+}
+
+template <int J, int W>
+struct Fwd {
+  static void run(const LnFwdArgs& a, hipStream_t st) {
+    ln_fwd_kernel<J, W><<<grid_of(W == 1 ? (a.rows + 3) / 4 : a.rows), 256, 0, st>>>(a);
+  }
+};
+template <int J, int W>
+struct Bwd {
+  static void run(const LnBwdArgs& a, int groups, hipStream_t st) { ln_bwd_kernel<J, W><<<groups, 256, 0, st>>>(a); }
+};
+
+}  // namespace
+
+void launch_layer_norm(const LnFwdArgs& a, hipStream_t st) {
+  if (a.rows > 0) by_width<Fwd>(a.cols, a, st);
+}
+
+int ln_bwd_groups(int rows, int cols) {
+  const int per = cols <= 2048 ? 4 : 1;   // rows a workgroup holds at a time
+  return std::min((rows + per - 1) / per, 512);
+}
+
+void launch_layer_norm_backward(const LnBwdArgs& a, hipStream_t st) {
+  const int groups = ln_bwd_groups(a.rows, a.cols);
+  if (groups > 0) by_width<Bwd>(a.cols, a, groups, st);
+  if (a.dgain)
+    ln_param_kernel<<<(2 * a.cols + 15) / 16, 256, 0, st>>>(groups, a.cols, a.part, a.dgain, a.dbias, a.accumulate);
+}
+
+void launch_ckpt_pack(int rows, int cols, const DMat& x, const DCkpt& k, hipStream_t st) {
+  const unsigned segs = (k.ld + 511) / 512, units = (unsigned)rows * segs;
+  if (units) ckpt_pack_kernel<<<grid_of((units + 3ull) / 4), 256, 0, st>>>(units, segs, cols, x, k);
+}
+
+void launch_ckpt_unpack(int rows, int cols, const DCkpt& k, bool gelu, const DMat& out, hipStream_t st) {
+  const unsigned segs = (k.ld + 511) / 512, units = (unsigned)rows * segs;
+  if (!units) return;
+  const int grid = grid_of((units + 3ull) / 4);
+  if (gelu) ckpt_unpack_kernel<true><<<grid, 256, 0, st>>>(units, segs, cols, k, out);
+  else ckpt_unpack_kernel<false><<<grid, 256, 0, st>>>(units, segs, cols, k, out);
+}
+
+}  // namespace ad

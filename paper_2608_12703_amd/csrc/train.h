@@ -1,0 +1,278 @@
+// Shared by the kernels of the draft block's training operators: typed strided matrices,
+// 8-bit checkpoints, GELU and its derivative, launcher declarations.
+#pragma once
+
+#include "common.h"
+
+namespace ad {
+
+// A matrix of float32 or bf16 rows.  vec: 8 columns at a multiple of 8 are whole and 16-byte
+// aligned; vec4: 4 columns at a multiple of 4 are aligned to the size of four elements.
+struct DMat {
+  void* p;
+  int64_t ld;
+  int bf16, vec, vec4;
+};
+
+// A vector of parameters (LayerNorm gain, bias): float32 or bf16.
+struct DVec {
+  const void* p;
+  int bf16;
+};
+__device__ __forceinline__ float ld_vec(const DVec& v, int i) {
+  return v.bf16 ? bf16_to_f32(((const uint16_t*)v.p)[i]) : ((const float*)v.p)[i];
+}
+
+// 8-bit checkpoint rows: q [rows][ld], scale [rows][ld / 32], ld a multiple of 128.
+struct DCkpt {
+  int8_t* q;
+  uint8_t* scale;
+  int ld;
+};
+constexpr int kCkptGroup = 32;
+inline int ckpt_ld(int cols) { return (cols + 127) / 128 * 128; }
+
+// Largest launch of a plain 1-D grid used here: the launchers check against it.
+constexpr int kLnMaxCols = 8192;
+
+// ----------------------------------------------------------------- elements
+
+// Columns c .. c + 7 of a row (columns from `cols` on read as 0).
+__device__ __forceinline__ void load8(const DMat& m, size_t row, int c, int cols, float (&v)[8]) {
+  if (m.bf16) {
+    const uint16_t* p = (const uint16_t*)m.p + row * m.ld + c;
+    if (m.vec) {
+      const uint4 u = c < cols ? *(const uint4*)p : uint4{0, 0, 0, 0};
+      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? bf16_to_f32(p[i]) : 0.f;
+    }
+  } else {
+    const float* p = (const float*)m.p + row * m.ld + c;
+    if (m.vec) {
+      const float4 z = {0.f, 0.f, 0.f, 0.f};
+      const float4 a = c < cols ? *(const float4*)p : z, b = c < cols ? *(const float4*)(p + 4) : z;
+      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+      v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? p[i] : 0.f;
+    }
+  }
+}
+
+__device__ __forceinline__ void store8(const DMat& m, size_t row, int c, int cols, const float (&v)[8]) {
+  if (m.bf16) {
+    uint16_t* p = (uint16_t*)m.p + row * m.ld + c;
+    if (m.vec) {
+      if (c < cols)
+        *(uint4*)p = uint4{f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]),
+                           f32x2_to_bf16x2(v[4], v[5]), f32x2_to_bf16x2(v[6], v[7])};
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (c + i < cols) p[i] = f32_to_bf16(v[i]);
+    }
+  } else {
+    float* p = (float*)m.p + row * m.ld + c;
+    if (m.vec) {
+      if (c < cols) {
+        *(float4*)p = float4{v[0], v[1], v[2], v[3]};
+        *(float4*)(p + 4) = float4{v[4], v[5], v[6], v[7]};
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (c + i < cols) p[i] = v[i];
+    }
+  }
+}
+
+// The same for four columns.
+__device__ __forceinline__ f32x4 load4(const DMat& m, size_t row, int c, int cols) {
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  if (m.bf16) {
+    const uint16_t* p = (const uint16_t*)m.p + row * m.ld + c;
+    if (m.vec4 && c + 3 < cols) {
+      const uint2 u = *(const uint2*)p;
+      v = f32x4{__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
+                __uint_as_float(u.y & 0xffff0000u)};
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (c + i < cols) v[i] = bf16_to_f32(p[i]);
+    }
+  } else {
+    const float* p = (const float*)m.p + row * m.ld + c;
+    if (m.vec4 && c + 3 < cols) {
+      v = *(const f32x4*)p;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (c + i < cols) v[i] = p[i];
+    }
+  }
+  return v;
+}
+
+__device__ __forceinline__ void store4(const DMat& m, size_t row, int c, int cols, f32x4 v) {
+  if (m.bf16) {
+    uint16_t* p = (uint16_t*)m.p + row * m.ld + c;
+    if (m.vec4 && c + 3 < cols) {
+      *(uint2*)p = uint2{f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3])};
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (c + i < cols) p[i] = f32_to_bf16(v[i]);
+    }
+  } else {
+    float* p = (float*)m.p + row * m.ld + c;
+    if (m.vec4 && c + 3 < cols) {
+      *(f32x4*)p = v;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (c + i < cols) p[i] = v[i];
+    }
+  }
+}
+
+// ----------------------------------------------------------------- 8-bit checkpoints
+
+// The scale byte of a group whose largest magnitude has these bits (sign cleared; NaN and
+// infinity give 255).  amax = m 2^(E - 127), 1 <= m < 2: 127 * 2^(s - 127) >= amax first
+// holds at s = E - 6 when m <= 127 / 64 (mantissa bits 0x7e0000), at E - 5 otherwise.
+__device__ __forceinline__ uint32_t ckpt_scale(uint32_t amax) {
+  const int s = (int)(amax >> 23) - 6 + ((amax & 0x7fffffu) > 0x7e0000u);
+  return amax >= 0x7f800000u ? 255u : (uint32_t)max(s, 1);
+}
+// 2^(127 - s), and 0 for a group that reads as NaN
+__device__ __forceinline__ float ckpt_inv(uint32_t s) { return s == 255u ? 0.f : __uint_as_float((254u - s) << 23); }
+// The integer nearest to v inv (ties to even) in the low byte: |v inv| <= 127, so adding
+// 1.5 * 2^23 in one rounding leaves it in the low mantissa bits.
+__device__ __forceinline__ uint32_t ckpt_round(float v, float inv) {
+  return __float_as_uint(fmaf(v, inv, 12582912.f));
+}
+// four low bytes in one word
+__device__ __forceinline__ uint32_t pack_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  const uint32_t ab = __builtin_amdgcn_perm(b, a, 0x0c0c0400u), cd = __builtin_amdgcn_perm(d, c, 0x0c0c0400u);
+  return __builtin_amdgcn_perm(cd, ab, 0x05040100u);
+}
+// (s = 255: infinity, and every q of the group is 0, so the product is NaN)
+__device__ __forceinline__ float ckpt_two(uint32_t s) { return __uint_as_float(s << 23); }
+template <int I>
+__device__ __forceinline__ float ckpt_int(uint32_t w) {
+  return (float)((int32_t)(w << (24 - 8 * I)) >> 24);
+}
+__device__ __forceinline__ void ckpt_value4(uint32_t w, float two, float (&v)[4]) {
+  v[0] = ckpt_int<0>(w) * two;
+  v[1] = ckpt_int<1>(w) * two;
+  v[2] = ckpt_int<2>(w) * two;
+  v[3] = ckpt_int<3>(w) * two;
+}
+__device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+
+// Columns c .. c + 7 (c a multiple of 8) into a checkpoint row; four neighbouring lanes, all
+// of them active, hold one group of 32.  v is 0 from the last column on.
+__device__ __forceinline__ void ckpt_store8(const DCkpt& k, size_t row, int c, const float (&v)[8]) {
+  uint32_t m = abs_bits(v[0]);
+#pragma unroll
+  for (int i = 1; i < 8; ++i) m = max(m, abs_bits(v[i]));
+  m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0xB1, 0xf, 0xf, false));   // lane ^ 1
+  m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x4E, 0xf, 0xf, false));   // lane ^ 2
+  const uint32_t s = ckpt_scale(m);
+  const float inv = ckpt_inv(s);
+  uint2 w = {pack_bytes(ckpt_round(v[0], inv), ckpt_round(v[1], inv), ckpt_round(v[2], inv), ckpt_round(v[3], inv)),
+             pack_bytes(ckpt_round(v[4], inv), ckpt_round(v[5], inv), ckpt_round(v[6], inv), ckpt_round(v[7], inv))};
+  if (s == 255u) w = uint2{0, 0};
+  if (c < k.ld) {
+    *(uint2*)(k.q + row * k.ld + c) = w;
+    if (c % kCkptGroup == 0) k.scale[row * (size_t)(k.ld / kCkptGroup) + c / kCkptGroup] = (uint8_t)s;
+  }
+}
+// Columns c .. c + 7 of a checkpoint row (0 past the padded row).
+__device__ __forceinline__ void ckpt_load8(const DCkpt& k, size_t row, int c, float (&v)[8]) {
+  uint2 w = {0, 0};
+  uint32_t s = 1;
+  if (c < k.ld) {
+    w = *(const uint2*)(k.q + row * k.ld + c);
+    s = k.scale[row * (size_t)(k.ld / kCkptGroup) + c / kCkptGroup];
+  }
+  const float two = ckpt_two(s);
+  float a[4], b[4];
+  ckpt_value4(w.x, two, a);
+  ckpt_value4(w.y, two, b);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
+}
+
+// ----------------------------------------------------------------- GELU
+
+__device__ __forceinline__ float gelu_value(float h) { return 0.5f * h * (1.0f + erff(h * 0.70710678118654752f)); }
+// d/dh (h Phi(h)) = Phi(h) + h phi(h)
+__device__ __forceinline__ float gelu_slope(float h) {
+  return 0.5f * (1.0f + erff(h * 0.70710678118654752f)) + h * (0.39894228040143268f * __expf(-0.5f * h * h));
+}
+
+// ----------------------------------------------------------------- launchers
+
+struct LnFwdArgs {
+  int rows, cols;
+  DMat x, y;
+  DVec gain, bias;
+  float *mean, *rstd;   // or NULL
+  DCkpt xhat;           // q NULL: none
+};
+void launch_layer_norm(const LnFwdArgs& a, hipStream_t st);
+
+struct LnBwdArgs {
+  int rows, cols;
+  DMat dy, x, dres, dx, copy;   // p NULL: absent
+  DVec gain;
+  const float *mean, *rstd;
+  DCkpt xhat;
+  float *dgain, *dbias;         // or NULL
+  int accumulate;
+  float* part;                  // [workgroups][2][cols]
+};
+int ln_bwd_groups(int rows, int cols);
+void launch_layer_norm_backward(const LnBwdArgs& a, hipStream_t st);
+
+void launch_ckpt_pack(int rows, int cols, const DMat& x, const DCkpt& k, hipStream_t st);
+void launch_ckpt_unpack(int rows, int cols, const DCkpt& k, bool gelu, const DMat& out, hipStream_t st);
+
+// One operand of a product, along its output dimension (`extent`) and the reduction.
+struct LinOp {
+  const uint16_t* p;     // bf16, or NULL: the checkpoint
+  int64_t ld;
+  DCkpt ck;
+  int extent;
+};
+enum LinKind : int { LIN_FWD = 0, LIN_DGRAD = 1, LIN_WGRAD = 2 };
+// out[q][p] = sum over K of Q(q, .) P(p, .) with the epilogue of the kind.
+struct LinArgs {
+  LinOp P, Q;
+  int K;
+  int S, steps;          // splits of the reduction and 64-wide steps of each (set by the launcher)
+  int tiles_p, tiles_q;
+  float* part;           // S > 1: [S][Q][ldp] partial products, then (wgrad) [S][Q] row sums of dy
+  float* part_sum;
+  int ldp;
+  // epilogue
+  DVec bias, gain, shift;
+  int gelu, accumulate;
+  DMat res, out, pre, act_out;
+  DCkpt ck;              // fwd: the pre-activation out; dgrad: in
+  float* dbias;
+};
+// Floats of workspace of a product with these extents.
+size_t lin_part_floats(int kind, int P, int Q, int K);
+void launch_linear(int kind, LinArgs a, hipStream_t st);
+
+}  // namespace ad

@@ -37,11 +37,6 @@ __device__ __forceinline__ float row_total(float v, float* red) {
   return v;
 }
 
-__device__ __forceinline__ void load_vec8(const DVec& g, int c, int cols, float (&v)[8]) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? ld_vec(g, c + i) : 0.f;
-}
-
 // W: waves per row (1 or 4).  The statistics are two passes over the registers: the mean,
 // then the squared deviations from it (no cancellation of large means).
 template <int J, int W>

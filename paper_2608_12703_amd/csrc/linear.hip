@@ -20,6 +20,7 @@
 // so the eight rows that 32 lanes read together do.  The direct loads store 1 KB in lane order;
 // the permutation is made by the lanes' source addresses.
 #include <algorithm>
+#include <type_traits>
 
 #include "train.h"
 
@@ -29,11 +30,25 @@ namespace {
 
 constexpr int kBK = 64;   // reduction elements of one LDS stage
 
-// 16 bytes that pieces past the end of the reduction read
-__device__ const uint4 g_zero16 = {0, 0, 0, 0};
-
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// Direct loads go through buffer descriptors: a scalar base per stage and one 32-bit offset per
+// lane (64-bit lane addresses cost twice the registers), and what lies past the descriptor's end
+// arrives as zeros, which ends the reduction without a branch.
+constexpr uint32_t kBufferFlags = 0x00020000;   // raw buffer of 32-bit elements
+constexpr uint32_t kPastEnd = 0x80000000u;      // further than any offset in a tile: 255 * 2^23 + 128 bytes
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t descriptor(const char* base, uint32_t size) {
+  return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, size, kBufferFlags);
+}
+__device__ __forceinline__ void buffer16(const char* base, uint32_t size, uint32_t off, uint4* lds) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(descriptor(base, size), (__attribute__((address_space(3))) void*)lds, 16, off, 0, 0, 0);
+}
+__device__ __forceinline__ const char* uniform(const void* p) {
+  const uint64_t v = (uint64_t)p;
+  return (const char*)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)v) |
+                       (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32);
+}
 
 enum Src : int { SRC_DIRECT = 0, SRC_ANY = 1, SRC_CKPT = 2 };
 
@@ -48,8 +63,10 @@ struct Loader {
   static constexpr int RB = R / 8;       // 16-byte pieces in a KS row
   LinOp o;
   int r0, K, k0, w, lane;
-  const uint16_t* base;   // of the stage's first element
-  uint32_t off[N];        // bytes
+  const char* base;       // the stage's first element
+  const char* sbase;      // checkpoint: its scale
+  int64_t left, sleft;    // KS: bytes from there to the end of the reduction's last row
+  uint32_t off[N], soff[SRC == SRC_CKPT ? N / 2 : 1];   // bytes
   uint4 reg[N];
   uint32_t sc[N];
 
@@ -76,7 +93,8 @@ struct Loader {
   __device__ __forceinline__ void init(const LinOp& op, int first, int K_, int k0_, int w_, int lane_) {
     o = op; r0 = first; K = K_; k0 = k0_; w = w_; lane = lane_;
     if constexpr (SRC == SRC_DIRECT) {
-      base = KS ? o.p + (size_t)k0 * o.ld + r0 : o.p + (size_t)r0 * o.ld + k0;
+      base = uniform(KS ? o.p + (size_t)k0 * o.ld + r0 : o.p + (size_t)r0 * o.ld + k0);
+      left = 2 * ((int64_t)(K - 1 - k0) * o.ld + (o.extent - r0));
 #pragma unroll
       for (int j = 0; j < N; ++j) {
         int row, r;
@@ -85,25 +103,45 @@ struct Loader {
         off[j] = KS ? 2u * ((uint32_t)r * (uint32_t)o.ld + (uint32_t)min(row, o.extent - 8 - r0))
                     : 2u * ((uint32_t)min(row, o.extent - 1 - r0) * (uint32_t)o.ld + (uint32_t)r);
       }
+    } else if constexpr (SRC == SRC_CKPT) {
+      const int ld = o.ck.ld, sld = ld / kCkptGroup;
+      base = uniform(o.ck.q + (size_t)k0 * ld + r0);
+      sbase = uniform(o.ck.scale + (size_t)k0 * sld + r0 / kCkptGroup);
+      left = (int64_t)(K - k0) * ld - r0;
+      sleft = (int64_t)(K - k0) * sld - r0 / kCkptGroup;
+#pragma unroll
+      for (int j = 0; j < N / 2; ++j) {
+        // (columns past the padded row read the next one's; their results are not stored)
+        int row, r;
+        place_ck(j, row, r);
+        off[j] = (uint32_t)r * ld + row;
+        soff[j] = (uint32_t)r * sld + row / kCkptGroup;
+      }
     }
   }
 
   // stage at k0: into `lds` (direct), or into registers
   __device__ __forceinline__ void issue(uint4* lds) {
     if constexpr (SRC == SRC_DIRECT) {
-      if (k0 + kBK <= K) {
+      if constexpr (KS) {
+        const uint32_t size = (uint32_t)min(left, (int64_t)kPastEnd);
 #pragma unroll
-        for (int j = 0; j < N; ++j) dma16((const char*)base + off[j], lds + (w * N + j) * 64);
+        for (int j = 0; j < N; ++j) buffer16(base, size, off[j], lds + (w * N + j) * 64);
+        base += 2 * kBK * o.ld;
+        left -= 2 * kBK * o.ld;
       } else {
+        if (k0 + kBK > K) {   // the reduction ends in this stage
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-          int row, r;
-          place(j, row, r);
-          const void* src = k0 + r < K ? (const void*)((const char*)base + off[j]) : (const void*)&g_zero16;
-          dma16(src, lds + (w * N + j) * 64);
+          for (int j = 0; j < N; ++j) {
+            int row, r;
+            place(j, row, r);
+            if (k0 + r >= K) off[j] = kPastEnd;
+          }
         }
+#pragma unroll
+        for (int j = 0; j < N; ++j) buffer16(base, kPastEnd, off[j], lds + (w * N + j) * 64);
+        base += 2 * kBK;
       }
-      base += KS ? (size_t)kBK * o.ld : (size_t)kBK;
     } else if constexpr (SRC == SRC_ANY) {
 #pragma unroll
       for (int j = 0; j < N; ++j) {
@@ -119,18 +157,18 @@ struct Loader {
         reg[j] = uint4{e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16};
       }
     } else {
+      // past the last row: q = 0, scale byte 0 (a scale of 0)
+      const __amdgpu_buffer_rsrc_t rq = descriptor(base, (uint32_t)min(left, (int64_t)kPastEnd));
+      const __amdgpu_buffer_rsrc_t rs = descriptor(sbase, (uint32_t)min(sleft, (int64_t)kPastEnd));
 #pragma unroll
       for (int j = 0; j < N / 2; ++j) {
-        int row, r;
-        place_ck(j, row, r);
-        const int c = r0 + row, k = k0 + r;
-        reg[j] = uint4{0, 0, 0, 0};
-        sc[j] = 1;
-        if (k < K && c < o.ck.ld) {
-          reg[j] = *(const uint4*)(o.ck.q + (size_t)k * o.ck.ld + c);
-          sc[j] = o.ck.scale[(size_t)k * (o.ck.ld / kCkptGroup) + c / kCkptGroup];
-        }
+        reg[j] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rq, off[j], 0, 0));
+        sc[j] = __builtin_amdgcn_raw_buffer_load_b8(rs, soff[j], 0, 0);
       }
+      base += kBK * (int64_t)o.ck.ld;
+      left -= kBK * (int64_t)o.ck.ld;
+      sbase += kBK * (int64_t)(o.ck.ld / kCkptGroup);
+      sleft -= kBK * (int64_t)(o.ck.ld / kCkptGroup);
     }
     k0 += kBK;
   }
@@ -164,141 +202,145 @@ struct Loader {
   }
 };
 
-// The matrix instruction's operand of 16-row (or column) tile t, 32-wide step s of a stage.
+// The matrix instruction's operands of a wave: 16-row (or column) tiles tile0 .. of a stage with R rows
+// (or columns).  Both layouts' permutations are exclusive-ors of address bits, so one lane
+// offset serves every tile and step.  x0: a KS tile t is tile0 + (t ^ x0).
 template <int R, bool KS>
-__device__ __forceinline__ bf16x8 fragment(const uint4* lds, int t, int s, int lane) {
-  const int c16 = lane & 15, g = lane >> 4;
-  if constexpr (KS) {
-    const int i = c16 >> 2, u = (t & ~7) | ((t & 7) ^ (i | ((g & 1) << 2)));
-    const uint16_t* p = (const uint16_t*)lds + (32 * s + 8 * g + i) * R + u * 16 + (c16 & 3) * 4;
-    typedef const __attribute__((address_space(3))) s16x4* lp;
-    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(lp)p);
-    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(lp)(p + 4 * R));
-    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
-  } else {
-    return as_bf16x8(lds[(t * 16 + c16) * 8 + ((4 * s + g) ^ (c16 >> 1))]);
+struct Reader {
+  uint32_t off;   // bytes
+  __device__ __forceinline__ void init(int tile0, int x0, int lane) {
+    const int c16 = lane & 15, g = lane >> 4;
+    if constexpr (KS) {
+      const int i = c16 >> 2;
+      off = (8 * g + i) * R * 2 + (tile0 >> 3) * 256 + (((tile0 & 7) ^ x0 ^ ks_swz(8 * g + i)) * 32) + (c16 & 3) * 8;
+    } else {
+      off = (tile0 * 16 + c16) * 128 + ((g ^ (c16 >> 1)) * 16);
+    }
   }
-}
+  // (the offsets of the tiles are recomputed at each use: kept, they would take the registers
+  // that hold the products)
+  __device__ __forceinline__ uint32_t fresh() const {
+    uint32_t o = off;
+    asm volatile("" : "+v"(o));
+    return o;
+  }
+  // tile t of at most 8 (KS: tile0 a multiple of the tiles read), 32-wide step s
+  static __device__ __forceinline__ bf16x8 read(const uint4* lds, uint32_t o, int t, int s) {
+    if constexpr (KS) {
+      const char* p = (const char*)lds + (o ^ (t * 32)) + s * 64 * R;
+      typedef __attribute__((address_space(3))) s16x4* lp;
+      const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)p);
+      const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(p + 8 * R));
+      return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+    } else {
+      return as_bf16x8(*(const uint4*)((const char*)lds + (o ^ (s * 64)) + t * 2048));
+    }
+  }
+};
 
-// Largest of a value over the four 16-lane rows of a wave, as bits.
-__device__ __forceinline__ uint32_t rows4_max_bits(uint32_t v) {
-  const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-  v = max((uint32_t)a[0], (uint32_t)a[1]);
-  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-  return max((uint32_t)b[0], (uint32_t)b[1]);
-}
-
-__device__ __forceinline__ f32x4 vec_at(const DVec& v, int c, int cols) {
-  f32x4 r;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) r[i] = c + i < cols ? ld_vec(v, c + i) : 0.f;
-  return r;
-}
-
-// Output row q, columns p .. p + 3 (h[0]) and p + 16 .. p + 19 (h[1]), p = 32 * n + 4 * (lane
-// / 16): the four lanes lane % 16 + 16 * {0 .. 3} hold one group of 32 columns.  Every lane of
-// the wave calls this.  qsum: wgrad's sum of dy for row q.
+// Columns c .. c + 7 of output row q (four neighbouring lanes hold one checkpoint group of 32; every
+// lane of the wave calls this).  qsum: wgrad's sum of dy for row q.
 template <int KIND>
-__device__ __forceinline__ void epilogue(const LinArgs& a, int q, int p, f32x4 (&h)[2], float qsum) {
-  const int Pn = a.P.extent;
+__device__ __forceinline__ void epilogue(const LinArgs& a, int q, int c, float (&h)[8], float qsum) {
+  const int cols = a.P.extent;
   const bool row = q < a.Q.extent;
   if constexpr (KIND == LIN_FWD) {
-    if (a.bias.p)
+    float b[8];
+    if (a.bias.p) {
+      load_vec8(a.bias, c, cols, b);
 #pragma unroll
-      for (int u = 0; u < 2; ++u) h[u] += vec_at(a.bias, p + 16 * u, Pn);
-    if (a.pre.p && row)
-#pragma unroll
-      for (int u = 0; u < 2; ++u) store4(a.pre, q, p + 16 * u, Pn, h[u]);
+      for (int i = 0; i < 8; ++i) h[i] += b[i];
+    }
+    if (a.pre.p && row) store8(a.pre, q, c, cols, h);
     if (a.ck.q) {
-      uint32_t m = 0;
+      float z[8];
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (p + 16 * u + i >= Pn) h[u][i] = 0.f;   // (padding is written as 0)
-          m = max(m, abs_bits(h[u][i]));
-        }
-      const uint32_t s = ckpt_scale(rows4_max_bits(m));
-      const float inv = ckpt_inv(s);
-      if (row && p < a.ck.ld) {
-        int8_t* to = a.ck.q + (size_t)q * a.ck.ld + p;
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const uint32_t b = pack_bytes(ckpt_round(h[u][0], inv), ckpt_round(h[u][1], inv),
-                                        ckpt_round(h[u][2], inv), ckpt_round(h[u][3], inv));
-          *(uint32_t*)(to + 16 * u) = s == 255u ? 0u : b;
-        }
-        if (p % kCkptGroup == 0) a.ck.scale[(size_t)q * (a.ck.ld / kCkptGroup) + p / kCkptGroup] = (uint8_t)s;
-      }
+      for (int i = 0; i < 8; ++i) z[i] = c + i < cols ? h[i] : 0.f;   // (padding is written as 0)
+      ckpt_store8(a.ck, q, row ? c : a.ck.ld, z);
     }
     if (!row) return;
+    if (a.gelu)
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      f32x4 y = h[u];
-      if (a.gelu)
+      for (int i = 0; i < 8; ++i) h[i] = gelu_value(h[i]);
+    if (a.res.p) {
+      load8(a.res, q, c, cols, b);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] = gelu_value(y[i]);
-      if (a.res.p) y += load4(a.res, q, p + 16 * u, Pn);
-      store4(a.out, q, p + 16 * u, Pn, y);
+      for (int i = 0; i < 8; ++i) h[i] += b[i];
     }
+    store8(a.out, q, c, cols, h);
   } else if constexpr (KIND == LIN_DGRAD) {
     if (!row) return;
+    if (a.gelu) {
+      float x[8];
+      if (a.ck.q) ckpt_load8(a.ck, q, c, x);
+      else load8(a.pre, q, c, cols, x);
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int c = p + 16 * u;
-      f32x4 v = h[u];
-      if (a.gelu) {
-        f32x4 x;
-        if (a.ck.q) {
-          uint32_t w = 0, s = 1;
-          if (c < a.ck.ld) {
-            w = *(const uint32_t*)(a.ck.q + (size_t)q * a.ck.ld + c);
-            s = a.ck.scale[(size_t)q * (a.ck.ld / kCkptGroup) + c / kCkptGroup];
-          }
-          float t[4];
-          ckpt_value4(w, ckpt_two(s), t);
-          x = f32x4{t[0], t[1], t[2], t[3]};
-        } else {
-          x = load4(a.pre, q, c, Pn);
-        }
-        if (a.act_out.p) {
-          f32x4 y;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) y[i] = gelu_value(x[i]);
-          store4(a.act_out, q, c, Pn, y);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] *= gelu_slope(x[i]);
+      for (int i = 0; i < 8; ++i) {
+        const Normal n = normal(x[i]);
+        h[i] *= gelu_slope(x[i], n);
+        x[i] *= n.cdf;
       }
-      store4(a.out, q, c, Pn, v);
+      if (a.act_out.p) store8(a.act_out, q, c, cols, x);
     }
+    store8(a.out, q, c, cols, h);
   } else {
     if (!row) return;
+    if (a.gain.p) {
+      float g[8], b[8];
+      load_vec8(a.gain, c, cols, g);
+      load_vec8(a.shift, c, cols, b);
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int c = p + 16 * u;
-      f32x4 v = h[u];
-      if (a.gain.p) v = v * vec_at(a.gain, c, Pn) + vec_at(a.shift, c, Pn) * qsum;
-      if (a.accumulate) v += load4(a.out, q, c, Pn);
-      store4(a.out, q, c, Pn, v);
+      for (int i = 0; i < 8; ++i) h[i] = fmaf(h[i], g[i], b[i] * qsum);
     }
-    if (a.dbias && p == 0) a.dbias[q] = a.accumulate ? a.dbias[q] + qsum : qsum;
+    if (a.accumulate) {
+      float o[8];
+      load8(a.out, q, c, cols, o);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) h[i] += o[i];
+    }
+    store8(a.out, q, c, cols, h);
+    if (a.dbias && c == 0) a.dbias[q] = a.accumulate ? a.dbias[q] + qsum : qsum;
   }
 }
 
-// Tile of workgroup id: workgroups are dealt round-robin over the 8 XCDs, so each XCD takes a
-// contiguous range of tiles, ordered in bands of 8 row tiles (column by column inside a
-// band), and its workgroups share both operands through its L2.
-__device__ __forceinline__ void tile_of(int id, int tp, int tq, int& ip, int& iq) {
-  const int T = tp * tq, x = id % 8, l = id / 8;
-  const int t = x * (T / 8) + min(x, T % 8) + l;
+// Workgroups are dealt round-robin over the 8 XCDs: number id of n, so ordered that each XCD has a
+// contiguous range.
+__device__ __forceinline__ int xcd_order(int id, int n) {
+  const int x = id % 8;
+  return x * (n / 8) + min(x, n % 8) + id / 8;
+}
+// Place of tile t: bands of 8 row tiles, column by column inside a band, so that neighbours in the
+// order (the workgroups of one XCD) share both operands through its L2.
+__device__ __forceinline__ void tile_of(int t, int tp, int tq, int& ip, int& iq) {
   const int band = t / (8 * tp), rest = t % (8 * tp), h = min(8, tq - band * 8);
   iq = band * 8 + rest % h;
   ip = rest / h;
 }
 
-// WP x WQ waves of TP x TQ 16 x 16 tiles.  Two LDS stages: the next one fills while this one is
-// multiplied; one barrier a stage.
+// The order inside a phase: its LDS reads spread between its products.
+// (VALU: and that many conversions of a checkpoint after each product)
+template <int READS, int PRODUCTS, int VALU = 0>
+__device__ __forceinline__ void interleave() {
+#pragma unroll
+  for (int i = 0; i < READS; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);                   // an LDS read
+    if constexpr (VALU == 0) {
+      __builtin_amdgcn_sched_group_barrier(0x008, PRODUCTS / READS, 0);  // products
+    } else {
+#pragma unroll
+      for (int j = 0; j < PRODUCTS / READS; ++j) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, VALU, 0);
+      }
+    }
+  }
+}
+
+// WP x WQ waves of TP x TQ 16 x 16 tiles, two LDS stages.  A stage is two 32-wide steps of two phases
+// each (the upper and the lower half of the wave's P tiles).  While a wave multiplies in one
+// phase it reads the next one's operands, so no product waits for LDS.  The barrier falls before
+// the stage's last phase, when all of it is in registers and its LDS is free: the loads of the
+// stage after the next start there.
 template <int KIND, int WP, int WQ, int TP, int TQ, bool PKS, int PSRC, bool QKS, int QSRC>
 __global__ void __launch_bounds__(WP* WQ* kWave) linear_kernel(LinArgs a) {
   constexpr int NW = WP * WQ, RP = WP * TP * 16, RQ = WQ * TQ * 16, NS = TQ / WP;
@@ -307,10 +349,13 @@ __global__ void __launch_bounds__(WP* WQ* kWave) linear_kernel(LinArgs a) {
   __shared__ float sums[KIND == LIN_WGRAD ? RQ : 1];
   const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int wp = w % WP, wq = w / WP, c16 = lane & 15, g = lane >> 4;
-  const int tiles = a.tiles_p * a.tiles_q, split = blockIdx.x / tiles;
+  // whole tiles first, then the last `rest` tiles in S parts of the reduction each
+  const int id = blockIdx.x, rest = a.tiles_p * a.tiles_q - a.whole;
+  const bool part = id >= a.whole;
+  const int split = part ? (id - a.whole) / rest : 0, nth = part ? (id - a.whole) % rest : 0;
   int ip, iq;
-  tile_of(blockIdx.x % tiles, a.tiles_p, a.tiles_q, ip, iq);
-  const int kbeg = split * a.steps * kBK, kend = min(a.K, kbeg + a.steps * kBK);
+  tile_of(part ? a.whole + xcd_order(nth, rest) : xcd_order(id, a.whole), a.tiles_p, a.tiles_q, ip, iq);
+  const int kbeg = split * a.steps * kBK, kend = part ? min(a.K, kbeg + a.steps * kBK) : a.K;
   const int steps = kend > kbeg ? (kend - kbeg + kBK - 1) / kBK : 0;
   Loader<RP, NW, PKS, PSRC> lp;
   Loader<RQ, NW, QKS, QSRC> lq;
@@ -326,49 +371,103 @@ __global__ void __launch_bounds__(WP* WQ* kWave) linear_kernel(LinArgs a) {
   for (int j = 0; j < NS; ++j) csum[j] = f32x4{0.f, 0.f, 0.f, 0.f};
   const bf16x8 ones = as_bf16x8(uint4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
   // wgrad: the WP waves that share a row of tiles sum dy for NS of them each; a wave's slot j is
-  // its tile (j + wp NS) % TQ, so the slots it sums are the first
-  auto slot = [&](int j) { return KIND == LIN_WGRAD ? (j + wp * NS) % TQ : j; };
+  // its tile j ^ (wp NS), so the slots it sums are the first
+  static_assert(KIND != LIN_WGRAD || (WP == 2 && TQ == 2 * NS && (TQ & (TQ - 1)) == 0));
+  const int x0 = KIND == LIN_WGRAD ? wp * NS : 0;
+  auto slot = [&](int j) { return j ^ x0; };
+  Reader<RP, PKS> rp;
+  Reader<RQ, QKS> rq;
+  rp.init(wp * TP, 0, lane);
+  rq.init(wq * TQ, x0, lane);
 
-  auto step = [&](const uint4* ps, const uint4* qs, uint4* pn, uint4* qn, bool more) {
-    // this wave's loads of the stage have landed, then everyone's; the other stage is free
+  constexpr int H = TP / 2;
+  auto read_p = [&](bf16x8 (&f)[H], const uint4* ps, int s, int half) {
+    const uint32_t o = rp.fresh();
+#pragma unroll
+    for (int i = 0; i < H; ++i) f[i] = rp.read(ps, o, half * H + i, s);
+  };
+  auto read_q = [&](bf16x8 (&f)[TQ], const uint4* qs, int s) {
+    const uint32_t o = rq.fresh();
+#pragma unroll
+    for (int j = 0; j < TQ; ++j) f[j] = rq.read(qs, o, j, s);
+  };
+  auto multiply = [&](const bf16x8 (&fp)[H], const bf16x8 (&fq)[TQ], auto half) {
+#pragma unroll
+    for (int i = 0; i < H; ++i)
+#pragma unroll
+      for (int j = 0; j < TQ; ++j) acc[half.value * H + i][j] = mfma_bf16(fp[i], fq[j], acc[half.value * H + i][j]);
+    if constexpr (KIND == LIN_WGRAD && half.value)
+#pragma unroll
+      for (int j = 0; j < NS; ++j) csum[j] = mfma_bf16(ones, fq[j], csum[j]);
+  };
+  constexpr std::integral_constant<int, 0> upper{};
+  constexpr std::integral_constant<int, 1> lower{};
+  constexpr int kReadsP = H * (PKS ? 2 : 1), kReadsQ = TQ * (QKS ? 2 : 1);
+  auto sync = [] {   // this wave's loads have landed and its LDS reads are in registers; then everyone's
     __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt 0, lgkmcnt 0
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    if (more) {
-      lp.issue(pn);
-      lq.issue(qn);
-    }
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      bf16x8 fp[TP], fq[TQ];
-#pragma unroll
-      for (int i = 0; i < TP; ++i) fp[i] = fragment<RP, PKS>(ps, wp * TP + i, s, lane);
-#pragma unroll
-      for (int j = 0; j < TQ; ++j) fq[j] = fragment<RQ, QKS>(qs, wq * TQ + slot(j), s, lane);
-#pragma unroll
-      for (int i = 0; i < TP; ++i)
-#pragma unroll
-        for (int j = 0; j < TQ; ++j) acc[i][j] = mfma_bf16(fp[i], fq[j], acc[i][j]);
-      if constexpr (KIND == LIN_WGRAD)
-#pragma unroll
-        for (int j = 0; j < NS; ++j) csum[j] = mfma_bf16(ones, fq[j], csum[j]);
-    }
-    if (more) {
-      lp.commit(pn);
-      lq.commit(qn);
-    }
   };
 
   if (steps > 0) {
+    bf16x8 pu[H], pl[H], qa[TQ], qb[TQ];
     lp.issue(p0);
     lq.issue(q0);
     lp.commit(p0);
     lq.commit(q0);
-    for (int t = 0; t < steps; t += 2) {
-      step(p0, q0, p1, q1, t + 1 < steps);
-      if (t + 1 < steps) step(p1, q1, p0, q0, t + 2 < steps);
+    sync();
+    if (steps > 1) {
+      lp.issue(p1);
+      lq.issue(q1);
     }
+    read_q(qa, q0, 0);
+    read_p(pu, p0, 0, 0);
+    // the first three phases of the stage in (pc, qc); the one before (pn, qn) fills from registers
+    auto phases = [&](const uint4* pc, const uint4* qc, uint4* pn, uint4* qn, bool next) {
+      __builtin_amdgcn_sched_barrier(0);
+      read_p(pl, pc, 0, 1);
+      multiply(pu, qa, upper);
+      interleave<kReadsP, H * TQ>();
+      __builtin_amdgcn_sched_barrier(0);
+      read_q(qb, qc, 1);
+      read_p(pu, pc, 1, 0);
+      multiply(pl, qa, lower);
+      interleave<kReadsP + kReadsQ, H * TQ>();
+      __builtin_amdgcn_sched_barrier(0);
+      read_p(pl, pc, 1, 1);
+      multiply(pu, qb, upper);
+      if (next) {
+        lp.commit(pn);
+        lq.commit(qn);
+      }
+      if constexpr (PSRC == SRC_DIRECT && QSRC == SRC_DIRECT) interleave<kReadsP, H * TQ>();
+      else if constexpr (PSRC == SRC_CKPT) interleave<kReadsP, H * TQ, 6>();
+    };
+    // all of a stage but the last one; `more`: the stage after the next exists
+    auto stage = [&](uint4* pc, uint4* qc, uint4* pn, uint4* qn, bool more) {
+      phases(pc, qc, pn, qn, true);
+      sync();
+      if (more) {
+        lp.issue(pc);
+        lq.issue(qc);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      read_q(qa, qn, 0);
+      read_p(pu, pn, 0, 0);
+      multiply(pl, qb, lower);
+      interleave<kReadsP + kReadsQ, H * TQ>();
+    };
+    int t = 0;
+    for (; t + 2 < steps; t += 2) {
+      stage(p0, q0, p1, q1, true);
+      stage(p1, q1, p0, q0, t + 3 < steps);
+    }
+    const bool odd = t + 1 < steps;
+    if (odd) stage(p0, q0, p1, q1, false);
+    phases(odd ? p1 : p0, odd ? q1 : q0, nullptr, nullptr, false);
+    multiply(pl, qb, lower);
   }
+  __syncthreads();   // the stages' LDS is free
 
   if constexpr (KIND == LIN_WGRAD) {
     if (g == 0)
@@ -376,83 +475,127 @@ __global__ void __launch_bounds__(WP* WQ* kWave) linear_kernel(LinArgs a) {
       for (int j = 0; j < NS; ++j) sums[(wq * TQ + slot(j)) * 16 + c16] = csum[j][0];
     __syncthreads();
   }
-  const int pw = ip * RP + wp * TP * 16 + 4 * g, qw = iq * RQ + wq * TQ * 16 + c16;
+  // One row of tiles at a time goes through the wave's own piece of LDS, [16][16 TP] floats (16-byte
+  // chunk ch of row r at place ch ^ r), to come back as 8 columns a lane, whole rows side by side.
+  constexpr int CPR = 2 * TP, kPiece = 16 * TP * 4;   // 8-column chunks in a row; 16-byte chunks in a piece
+  uint4* mine = w < NW / 2 ? p0 + w * kPiece : p1 + (w - NW / 2) * kPiece;
+  static_assert(NW / 2 * kPiece <= RP * 8);
 #pragma unroll
   for (int j = 0; j < TQ; ++j) {
-    const int q = qw + slot(j) * 16;
-    const float qsum = KIND == LIN_WGRAD ? sums[(wq * TQ + slot(j)) * 16 + c16] : 0.f;
-    if (a.S > 1) {
-      if (q < a.Q.extent) {
 #pragma unroll
-        for (int i = 0; i < TP; ++i)
-          if (pw + 16 * i < a.ldp)
-            *(f32x4*)(a.part + ((size_t)split * a.Q.extent + q) * a.ldp + pw + 16 * i) = acc[i][j];
-        if (KIND == LIN_WGRAD && ip == 0 && wp == 0 && g == 0) a.part_sum[(size_t)split * a.Q.extent + q] = qsum;
+    for (int i = 0; i < TP; ++i)
+      mine[c16 * 4 * TP + ((4 * i + g) ^ c16)] = __builtin_bit_cast(uint4, acc[i][j]);
+    const int q_tile = wq * TQ + slot(j);
+#pragma unroll 1
+    for (int it = 0; it < 16 * CPR / kWave; ++it) {
+      const int r = it * (kWave / CPR) + lane / CPR, k = lane % CPR;
+      const f32x4 lo = __builtin_bit_cast(f32x4, mine[r * 4 * TP + ((2 * k) ^ r)]);
+      const f32x4 hi = __builtin_bit_cast(f32x4, mine[r * 4 * TP + ((2 * k + 1) ^ r)]);
+      const int q = iq * RQ + q_tile * 16 + r, c = ip * RP + wp * TP * 16 + 8 * k;
+      const float qsum = KIND == LIN_WGRAD ? sums[q_tile * 16 + r] : 0.f;
+      if (part) {
+        // tile [RQ][RP] of split, tile, then its rows' sums
+        const size_t at = (size_t)split * rest + xcd_order(nth, rest);
+        float* to = a.part + (at * RQ + q_tile * 16 + r) * RP + wp * TP * 16 + 8 * k;
+        *(f32x4*)to = lo;
+        *(f32x4*)(to + 4) = hi;
+        if (KIND == LIN_WGRAD && wp == 0 && k == 0) a.part_sum[at * RQ + q_tile * 16 + r] = qsum;
+      } else {
+        float h[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        epilogue<KIND>(a, q, c, h, qsum);
       }
-      continue;
-    }
-#pragma unroll
-    for (int i = 0; i < TP; i += 2) {
-      f32x4 h[2] = {acc[i][j], acc[i + 1][j]};
-      epilogue<KIND>(a, q, pw + 16 * i, h, qsum);
     }
   }
 }
 
-// Columns that the epilogue writes: a checkpoint's padding too.
-__host__ __device__ inline int join_cols(const LinArgs& a, int kind) {
-  return kind == LIN_FWD && a.ck.q ? a.ck.ld : a.P.extent;
-}
-
-// The partial products of a split reduction, joined in split order, and the epilogue: a wave
-// takes 16 rows x 32 columns in the lane order of the matrix instruction's output.
-template <int KIND>
+// The tiles that were computed in S parts: joined in order, then the epilogue.  A wave takes 512
+// columns of the tile's rows (TILE of them to a row).
+template <int KIND, int TILE>
 __global__ void __launch_bounds__(256) linear_join_kernel(LinArgs a) {
-  const int lane = threadIdx.x % kWave, c16 = lane & 15, g = lane >> 4;
-  const unsigned cols = (join_cols(a, KIND) + 31) / 32, rows = (a.Q.extent + 15) / 16;
-  const unsigned u = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + threadIdx.x / kWave);
-  if (u >= cols * rows) return;
-  const int q = (int)(u / cols) * 16 + c16, p = (int)(u % cols) * 32 + 4 * g;
-  f32x4 h[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+  const int rest = a.tiles_p * a.tiles_q - a.whole;
+  constexpr int kRows = 512 / TILE, kUnits = TILE / kRows;   // rows of a wave, waves of a tile
+  const int u = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + threadIdx.x / kWave);
+  const int t = u / kUnits, lane = threadIdx.x % kWave;
+  if (t >= rest) return;
+  const int r = (u % kUnits) * kRows + lane / (TILE / 8), k = lane % (TILE / 8) * 8;
+  int ip, iq;
+  tile_of(a.whole + t, a.tiles_p, a.tiles_q, ip, iq);
+  const int q = iq * TILE + r, c = ip * TILE + k;
+  float h[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   float qsum = 0.f;
-  if (q < a.Q.extent) {
-    for (int s = 0; s < a.S; ++s) {
-      const float* from = a.part + ((size_t)s * a.Q.extent + q) * a.ldp + p;
-      if (p < a.ldp) h[0] += *(const f32x4*)from;
-      if (p + 16 < a.ldp) h[1] += *(const f32x4*)(from + 16);
-      if (KIND == LIN_WGRAD) qsum += a.part_sum[(size_t)s * a.Q.extent + q];
+#pragma unroll 4
+  for (int s = 0; s < a.S; ++s) {
+    const size_t at = ((size_t)s * rest + t) * TILE + r;
+    const f32x4 lo = *(const f32x4*)(a.part + at * TILE + k), hi = *(const f32x4*)(a.part + at * TILE + k + 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      h[i] += lo[i];
+      h[4 + i] += hi[i];
     }
+    if (KIND == LIN_WGRAD) qsum += a.part_sum[at];
   }
-  epilogue<KIND>(a, q, p, h, qsum);
+  epilogue<KIND>(a, q, c, h, qsum);
 }
 
+// How a product is cut.  Tiles that fill whole rounds of the chip are computed by one workgroup
+// each; the tiles of the last, partly filled round in S parts of the reduction, so that the
+// chip is about full there too.
 struct Plan {
-  int S, steps, tiles_p, tiles_q;
+  int tile;              // 128 (four waves, two workgroups a CU) or 256 (eight waves, one)
+  int tiles_p, tiles_q, whole, S, steps;
+  double cost;           // microseconds, to compare plans
 };
 constexpr int kCUs = 256;
 
-// (sizes only: the workspace is asked for before the operands' alignment is known)
-Plan plan(int P, int Q, int K) {
+Plan plan_of(int P, int Q, int K, int tile) {
   Plan r;
-  r.tiles_p = (P + 127) / 128;
-  r.tiles_q = (Q + 127) / 128;
-  const int64_t tiles = (int64_t)r.tiles_p * r.tiles_q;
-  const int steps = (K + kBK - 1) / kBK;
-  // few tiles: the reduction is split until about every CU has a workgroup, in ranges of at
-  // least four steps
-  r.S = tiles >= kCUs ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(kCUs / tiles, steps / 4));
-  r.steps = (steps + r.S - 1) / r.S;
-  r.S = r.steps ? (steps + r.steps - 1) / r.steps : 1;
+  r.tile = tile;
+  r.tiles_p = (P + tile - 1) / tile;
+  r.tiles_q = (Q + tile - 1) / tile;
+  const int slots = tile == 128 ? 2 * kCUs : kCUs, all = (K + kBK - 1) / kBK;
+  const double step = tile == 128 ? 1.05 : 1.6;   // measured with the chip full (8192 cubed: 1.04 and 1.59)
+  const int64_t T = (int64_t)r.tiles_p * r.tiles_q;
+  const int rest = (int)(T % slots);
+  r.whole = (int)T;
+  r.S = 1;
+  r.steps = all;
+  r.cost = step * all * (double)((T + slots - 1) / slots);
+  for (int S = 2; rest && S <= 64 && rest * S <= slots && all / S >= 4; ++S) {
+    // the parts, their way through memory twice, and another launch
+    const int steps = (all + S - 1) / S, parts = (all + steps - 1) / steps;
+    const double cost = step * (all * (double)(T / slots) + steps) + 5.0 + 8e-6 * tile * tile * parts * rest / 4.0;
+    if (cost < r.cost) {
+      r.whole = (int)(T - rest);
+      r.S = parts;
+      r.steps = steps;
+      r.cost = cost;
+    }
+  }
   return r;
 }
 
+// (sizes only, and whether the operands allow direct loads: the large tile exists for those)
+Plan plan(int P, int Q, int K, bool direct) {
+  const Plan small = plan_of(P, Q, K, 128), large = plan_of(P, Q, K, 256);
+  return direct && large.cost < small.cost ? large : small;
+}
+
+size_t part_floats(const Plan& r) {
+  return r.S > 1 ? (size_t)r.S * (r.tiles_p * r.tiles_q - r.whole) * ((size_t)r.tile * r.tile + r.tile) : 0;
+}
+
 template <int KIND, bool PKS, int PSRC, bool QKS, int QSRC>
-void launch_one(const LinArgs& a, hipStream_t st) {
-  linear_kernel<KIND, 2, 2, 4, 4, PKS, PSRC, QKS, QSRC><<<a.tiles_p * a.tiles_q * a.S, 256, 0, st>>>(a);
-  if (a.S > 1) {
-    const unsigned units = (unsigned)((join_cols(a, KIND) + 31) / 32) * (unsigned)((a.Q.extent + 15) / 16);
-    linear_join_kernel<KIND><<<(units + 3) / 4, 256, 0, st>>>(a);
+void launch_one(const LinArgs& a, int tile, hipStream_t st) {
+  const unsigned rest = a.tiles_p * a.tiles_q - a.whole, grid = a.whole + rest * a.S;
+  if constexpr (PSRC != SRC_ANY && QSRC == SRC_DIRECT) {
+    if (tile == 256) {
+      linear_kernel<KIND, 2, 4, 8, 4, PKS, PSRC, QKS, QSRC><<<grid, 512, 0, st>>>(a);
+      if (rest) linear_join_kernel<KIND, 256><<<rest * 32, 256, 0, st>>>(a);
+      return;
+    }
   }
+  linear_kernel<KIND, 2, 2, 4, 4, PKS, PSRC, QKS, QSRC><<<grid, 256, 0, st>>>(a);
+  if (rest) linear_join_kernel<KIND, 128><<<rest * 8, 256, 0, st>>>(a);
 }
 
 // Direct loads move 8 elements at a time: along the reduction (KC) or the output (KS).
@@ -462,30 +605,29 @@ bool direct_ok(const LinOp& o, int contiguous) {
 
 }  // namespace
 
-size_t lin_part_floats(int kind, int P, int Q, int K) {
-  const Plan r = plan(P, Q, K);
-  if (r.S <= 1) return 0;
-  const size_t ldp = (P + 3) / 4 * 4;
-  return (size_t)r.S * Q * ldp + (kind == LIN_WGRAD ? (size_t)r.S * Q : 0);
+size_t lin_part_floats(int P, int Q, int K) {
+  return std::max(part_floats(plan(P, Q, K, true)), part_floats(plan(P, Q, K, false)));
 }
 
 void launch_linear(int kind, LinArgs a, hipStream_t st) {
-  const Plan r = plan(a.P.extent, a.Q.extent, a.K);
-  a.S = r.S; a.steps = r.steps; a.tiles_p = r.tiles_p; a.tiles_q = r.tiles_q;
-  a.ldp = (a.P.extent + 3) / 4 * 4;
-  a.part_sum = a.part ? a.part + (size_t)a.S * a.Q.extent * a.ldp : nullptr;
+  const bool pk = kind == LIN_FWD, qk = kind != LIN_WGRAD;   // contiguous along the reduction
+  const bool q_direct = direct_ok(a.Q, qk ? a.K : a.Q.extent);
+  const bool direct = q_direct && (!a.P.p || direct_ok(a.P, pk ? a.K : a.P.extent));
+  const Plan r = plan(a.P.extent, a.Q.extent, a.K, direct);
+  a.tiles_p = r.tiles_p; a.tiles_q = r.tiles_q; a.whole = r.whole; a.S = r.S; a.steps = r.steps;
+  a.part_sum = r.S > 1 ? a.part + (size_t)r.S * (r.tiles_p * r.tiles_q - r.whole) * r.tile * r.tile : nullptr;
   if (kind == LIN_FWD) {
-    if (direct_ok(a.P, a.K) && direct_ok(a.Q, a.K)) launch_one<LIN_FWD, false, SRC_DIRECT, false, SRC_DIRECT>(a, st);
-    else launch_one<LIN_FWD, false, SRC_ANY, false, SRC_ANY>(a, st);
+    if (direct) launch_one<LIN_FWD, false, SRC_DIRECT, false, SRC_DIRECT>(a, r.tile, st);
+    else launch_one<LIN_FWD, false, SRC_ANY, false, SRC_ANY>(a, r.tile, st);
   } else if (kind == LIN_DGRAD) {
-    if (direct_ok(a.P, a.P.extent) && direct_ok(a.Q, a.K)) launch_one<LIN_DGRAD, true, SRC_DIRECT, false, SRC_DIRECT>(a, st);
-    else launch_one<LIN_DGRAD, true, SRC_ANY, false, SRC_ANY>(a, st);
+    if (direct) launch_one<LIN_DGRAD, true, SRC_DIRECT, false, SRC_DIRECT>(a, r.tile, st);
+    else launch_one<LIN_DGRAD, true, SRC_ANY, false, SRC_ANY>(a, r.tile, st);
   } else if (!a.P.p) {
-    if (direct_ok(a.Q, a.Q.extent)) launch_one<LIN_WGRAD, true, SRC_CKPT, true, SRC_DIRECT>(a, st);
-    else launch_one<LIN_WGRAD, true, SRC_CKPT, true, SRC_ANY>(a, st);
+    if (direct) launch_one<LIN_WGRAD, true, SRC_CKPT, true, SRC_DIRECT>(a, r.tile, st);
+    else launch_one<LIN_WGRAD, true, SRC_CKPT, true, SRC_ANY>(a, r.tile, st);
   } else {
-    if (direct_ok(a.P, a.P.extent) && direct_ok(a.Q, a.Q.extent)) launch_one<LIN_WGRAD, true, SRC_DIRECT, true, SRC_DIRECT>(a, st);
-    else launch_one<LIN_WGRAD, true, SRC_ANY, true, SRC_ANY>(a, st);
+    if (direct) launch_one<LIN_WGRAD, true, SRC_DIRECT, true, SRC_DIRECT>(a, r.tile, st);
+    else launch_one<LIN_WGRAD, true, SRC_ANY, true, SRC_ANY>(a, r.tile, st);
   }
 }
 

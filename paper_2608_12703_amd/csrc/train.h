@@ -7,21 +7,18 @@
 namespace ad {
 
 // A matrix of float32 or bf16 rows.  vec: 8 columns at a multiple of 8 are whole and 16-byte
-// aligned; vec4: 4 columns at a multiple of 4 are aligned to the size of four elements.
+// aligned.
 struct DMat {
   void* p;
   int64_t ld;
-  int bf16, vec, vec4;
+  int bf16, vec;
 };
 
-// A vector of parameters (LayerNorm gain, bias): float32 or bf16.
+// A vector of parameters (LayerNorm gain, bias): float32 or bf16.  vec: 16-byte aligned.
 struct DVec {
   const void* p;
-  int bf16;
+  int bf16, vec;
 };
-__device__ __forceinline__ float ld_vec(const DVec& v, int i) {
-  return v.bf16 ? bf16_to_f32(((const uint16_t*)v.p)[i]) : ((const float*)v.p)[i];
-}
 
 // 8-bit checkpoint rows: q [rows][ld], scale [rows][ld / 32], ld a multiple of 128.
 struct DCkpt {
@@ -94,52 +91,26 @@ __device__ __forceinline__ void store8(const DMat& m, size_t row, int c, int col
   }
 }
 
-// The same for four columns.
-__device__ __forceinline__ f32x4 load4(const DMat& m, size_t row, int c, int cols) {
-  f32x4 v = {0.f, 0.f, 0.f, 0.f};
-  if (m.bf16) {
-    const uint16_t* p = (const uint16_t*)m.p + row * m.ld + c;
-    if (m.vec4 && c + 3 < cols) {
-      const uint2 u = *(const uint2*)p;
-      v = f32x4{__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
-                __uint_as_float(u.y & 0xffff0000u)};
-    } else {
+// Elements c .. c + 7 of a parameter vector of n (0 from n on).
+__device__ __forceinline__ void load_vec8(const DVec& g, int c, int n, float (&v)[8]) {
+  if (g.vec && c + 8 <= n) {
+    if (g.bf16) {
+      const uint4 u = *(const uint4*)((const uint16_t*)g.p + c);
+      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (c + i < cols) v[i] = bf16_to_f32(p[i]);
+      for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      }
+    } else {
+      const float4 a = *(const float4*)((const float*)g.p + c), b = *(const float4*)((const float*)g.p + c + 4);
+      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+      v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
     }
   } else {
-    const float* p = (const float*)m.p + row * m.ld + c;
-    if (m.vec4 && c + 3 < cols) {
-      v = *(const f32x4*)p;
-    } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (c + i < cols) v[i] = p[i];
-    }
-  }
-  return v;
-}
-
-__device__ __forceinline__ void store4(const DMat& m, size_t row, int c, int cols, f32x4 v) {
-  if (m.bf16) {
-    uint16_t* p = (uint16_t*)m.p + row * m.ld + c;
-    if (m.vec4 && c + 3 < cols) {
-      *(uint2*)p = uint2{f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3])};
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (c + i < cols) p[i] = f32_to_bf16(v[i]);
-    }
-  } else {
-    float* p = (float*)m.p + row * m.ld + c;
-    if (m.vec4 && c + 3 < cols) {
-      *(f32x4*)p = v;
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (c + i < cols) p[i] = v[i];
-    }
+    for (int i = 0; i < 8; ++i)
+      v[i] = c + i >= n ? 0.f : g.bf16 ? bf16_to_f32(((const uint16_t*)g.p)[c + i]) : ((const float*)g.p)[c + i];
   }
 }
 
@@ -166,15 +137,15 @@ __device__ __forceinline__ uint32_t pack_bytes(uint32_t a, uint32_t b, uint32_t 
 }
 // (s = 255: infinity, and every q of the group is 0, so the product is NaN)
 __device__ __forceinline__ float ckpt_two(uint32_t s) { return __uint_as_float(s << 23); }
-template <int I>
-__device__ __forceinline__ float ckpt_int(uint32_t w) {
-  return (float)((int32_t)(w << (24 - 8 * I)) >> 24);
-}
+// Four values q * two: the bytes with their sign bit turned are q + 128 unsigned, which converts
+// in one instruction, and (q + 128) two - 128 two is exact.
 __device__ __forceinline__ void ckpt_value4(uint32_t w, float two, float (&v)[4]) {
-  v[0] = ckpt_int<0>(w) * two;
-  v[1] = ckpt_int<1>(w) * two;
-  v[2] = ckpt_int<2>(w) * two;
-  v[3] = ckpt_int<3>(w) * two;
+  const uint32_t u = w ^ 0x80808080u;
+  const float low = -128.f * two;
+  v[0] = fmaf((float)(u & 0xffu), two, low);
+  v[1] = fmaf((float)((u >> 8) & 0xffu), two, low);
+  v[2] = fmaf((float)((u >> 16) & 0xffu), two, low);
+  v[3] = fmaf((float)(u >> 24), two, low);
 }
 __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
@@ -214,11 +185,27 @@ __device__ __forceinline__ void ckpt_load8(const DCkpt& k, size_t row, int c, fl
 
 // ----------------------------------------------------------------- GELU
 
-__device__ __forceinline__ float gelu_value(float h) { return 0.5f * h * (1.0f + erff(h * 0.70710678118654752f)); }
-// d/dh (h Phi(h)) = Phi(h) + h phi(h)
-__device__ __forceinline__ float gelu_slope(float h) {
-  return 0.5f * (1.0f + erff(h * 0.70710678118654752f)) + h * (0.39894228040143268f * __expf(-0.5f * h * h));
+// Phi(h) and e = exp(-h^2 / 2), from erf's rational approximation in Abramowitz and Stegun, Handbook of
+// Mathematical Functions, 7.1.26 (absolute error 1.5e-7 in erf): for x = |h| / sqrt(2),
+//   1 - erf(x) = (a1 t + a2 t^2 + a3 t^3 + a4 t^4 + a5 t^5) exp(-x^2),  t = 1 / (1 + p x).
+// One exponential serves the value and the slope; erff() alone takes about three times as long,
+// and the epilogues that call this are as long as a quarter of their product.
+struct Normal {
+  float cdf, e;
+};
+__device__ __forceinline__ Normal normal(float h) {
+  const float e = __builtin_amdgcn_exp2f(h * h * -0.72134752044448170f);          // -log2(e) / 2
+  const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(h), 0.23164189f, 1.0f));        // p / sqrt(2)
+  float q = fmaf(t, 1.061405429f, -1.453152027f);
+  q = fmaf(q, t, 1.421413741f);
+  q = fmaf(q, t, -0.284496736f);
+  q = fmaf(q, t, 0.254829592f);
+  const float tail = 0.5f * q * t * e;
+  return Normal{h >= 0.f ? 1.0f - tail : tail, e};
 }
+__device__ __forceinline__ float gelu_value(float h) { return h * normal(h).cdf; }
+// d/dh (h Phi(h)) = Phi(h) + h phi(h)
+__device__ __forceinline__ float gelu_slope(float h, Normal n) { return fmaf(h, 0.39894228040143268f * n.e, n.cdf); }
 
 // ----------------------------------------------------------------- launchers
 
@@ -259,11 +246,11 @@ enum LinKind : int { LIN_FWD = 0, LIN_DGRAD = 1, LIN_WGRAD = 2 };
 struct LinArgs {
   LinOp P, Q;
   int K;
-  int S, steps;          // splits of the reduction and 64-wide steps of each (set by the launcher)
-  int tiles_p, tiles_q;
-  float* part;           // S > 1: [S][Q][ldp] partial products, then (wgrad) [S][Q] row sums of dy
+  // set by the launcher: the tiles, how many of them are computed whole, and the parts of the
+  // reduction (of `steps` 64-wide steps each) that the others are computed in
+  int tiles_p, tiles_q, whole, S, steps;
+  float* part;           // S > 1: partial tiles [S][tiles - whole], then (wgrad) their rows' sums of dy
   float* part_sum;
-  int ldp;
   // epilogue
   DVec bias, gain, shift;
   int gelu, accumulate;
@@ -272,7 +259,7 @@ struct LinArgs {
   float* dbias;
 };
 // Floats of workspace of a product with these extents.
-size_t lin_part_floats(int kind, int P, int Q, int K);
+size_t lin_part_floats(int P, int Q, int K);
 void launch_linear(int kind, LinArgs a, hipStream_t st);
 
 }  // namespace ad

@@ -76,11 +76,10 @@ ad::DMat mat(const ad_mat* m, int32_t cols) {
   d.bf16 = m->dtype == AD_BF16;
   const uintptr_t p = (uintptr_t)m->data;
   d.vec = p % 16 == 0 && m->ld % (d.bf16 ? 8 : 4) == 0 && cols % 8 == 0;
-  d.vec4 = p % (d.bf16 ? 8 : 16) == 0 && m->ld % 4 == 0;
   return d;
 }
 
-ad::DVec vec(const void* p, int32_t dtype) { return ad::DVec{p, dtype == AD_BF16}; }
+ad::DVec vec(const void* p, int32_t dtype) { return ad::DVec{p, dtype == AD_BF16, (uintptr_t)p % 16 == 0}; }
 
 ad::DCkpt ckpt(const ad_ckpt* k, int32_t cols) {
   return k ? ad::DCkpt{k->q, k->scale, ad::ckpt_ld(cols)} : ad::DCkpt{nullptr, nullptr, ad::ckpt_ld(cols)};
@@ -94,7 +93,7 @@ size_t ln_bwd_bytes(int32_t rows, int32_t cols) {
 size_t linear_bytes(int kind, int32_t rows, int32_t n, int32_t k) {
   const int P = kind == ad::LIN_FWD ? n : k, Q = kind == ad::LIN_WGRAD ? n : rows,
             K = kind == ad::LIN_FWD ? k : kind == ad::LIN_DGRAD ? n : rows;
-  return Q > 0 ? align256(4 * ad::lin_part_floats(kind, P, Q, K)) : 0;
+  return Q > 0 ? align256(4 * ad::lin_part_floats(P, Q, K)) : 0;
 }
 ad_status linear_space(int kind, int32_t rows, int32_t n, int32_t k, size_t* bytes) {
   if (!bytes) return bad("NULL argument");

@@ -152,9 +152,16 @@ def ptr(t) -> int | None:
     return None if t is None else t.data_ptr()
 
 
+# the current stream's handle without a Stream object around it (3 us a call, as long as a launch)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def stream_handle(stream=None) -> int:
-    s = torch.cuda.current_stream() if stream is None else stream
-    return s.cuda_stream
+    if stream is not None:
+        return stream.cuda_stream
+    if _raw_stream is not None:
+        return _raw_stream(torch.cuda.current_device())
+    return torch.cuda.current_stream().cuda_stream
 
 
 def model_desc(cfg, max_pos=448, max_frames=1500) -> ModelDesc:
@@ -296,50 +303,59 @@ def draft_input(model: Model, w_fuse, b_fuse, w_in, b_in, batch: int, taps, hidd
 _DTYPE = {torch.float32: AD_F32, torch.bfloat16: AD_BF16}
 
 
-def _on_device(name: str, t):
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+def _device(name: str, t) -> int:
+    """The current GPU, where the call's tensors have to be."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} is on {t.device}, not on the current GPU")
+    return torch.cuda.current_device()
+
+
+def _on_device(name: str, t, dev: int):
+    if t.get_device() != dev:
         raise ValueError(f"{name} is on {t.device}, not on the current GPU")
 
 
-def _mat(name: str, t, rows: int, cols: int):
+def _mat(name: str, t, rows: int, cols: int, dev: int):
     """A [rows][cols] float32 or bf16 tensor with adjacent columns as an ad_mat (None for None)."""
     if t is None:
         return None
-    _on_device(name, t)
-    if tuple(t.shape) != (rows, cols):
+    _on_device(name, t, dev)
+    if t.shape != (rows, cols):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(rows, cols)}")
-    if t.dtype not in _DTYPE:
+    dtype = _DTYPE.get(t.dtype)
+    if dtype is None:
         raise ValueError(f"{name} is {t.dtype}, expected float32 or bfloat16")
-    if cols > 1 and t.stride(1) != 1:
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
         raise ValueError(f"{name}: the columns of a row must be adjacent")
-    return ctypes.byref(Mat(t.data_ptr(), cols if rows <= 1 else t.stride(0), _DTYPE[t.dtype]))
+    return ctypes.byref(Mat(t.data_ptr(), cols if rows <= 1 else ld, dtype))
 
 
-def _vec(name: str, t, n: int, dtypes=(torch.float32, torch.bfloat16)):
+def _vec(name: str, t, n: int, dev: int, dtypes=(torch.float32, torch.bfloat16)):
     """The address of a contiguous [n] tensor (None for None)."""
     if t is None:
         return None
-    _on_device(name, t)
-    if tuple(t.shape) != (n,) or t.dtype not in dtypes or not t.is_contiguous():
+    _on_device(name, t, dev)
+    if t.shape != (n,) or t.dtype not in dtypes or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous [{n}] tensor of {' or '.join(map(str, dtypes))}")
     return t.data_ptr()
 
 
-def _floats(name: str, t, n: int):
-    return _vec(name, t, n, (torch.float32,))
+def _floats(name: str, t, n: int, dev: int):
+    return None if t is None else _vec(name, t, n, dev, (torch.float32,))
 
 
-def _params(a_name: str, a, b_name: str, b, n: int):
+def _params(a_name: str, a, b_name: str, b, n: int, dev: int):
     """Two parameter vectors of one dtype: their addresses and that dtype."""
     if a is not None and b is not None and a.dtype != b.dtype:
         raise ValueError(f"{a_name} and {b_name} must have the same dtype")
-    return _vec(a_name, a, n), _vec(b_name, b, n), AD_F32 if a is None else _DTYPE[a.dtype]
+    return _vec(a_name, a, n, dev), _vec(b_name, b, n, dev), AD_F32 if a is None else _DTYPE[a.dtype]
 
 
-def _space(workspace):
+def _space(workspace, dev: int):
     if workspace is None:
         return None, 0
-    _on_device("workspace", workspace)
+    _on_device("workspace", workspace, dev)
     if not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous")
     return workspace.data_ptr(), workspace.numel() * workspace.element_size()
@@ -364,11 +380,11 @@ class Ckpt:
                    torch.empty(rows, ld // 32, dtype=torch.uint8, device=device), cols)
 
 
-def _ckpt(name: str, k, rows: int, cols: int):
+def _ckpt(name: str, k, rows: int, cols: int, dev: int):
     if k is None:
         return None
-    _on_device(name, k.q)
-    _on_device(name, k.scale)
+    _on_device(name, k.q, dev)
+    _on_device(name, k.scale, dev)
     if (k.rows, k.cols) != (rows, cols):
         raise ValueError(f"{name} holds {(k.rows, k.cols)}, expected {(rows, cols)}")
     return ctypes.byref(CkptView(k.q.data_ptr(), k.scale.data_ptr()))
@@ -376,26 +392,26 @@ def _ckpt(name: str, k, rows: int, cols: int):
 
 def ckpt_pack(x, ckpt: Ckpt, stream=None):
     """ckpt <- the rows of x in 8 bits."""
-    rows, cols = ckpt.rows, ckpt.cols
-    check(LIB.ad_ckpt_pack(rows, cols, _mat("x", x, rows, cols), _ckpt("ckpt", ckpt, rows, cols),
+    rows, cols, dev = ckpt.rows, ckpt.cols, _device("ckpt", ckpt.q)
+    check(LIB.ad_ckpt_pack(rows, cols, _mat("x", x, rows, cols, dev), _ckpt("ckpt", ckpt, rows, cols, dev),
                            stream_handle(stream)), "ad_ckpt_pack")
 
 
 def ckpt_unpack(ckpt: Ckpt, out, act: int = ACT_NONE, stream=None):
     """out <- act(the values of ckpt)."""
-    rows, cols = ckpt.rows, ckpt.cols
-    check(LIB.ad_ckpt_unpack(rows, cols, _ckpt("ckpt", ckpt, rows, cols), act, _mat("out", out, rows, cols),
+    rows, cols, dev = ckpt.rows, ckpt.cols, _device("ckpt", ckpt.q)
+    check(LIB.ad_ckpt_unpack(rows, cols, _ckpt("ckpt", ckpt, rows, cols, dev), act, _mat("out", out, rows, cols, dev),
                              stream_handle(stream)), "ad_ckpt_unpack")
 
 
 def layer_norm(x, gain, bias, y, mean=None, rstd=None, xhat: Ckpt | None = None, stream=None):
     """LayerNorm of the rows of x into y (ad.h: ad_layer_norm); mean, rstd and xhat (the
     normalised rows in 8 bits) are kept for the backward pass when given."""
-    rows, cols = x.shape
-    g, b, dt = _params("gain", gain, "bias", bias, cols)
-    check(LIB.ad_layer_norm(rows, cols, _mat("x", x, rows, cols), g, b, dt, _mat("y", y, rows, cols),
-                            _floats("mean", mean, rows), _floats("rstd", rstd, rows),
-                            _ckpt("xhat", xhat, rows, cols), stream_handle(stream)), "ad_layer_norm")
+    (rows, cols), dev = x.shape, _device("x", x)
+    g, b, dt = _params("gain", gain, "bias", bias, cols, dev)
+    check(LIB.ad_layer_norm(rows, cols, _mat("x", x, rows, cols, dev), g, b, dt, _mat("y", y, rows, cols, dev),
+                            _floats("mean", mean, rows, dev), _floats("rstd", rstd, rows, dev),
+                            _ckpt("xhat", xhat, rows, cols, dev), stream_handle(stream)), "ad_layer_norm")
 
 
 def _workspace_size(name: str, *sizes) -> int:
@@ -412,14 +428,15 @@ def layer_norm_backward(dy, x, mean, rstd, xhat, gain, dres, dx, dx_copy, dgain,
                         accumulate: bool = False, stream=None):
     """LayerNorm's gradients (ad.h: ad_layer_norm_backward) from x and mean, or from the
     checkpoint xhat (x and mean None); dres, dx_copy and the pair dgain, dbias may be None."""
-    rows, cols = dy.shape
-    ws, ws_bytes = _space(workspace)
-    g, _, dt = _params("gain", gain, "gain", None, cols)
+    (rows, cols), dev = dy.shape, _device("dy", dy)
+    ws, ws_bytes = _space(workspace, dev)
+    g, _, dt = _params("gain", gain, "gain", None, cols, dev)
     check(LIB.ad_layer_norm_backward(
-        rows, cols, _mat("dy", dy, rows, cols), _mat("x", x, rows, cols), _floats("mean", mean, rows),
-        _floats("rstd", rstd, rows), _ckpt("xhat", xhat, rows, cols), g, dt, _mat("dres", dres, rows, cols),
-        _mat("dx", dx, rows, cols), _mat("dx_copy", dx_copy, rows, cols), _floats("dgain", dgain, cols),
-        _floats("dbias", dbias, cols), int(accumulate), ws, ws_bytes, stream_handle(stream)),
+        rows, cols, _mat("dy", dy, rows, cols, dev), _mat("x", x, rows, cols, dev),
+        _floats("mean", mean, rows, dev), _floats("rstd", rstd, rows, dev), _ckpt("xhat", xhat, rows, cols, dev),
+        g, dt, _mat("dres", dres, rows, cols, dev), _mat("dx", dx, rows, cols, dev),
+        _mat("dx_copy", dx_copy, rows, cols, dev), _floats("dgain", dgain, cols, dev),
+        _floats("dbias", dbias, cols, dev), int(accumulate), ws, ws_bytes, stream_handle(stream)),
         "ad_layer_norm_backward")
 
 
@@ -430,12 +447,12 @@ def linear_workspace_size(rows: int, n: int, k: int) -> int:
 def linear(x, w, bias, act: int, residual, y, pre, pre_ckpt, workspace, stream=None):
     """y = act(x w^T + bias) + residual (ad.h: ad_linear); bias, residual and the kept
     pre-activation (pre in bf16, or pre_ckpt in 8 bits) may be None."""
-    (rows, k), n = x.shape, w.shape[0]
-    ws, ws_bytes = _space(workspace)
-    b, _, dt = _params("bias", bias, "bias", None, n)
-    check(LIB.ad_linear(rows, n, k, _mat("x", x, rows, k), _mat("w", w, n, k), b, dt, act,
-                        _mat("residual", residual, rows, n), _mat("y", y, rows, n), _mat("pre", pre, rows, n),
-                        _ckpt("pre_ckpt", pre_ckpt, rows, n), ws, ws_bytes, stream_handle(stream)), "ad_linear")
+    (rows, k), n, dev = x.shape, w.shape[0], _device("x", x)
+    ws, ws_bytes = _space(workspace, dev)
+    b, _, dt = _params("bias", bias, "bias", None, n, dev)
+    check(LIB.ad_linear(rows, n, k, _mat("x", x, rows, k, dev), _mat("w", w, n, k, dev), b, dt, act,
+                        _mat("residual", residual, rows, n, dev), _mat("y", y, rows, n, dev),
+                        _mat("pre", pre, rows, n, dev), _ckpt("pre_ckpt", pre_ckpt, rows, n, dev), ws, ws_bytes, stream_handle(stream)), "ad_linear")
 
 
 def linear_dgrad_workspace_size(rows: int, n: int, k: int) -> int:
@@ -444,11 +461,11 @@ def linear_dgrad_workspace_size(rows: int, n: int, k: int) -> int:
 
 def linear_dgrad(dy, w, act: int, pre, pre_ckpt, dx, act_out, workspace, stream=None):
     """dx = (dy w) act'(pre) (ad.h: ad_linear_dgrad); act_out, when given, receives act(pre)."""
-    (rows, n), k = dy.shape, w.shape[1]
-    ws, ws_bytes = _space(workspace)
-    check(LIB.ad_linear_dgrad(rows, n, k, _mat("dy", dy, rows, n), _mat("w", w, n, k), act,
-                              _mat("pre", pre, rows, k), _ckpt("pre_ckpt", pre_ckpt, rows, k),
-                              _mat("dx", dx, rows, k), _mat("act_out", act_out, rows, k), ws, ws_bytes,
+    (rows, n), k, dev = dy.shape, w.shape[1], _device("dy", dy)
+    ws, ws_bytes = _space(workspace, dev)
+    check(LIB.ad_linear_dgrad(rows, n, k, _mat("dy", dy, rows, n, dev), _mat("w", w, n, k, dev), act,
+                              _mat("pre", pre, rows, k, dev), _ckpt("pre_ckpt", pre_ckpt, rows, k, dev),
+                              _mat("dx", dx, rows, k, dev), _mat("act_out", act_out, rows, k, dev), ws, ws_bytes,
                               stream_handle(stream)), "ad_linear_dgrad")
 
 
@@ -459,12 +476,12 @@ def linear_wgrad_workspace_size(rows: int, n: int, k: int) -> int:
 def linear_wgrad(dy, x, x_ckpt, gain, shift, dw, dbias, workspace, accumulate: bool = False, stream=None):
     """dw = dy^T x and dbias = the column sums of dy (ad.h: ad_linear_wgrad), x in bf16 or as the
     checkpoint x_ckpt, of which gain and shift make the input; dbias may be None."""
-    (rows, n), k = dy.shape, dw.shape[1]
-    ws, ws_bytes = _space(workspace)
-    g, s, dt = _params("gain", gain, "shift", shift, k)
-    check(LIB.ad_linear_wgrad(rows, n, k, _mat("dy", dy, rows, n), _mat("x", x, rows, k),
-                              _ckpt("x_ckpt", x_ckpt, rows, k), g, s, dt, _mat("dw", dw, n, k),
-                              _floats("dbias", dbias, n), int(accumulate), ws, ws_bytes, stream_handle(stream)),
+    (rows, n), k, dev = dy.shape, dw.shape[1], _device("dy", dy)
+    ws, ws_bytes = _space(workspace, dev)
+    g, s, dt = _params("gain", gain, "shift", shift, k, dev)
+    check(LIB.ad_linear_wgrad(rows, n, k, _mat("dy", dy, rows, n, dev), _mat("x", x, rows, k, dev),
+                              _ckpt("x_ckpt", x_ckpt, rows, k, dev), g, s, dt, _mat("dw", dw, n, k, dev),
+                              _floats("dbias", dbias, n, dev), int(accumulate), ws, ws_bytes, stream_handle(stream)),
           "ad_linear_wgrad")
 
 

@@ -37,51 +37,79 @@ __device__ __forceinline__ float row_total(float v, float* red) {
   return v;
 }
 
-// W: waves per row (1 or 4).  The statistics are two passes over the registers: the mean,
-// then the squared deviations from it (no cancellation of large means).
-template <int J, int W>
+// W: waves per row (1 or 4), R rows at a time, VEC: every matrix and parameter allows whole vectors.
+// The statistics are two passes over the registers: the mean, then the squared deviations from it
+// (no cancellation of large means).  Columns past the row's end hold 0 throughout: with whole
+// vectors a lane's piece is all in or all out, so it deviates from 0 instead of the mean.
+template <int J, int W, int R, bool VEC>
 __global__ void __launch_bounds__(256) ln_fwd_kernel(LnFwdArgs a) {
   __shared__ float red[4];
   const int t = W == 1 ? threadIdx.x % kWave : threadIdx.x;
-  const int first = W == 1 ? blockIdx.x * 4 + threadIdx.x / kWave : blockIdx.x, stride = W == 1 ? gridDim.x * 4 : gridDim.x;
+  const int first = R * (W == 1 ? blockIdx.x * 4 + threadIdx.x / kWave : blockIdx.x);
+  const int stride = R * (W == 1 ? gridDim.x * 4 : gridDim.x);
   constexpr int kStep = 8 * kWave * W;
+  const float inv_n = 1.0f / (float)a.cols;
   // (with W == 4 every wave of the workgroup has the same rows, so the barriers are met by all)
-  for (int row = first; row < a.rows; row += stride) {
-    float x[J][8];
+  for (int row0 = first; row0 < a.rows; row0 += stride) {
+    float x[R][J][8], mean[R], rstd[R];
 #pragma unroll
-    for (int j = 0; j < J; ++j) load8(a.x, row, 8 * t + j * kStep, a.cols, x[j]);
-    float s = 0.f;
+    for (int u = 0; u < R; ++u)
 #pragma unroll
-    for (int j = 0; j < J; ++j)
+      for (int j = 0; j < J; ++j) load8<VEC>(a.x, min(row0 + u, a.rows - 1), 8 * t + j * kStep, a.cols, x[u][j]);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s += x[j][i];
-    const float mean = row_total<W>(s, red) / (float)a.cols;
-    float v = 0.f;
+    for (int u = 0; u < R; ++u) {
+      float s = 0.f;
 #pragma unroll
-    for (int j = 0; j < J; ++j)
+      for (int j = 0; j < J; ++j)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        x[j][i] -= mean;
-        if (8 * t + j * kStep + i < a.cols) v = fmaf(x[j][i], x[j][i], v);
+        for (int i = 0; i < 8; ++i) s += x[u][j][i];
+      mean[u] = row_total<W>(s, red) * inv_n;
+    }
+#pragma unroll
+    for (int u = 0; u < R; ++u) {
+      float v = 0.f;
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        const float m = 8 * t + j * kStep < a.cols ? mean[u] : 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          x[u][j][i] = VEC || 8 * t + j * kStep + i < a.cols ? x[u][j][i] - m : 0.f;
+          v = fmaf(x[u][j][i], x[u][j][i], v);
+        }
       }
-    const float rstd = 1.0f / sqrtf(row_total<W>(v, red) / (float)a.cols + kEps);
+      rstd[u] = 1.0f / sqrtf(row_total<W>(v, red) * inv_n + kEps);
+    }
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       const int c = 8 * t + j * kStep;
       float g[8], b[8], y[8];
-      load_vec8(a.gain, c, a.cols, g);
-      load_vec8(a.bias, c, a.cols, b);
+      load_vec8<VEC>(a.gain, c, a.cols, g);
+      load_vec8<VEC>(a.bias, c, a.cols, b);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        x[j][i] = c + i < a.cols ? x[j][i] * rstd : 0.f;
-        y[i] = fmaf(x[j][i], g[i], b[i]);
+      for (int u = 0; u < R; ++u) {
+        if (R > 1 && row0 + u >= a.rows) break;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          x[u][j][i] *= rstd[u];
+          y[i] = fmaf(x[u][j][i], g[i], b[i]);
+        }
+        if (!VEC && rstd[u] != rstd[u])   // a NaN row: its padding is 0 all the same
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[u][j][i] = c + i < a.cols ? x[u][j][i] : 0.f;
+        if (VEC && c >= a.cols)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[u][j][i] = 0.f;
+        store8<VEC>(a.y, row0 + u, c, a.cols, y);
+        if (a.xhat.q) ckpt_store8(a.xhat, row0 + u, c, x[u][j]);
       }
-      store8(a.y, row, c, a.cols, y);
-      if (a.xhat.q) ckpt_store8(a.xhat, row, c, x[j]);
     }
     if (t == 0) {
-      if (a.mean) a.mean[row] = mean;
-      if (a.rstd) a.rstd[row] = rstd;
+#pragma unroll
+      for (int u = 0; u < R; ++u)
+        if (row0 + u < a.rows) {
+          if (a.mean) a.mean[row0 + u] = mean[u];
+          if (a.rstd) a.rstd[row0 + u] = rstd[u];
+        }
     }
   }
 }
@@ -89,7 +117,7 @@ __global__ void __launch_bounds__(256) ln_fwd_kernel(LnFwdArgs a) {
 // A workgroup walks rows g, g + G, ... and keeps the sums for dgain and dbias of its columns
 // in registers; they leave once, as one of G partial rows.  The order of the sums depends
 // on the number of rows and columns only.
-template <int J, int W>
+template <int J, int W, bool VEC>
 __global__ void __launch_bounds__(256) ln_bwd_kernel(LnBwdArgs a) {
   __shared__ float red[4];
   constexpr int kStep = 8 * kWave * W;
@@ -98,7 +126,7 @@ __global__ void __launch_bounds__(256) ln_bwd_kernel(LnBwdArgs a) {
   float g[J][8], dg[J][8], db[J][8];
 #pragma unroll
   for (int j = 0; j < J; ++j) {
-    load_vec8(a.gain, 8 * t + j * kStep, a.cols, g[j]);
+    load_vec8<VEC>(a.gain, 8 * t + j * kStep, a.cols, g[j]);
 #pragma unroll
     for (int i = 0; i < 8; ++i) dg[j][i] = db[j][i] = 0.f;
   }
@@ -106,14 +134,14 @@ __global__ void __launch_bounds__(256) ln_bwd_kernel(LnBwdArgs a) {
   for (int row = first; row < a.rows; row += stride) {
     float xh[J][8], dy[J][8];
 #pragma unroll
-    for (int j = 0; j < J; ++j) load8(a.dy, row, 8 * t + j * kStep, a.cols, dy[j]);
+    for (int j = 0; j < J; ++j) load8<VEC>(a.dy, row, 8 * t + j * kStep, a.cols, dy[j]);
     const float rstd = a.rstd[row];
     if (a.xhat.q) {
 #pragma unroll
       for (int j = 0; j < J; ++j) ckpt_load8(a.xhat, row, 8 * t + j * kStep, xh[j]);
     } else {
 #pragma unroll
-      for (int j = 0; j < J; ++j) load8(a.x, row, 8 * t + j * kStep, a.cols, xh[j]);
+      for (int j = 0; j < J; ++j) load8<VEC>(a.x, row, 8 * t + j * kStep, a.cols, xh[j]);
       const float mean = a.mean[row];
 #pragma unroll
       for (int j = 0; j < J; ++j)
@@ -125,9 +153,8 @@ __global__ void __launch_bounds__(256) ln_bwd_kernel(LnBwdArgs a) {
     for (int j = 0; j < J; ++j)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        // (a column past the last has dy = 0 and gain 0, and its xhat is not used)
-        const bool in = 8 * t + j * kStep + i < a.cols;
-        xh[j][i] = in ? xh[j][i] : 0.f;
+        // (past the last column dy and the gain are 0; xhat may be anything there)
+        if (!VEC) xh[j][i] = 8 * t + j * kStep + i < a.cols ? xh[j][i] : 0.f;
         dg[j][i] = fmaf(dy[j][i], xh[j][i], dg[j][i]);
         db[j][i] += dy[j][i];
         dy[j][i] *= g[j][i];
@@ -143,12 +170,12 @@ __global__ void __launch_bounds__(256) ln_bwd_kernel(LnBwdArgs a) {
       for (int i = 0; i < 8; ++i) d[i] = rstd * (dy[j][i] - m - xh[j][i] * mx);
       if (a.dres.p) {
         float r[8];
-        load8(a.dres, row, c, a.cols, r);
+        load8<VEC>(a.dres, row, c, a.cols, r);
 #pragma unroll
         for (int i = 0; i < 8; ++i) d[i] += r[i];
       }
-      store8(a.dx, row, c, a.cols, d);
-      if (a.copy.p) store8(a.copy, row, c, a.cols, d);
+      store8<VEC>(a.dx, row, c, a.cols, d);
+      if (a.copy.p) store8<VEC>(a.copy, row, c, a.cols, d);
     }
   }
   if (!a.dgain) return;
@@ -163,40 +190,57 @@ __global__ void __launch_bounds__(256) ln_bwd_kernel(LnBwdArgs a) {
       }
   } else {
     // the four waves hold the same columns: they add in turn
-    __shared__ float sum[2][J * kStep];
+    __shared__ float4 sum[2][J * kStep / 4];
     for (int v = 0; v < 4; ++v) {
       if (w == v) {
 #pragma unroll
         for (int j = 0; j < J; ++j)
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int c = 8 * t + j * kStep + i;
-            sum[0][c] = v ? sum[0][c] + dg[j][i] : dg[j][i];
-            sum[1][c] = v ? sum[1][c] + db[j][i] : db[j][i];
+          for (int h = 0; h < 2; ++h) {
+            const int c = (8 * t + j * kStep) / 4 + h;
+            float4 p = {dg[j][4 * h], dg[j][4 * h + 1], dg[j][4 * h + 2], dg[j][4 * h + 3]};
+            float4 q = {db[j][4 * h], db[j][4 * h + 1], db[j][4 * h + 2], db[j][4 * h + 3]};
+            if (v) {
+              const float4 o = sum[0][c], r = sum[1][c];
+              p = float4{o.x + p.x, o.y + p.y, o.z + p.z, o.w + p.w};
+              q = float4{r.x + q.x, r.y + q.y, r.z + q.z, r.w + q.w};
+            }
+            sum[0][c] = p;
+            sum[1][c] = q;
           }
       }
       __syncthreads();
     }
     for (int c = threadIdx.x; c < a.cols; c += 256) {
-      part[c] = sum[0][c];
-      part[a.cols + c] = sum[1][c];
+      part[c] = ((const float*)sum[0])[c];
+      part[a.cols + c] = ((const float*)sum[1])[c];
     }
   }
 }
 
-// dgain | dbias: column c of [groups][2 cols] partial rows, 16 columns x 16 row slices a
+// dgain | dbias: column c of [groups][2 cols] partial rows, 16 columns x 64 row slices a
 // workgroup, the slices joined in order.
-__global__ void __launch_bounds__(256) ln_param_kernel(int groups, int cols, const float* part, float* dgain,
-                                                       float* dbias, int accumulate) {
-  __shared__ float red[16][17];
+__global__ void __launch_bounds__(1024) ln_param_kernel(int groups, int cols, const float* part, float* dgain,
+                                                        float* dbias, int accumulate) {
+  __shared__ float red[64][17];
   const int x = threadIdx.x % 16, y = threadIdx.x / 16, c = blockIdx.x * 16 + x;
   float s = 0.f;
   if (c < 2 * cols)
-    for (int r = y; r < groups; r += 16) s += part[(size_t)r * 2 * cols + c];
+#pragma unroll 8
+    for (int r = y; r < groups; r += 64) s += part[(size_t)r * 2 * cols + c];
   red[y][x] = s;
   __syncthreads();
+  if (y < 8) {
+    s = red[8 * y][x];
+#pragma unroll
+    for (int r = 1; r < 8; ++r) s += red[8 * y + r][x];
+  }
+  __syncthreads();
+  if (y < 8) red[y][x] = s;
+  __syncthreads();
   if (y == 0 && c < 2 * cols) {
-    for (int r = 1; r < 16; ++r) s += red[r][x];
+#pragma unroll
+    for (int r = 1; r < 8; ++r) s += red[r][x];
     float* o = c < cols ? dgain + c : dbias + (c - cols);
     *o = accumulate ? *o + s : s;
   }
@@ -240,15 +284,32 @@ void by_width(int cols, A&&... args) {
   else F<4, 4>::run(args...);
 }
 
+bool whole(const DMat& m) { return !m.p || m.vec; }
+bool whole(const DVec& v, int cols) { return v.vec && cols % 8 == 0; }
+
+constexpr int kTwoRows = 8192;   // rows from which a wave takes two at a time (with fewer, one keeps more waves busy)
+
 template <int J, int W>
 struct Fwd {
+  template <int R, bool VEC>
+  static void go(const LnFwdArgs& a, hipStream_t st) {
+    const int rows = (a.rows + R - 1) / R;
+    ln_fwd_kernel<J, W, R, VEC><<<grid_of(W == 1 ? (rows + 3) / 4 : rows), 256, 0, st>>>(a);
+  }
   static void run(const LnFwdArgs& a, hipStream_t st) {
-    ln_fwd_kernel<J, W><<<grid_of(W == 1 ? (a.rows + 3) / 4 : a.rows), 256, 0, st>>>(a);
+    const bool vec = whole(a.x) && whole(a.y) && whole(a.gain, a.cols) && whole(a.bias, a.cols);
+    if (!vec) go<1, false>(a, st);
+    else if (W == 1 && a.rows >= kTwoRows) go<W == 1 ? 2 : 1, true>(a, st);
+    else go<1, true>(a, st);
   }
 };
 template <int J, int W>
 struct Bwd {
-  static void run(const LnBwdArgs& a, int groups, hipStream_t st) { ln_bwd_kernel<J, W><<<groups, 256, 0, st>>>(a); }
+  static void run(const LnBwdArgs& a, int groups, hipStream_t st) {
+    const bool vec = whole(a.dy) && whole(a.x) && whole(a.dres) && whole(a.dx) && whole(a.copy) && whole(a.gain, a.cols);
+    if (vec) ln_bwd_kernel<J, W, true><<<groups, 256, 0, st>>>(a);
+    else ln_bwd_kernel<J, W, false><<<groups, 256, 0, st>>>(a);
+  }
 };
 
 }  // namespace
@@ -266,7 +327,7 @@ void launch_layer_norm_backward(const LnBwdArgs& a, hipStream_t st) {
   const int groups = ln_bwd_groups(a.rows, a.cols);
   if (groups > 0) by_width<Bwd>(a.cols, a, groups, st);
   if (a.dgain)
-    ln_param_kernel<<<(2 * a.cols + 15) / 16, 256, 0, st>>>(groups, a.cols, a.part, a.dgain, a.dbias, a.accumulate);
+    ln_param_kernel<<<(2 * a.cols + 15) / 16, 1024, 0, st>>>(groups, a.cols, a.part, a.dgain, a.dbias, a.accumulate);
 }
 
 void launch_ckpt_pack(int rows, int cols, const DMat& x, const DCkpt& k, hipStream_t st) {

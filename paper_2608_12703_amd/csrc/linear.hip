@@ -173,14 +173,16 @@ struct Loader {
     k0 += kBK;
   }
 
-  // registers into LDS
+  // registers into LDS, one half of them
+  template <int HALF>
   __device__ __forceinline__ void commit(uint4* lds) {
+    static_assert(N % 4 == 0);
     if constexpr (SRC == SRC_ANY) {
 #pragma unroll
-      for (int j = 0; j < N; ++j) lds[(w * N + j) * 64 + lane] = reg[j];
+      for (int j = HALF * N / 2; j < (HALF + 1) * N / 2; ++j) lds[(w * N + j) * 64 + lane] = reg[j];
     } else if constexpr (SRC == SRC_CKPT) {
 #pragma unroll
-      for (int j = 0; j < N / 2; ++j) {
+      for (int j = HALF * N / 4; j < (HALF + 1) * N / 4; ++j) {
         int row, r;
         place_ck(j, row, r);
         const int t = row / 16, u = (t & ~7) | ((t & 7) ^ ks_swz(r));
@@ -238,24 +240,74 @@ struct Reader {
   }
 };
 
-// Columns c .. c + 7 of output row q (four neighbouring lanes hold one checkpoint group of 32; every
-// lane of the wave calls this).  qsum: wgrad's sum of dy for row q.
+// What an epilogue reads from memory for 8 columns of a row, requested before it is needed (whole
+// vectors only): the residual, the pre-activation, or the gradient that is added to.
+struct Extra {
+  u32x4 lo, hi;
+  uint32_t scale;
+};
+__device__ __forceinline__ void request8(const DMat& m, size_t row, int c, Extra& e) {
+  if (m.bf16) {
+    e.lo = *(const u32x4*)((const uint16_t*)m.p + row * m.ld + c);
+  } else {
+    const float* p = (const float*)m.p + row * m.ld + c;
+    e.lo = *(const u32x4*)p;
+    e.hi = *(const u32x4*)(p + 4);
+  }
+}
+__device__ __forceinline__ void received8(const DMat& m, const Extra& e, float (&v)[8]) {
+  if (m.bf16) {
+    widen8(e.lo, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[i] = __uint_as_float(e.lo[i]);
+      v[4 + i] = __uint_as_float(e.hi[i]);
+    }
+  }
+}
 template <int KIND>
-__device__ __forceinline__ void epilogue(const LinArgs& a, int q, int c, float (&h)[8], float qsum) {
+__device__ __forceinline__ Extra request(const LinArgs& a, int q, int c) {
+  Extra e{};
+  if (q >= a.Q.extent || c >= a.P.extent) return e;
+  if constexpr (KIND == LIN_FWD) {
+    if (a.res.p) request8(a.res, q, c, e);
+  } else if constexpr (KIND == LIN_DGRAD) {
+    if (a.gelu) {
+      if (a.ck.q) {
+        const u32x2 w = *(const u32x2*)(a.ck.q + (size_t)q * a.ck.ld + c);
+        e.lo[0] = w[0];
+        e.lo[1] = w[1];
+        e.scale = a.ck.scale[(size_t)q * (a.ck.ld / kCkptGroup) + c / kCkptGroup];
+      } else {
+        request8(a.pre, q, c, e);
+      }
+    }
+  } else {
+    if (a.accumulate) request8(a.out, q, c, e);
+  }
+  return e;
+}
+
+// Columns c .. c + 7 of output row q (four neighbouring lanes hold one checkpoint group of 32; every
+// lane of the wave calls this).  qsum: wgrad's sum of dy for row q.  VEC: every matrix and
+// parameter allows whole vectors, and `e` is what request() asked for.
+template <int KIND, bool VEC>
+__device__ __forceinline__ void epilogue(const LinArgs& a, int q, int c, float (&h)[8], float qsum, const Extra& e) {
   const int cols = a.P.extent;
   const bool row = q < a.Q.extent;
   if constexpr (KIND == LIN_FWD) {
     float b[8];
     if (a.bias.p) {
-      load_vec8(a.bias, c, cols, b);
+      load_vec8<VEC>(a.bias, c, cols, b);
 #pragma unroll
       for (int i = 0; i < 8; ++i) h[i] += b[i];
     }
-    if (a.pre.p && row) store8(a.pre, q, c, cols, h);
+    if (a.pre.p && row) store8<VEC>(a.pre, q, c, cols, h);
     if (a.ck.q) {
       float z[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) z[i] = c + i < cols ? h[i] : 0.f;   // (padding is written as 0)
+      for (int i = 0; i < 8; ++i) z[i] = c + (VEC ? 0 : i) < cols ? h[i] : 0.f;   // (padding is written as 0)
       ckpt_store8(a.ck, q, row ? c : a.ck.ld, z);
     }
     if (!row) return;
@@ -263,42 +315,49 @@ __device__ __forceinline__ void epilogue(const LinArgs& a, int q, int c, float (
 #pragma unroll
       for (int i = 0; i < 8; ++i) h[i] = gelu_value(h[i]);
     if (a.res.p) {
-      load8(a.res, q, c, cols, b);
+      if (VEC) received8(a.res, e, b);
+      else load8(a.res, q, c, cols, b);
 #pragma unroll
       for (int i = 0; i < 8; ++i) h[i] += b[i];
     }
-    store8(a.out, q, c, cols, h);
+    store8<VEC>(a.out, q, c, cols, h);
   } else if constexpr (KIND == LIN_DGRAD) {
     if (!row) return;
     if (a.gelu) {
       float x[8];
-      if (a.ck.q) ckpt_load8(a.ck, q, c, x);
-      else load8(a.pre, q, c, cols, x);
+      if (a.ck.q) {
+        if (VEC) ckpt_value8(u32x2{e.lo[0], e.lo[1]}, e.scale, x);
+        else ckpt_load8(a.ck, q, c, x);
+      } else {
+        if (VEC) received8(a.pre, e, x);
+        else load8(a.pre, q, c, cols, x);
+      }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const Normal n = normal(x[i]);
         h[i] *= gelu_slope(x[i], n);
         x[i] *= n.cdf;
       }
-      if (a.act_out.p) store8(a.act_out, q, c, cols, x);
+      if (a.act_out.p) store8<VEC>(a.act_out, q, c, cols, x);
     }
-    store8(a.out, q, c, cols, h);
+    store8<VEC>(a.out, q, c, cols, h);
   } else {
     if (!row) return;
     if (a.gain.p) {
       float g[8], b[8];
-      load_vec8(a.gain, c, cols, g);
-      load_vec8(a.shift, c, cols, b);
+      load_vec8<VEC>(a.gain, c, cols, g);
+      load_vec8<VEC>(a.shift, c, cols, b);
 #pragma unroll
       for (int i = 0; i < 8; ++i) h[i] = fmaf(h[i], g[i], b[i] * qsum);
     }
     if (a.accumulate) {
       float o[8];
-      load8(a.out, q, c, cols, o);
+      if (VEC) received8(a.out, e, o);
+      else load8(a.out, q, c, cols, o);
 #pragma unroll
       for (int i = 0; i < 8; ++i) h[i] += o[i];
     }
-    store8(a.out, q, c, cols, h);
+    store8<VEC>(a.out, q, c, cols, h);
     if (a.dbias && c == 0) a.dbias[q] = a.accumulate ? a.dbias[q] + qsum : qsum;
   }
 }
@@ -400,6 +459,7 @@ __global__ void __launch_bounds__(WP* WQ* kWave) linear_kernel(LinArgs a) {
 #pragma unroll
       for (int j = 0; j < NS; ++j) csum[j] = mfma_bf16(ones, fq[j], csum[j]);
   };
+  constexpr int kConvert = PSRC == SRC_CKPT ? 3 : 0;
   constexpr std::integral_constant<int, 0> upper{};
   constexpr std::integral_constant<int, 1> lower{};
   constexpr int kReadsP = H * (PKS ? 2 : 1), kReadsQ = TQ * (QKS ? 2 : 1);
@@ -413,8 +473,10 @@ __global__ void __launch_bounds__(WP* WQ* kWave) linear_kernel(LinArgs a) {
     bf16x8 pu[H], pl[H], qa[TQ], qb[TQ];
     lp.issue(p0);
     lq.issue(q0);
-    lp.commit(p0);
-    lq.commit(q0);
+    lp.template commit<0>(p0);
+    lp.template commit<1>(p0);
+    lq.template commit<0>(q0);
+    lq.template commit<1>(q0);
     sync();
     if (steps > 1) {
       lp.issue(p1);
@@ -432,16 +494,19 @@ __global__ void __launch_bounds__(WP* WQ* kWave) linear_kernel(LinArgs a) {
       read_q(qb, qc, 1);
       read_p(pu, pc, 1, 0);
       multiply(pl, qa, lower);
-      interleave<kReadsP + kReadsQ, H * TQ>();
+      if (next) {
+        lp.template commit<0>(pn);
+        lq.template commit<0>(qn);
+      }
+      interleave<kReadsP + kReadsQ, H * TQ, kConvert>();
       __builtin_amdgcn_sched_barrier(0);
       read_p(pl, pc, 1, 1);
       multiply(pu, qb, upper);
       if (next) {
-        lp.commit(pn);
-        lq.commit(qn);
+        lp.template commit<1>(pn);
+        lq.template commit<1>(qn);
       }
-      if constexpr (PSRC == SRC_DIRECT && QSRC == SRC_DIRECT) interleave<kReadsP, H * TQ>();
-      else if constexpr (PSRC == SRC_CKPT) interleave<kReadsP, H * TQ, 6>();
+      interleave<kReadsP, H * TQ, kConvert>();
     };
     // all of a stage but the last one; `more`: the stage after the next exists
     auto stage = [&](uint4* pc, uint4* qc, uint4* pn, uint4* qn, bool more) {
@@ -480,18 +545,23 @@ __global__ void __launch_bounds__(WP* WQ* kWave) linear_kernel(LinArgs a) {
   constexpr int CPR = 2 * TP, kPiece = 16 * TP * 4;   // 8-column chunks in a row; 16-byte chunks in a piece
   uint4* mine = w < NW / 2 ? p0 + w * kPiece : p1 + (w - NW / 2) * kPiece;
   static_assert(NW / 2 * kPiece <= RP * 8);
+  constexpr bool VEC = PSRC != SRC_ANY && QSRC != SRC_ANY;
+  constexpr int NI = 16 * CPR / kWave;
+  const int r0 = lane / CPR, k = lane % CPR, c = ip * RP + wp * TP * 16 + 8 * k;
 #pragma unroll
   for (int j = 0; j < TQ; ++j) {
+    const int q_tile = wq * TQ + slot(j), q0r = iq * RQ + q_tile * 16 + r0;
+    Extra ex[NI];
+    if (VEC && !part)
+#pragma unroll
+      for (int it = 0; it < NI; ++it) ex[it] = request<KIND>(a, q0r + it * (kWave / CPR), c);
 #pragma unroll
     for (int i = 0; i < TP; ++i)
       mine[c16 * 4 * TP + ((4 * i + g) ^ c16)] = __builtin_bit_cast(uint4, acc[i][j]);
-    const int q_tile = wq * TQ + slot(j);
-#pragma unroll 1
-    for (int it = 0; it < 16 * CPR / kWave; ++it) {
-      const int r = it * (kWave / CPR) + lane / CPR, k = lane % CPR;
+    auto item = [&](int it, const Extra& e) {
+      const int r = it * (kWave / CPR) + r0, q = q0r + it * (kWave / CPR);
       const f32x4 lo = __builtin_bit_cast(f32x4, mine[r * 4 * TP + ((2 * k) ^ r)]);
       const f32x4 hi = __builtin_bit_cast(f32x4, mine[r * 4 * TP + ((2 * k + 1) ^ r)]);
-      const int q = iq * RQ + q_tile * 16 + r, c = ip * RP + wp * TP * 16 + 8 * k;
       const float qsum = KIND == LIN_WGRAD ? sums[q_tile * 16 + r] : 0.f;
       if (part) {
         // tile [RQ][RP] of split, tile, then its rows' sums
@@ -502,8 +572,15 @@ __global__ void __launch_bounds__(WP* WQ* kWave) linear_kernel(LinArgs a) {
         if (KIND == LIN_WGRAD && wp == 0 && k == 0) a.part_sum[at * RQ + q_tile * 16 + r] = qsum;
       } else {
         float h[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        epilogue<KIND>(a, q, c, h, qsum);
+        epilogue<KIND, VEC>(a, q, c, h, qsum, e);
       }
+    };
+    if constexpr (VEC) {
+#pragma unroll
+      for (int it = 0; it < NI; ++it) item(it, ex[it]);
+    } else {
+#pragma unroll 1
+      for (int it = 0; it < NI; ++it) item(it, Extra{});
     }
   }
 }
@@ -534,7 +611,7 @@ __global__ void __launch_bounds__(256) linear_join_kernel(LinArgs a) {
     }
     if (KIND == LIN_WGRAD) qsum += a.part_sum[at];
   }
-  epilogue<KIND>(a, q, c, h, qsum);
+  epilogue<KIND, false>(a, q, c, h, qsum, Extra{});
 }
 
 // How a product is cut.  Tiles that fill whole rounds of the chip are computed by one workgroup
@@ -598,6 +675,9 @@ void launch_one(const LinArgs& a, int tile, hipStream_t st) {
   if (rest) linear_join_kernel<KIND, 128><<<rest * 8, 256, 0, st>>>(a);
 }
 
+bool whole(const DMat& m) { return !m.p || m.vec; }
+bool whole(const DVec& v, int cols) { return !v.p || (v.vec && cols % 8 == 0); }
+
 // Direct loads move 8 elements at a time: along the reduction (KC) or the output (KS).
 bool direct_ok(const LinOp& o, int contiguous) {
   return (uintptr_t)o.p % 16 == 0 && o.ld % 8 == 0 && contiguous % 8 == 0;
@@ -612,7 +692,10 @@ size_t lin_part_floats(int P, int Q, int K) {
 void launch_linear(int kind, LinArgs a, hipStream_t st) {
   const bool pk = kind == LIN_FWD, qk = kind != LIN_WGRAD;   // contiguous along the reduction
   const bool q_direct = direct_ok(a.Q, qk ? a.K : a.Q.extent);
-  const bool direct = q_direct && (!a.P.p || direct_ok(a.P, pk ? a.K : a.P.extent));
+  // (the kernels of direct operands move whole vectors in their epilogues too)
+  const int cols = a.P.extent;
+  const bool direct = q_direct && (!a.P.p || direct_ok(a.P, pk ? a.K : cols)) && whole(a.out) && whole(a.res) &&
+                      whole(a.pre) && whole(a.act_out) && whole(a.bias, cols) && whole(a.gain, cols) && whole(a.shift, cols);
   const Plan r = plan(a.P.extent, a.Q.extent, a.K, direct);
   a.tiles_p = r.tiles_p; a.tiles_q = r.tiles_q; a.whole = r.whole; a.S = r.S; a.steps = r.steps;
   a.part_sum = r.S > 1 ? a.part + (size_t)r.S * (r.tiles_p * r.tiles_q - r.whole) * r.tile * r.tile : nullptr;

@@ -34,29 +34,41 @@ constexpr int kLnMaxCols = 8192;
 
 // ----------------------------------------------------------------- elements
 
-// Columns c .. c + 7 of a row (columns from `cols` on read as 0).
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// eight bf16 of 16 bytes
+__device__ __forceinline__ void widen8(u32x4 u, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = __uint_as_float(u[i] << 16);
+    v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+  }
+}
+
+// Columns c .. c + 7 of a row (columns from `cols` on read as 0).  VEC: the caller knows that m.vec.
+template <bool VEC = false>
 __device__ __forceinline__ void load8(const DMat& m, size_t row, int c, int cols, float (&v)[8]) {
   if (m.bf16) {
     const uint16_t* p = (const uint16_t*)m.p + row * m.ld + c;
-    if (m.vec) {
-      const uint4 u = c < cols ? *(const uint4*)p : uint4{0, 0, 0, 0};
-      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(w[i] << 16);
-        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-      }
+    if (VEC || m.vec) {
+      u32x4 u = {0, 0, 0, 0};
+      if (c < cols) u = *(const u32x4*)p;
+      widen8(u, v);
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? bf16_to_f32(p[i]) : 0.f;
     }
   } else {
     const float* p = (const float*)m.p + row * m.ld + c;
-    if (m.vec) {
-      const float4 z = {0.f, 0.f, 0.f, 0.f};
-      const float4 a = c < cols ? *(const float4*)p : z, b = c < cols ? *(const float4*)(p + 4) : z;
-      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-      v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    if (VEC || m.vec) {
+      f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
+      if (c < cols) {
+        a = *(const f32x4*)p;
+        b = *(const f32x4*)(p + 4);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? p[i] : 0.f;
@@ -64,12 +76,13 @@ __device__ __forceinline__ void load8(const DMat& m, size_t row, int c, int cols
   }
 }
 
+template <bool VEC = false>
 __device__ __forceinline__ void store8(const DMat& m, size_t row, int c, int cols, const float (&v)[8]) {
   if (m.bf16) {
     uint16_t* p = (uint16_t*)m.p + row * m.ld + c;
-    if (m.vec) {
+    if (VEC || m.vec) {
       if (c < cols)
-        *(uint4*)p = uint4{f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]),
+        *(u32x4*)p = u32x4{f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]),
                            f32x2_to_bf16x2(v[4], v[5]), f32x2_to_bf16x2(v[6], v[7])};
     } else {
 #pragma unroll
@@ -78,10 +91,10 @@ __device__ __forceinline__ void store8(const DMat& m, size_t row, int c, int col
     }
   } else {
     float* p = (float*)m.p + row * m.ld + c;
-    if (m.vec) {
+    if (VEC || m.vec) {
       if (c < cols) {
-        *(float4*)p = float4{v[0], v[1], v[2], v[3]};
-        *(float4*)(p + 4) = float4{v[4], v[5], v[6], v[7]};
+        *(f32x4*)p = f32x4{v[0], v[1], v[2], v[3]};
+        *(f32x4*)(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
       }
     } else {
 #pragma unroll
@@ -91,21 +104,20 @@ __device__ __forceinline__ void store8(const DMat& m, size_t row, int c, int col
   }
 }
 
-// Elements c .. c + 7 of a parameter vector of n (0 from n on).
+// Elements c .. c + 7 of a parameter vector of n (0 from n on).  VEC: the caller knows that g.vec and
+// n % 8 == 0.
+template <bool VEC = false>
 __device__ __forceinline__ void load_vec8(const DVec& g, int c, int n, float (&v)[8]) {
-  if (g.vec && c + 8 <= n) {
-    if (g.bf16) {
-      const uint4 u = *(const uint4*)((const uint16_t*)g.p + c);
-      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+  if (VEC && c >= n) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(w[i] << 16);
-        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-      }
+    for (int i = 0; i < 8; ++i) v[i] = 0.f;
+  } else if (VEC || (g.vec && c + 8 <= n)) {
+    if (g.bf16) {
+      widen8(*(const u32x4*)((const uint16_t*)g.p + c), v);
     } else {
-      const float4 a = *(const float4*)((const float*)g.p + c), b = *(const float4*)((const float*)g.p + c + 4);
-      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-      v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+      const f32x4 a = *(const f32x4*)((const float*)g.p + c), b = *(const f32x4*)((const float*)g.p + c + 4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
     }
   } else {
 #pragma unroll
@@ -167,20 +179,23 @@ __device__ __forceinline__ void ckpt_store8(const DCkpt& k, size_t row, int c, c
     if (c % kCkptGroup == 0) k.scale[row * (size_t)(k.ld / kCkptGroup) + c / kCkptGroup] = (uint8_t)s;
   }
 }
-// Columns c .. c + 7 of a checkpoint row (0 past the padded row).
-__device__ __forceinline__ void ckpt_load8(const DCkpt& k, size_t row, int c, float (&v)[8]) {
-  uint2 w = {0, 0};
-  uint32_t s = 1;
-  if (c < k.ld) {
-    w = *(const uint2*)(k.q + row * k.ld + c);
-    s = k.scale[row * (size_t)(k.ld / kCkptGroup) + c / kCkptGroup];
-  }
+__device__ __forceinline__ void ckpt_value8(u32x2 w, uint32_t s, float (&v)[8]) {
   const float two = ckpt_two(s);
   float a[4], b[4];
-  ckpt_value4(w.x, two, a);
-  ckpt_value4(w.y, two, b);
+  ckpt_value4(w[0], two, a);
+  ckpt_value4(w[1], two, b);
 #pragma unroll
   for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
+}
+// Columns c .. c + 7 of a checkpoint row (0 past the padded row).
+__device__ __forceinline__ void ckpt_load8(const DCkpt& k, size_t row, int c, float (&v)[8]) {
+  u32x2 w = {0, 0};
+  uint32_t s = 1;
+  if (c < k.ld) {
+    w = *(const u32x2*)(k.q + row * k.ld + c);
+    s = k.scale[row * (size_t)(k.ld / kCkptGroup) + c / kCkptGroup];
+  }
+  ckpt_value8(w, s, v);
 }
 
 // ----------------------------------------------------------------- GELU

@@ -404,6 +404,94 @@ def test_linear_wgrad(rows, n, k, pad, shift, src):
     assert torch.equal(dw.get(), one.double().cpu()), "the same call gives the same bits"
 
 
+# Products of several rounds of large tiles, the last round's in parts of the reduction (289 and 300
+# tiles of 256 x 256), tiles past the last row and column, a reduction that ends inside a stage;
+# the references are float64 products on the GPU.
+LARGE = [(4104, 4200, 200, 0, 0), (4500, 1032, 4104, 8, 8), (1000, 4104, 4360, 0, 0)]
+
+
+@pytest.mark.parametrize("rows,n,k,pad,shift", LARGE)
+@pytest.mark.parametrize("act,rt,yt,keep", [(ad.ACT_GELU, None, BF16, "ckpt"), (ad.ACT_NONE, F32, F32, None),
+                                            (ad.ACT_GELU, BF16, F32, "bf16")])
+def test_linear_large(rows, n, k, pad, shift, act, rt, yt, keep):
+    g = torch.Generator(device="cuda").manual_seed(rows + n + k)
+    rnd = lambda *s, scale=1.0, dtype=BF16: (torch.randn(*s, generator=g, device="cuda") * scale).to(dtype)  # noqa: E731
+    x, w, bias = rnd(rows, k), rnd(n, k, scale=k ** -0.5), rnd(n)
+    res = None if rt is None else rnd(rows, n, dtype=rt)
+    y = Out(rows, n, yt, pad, shift)
+    pre = Out(rows, n, BF16, pad, shift) if keep == "bf16" else None
+    kept = ad.Ckpt.empty(rows, n) if keep == "ckpt" else None
+    ad.linear(_put(x, pad, shift), _put(w, pad, shift), bias, act, None if res is None else _put(res, pad, shift), y.t,
+              None if pre is None else pre.t, kept, _space(ad.linear_workspace_size(rows, n, k)))
+    h = x.double() @ w.double().t().contiguous() + bias.double()
+    th = 2 * k * U * (x.double().abs() @ w.double().abs().t().contiguous()) + 2 * U * (h.abs() + bias.double().abs())
+    out, tol = (_gelu(h), 1.13 * th + h.abs() * (1e-7 + 8 * U)) if act == ad.ACT_GELU else (h, th)
+    if res is not None:
+        out = out + res.double()
+        tol = tol + 2 * U * (out.abs() + res.double().abs())
+    _near(y.get(), out.cpu(), (tol * 1.01 + out.abs() * _two(yt)).cpu(), "y")
+    if pre is not None:
+        _near(pre.get(), h.cpu(), (th * 1.01 + h.abs() * 2.0 ** -8).cpu(), "pre")
+    if kept is not None:
+        _check_ckpt(kept, h.cpu(), th.cpu(), "pre")
+
+
+@pytest.mark.parametrize("rows,n,k,pad,shift", LARGE)
+@pytest.mark.parametrize("src,ot,again", [("none", BF16, False), ("bf16", F32, True), ("ckpt", BF16, True)])
+def test_linear_dgrad_large(rows, n, k, pad, shift, src, ot, again):
+    g = torch.Generator(device="cuda").manual_seed(rows + n + k)
+    rnd = lambda *s, scale=1.0, dtype=BF16: (torch.randn(*s, generator=g, device="cuda") * scale).to(dtype)  # noqa: E731
+    n, k = k, n                    # the wide side is dx's
+    dy, w, h16 = rnd(rows, n), rnd(n, k, scale=n ** -0.5), rnd(rows, k, scale=2.0)
+    kept = None
+    h = h16.double()
+    if src == "ckpt":
+        kept, v = ad.Ckpt.empty(rows, k), torch.empty(rows, k, device="cuda")
+        ad.ckpt_pack(h16, kept)
+        ad.ckpt_unpack(kept, v)    # (exact, tested by itself)
+        h = v.double()
+    dx = Out(rows, k, ot, pad, shift)
+    act_out = Out(rows, k, BF16, pad, shift) if again else None
+    ad.linear_dgrad(_put(dy, pad, shift), _put(w, pad, shift), ad.ACT_NONE if src == "none" else ad.ACT_GELU,
+                    _put(h16, pad, shift) if src == "bf16" else None, kept, dx.t, act_out.t if again else None,
+                    _space(ad.linear_dgrad_workspace_size(rows, n, k)))
+    want, tol = dy.double() @ w.double(), 2 * n * U * (dy.double().abs() @ w.double().abs())
+    if src != "none":
+        s = _slope(h)
+        tol = tol * 1.13 + want.abs() * (1e-7 + 16 * U) + 2 * U * (want * s).abs()
+        want = want * s
+    _near(dx.get(), want.cpu(), (tol * 1.01 + want.abs() * _two(ot)).cpu(), "dx")
+    if again:
+        _near(act_out.get(), _gelu(h).cpu(), (h.abs() * 1e-7 + _gelu(h).abs() * (8 * U + 2.0 ** -8) + 1e-37).cpu(), "act_out")
+
+
+@pytest.mark.parametrize("rows,n,k,pad,shift", [(200, 4200, 4104, 0, 0), (4104, 1032, 4360, 8, 8), (9000, 1288, 1544, 0, 0)])
+@pytest.mark.parametrize("src", ["bf16", "ckpt", "affine"])
+def test_linear_wgrad_large(rows, n, k, pad, shift, src):
+    g = torch.Generator(device="cuda").manual_seed(rows + n + k)
+    rnd = lambda *s, scale=1.0, dtype=BF16: (torch.randn(*s, generator=g, device="cuda") * scale).to(dtype)  # noqa: E731
+    dy, x16, kept, gain, shift_v = rnd(rows, n), rnd(rows, k), None, None, None
+    x = mag = x16.double()
+    if src != "bf16":
+        kept, v = ad.Ckpt.empty(rows, k), torch.empty(rows, k, device="cuda")
+        ad.ckpt_pack(x16, kept)
+        ad.ckpt_unpack(kept, v)
+        x = mag = v.double()
+    if src == "affine":
+        gain, shift_v = 1 + rnd(k, scale=0.1), rnd(k)
+        x, mag = x * gain.double() + shift_v.double(), x.abs() * gain.double().abs() + shift_v.double().abs()
+    dw, dbias = Out(n, k, F32, pad, shift), torch.empty(n, device="cuda")
+    ws = _space(ad.linear_wgrad_workspace_size(rows, n, k))
+    args = (_put(dy, pad, shift), _put(x16, pad, shift) if kept is None else None, kept, gain, shift_v)
+    ad.linear_wgrad(*args, dw.t, dbias, ws)
+    d = dy.double().t().contiguous()
+    one = dw.t.clone()
+    _near(one.double().cpu(), (d @ x).cpu(), (2 * (rows + 4) * U * (d.abs() @ mag.abs())).cpu(), "dw")
+    _near(dbias.double().cpu(), d.sum(1).cpu(), (2 * (rows + 4) * U * d.abs().sum(1)).cpu(), "dbias")
+    ad.linear_wgrad(*args, dw.t, None, ws, accumulate=True)
+    assert torch.equal(dw.get(), (one + one).double().cpu())
+
+
 def test_rows_past_32_bit_offsets():
     """Rows whose elements lie past 2^31 of their matrix (and 2^32 bytes)."""
     rows, ld, n, k = 40000, 1 << 16, 72, 64

@@ -66,6 +66,7 @@ struct Loader {
   const char* base;       // the stage's first element
   const char* sbase;      // checkpoint: its scale
   int64_t left, sleft;    // KS: bytes from there to the end of the reduction's last row
+  uint32_t size;          // the descriptor's, for the stage being loaded
   uint32_t off[N], soff[SRC == SRC_CKPT ? N / 2 : 1];   // bytes
   uint4 reg[N];
   uint32_t sc[N];
@@ -120,33 +121,41 @@ struct Loader {
     }
   }
 
-  // stage at k0: into `lds` (direct), or into registers
-  __device__ __forceinline__ void issue(uint4* lds) {
-    if constexpr (SRC == SRC_DIRECT) {
-      if constexpr (KS) {
-        const uint32_t size = (uint32_t)min(left, (int64_t)kPastEnd);
+  // The stage at k0 into `lds` (direct) or into registers, in four parts between begin() and end().
+  // Past the end of the reduction a direct load moves nothing (its descriptor is empty), so that a
+  // wave's count of loads in flight does not depend on the stage.
+  __device__ __forceinline__ void begin() {
+    if constexpr (SRC == SRC_DIRECT && KS) {
+      size = (uint32_t)max(min(left, (int64_t)kPastEnd), (int64_t)0);
+    } else if constexpr (SRC == SRC_DIRECT) {
+      size = k0 < K ? kPastEnd : 0;
+      if (k0 + kBK > K) {   // the reduction ends in this stage
 #pragma unroll
-        for (int j = 0; j < N; ++j) buffer16(base, size, off[j], lds + (w * N + j) * 64);
-        base += 2 * kBK * o.ld;
-        left -= 2 * kBK * o.ld;
-      } else {
-        if (k0 + kBK > K) {   // the reduction ends in this stage
-#pragma unroll
-          for (int j = 0; j < N; ++j) {
-            int row, r;
-            place(j, row, r);
-            if (k0 + r >= K) off[j] = kPastEnd;
-          }
+        for (int j = 0; j < N; ++j) {
+          int row, r;
+          place(j, row, r);
+          if (k0 + r >= K) off[j] = kPastEnd;
         }
-#pragma unroll
-        for (int j = 0; j < N; ++j) buffer16(base, kPastEnd, off[j], lds + (w * N + j) * 64);
-        base += 2 * kBK;
       }
-    } else if constexpr (SRC == SRC_ANY) {
+    }
+  }
+  template <int PART>
+  __device__ __forceinline__ void part(uint4* lds) {
+    if constexpr (SRC == SRC_DIRECT) {
+#pragma unroll
+      for (int j = PART * N / 4; j < (PART + 1) * N / 4; ++j) buffer16(base, size, off[j], lds + (w * N + j) * 64);
+    } else if constexpr (SRC == SRC_ANY && PART == 0) {
+      if (k0 >= K) return;
+      // a stage inside the matrix in 16-byte loads of whatever alignment, others by elements
+      const bool inside = r0 + R <= o.extent && k0 + kBK <= K;
 #pragma unroll
       for (int j = 0; j < N; ++j) {
         int row, r;
         place(j, row, r);
+        if (inside) {
+          __builtin_memcpy(&reg[j], KS ? o.p + (size_t)(k0 + r) * o.ld + r0 + row : o.p + (size_t)(r0 + row) * o.ld + k0 + r, 16);
+          continue;
+        }
         uint32_t e[8];
         const int a = r0 + row, k = k0 + r;
 #pragma unroll
@@ -156,21 +165,39 @@ struct Loader {
         }
         reg[j] = uint4{e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16};
       }
-    } else {
+    } else if constexpr (SRC == SRC_CKPT && PART == 0) {
       // past the last row: q = 0, scale byte 0 (a scale of 0)
-      const __amdgpu_buffer_rsrc_t rq = descriptor(base, (uint32_t)min(left, (int64_t)kPastEnd));
-      const __amdgpu_buffer_rsrc_t rs = descriptor(sbase, (uint32_t)min(sleft, (int64_t)kPastEnd));
+      const __amdgpu_buffer_rsrc_t rq = descriptor(base, (uint32_t)max(min(left, (int64_t)kPastEnd), (int64_t)0));
+      const __amdgpu_buffer_rsrc_t rs = descriptor(sbase, (uint32_t)max(min(sleft, (int64_t)kPastEnd), (int64_t)0));
 #pragma unroll
       for (int j = 0; j < N / 2; ++j) {
         reg[j] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rq, off[j], 0, 0));
         sc[j] = __builtin_amdgcn_raw_buffer_load_b8(rs, soff[j], 0, 0);
       }
+    }
+  }
+  __device__ __forceinline__ void end() {
+    if constexpr (SRC == SRC_DIRECT) {
+      base += KS ? 2 * kBK * o.ld : (int64_t)(2 * kBK);
+      if (KS) left -= 2 * kBK * o.ld;
+    } else if constexpr (SRC == SRC_CKPT) {
       base += kBK * (int64_t)o.ck.ld;
       left -= kBK * (int64_t)o.ck.ld;
       sbase += kBK * (int64_t)(o.ck.ld / kCkptGroup);
       sleft -= kBK * (int64_t)(o.ck.ld / kCkptGroup);
     }
     k0 += kBK;
+  }
+  __device__ __forceinline__ void all(uint4* lds) {
+    part<0>(lds);
+    part<1>(lds);
+    part<2>(lds);
+    part<3>(lds);
+  }
+  __device__ __forceinline__ void issue(uint4* lds) {
+    begin();
+    all(lds);
+    end();
   }
 
   // registers into LDS, one half of them
@@ -376,15 +403,16 @@ __device__ __forceinline__ void tile_of(int t, int tp, int tq, int& ip, int& iq)
   ip = rest / h;
 }
 
-// The order inside a phase: its LDS reads spread between its products.
-// (VALU: and that many conversions of a checkpoint after each product)
-template <int READS, int PRODUCTS, int VALU = 0>
+// The order inside a phase: its LDS reads, and LOADS loads of a later stage, spread between its
+// products (VALU: and that many conversions of a checkpoint after each product).
+template <int READS, int PRODUCTS, int LOADS = 0, int VALU = 0, int I = 0>
 __device__ __forceinline__ void interleave() {
-#pragma unroll
-  for (int i = 0; i < READS; ++i) {
-    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);                   // an LDS read
+  if constexpr (I < READS) {
+    constexpr int kLoad = LOADS * (I + 1) / READS - LOADS * I / READS;
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);                                 // an LDS read
+    if constexpr (kLoad > 0) __builtin_amdgcn_sched_group_barrier(0x020, kLoad, 0);    // loads
     if constexpr (VALU == 0) {
-      __builtin_amdgcn_sched_group_barrier(0x008, PRODUCTS / READS, 0);  // products
+      __builtin_amdgcn_sched_group_barrier(0x008, PRODUCTS / READS, 0);                // products
     } else {
 #pragma unroll
       for (int j = 0; j < PRODUCTS / READS; ++j) {
@@ -392,19 +420,29 @@ __device__ __forceinline__ void interleave() {
         __builtin_amdgcn_sched_group_barrier(0x002, VALU, 0);
       }
     }
+    interleave<READS, PRODUCTS, LOADS, VALU, I + 1>();
   }
 }
 
-// WP x WQ waves of TP x TQ 16 x 16 tiles, two LDS stages.  A stage is two 32-wide steps of two phases
-// each (the upper and the lower half of the wave's P tiles).  While a wave multiplies in one
-// phase it reads the next one's operands, so no product waits for LDS.  The barrier falls before
-// the stage's last phase, when all of it is in registers and its LDS is free: the loads of the
-// stage after the next start there.
-template <int KIND, int WP, int WQ, int TP, int TQ, bool PKS, int PSRC, bool QKS, int QSRC>
+// The s_waitcnt immediate for at most n vector-memory operations outstanding and every LDS read done.
+constexpr int wait_for(int n) { return (n & 15) | ((n >> 4) << 14) | 0x0070; }
+
+// WP x WQ waves of TP x TQ 16 x 16 tiles, a ring of ST LDS stages (2 or 4; 2 where an operand goes
+// through registers).  A stage is two 32-wide steps of two phases each (the upper and the lower
+// half of the wave's P tiles).  While a wave multiplies in one phase it reads the next one's
+// operands, so no product waits for LDS.  The barrier falls before the stage's last phase, when all
+// of it is in registers and its LDS is free: the loads of the stage ST later start there.
+template <int KIND, int WP, int WQ, int TP, int TQ, int ST, bool PKS, int PSRC, bool QKS, int QSRC>
 __global__ void __launch_bounds__(WP* WQ* kWave) linear_kernel(LinArgs a) {
   constexpr int NW = WP * WQ, RP = WP * TP * 16, RQ = WQ * TQ * 16, NS = TQ / WP;
   static_assert(TP % 2 == 0 && TQ % WP == 0);
+  static_assert(ST == 2 || (ST == 4 && PSRC == SRC_DIRECT && QSRC == SRC_DIRECT));
+  // distinct objects, so that the compiler can tell a read of one stage from the direct loads that
+  // fill another
+  constexpr int kMore = ST > 2 ? 1 : 0;
   __shared__ uint4 p0[RP * 8], p1[RP * 8], q0[RQ * 8], q1[RQ * 8];
+  __shared__ uint4 p2[kMore * RP * 8 + 1 - kMore], p3[kMore * RP * 8 + 1 - kMore];
+  __shared__ uint4 q2[kMore * RQ * 8 + 1 - kMore], q3[kMore * RQ * 8 + 1 - kMore];
   __shared__ float sums[KIND == LIN_WGRAD ? RQ : 1];
   const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int wp = w % WP, wq = w / WP, c16 = lane & 15, g = lane >> 4;
@@ -463,11 +501,25 @@ __global__ void __launch_bounds__(WP* WQ* kWave) linear_kernel(LinArgs a) {
   constexpr std::integral_constant<int, 0> upper{};
   constexpr std::integral_constant<int, 1> lower{};
   constexpr int kReadsP = H * (PKS ? 2 : 1), kReadsQ = TQ * (QKS ? 2 : 1);
-  auto sync = [] {   // this wave's loads have landed and its LDS reads are in registers; then everyone's
-    __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt 0, lgkmcnt 0
+  // this wave's loads but the newest `stages` stages' have landed and its LDS reads are in
+  // registers; then everyone's
+  constexpr int kLoads = (RP + RQ) / 8 / NW;
+  static_assert(kLoads * (ST - 1) < 64);
+  auto sync = [](auto stages) {
+    __builtin_amdgcn_s_waitcnt(wait_for(kLoads * stages.value));
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
+  constexpr std::integral_constant<int, ST - 2> ahead{};
+  constexpr bool kDirect = PSRC == SRC_DIRECT && QSRC == SRC_DIRECT;
+  // A wave's loads of a stage.  With four stages they are spread over the four phases after the barrier
+  // that freed its LDS: issued together, they hold up the products behind them for as long as they
+  // take to be accepted (0.3 us a stage with one wave a SIMD).  With two stages they all start right
+  // after the barrier, to have the rest of a stage to arrive in: before the products of that
+  // phase, or between them in the weight gradient, which fits into its registers that way (eight
+  // waves of 256: 199 against 239 us for 14336 x 1280 x 5120).
+  constexpr bool kSpread = ST == 4, kBetween = !kSpread && kDirect && KIND == LIN_WGRAD;
+  constexpr int kPart = kSpread ? (RP + RQ) / 32 / NW : 0;
 
   if (steps > 0) {
     bf16x8 pu[H], pl[H], qa[TQ], qb[TQ];
@@ -477,61 +529,142 @@ __global__ void __launch_bounds__(WP* WQ* kWave) linear_kernel(LinArgs a) {
     lp.template commit<1>(p0);
     lq.template commit<0>(q0);
     lq.template commit<1>(q0);
-    sync();
-    if (steps > 1) {
+    if constexpr (ST == 4) {
+      lp.issue(p1);
+      lq.issue(q1);
+      lp.issue(p2);
+      lq.issue(q2);
+      lp.issue(p3);
+      lq.issue(q3);
+      sync(std::integral_constant<int, ST - 1>{});
+    } else if constexpr (kDirect) {
+      lp.issue(p1);
+      lq.issue(q1);
+      sync(std::integral_constant<int, 1>{});
+    } else {
+      sync(upper);
       lp.issue(p1);
       lq.issue(q1);
     }
     read_q(qa, q0, 0);
     read_p(pu, p0, 0, 0);
-    // the first three phases of the stage in (pc, qc); the one before (pn, qn) fills from registers
-    auto phases = [&](const uint4* pc, const uint4* qc, uint4* pn, uint4* qn, bool next) {
+    // the first three phases of the stage in (pc, qc); the loads of a later one, whose first part has
+    // been issued, go on into (pf, qf); the next stage fills (pn, qn) from registers
+    auto phases = [&](const uint4* pc, const uint4* qc, uint4* pn, uint4* qn, uint4* pf, uint4* qf, bool next, auto load) {
       __builtin_amdgcn_sched_barrier(0);
       read_p(pl, pc, 0, 1);
+      if constexpr (load.value && kSpread) {
+        lp.template part<1>(pf);
+        lq.template part<1>(qf);
+      }
       multiply(pu, qa, upper);
-      interleave<kReadsP, H * TQ>();
+      interleave<kReadsP, H * TQ, load.value ? kPart : 0>();
       __builtin_amdgcn_sched_barrier(0);
       read_q(qb, qc, 1);
       read_p(pu, pc, 1, 0);
+      if constexpr (load.value && kSpread) {
+        lp.template part<2>(pf);
+        lq.template part<2>(qf);
+      }
       multiply(pl, qa, lower);
       if (next) {
         lp.template commit<0>(pn);
         lq.template commit<0>(qn);
       }
-      interleave<kReadsP + kReadsQ, H * TQ, kConvert>();
+      interleave<kReadsP + kReadsQ, H * TQ, load.value ? kPart : 0, kConvert>();
       __builtin_amdgcn_sched_barrier(0);
       read_p(pl, pc, 1, 1);
+      if constexpr (load.value && kSpread) {
+        lp.template part<3>(pf);
+        lq.template part<3>(qf);
+      }
       multiply(pu, qb, upper);
       if (next) {
         lp.template commit<1>(pn);
         lq.template commit<1>(qn);
       }
-      interleave<kReadsP, H * TQ, kConvert>();
+      interleave<kReadsP, H * TQ, load.value ? kPart : 0, kConvert>();
+      if constexpr (load.value && kSpread) {
+        lp.end();
+        lq.end();
+      }
     };
-    // all of a stage but the last one; `more`: the stage after the next exists
-    auto stage = [&](uint4* pc, uint4* qc, uint4* pn, uint4* qn, bool more) {
-      phases(pc, qc, pn, qn, true);
-      sync();
-      if (more) {
+    constexpr std::true_type loads{};
+    constexpr std::false_type no_loads{};
+    // Stage t, not the last one, from (pc, qc); (pf, qf): the stage before it, which the loads fill.
+    int t = 0;
+    auto stage = [&](uint4* pc, uint4* qc, uint4* pn, uint4* qn, uint4* pf, uint4* qf, auto load) {
+      phases(pc, qc, pn, qn, pf, qf, true, load);
+      sync(ahead);
+      if constexpr (kSpread || kBetween) {
+        lp.begin();
+        lq.begin();
+      } else {
         lp.issue(pc);
         lq.issue(qc);
       }
       __builtin_amdgcn_sched_barrier(0);
       read_q(qa, qn, 0);
       read_p(pu, pn, 0, 0);
+      if constexpr (kSpread) {
+        lp.template part<0>(pc);
+        lq.template part<0>(qc);
+      } else if constexpr (kBetween) {
+        lp.all(pc);
+        lq.all(qc);
+        lp.end();
+        lq.end();
+      }
       multiply(pl, qb, lower);
-      interleave<kReadsP + kReadsQ, H * TQ>();
+      interleave<kReadsP + kReadsQ, H * TQ, kBetween ? kLoads : kPart>();
+      ++t;
     };
-    int t = 0;
-    for (; t + 2 < steps; t += 2) {
-      stage(p0, q0, p1, q1, true);
-      stage(p1, q1, p0, q0, t + 3 < steps);
+    const uint4 *pe = p0, *qe = q0;   // the last stage
+    if (steps > 1) {
+      // (the first stage has no loads to go on with)
+      stage(p0, q0, p1, q1, nullptr, nullptr, no_loads);
+      if constexpr (ST == 2) {
+        while (t + 2 < steps) {
+          stage(p1, q1, p0, q0, p0, q0, loads);
+          stage(p0, q0, p1, q1, p1, q1, loads);
+        }
+        pe = p1;
+        qe = q1;
+        if (t + 1 < steps) {
+          stage(p1, q1, p0, q0, p0, q0, loads);
+          pe = p0;
+          qe = q0;
+        }
+      } else {
+        while (t + 4 < steps) {
+          stage(p1, q1, p2, q2, p0, q0, loads);
+          stage(p2, q2, p3, q3, p1, q1, loads);
+          stage(p3, q3, p0, q0, p2, q2, loads);
+          stage(p0, q0, p1, q1, p3, q3, loads);
+        }
+        pe = p1;
+        qe = q1;
+        if (t + 1 < steps) {
+          stage(p1, q1, p2, q2, p0, q0, loads);
+          pe = p2;
+          qe = q2;
+          if (t + 1 < steps) {
+            stage(p2, q2, p3, q3, p1, q1, loads);
+            pe = p3;
+            qe = q3;
+            if (t + 1 < steps) {
+              stage(p3, q3, p0, q0, p2, q2, loads);
+              pe = p0;
+              qe = q0;
+            }
+          }
+        }
+      }
     }
-    const bool odd = t + 1 < steps;
-    if (odd) stage(p0, q0, p1, q1, false);
-    phases(odd ? p1 : p0, odd ? q1 : q0, nullptr, nullptr, false);
+    phases(pe, qe, nullptr, nullptr, nullptr, nullptr, false, no_loads);
     multiply(pl, qb, lower);
   }
+  sync(upper);   // no direct load is on its way
   __syncthreads();   // the stages' LDS is free
 
   if constexpr (KIND == LIN_WGRAD) {
@@ -618,29 +751,44 @@ __global__ void __launch_bounds__(256) linear_join_kernel(LinArgs a) {
 // each; the tiles of the last, partly filled round in S parts of the reduction, so that the
 // chip is about full there too.
 struct Plan {
-  int tile;              // 128 (four waves, two workgroups a CU) or 256 (eight waves, one)
+  int tile;              // 128 (four waves) or 256 (eight waves, one workgroup a CU)
+  bool deep;             // 128: one workgroup a CU with a ring of four stages, not two with two
   int tiles_p, tiles_q, whole, S, steps;
   double cost;           // microseconds, to compare plans
 };
 constexpr int kCUs = 256;
 
-Plan plan_of(int P, int Q, int K, int tile) {
+// Workgroups at once, and measured microseconds: of a 64-wide step, and of a round of workgroups besides
+// (its first loads, its epilogues).  14336 rows, width 1280 to 5120 (20 steps) and 5120 to 1280 (80):
+// large 206 and 175, pairs 219 and 204, deep 276 and 215; 1536 rows, 1280 to 2560: 45, 27, 20.
+struct Shape {
+  int tile;
+  bool deep;
+  int slots;
+  double step, round;
+};
+constexpr Shape kLarge = {256, false, kCUs, 1.6, 13.0}, kPairs = {128, false, 2 * kCUs, 1.05, 5.0},
+                kDeep = {128, true, kCUs, 0.42, 7.4}, kAny = {128, false, 2 * kCUs, 1.6, 5.0};
+
+Plan plan_of(int P, int Q, int K, Shape sh) {
   Plan r;
-  r.tile = tile;
-  r.tiles_p = (P + tile - 1) / tile;
-  r.tiles_q = (Q + tile - 1) / tile;
-  const int slots = tile == 128 ? 2 * kCUs : kCUs, all = (K + kBK - 1) / kBK;
-  const double step = tile == 128 ? 1.05 : 1.6;   // measured with the chip full (8192 cubed: 1.04 and 1.59)
+  r.tile = sh.tile;
+  r.deep = sh.deep;
+  r.tiles_p = (P + sh.tile - 1) / sh.tile;
+  r.tiles_q = (Q + sh.tile - 1) / sh.tile;
+  const int all = (K + kBK - 1) / kBK;
   const int64_t T = (int64_t)r.tiles_p * r.tiles_q;
-  const int rest = (int)(T % slots);
+  const int rest = (int)(T % sh.slots);
   r.whole = (int)T;
   r.S = 1;
   r.steps = all;
-  r.cost = step * all * (double)((T + slots - 1) / slots);
-  for (int S = 2; rest && S <= 64 && rest * S <= slots && all / S >= 4; ++S) {
+  const double whole = sh.round + sh.step * all;
+  r.cost = whole * (double)((T + sh.slots - 1) / sh.slots);
+  for (int S = 2; rest && S <= 64 && rest * S <= sh.slots && all / S >= 4; ++S) {
     // the parts, their way through memory twice, and another launch
     const int steps = (all + S - 1) / S, parts = (all + steps - 1) / steps;
-    const double cost = step * (all * (double)(T / slots) + steps) + 5.0 + 8e-6 * tile * tile * parts * rest / 4.0;
+    const double cost = whole * (double)(T / sh.slots) + sh.round + sh.step * steps + 5.0 +
+                        2e-6 * sh.tile * sh.tile * parts * rest;
     if (cost < r.cost) {
       r.whole = (int)(T - rest);
       r.S = parts;
@@ -651,10 +799,16 @@ Plan plan_of(int P, int Q, int K, int tile) {
   return r;
 }
 
-// (sizes only, and whether the operands allow direct loads: the large tile exists for those)
-Plan plan(int P, int Q, int K, bool direct) {
-  const Plan small = plan_of(P, Q, K, 128), large = plan_of(P, Q, K, 256);
-  return direct && large.cost < small.cost ? large : small;
+// From the sizes, whether the operands allow direct loads, and whether P is a checkpoint.
+Plan plan(int P, int Q, int K, bool direct, bool ckpt) {
+  if (!direct) return plan_of(P, Q, K, kAny);
+  Plan best = plan_of(P, Q, K, kPairs);
+  for (const Shape& sh : {kLarge, kDeep}) {
+    if (sh.deep && ckpt) continue;
+    const Plan r = plan_of(P, Q, K, sh);
+    if (r.cost < best.cost) best = r;
+  }
+  return best;
 }
 
 size_t part_floats(const Plan& r) {
@@ -662,16 +816,21 @@ size_t part_floats(const Plan& r) {
 }
 
 template <int KIND, bool PKS, int PSRC, bool QKS, int QSRC>
-void launch_one(const LinArgs& a, int tile, hipStream_t st) {
+void launch_one(const LinArgs& a, const Plan& r, hipStream_t st) {
   const unsigned rest = a.tiles_p * a.tiles_q - a.whole, grid = a.whole + rest * a.S;
-  if constexpr (PSRC != SRC_ANY && QSRC == SRC_DIRECT) {
-    if (tile == 256) {
-      linear_kernel<KIND, 2, 4, 8, 4, PKS, PSRC, QKS, QSRC><<<grid, 512, 0, st>>>(a);
+  if (r.tile == 256) {
+    if constexpr (PSRC != SRC_ANY && QSRC == SRC_DIRECT) {
+      linear_kernel<KIND, 2, 4, 8, 4, 2, PKS, PSRC, QKS, QSRC><<<grid, 512, 0, st>>>(a);
       if (rest) linear_join_kernel<KIND, 256><<<rest * 32, 256, 0, st>>>(a);
-      return;
     }
+    return;
   }
-  linear_kernel<KIND, 2, 2, 4, 4, PKS, PSRC, QKS, QSRC><<<grid, 256, 0, st>>>(a);
+  if constexpr (PSRC == SRC_DIRECT && QSRC == SRC_DIRECT) {
+    if (r.deep) linear_kernel<KIND, 2, 2, 4, 4, 4, PKS, PSRC, QKS, QSRC><<<grid, 256, 0, st>>>(a);
+    else linear_kernel<KIND, 2, 2, 4, 4, 2, PKS, PSRC, QKS, QSRC><<<grid, 256, 0, st>>>(a);
+  } else {
+    linear_kernel<KIND, 2, 2, 4, 4, 2, PKS, PSRC, QKS, QSRC><<<grid, 256, 0, st>>>(a);
+  }
   if (rest) linear_join_kernel<KIND, 128><<<rest * 8, 256, 0, st>>>(a);
 }
 
@@ -686,7 +845,9 @@ bool direct_ok(const LinOp& o, int contiguous) {
 }  // namespace
 
 size_t lin_part_floats(int P, int Q, int K) {
-  return std::max(part_floats(plan(P, Q, K, true)), part_floats(plan(P, Q, K, false)));
+  // (asked for before the operands are known)
+  return std::max({part_floats(plan(P, Q, K, true, false)), part_floats(plan(P, Q, K, true, true)),
+                   part_floats(plan(P, Q, K, false, false))});
 }
 
 void launch_linear(int kind, LinArgs a, hipStream_t st) {
@@ -696,21 +857,21 @@ void launch_linear(int kind, LinArgs a, hipStream_t st) {
   const int cols = a.P.extent;
   const bool direct = q_direct && (!a.P.p || direct_ok(a.P, pk ? a.K : cols)) && whole(a.out) && whole(a.res) &&
                       whole(a.pre) && whole(a.act_out) && whole(a.bias, cols) && whole(a.gain, cols) && whole(a.shift, cols);
-  const Plan r = plan(a.P.extent, a.Q.extent, a.K, direct);
+  const Plan r = plan(a.P.extent, a.Q.extent, a.K, direct, !a.P.p);
   a.tiles_p = r.tiles_p; a.tiles_q = r.tiles_q; a.whole = r.whole; a.S = r.S; a.steps = r.steps;
   a.part_sum = r.S > 1 ? a.part + (size_t)r.S * (r.tiles_p * r.tiles_q - r.whole) * r.tile * r.tile : nullptr;
   if (kind == LIN_FWD) {
-    if (direct) launch_one<LIN_FWD, false, SRC_DIRECT, false, SRC_DIRECT>(a, r.tile, st);
-    else launch_one<LIN_FWD, false, SRC_ANY, false, SRC_ANY>(a, r.tile, st);
+    if (direct) launch_one<LIN_FWD, false, SRC_DIRECT, false, SRC_DIRECT>(a, r, st);
+    else launch_one<LIN_FWD, false, SRC_ANY, false, SRC_ANY>(a, r, st);
   } else if (kind == LIN_DGRAD) {
-    if (direct) launch_one<LIN_DGRAD, true, SRC_DIRECT, false, SRC_DIRECT>(a, r.tile, st);
-    else launch_one<LIN_DGRAD, true, SRC_ANY, false, SRC_ANY>(a, r.tile, st);
+    if (direct) launch_one<LIN_DGRAD, true, SRC_DIRECT, false, SRC_DIRECT>(a, r, st);
+    else launch_one<LIN_DGRAD, true, SRC_ANY, false, SRC_ANY>(a, r, st);
   } else if (!a.P.p) {
-    if (direct) launch_one<LIN_WGRAD, true, SRC_CKPT, true, SRC_DIRECT>(a, r.tile, st);
-    else launch_one<LIN_WGRAD, true, SRC_CKPT, true, SRC_ANY>(a, r.tile, st);
+    if (direct) launch_one<LIN_WGRAD, true, SRC_CKPT, true, SRC_DIRECT>(a, r, st);
+    else launch_one<LIN_WGRAD, true, SRC_CKPT, true, SRC_ANY>(a, r, st);
   } else {
-    if (direct) launch_one<LIN_WGRAD, true, SRC_DIRECT, true, SRC_DIRECT>(a, r.tile, st);
-    else launch_one<LIN_WGRAD, true, SRC_ANY, true, SRC_ANY>(a, r.tile, st);
+    if (direct) launch_one<LIN_WGRAD, true, SRC_DIRECT, true, SRC_DIRECT>(a, r, st);
+    else launch_one<LIN_WGRAD, true, SRC_ANY, true, SRC_ANY>(a, r, st);
   }
 }
 

@@ -54,6 +54,24 @@ enum Src : int { SRC_DIRECT = 0, SRC_ANY = 1, SRC_CKPT = 2 };
 
 __device__ __forceinline__ int ks_swz(int r) { return (r & 3) | ((r >> 1) & 4); }
 
+// Eight elements moved down by `move` (0 to 8) places, zeros behind them.
+__device__ __forceinline__ uint4 move_down(uint4 x, int move) {
+  uint64_t lo = (uint64_t)x.y << 32 | x.x, hi = (uint64_t)x.w << 32 | x.z;
+  const int bits = 16 * (move & 3);
+  if (move >= 4) { lo = hi; hi = 0; }
+  if (move >= 8) lo = 0;
+  lo = lo >> bits | (bits ? hi << (64 - bits) : 0);
+  hi >>= bits;
+  return uint4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+}
+// Elements i .. i + 7 of a row of n < 8 (0 from n on).
+__device__ __forceinline__ uint4 short_row(const uint16_t* row, int i, int n) {
+  uint32_t e[8];
+#pragma unroll
+  for (int u = 0; u < 8; ++u) e[u] = i + u < n ? row[i + u] : 0;
+  return uint4{e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16};
+}
+
 // The part of one operand's stage that a wave moves: R rows (KC) or columns (KS) x 64 of r in
 // pieces of 1 KB, NW waves.  Direct: memory to LDS; otherwise through registers (any
 // alignment, element by element; or a checkpoint's 8-bit values, dequantised on the way).
@@ -104,6 +122,15 @@ struct Loader {
         off[j] = KS ? 2u * ((uint32_t)r * (uint32_t)o.ld + (uint32_t)min(row, o.extent - 8 - r0))
                     : 2u * ((uint32_t)min(row, o.extent - 1 - r0) * (uint32_t)o.ld + (uint32_t)r);
       }
+    } else if constexpr (SRC == SRC_ANY) {
+      base = uniform(KS ? o.p + (size_t)k0 * o.ld : o.p + (size_t)r0 * o.ld);
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        int row, r;
+        place(j, row, r);
+        off[j] = KS ? 2u * ((uint32_t)r * (uint32_t)o.ld + (uint32_t)min(r0 + row, max(o.extent - 8, 0)))
+                    : 2u * ((uint32_t)min(row, o.extent - 1 - r0) * (uint32_t)o.ld + (uint32_t)(k0 + r));
+      }
     } else if constexpr (SRC == SRC_CKPT) {
       const int ld = o.ck.ld, sld = ld / kCkptGroup;
       base = uniform(o.ck.q + (size_t)k0 * ld + r0);
@@ -137,6 +164,16 @@ struct Loader {
           if (k0 + r >= K) off[j] = kPastEnd;
         }
       }
+    } else if constexpr (SRC == SRC_ANY) {
+      if (k0 < K && k0 + kBK > K && (KS || K >= 8)) {   // (KC: off counts from the row's start)
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          int row, r;
+          place(j, row, r);
+          if (KS) off[j] -= 2u * (uint32_t)max(k0 + r - (K - 1), 0) * (uint32_t)o.ld;
+          else off[j] -= 2u * (uint32_t)max(k0 + r - (K - 8), 0);
+        }
+      }
     }
   }
   template <int PART>
@@ -146,24 +183,20 @@ struct Loader {
       for (int j = PART * N / 4; j < (PART + 1) * N / 4; ++j) buffer16(base, size, off[j], lds + (w * N + j) * 64);
     } else if constexpr (SRC == SRC_ANY && PART == 0) {
       if (k0 >= K) return;
-      // a stage inside the matrix in 16-byte loads of whatever alignment, others by elements
-      const bool inside = r0 + R <= o.extent && k0 + kBK <= K;
+      // 16-byte loads of whatever alignment; a piece that reaches past the end of its row is the row's
+      // last whole one for now, and commit() moves it into place (rows past the last are the last)
+      const int n = KS ? o.extent : K;   // elements of a row
+      if (n >= 8) {
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
-        int row, r;
-        place(j, row, r);
-        if (inside) {
-          __builtin_memcpy(&reg[j], KS ? o.p + (size_t)(k0 + r) * o.ld + r0 + row : o.p + (size_t)(r0 + row) * o.ld + k0 + r, 16);
-          continue;
-        }
-        uint32_t e[8];
-        const int a = r0 + row, k = k0 + r;
+        for (int j = 0; j < N; ++j) __builtin_memcpy(&reg[j], base + off[j], 16);
+      } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          if constexpr (KS) e[i] = k < K && a + i < o.extent ? o.p[(size_t)k * o.ld + a + i] : 0;
-          else e[i] = a < o.extent && k + i < K ? o.p[(size_t)a * o.ld + k + i] : 0;
+        for (int j = 0; j < N; ++j) {
+          int row, r;
+          place(j, row, r);
+          reg[j] = short_row(o.p + (size_t)(KS ? min(k0 + r, K - 1) : min(r0 + row, o.extent - 1)) * o.ld,
+                             KS ? r0 + row : k0 + r, n);
         }
-        reg[j] = uint4{e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16};
       }
     } else if constexpr (SRC == SRC_CKPT && PART == 0) {
       // past the last row: q = 0, scale byte 0 (a scale of 0)
@@ -180,6 +213,11 @@ struct Loader {
     if constexpr (SRC == SRC_DIRECT) {
       base += KS ? 2 * kBK * o.ld : (int64_t)(2 * kBK);
       if (KS) left -= 2 * kBK * o.ld;
+    } else if constexpr (SRC == SRC_ANY) {
+      if (KS) base += 2 * kBK * o.ld;
+      else
+#pragma unroll
+        for (int j = 0; j < N; ++j) off[j] += 2 * kBK;
     } else if constexpr (SRC == SRC_CKPT) {
       base += kBK * (int64_t)o.ck.ld;
       left -= kBK * (int64_t)o.ck.ld;
@@ -206,7 +244,17 @@ struct Loader {
     static_assert(N % 4 == 0);
     if constexpr (SRC == SRC_ANY) {
 #pragma unroll
-      for (int j = HALF * N / 2; j < (HALF + 1) * N / 2; ++j) lds[(w * N + j) * 64 + lane] = reg[j];
+      for (int j = HALF * N / 2; j < (HALF + 1) * N / 2; ++j) {
+        int row, r;
+        place(j, row, r);
+        const int n = KS ? o.extent : K, first = k0 - kBK;   // (k0 is the next stage's by now)
+        if (n >= 8 && (KS ? r0 + R > n : first + kBK > n)) {
+          const int at = KS ? r0 + row : first + r;
+          reg[j] = move_down(reg[j], min(max(at - (n - 8), 0), 8));
+        }
+        if (KS && first + kBK > K && first + r >= K) reg[j] = uint4{0, 0, 0, 0};
+        lds[(w * N + j) * 64 + lane] = reg[j];
+      }
     } else if constexpr (SRC == SRC_CKPT) {
 #pragma unroll
       for (int j = HALF * N / 4; j < (HALF + 1) * N / 4; ++j) {
@@ -272,6 +320,7 @@ struct Reader {
 struct Extra {
   u32x4 lo, hi;
   uint32_t scale;
+  float bias[8];   // forward, few rows only
 };
 __device__ __forceinline__ void request8(const DMat& m, size_t row, int c, Extra& e) {
   if (m.bf16) {
@@ -319,16 +368,17 @@ __device__ __forceinline__ Extra request(const LinArgs& a, int q, int c) {
 // Columns c .. c + 7 of output row q (four neighbouring lanes hold one checkpoint group of 32; every
 // lane of the wave calls this).  qsum: wgrad's sum of dy for row q.  VEC: every matrix and
 // parameter allows whole vectors, and `e` is what request() asked for.
-template <int KIND, bool VEC>
+// FEW: the bias has been asked for too.
+template <int KIND, bool VEC, bool FEW = false>
 __device__ __forceinline__ void epilogue(const LinArgs& a, int q, int c, float (&h)[8], float qsum, const Extra& e) {
   const int cols = a.P.extent;
   const bool row = q < a.Q.extent;
   if constexpr (KIND == LIN_FWD) {
     float b[8];
     if (a.bias.p) {
-      load_vec8<VEC>(a.bias, c, cols, b);
+      if (!FEW) load_vec8<VEC>(a.bias, c, cols, b);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) h[i] += b[i];
+      for (int i = 0; i < 8; ++i) h[i] += FEW ? e.bias[i] : b[i];
     }
     if (a.pre.p && row) store8<VEC>(a.pre, q, c, cols, h);
     if (a.ck.q) {
@@ -433,7 +483,7 @@ constexpr int wait_for(int n) { return (n & 15) | ((n >> 4) << 14) | 0x0070; }
 // operands, so no product waits for LDS.  The barrier falls before the stage's last phase, when all
 // of it is in registers and its LDS is free: the loads of the stage ST later start there.
 template <int KIND, int WP, int WQ, int TP, int TQ, int ST, bool PKS, int PSRC, bool QKS, int QSRC>
-__global__ void __launch_bounds__(WP* WQ* kWave) linear_kernel(LinArgs a) {
+__global__ void __launch_bounds__(WP* WQ* kWave, ST == 2 && !(PSRC == SRC_CKPT && QSRC == SRC_ANY) ? 2 : 1) linear_kernel(LinArgs a) {
   constexpr int NW = WP * WQ, RP = WP * TP * 16, RQ = WQ * TQ * 16, NS = TQ / WP;
   static_assert(TP % 2 == 0 && TQ % WP == 0);
   static_assert(ST == 2 || (ST == 4 && PSRC == SRC_DIRECT && QSRC == SRC_DIRECT));
@@ -747,6 +797,72 @@ __global__ void __launch_bounds__(256) linear_join_kernel(LinArgs a) {
   epilogue<KIND, false>(a, q, c, h, qsum, Extra{});
 }
 
+// Forward product of at most 16 RT rows (single tokens, a decoding batch): the weight is read once and
+// that is the floor, so it goes from memory straight to registers, many loads at a time, with no LDS
+// and no second launch.  A workgroup owns PC columns; its eight waves share the reduction and add up
+// in LDS, in order (sixteen were no faster: 8.4 against 8.1 us for 1280 x 5120).
+constexpr int kFewWaves = 8, kFewSteps = 5;   // and the 32-wide steps that a wave has in flight
+template <int RT, int PC>
+__global__ void __launch_bounds__(kFewWaves* kWave) linear_few_kernel(LinArgs a) {
+  constexpr int U = kFewSteps, NW = kFewWaves;
+  __shared__ f32x4 part[NW][RT * 16][PC / 4];
+  const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int c16 = lane & 15, g = lane >> 4, p0 = blockIdx.x * PC;
+  constexpr int kItems = RT * 16 * PC / 8;
+  const int t = threadIdx.x, q = t / (PC / 8), c = p0 + t % (PC / 8) * 8;
+  Extra e{};
+  if (t < kItems) {
+    e = request<LIN_FWD>(a, q, c);
+    if (a.bias.p) load_vec8<true>(a.bias, c, a.P.extent, e.bias);
+  }
+  const int all = (a.K + 31) / 32, each = (all + NW - 1) / NW;
+  const int beg = w * each, end = min(all, beg + each);
+  const uint16_t* pw = a.P.p + (size_t)min(p0 + c16 % PC, a.P.extent - 1) * a.P.ld + 8 * g;
+  const uint16_t* px[RT];
+  f32x4 acc[RT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    px[r] = a.Q.p + (size_t)min(16 * r + c16, a.Q.extent - 1) * a.Q.ld + 8 * g;
+    acc[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  for (int s = beg; s < end; s += U) {
+    u32x4 fw[U], fx[RT][U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      fw[u] = u32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int r = 0; r < RT; ++r) fx[r][u] = u32x4{0, 0, 0, 0};
+      if (s + u < end && 32 * (s + u) + 8 * g < a.K) {
+        fw[u] = *(const u32x4*)(pw + 32 * (s + u));
+#pragma unroll
+        for (int r = 0; r < RT; ++r) fx[r][u] = *(const u32x4*)(px[r] + 32 * (s + u));
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int r = 0; r < RT; ++r)
+        acc[r] = mfma_bf16(__builtin_bit_cast(bf16x8, fw[u]), __builtin_bit_cast(bf16x8, fx[r][u]), acc[r]);
+  }
+  if (4 * g < PC)
+#pragma unroll
+    for (int r = 0; r < RT; ++r) part[w][16 * r + c16][g] = acc[r];
+  __syncthreads();
+  if (t < kItems) {
+    float h[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int v = 0; v < NW; ++v) {
+      const f32x4 lo = part[v][q][t % (PC / 8) * 2], hi = part[v][q][t % (PC / 8) * 2 + 1];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        h[i] += lo[i];
+        h[4 + i] += hi[i];
+      }
+    }
+    epilogue<LIN_FWD, true, true>(a, q, c, h, 0.f, e);
+  }
+}
+
 // How a product is cut.  Tiles that fill whole rounds of the chip are computed by one workgroup
 // each; the tiles of the last, partly filled round in S parts of the reduction, so that the
 // chip is about full there too.
@@ -768,7 +884,7 @@ struct Shape {
   double step, round;
 };
 constexpr Shape kLarge = {256, false, kCUs, 1.6, 13.0}, kPairs = {128, false, 2 * kCUs, 1.05, 5.0},
-                kDeep = {128, true, kCUs, 0.42, 7.4}, kAny = {128, false, 2 * kCUs, 1.6, 5.0};
+                kDeep = {128, true, kCUs, 0.52, 5.6}, kAny = {128, false, 2 * kCUs, 1.6, 5.0};
 
 Plan plan_of(int P, int Q, int K, Shape sh) {
   Plan r;
@@ -844,6 +960,31 @@ bool direct_ok(const LinOp& o, int contiguous) {
 
 }  // namespace
 
+// The forward product of few rows straight from registers: how it is cut, and its microseconds, to
+// compare with a plan's: what the weight's loads take one after the other or at the memory's rate,
+// and the rows, which every workgroup reads from L2 (measured from 1 to 32 rows at 1280 x 1280 to
+// 51864 x 1280 and 1280 x 5120, within 20%; a 51864-wide head takes 27 us for a row, 42 for 16
+// and 62 for 32, against 31, 31 and 32 in tiles).
+struct FewPlan {
+  bool narrow;   // 8 columns a workgroup where 16 would leave CUs without one
+  int grid;
+  double cost;
+};
+constexpr int kFewRows = 32;
+FewPlan few_plan(int P, int Q, int K) {
+  FewPlan f;
+  f.narrow = (P + 15) / 16 < kCUs;
+  f.grid = f.narrow ? (P + 7) / 8 : (P + 15) / 16;
+  const int turns = ((K + 31) / 32 + kFewWaves * kFewSteps - 1) / (kFewWaves * kFewSteps);
+  f.cost = std::max(3.0 + 1.2 * turns, 2.0 * P * K / 4.9e6) + 2.0 * f.grid * Q * K / 8e6;
+  return f;
+}
+
+template <int RT, int PC>
+void launch_few(const LinArgs& a, const FewPlan& f, hipStream_t st) {
+  linear_few_kernel<RT, PC><<<f.grid, kFewWaves * kWave, 0, st>>>(a);
+}
+
 size_t lin_part_floats(int P, int Q, int K) {
   // (asked for before the operands are known)
   return std::max({part_floats(plan(P, Q, K, true, false)), part_floats(plan(P, Q, K, true, true)),
@@ -860,6 +1001,16 @@ void launch_linear(int kind, LinArgs a, hipStream_t st) {
   const Plan r = plan(a.P.extent, a.Q.extent, a.K, direct, !a.P.p);
   a.tiles_p = r.tiles_p; a.tiles_q = r.tiles_q; a.whole = r.whole; a.S = r.S; a.steps = r.steps;
   a.part_sum = r.S > 1 ? a.part + (size_t)r.S * (r.tiles_p * r.tiles_q - r.whole) * r.tile * r.tile : nullptr;
+  if (kind == LIN_FWD && direct && !a.ck.q && a.Q.extent <= kFewRows) {
+    // (a checkpoint's groups of 32 columns do not fit the workgroups of few rows)
+    const FewPlan f = few_plan(a.P.extent, a.Q.extent, a.K);
+    // (tiles read the weight at 4.2 TB/s at best)
+    if (f.cost < std::max(r.cost, 2.0 * a.P.extent * a.K / 4.2e6)) {
+      if (a.Q.extent <= 16) f.narrow ? launch_few<1, 8>(a, f, st) : launch_few<1, 16>(a, f, st);
+      else f.narrow ? launch_few<2, 8>(a, f, st) : launch_few<2, 16>(a, f, st);
+      return;
+    }
+  }
   if (kind == LIN_FWD) {
     if (direct) launch_one<LIN_FWD, false, SRC_DIRECT, false, SRC_DIRECT>(a, r, st);
     else launch_one<LIN_FWD, false, SRC_ANY, false, SRC_ANY>(a, r, st);

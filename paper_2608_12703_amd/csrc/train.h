@@ -46,7 +46,8 @@ __device__ __forceinline__ void widen8(u32x4 u, float (&v)[8]) {
   }
 }
 
-// Columns c .. c + 7 of a row (columns from `cols` on read as 0).  VEC: the caller knows that m.vec.
+// Columns c .. c + 7 of a row (columns from `cols` on read as 0), in 16-byte accesses of whatever
+// alignment where all eight are there.  VEC: the caller knows that m.vec.
 template <bool VEC = false>
 __device__ __forceinline__ void load8(const DMat& m, size_t row, int c, int cols, float (&v)[8]) {
   if (m.bf16) {
@@ -54,6 +55,10 @@ __device__ __forceinline__ void load8(const DMat& m, size_t row, int c, int cols
     if (VEC || m.vec) {
       u32x4 u = {0, 0, 0, 0};
       if (c < cols) u = *(const u32x4*)p;
+      widen8(u, v);
+    } else if (c + 8 <= cols) {
+      u32x4 u;
+      __builtin_memcpy(&u, p, 16);
       widen8(u, v);
     } else {
 #pragma unroll
@@ -69,6 +74,8 @@ __device__ __forceinline__ void load8(const DMat& m, size_t row, int c, int cols
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
+    } else if (c + 8 <= cols) {
+      __builtin_memcpy(v, p, 32);
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? p[i] : 0.f;
@@ -84,6 +91,10 @@ __device__ __forceinline__ void store8(const DMat& m, size_t row, int c, int col
       if (c < cols)
         *(u32x4*)p = u32x4{f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]),
                            f32x2_to_bf16x2(v[4], v[5]), f32x2_to_bf16x2(v[6], v[7])};
+    } else if (c + 8 <= cols) {
+      const u32x4 u = {f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]), f32x2_to_bf16x2(v[4], v[5]),
+                       f32x2_to_bf16x2(v[6], v[7])};
+      __builtin_memcpy(p, &u, 16);
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
@@ -96,6 +107,8 @@ __device__ __forceinline__ void store8(const DMat& m, size_t row, int c, int col
         *(f32x4*)p = f32x4{v[0], v[1], v[2], v[3]};
         *(f32x4*)(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
       }
+    } else if (c + 8 <= cols) {
+      __builtin_memcpy(p, v, 32);
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i)

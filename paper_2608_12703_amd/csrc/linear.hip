@@ -85,7 +85,7 @@ struct Loader {
   const char* sbase;      // checkpoint: its scale
   int64_t left, sleft;    // KS: bytes from there to the end of the reduction's last row
   uint32_t size;          // the descriptor's, for the stage being loaded
-  uint32_t off[N], soff[SRC == SRC_CKPT ? N / 2 : 1];   // bytes
+  uint32_t off[N];        // bytes (a checkpoint's scale: a 32nd of its q's)
   uint4 reg[N];
   uint32_t sc[N];
 
@@ -143,7 +143,6 @@ struct Loader {
         int row, r;
         place_ck(j, row, r);
         off[j] = (uint32_t)r * ld + row;
-        soff[j] = (uint32_t)r * sld + row / kCkptGroup;
       }
     }
   }
@@ -205,7 +204,7 @@ struct Loader {
 #pragma unroll
       for (int j = 0; j < N / 2; ++j) {
         reg[j] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rq, off[j], 0, 0));
-        sc[j] = __builtin_amdgcn_raw_buffer_load_b8(rs, soff[j], 0, 0);
+        sc[j] = __builtin_amdgcn_raw_buffer_load_b8(rs, off[j] / kCkptGroup, 0, 0);
       }
     }
   }
@@ -413,7 +412,7 @@ __device__ __forceinline__ void epilogue(const LinArgs& a, int q, int c, float (
       for (int i = 0; i < 8; ++i) {
         const Normal n = normal(x[i]);
         h[i] *= gelu_slope(x[i], n);
-        x[i] *= n.cdf;
+        x[i] = gelu_value(x[i], n);
       }
       if (a.act_out.p) store8<VEC>(a.act_out, q, c, cols, x);
     }
@@ -439,6 +438,188 @@ __device__ __forceinline__ void epilogue(const LinArgs& a, int q, int c, float (
   }
 }
 
+// The same where every matrix and parameter allows whole vectors, for the rows of one tile from q0 on and
+// this lane's columns c .. c + 7: memory is reached through buffer descriptors, which leave out rows
+// and columns past the last (no branches, 32-bit offsets), and parameters are read once.
+struct TileMat {
+  const char* base;
+  uint32_t size, row, lane;   // bytes: to the end of the last row, of a row, of this lane's columns
+  __device__ __forceinline__ void init(const void* p, int64_t ld, int bytes, int width, int q0, int rows, int c, int cols) {
+    base = uniform((const char*)p + (int64_t)q0 * ld * bytes);
+    size = rows > q0 ? (uint32_t)min(((int64_t)(rows - 1 - q0) * ld + width) * bytes, (int64_t)kPastEnd) : 0;
+    row = (uint32_t)ld * bytes;
+    lane = c < cols ? (uint32_t)c * bytes : kPastEnd;
+  }
+  __device__ __forceinline__ uint32_t at(int r) const { return lane + (uint32_t)r * row; }
+  __device__ __forceinline__ u32x4 get(uint32_t off) const {
+    return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(descriptor(base, size), off, 0, 0));
+  }
+  __device__ __forceinline__ void put(u32x4 v, uint32_t off) const {
+    __builtin_amdgcn_raw_buffer_store_b128(v, descriptor(base, size), off, 0, 0);
+  }
+};
+struct TileRows {   // float32 or bf16 rows
+  TileMat m;
+  bool bf16;
+  __device__ __forceinline__ void init(const DMat& d, int q0, int rows, int c, int cols) {
+    bf16 = d.bf16;
+    m.init(d.p, d.ld, bf16 ? 2 : 4, cols, q0, d.p ? rows : 0, c, cols);
+  }
+  template <int N>
+  __device__ __forceinline__ void store(int r, int step, const float (&v)[N][8]) const {
+    if (bf16) {
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+        m.put(u32x4{f32x2_to_bf16x2(v[n][0], v[n][1]), f32x2_to_bf16x2(v[n][2], v[n][3]),
+                    f32x2_to_bf16x2(v[n][4], v[n][5]), f32x2_to_bf16x2(v[n][6], v[n][7])}, m.at(r + n * step));
+    } else {
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        m.put(__builtin_bit_cast(u32x4, f32x4{v[n][0], v[n][1], v[n][2], v[n][3]}), m.at(r + n * step));
+        m.put(__builtin_bit_cast(u32x4, f32x4{v[n][4], v[n][5], v[n][6], v[n][7]}), m.at(r + n * step) + 16);
+      }
+    }
+  }
+};
+template <int KIND>
+struct TileEpilogue {
+  TileRows out, in, also;    // in: residual, pre-activation or old gradient; also: pre or act_out
+  TileMat q, scale;          // the checkpoint
+  float b[8], g[8];          // bias; wgrad: shift and gain
+  int c;
+  struct Ask {
+    u32x4 lo, hi;
+    uint32_t s;
+  };
+  __device__ __forceinline__ void init(const LinArgs& a, int q0, int c_) {
+    c = c_;
+    const int cols = a.P.extent, rows = a.Q.extent;
+    out.init(a.out, q0, rows, c, cols);
+    in.init(KIND == LIN_FWD ? a.res : KIND == LIN_DGRAD ? a.pre : a.out, q0, rows, c, cols);
+    also.init(KIND == LIN_FWD ? a.pre : a.act_out, q0, rows, c, cols);
+    if constexpr (KIND != LIN_WGRAD) {
+      const int ld = a.ck.ld, n = a.ck.q ? rows : 0;
+      q.init(a.ck.q, ld, 1, ld, q0, n, c, ld);
+      // (one lane of a group's four holds its scale's place when storing)
+      scale.init(a.ck.scale, ld / kCkptGroup, 1, ld / kCkptGroup, q0, n, c / kCkptGroup,
+                 c < ld && (KIND == LIN_DGRAD || c % kCkptGroup == 0) ? ld : 0);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) b[i] = g[i] = 0.f;
+    if (KIND == LIN_FWD && a.bias.p) load_vec8<true>(a.bias, c, cols, b);
+    if (KIND == LIN_WGRAD && a.gain.p) {
+      load_vec8<true>(a.gain, c, cols, g);
+      load_vec8<true>(a.shift, c, cols, b);
+    }
+  }
+  // N rows, `step` apart from r on.  Every choice is made once for all of them: the compiler waits for
+  // everything in flight where two ways meet.
+  template <int N>
+  __device__ __forceinline__ void ask(const LinArgs& a, int r, int step, Ask (&e)[N]) const {
+    if constexpr (KIND == LIN_DGRAD) {
+      if (a.gelu && a.ck.q) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+          const auto w = __builtin_amdgcn_raw_buffer_load_b64(descriptor(q.base, q.size), q.at(r + n * step), 0, 0);
+          e[n].lo[0] = w[0];
+          e[n].lo[1] = w[1];
+          e[n].s = __builtin_amdgcn_raw_buffer_load_b8(descriptor(scale.base, scale.size), scale.at(r + n * step), 0, 0);
+        }
+        return;
+      }
+      if (!a.gelu) return;
+    } else if (KIND == LIN_FWD ? !a.res.p : !a.accumulate) {
+      return;
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n) e[n].lo = in.m.get(in.m.at(r + n * step));
+    if (in.bf16) return;
+#pragma unroll
+    for (int n = 0; n < N; ++n) e[n].hi = in.m.get(in.m.at(r + n * step) + 16);
+  }
+  // (items I0 .. I0 + N - 1 of those asked for)
+  template <int I0, int N, int M>
+  __device__ __forceinline__ void received(const Ask (&e)[M], float (&v)[N][8]) const {
+    if (in.bf16) {
+#pragma unroll
+      for (int n = 0; n < N; ++n) widen8(e[I0 + n].lo, v[n]);
+    } else {
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          v[n][i] = __uint_as_float(e[I0 + n].lo[i]);
+          v[n][4 + i] = __uint_as_float(e[I0 + n].hi[i]);
+        }
+    }
+  }
+  template <int I0, int N, int M>
+  __device__ __forceinline__ void rows(const LinArgs& a, int r, int step, float (&h)[N][8], const float (&qsum)[N],
+                                       const Ask (&e)[M]) const {
+    float x[N][8];
+    if constexpr (KIND == LIN_FWD) {
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[n][i] += b[i];
+      if (a.pre.p) also.store(r, step, h);
+      if (a.ck.q) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+          uint32_t s;
+          const u32x2 w = ckpt_of8(c < a.P.extent, h[n], s);
+          __builtin_amdgcn_raw_buffer_store_b64(w, descriptor(q.base, q.size), q.at(r + n * step), 0, 0);
+          __builtin_amdgcn_raw_buffer_store_b8((uint8_t)s, descriptor(scale.base, scale.size), scale.at(r + n * step), 0, 0);
+        }
+      }
+      if (a.gelu)
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) h[n][i] = gelu_value(h[n][i]);
+      if (a.res.p) {
+        received<I0>(e, x);
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) h[n][i] += x[n][i];
+      }
+    } else if constexpr (KIND == LIN_DGRAD) {
+      if (a.gelu) {
+        if (a.ck.q) {
+#pragma unroll
+          for (int n = 0; n < N; ++n) ckpt_value8(u32x2{e[I0 + n].lo[0], e[I0 + n].lo[1]}, e[I0 + n].s, x[n]);
+        } else {
+          received<I0>(e, x);
+        }
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const Normal z = normal(x[n][i]);
+            h[n][i] *= gelu_slope(x[n][i], z);
+            x[n][i] = gelu_value(x[n][i], z);
+          }
+        if (a.act_out.p) also.store(r, step, x);
+      }
+    } else {
+      if (a.gain.p)
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) h[n][i] = fmaf(h[n][i], g[i], b[i] * qsum[n]);
+      if (a.accumulate) {
+        received<I0>(e, x);
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) h[n][i] += x[n][i];
+      }
+    }
+    out.store(r, step, h);
+  }
+};
+
 // Workgroups are dealt round-robin over the 8 XCDs: number id of n, so ordered that each XCD has a
 // contiguous range.
 __device__ __forceinline__ int xcd_order(int id, int n) {
@@ -459,13 +640,14 @@ template <int READS, int PRODUCTS, int LOADS = 0, int VALU = 0, int I = 0>
 __device__ __forceinline__ void interleave() {
   if constexpr (I < READS) {
     constexpr int kLoad = LOADS * (I + 1) / READS - LOADS * I / READS;
+    constexpr int kProducts = PRODUCTS * (I + 1) / READS - PRODUCTS * I / READS;
     __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);                                 // an LDS read
     if constexpr (kLoad > 0) __builtin_amdgcn_sched_group_barrier(0x020, kLoad, 0);    // loads
-    if constexpr (VALU == 0) {
-      __builtin_amdgcn_sched_group_barrier(0x008, PRODUCTS / READS, 0);                // products
-    } else {
+    if constexpr (VALU == 0 && kProducts > 0) {
+      __builtin_amdgcn_sched_group_barrier(0x008, kProducts, 0);                       // products
+    } else if constexpr (VALU > 0) {
 #pragma unroll
-      for (int j = 0; j < PRODUCTS / READS; ++j) {
+      for (int j = 0; j < kProducts; ++j) {
         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
         __builtin_amdgcn_sched_group_barrier(0x002, VALU, 0);
       }
@@ -495,7 +677,7 @@ __global__ void __launch_bounds__(WP* WQ* kWave, ST == 2 && !(PSRC == SRC_CKPT &
   __shared__ uint4 q2[kMore * RQ * 8 + 1 - kMore], q3[kMore * RQ * 8 + 1 - kMore];
   __shared__ float sums[KIND == LIN_WGRAD ? RQ : 1];
   const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int wp = w % WP, wq = w / WP, c16 = lane & 15, g = lane >> 4;
+  const int wp = w % WP, wq = w / WP;
   // whole tiles first, then the last `rest` tiles in S parts of the reduction each
   const int id = blockIdx.x, rest = a.tiles_p * a.tiles_q - a.whole;
   const bool part = id >= a.whole;
@@ -527,29 +709,29 @@ __global__ void __launch_bounds__(WP* WQ* kWave, ST == 2 && !(PSRC == SRC_CKPT &
   rp.init(wp * TP, 0, lane);
   rq.init(wq * TQ, x0, lane);
 
-  constexpr int H = TP / 2;
-  auto read_p = [&](bf16x8 (&f)[H], const uint4* ps, int s, int half) {
+  // P tiles of a phase: half of them, or a quarter where a half's operands do not fit the registers
+  constexpr int G = KIND == LIN_WGRAD && PSRC == SRC_CKPT && TP == 8 ? 4 : 2, H = TP / G;
+  auto read_p = [&](bf16x8 (&f)[H], const uint4* ps, int s, int group) {
     const uint32_t o = rp.fresh();
 #pragma unroll
-    for (int i = 0; i < H; ++i) f[i] = rp.read(ps, o, half * H + i, s);
+    for (int i = 0; i < H; ++i) f[i] = rp.read(ps, o, group * H + i, s);
   };
   auto read_q = [&](bf16x8 (&f)[TQ], const uint4* qs, int s) {
     const uint32_t o = rq.fresh();
 #pragma unroll
     for (int j = 0; j < TQ; ++j) f[j] = rq.read(qs, o, j, s);
   };
-  auto multiply = [&](const bf16x8 (&fp)[H], const bf16x8 (&fq)[TQ], auto half) {
+  auto multiply = [&](const bf16x8 (&fp)[H], const bf16x8 (&fq)[TQ], auto group) {
 #pragma unroll
     for (int i = 0; i < H; ++i)
 #pragma unroll
-      for (int j = 0; j < TQ; ++j) acc[half.value * H + i][j] = mfma_bf16(fp[i], fq[j], acc[half.value * H + i][j]);
-    if constexpr (KIND == LIN_WGRAD && half.value)
+      for (int j = 0; j < TQ; ++j) acc[group.value * H + i][j] = mfma_bf16(fp[i], fq[j], acc[group.value * H + i][j]);
+    if constexpr (KIND == LIN_WGRAD && group.value == G - 1)
 #pragma unroll
       for (int j = 0; j < NS; ++j) csum[j] = mfma_bf16(ones, fq[j], csum[j]);
   };
   constexpr int kConvert = PSRC == SRC_CKPT ? 3 : 0;
-  constexpr std::integral_constant<int, 0> upper{};
-  constexpr std::integral_constant<int, 1> lower{};
+  constexpr std::integral_constant<int, 0> none{};
   constexpr int kReadsP = H * (PKS ? 2 : 1), kReadsQ = TQ * (QKS ? 2 : 1);
   // this wave's loads but the newest `stages` stages' have landed and its LDS reads are in
   // registers; then everyone's
@@ -572,7 +754,7 @@ __global__ void __launch_bounds__(WP* WQ* kWave, ST == 2 && !(PSRC == SRC_CKPT &
   constexpr int kPart = kSpread ? (RP + RQ) / 32 / NW : 0;
 
   if (steps > 0) {
-    bf16x8 pu[H], pl[H], qa[TQ], qb[TQ];
+    bf16x8 pb[2][H], qa[TQ], qb[TQ];   // P operands of this phase and the next; Q's of the two steps
     lp.issue(p0);
     lq.issue(q0);
     lp.template commit<0>(p0);
@@ -592,53 +774,48 @@ __global__ void __launch_bounds__(WP* WQ* kWave, ST == 2 && !(PSRC == SRC_CKPT &
       lq.issue(q1);
       sync(std::integral_constant<int, 1>{});
     } else {
-      sync(upper);
+      sync(none);
       lp.issue(p1);
       lq.issue(q1);
     }
     read_q(qa, q0, 0);
-    read_p(pu, p0, 0, 0);
-    // the first three phases of the stage in (pc, qc); the loads of a later one, whose first part has
-    // been issued, go on into (pf, qf); the next stage fills (pn, qn) from registers
+    read_p(pb[0], p0, 0, 0);
+    // All phases but the last of the stage in (pc, qc); the loads of a later one, whose first part has
+    // been issued, go on into (pf, qf); the next stage fills (pn, qn) from registers in the last two.
     auto phases = [&](const uint4* pc, const uint4* qc, uint4* pn, uint4* qn, uint4* pf, uint4* qf, bool next, auto load) {
-      __builtin_amdgcn_sched_barrier(0);
-      read_p(pl, pc, 0, 1);
-      if constexpr (load.value && kSpread) {
-        lp.template part<1>(pf);
-        lq.template part<1>(qf);
+      auto phase = [&](auto number) {
+        constexpr int I = number.value, S = (I + 1) / G;
+        constexpr bool kTurn = (I + 1) % G == 0;   // the next phase is the second step's first
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (kTurn) read_q(qb, qc, S);
+        read_p(pb[(I + 1) % 2], pc, S, (I + 1) % G);
+        if constexpr (load.value && kSpread) {
+          lp.template part<I + 1>(pf);
+          lq.template part<I + 1>(qf);
+        }
+        multiply(pb[I % 2], I < G ? qa : qb, std::integral_constant<int, I % G>{});
+        if constexpr (I >= 2 * G - 3)
+          if (next) {
+            lp.template commit<I - (2 * G - 3)>(pn);
+            lq.template commit<I - (2 * G - 3)>(qn);
+          }
+        interleave<kReadsP + (kTurn ? kReadsQ : 0), H * TQ, load.value ? kPart : 0, I >= 2 * G - 3 ? kConvert : 0>();
+      };
+      phase(std::integral_constant<int, 0>{});
+      phase(std::integral_constant<int, 1>{});
+      phase(std::integral_constant<int, 2>{});
+      if constexpr (G == 4) {
+        phase(std::integral_constant<int, 3>{});
+        phase(std::integral_constant<int, 4>{});
+        phase(std::integral_constant<int, 5>{});
+        phase(std::integral_constant<int, 6>{});
       }
-      multiply(pu, qa, upper);
-      interleave<kReadsP, H * TQ, load.value ? kPart : 0>();
-      __builtin_amdgcn_sched_barrier(0);
-      read_q(qb, qc, 1);
-      read_p(pu, pc, 1, 0);
-      if constexpr (load.value && kSpread) {
-        lp.template part<2>(pf);
-        lq.template part<2>(qf);
-      }
-      multiply(pl, qa, lower);
-      if (next) {
-        lp.template commit<0>(pn);
-        lq.template commit<0>(qn);
-      }
-      interleave<kReadsP + kReadsQ, H * TQ, load.value ? kPart : 0, kConvert>();
-      __builtin_amdgcn_sched_barrier(0);
-      read_p(pl, pc, 1, 1);
-      if constexpr (load.value && kSpread) {
-        lp.template part<3>(pf);
-        lq.template part<3>(qf);
-      }
-      multiply(pu, qb, upper);
-      if (next) {
-        lp.template commit<1>(pn);
-        lq.template commit<1>(qn);
-      }
-      interleave<kReadsP, H * TQ, load.value ? kPart : 0, kConvert>();
       if constexpr (load.value && kSpread) {
         lp.end();
         lq.end();
       }
     };
+    constexpr std::integral_constant<int, G - 1> last{};
     constexpr std::true_type loads{};
     constexpr std::false_type no_loads{};
     // Stage t, not the last one, from (pc, qc); (pf, qf): the stage before it, which the loads fill.
@@ -655,7 +832,7 @@ __global__ void __launch_bounds__(WP* WQ* kWave, ST == 2 && !(PSRC == SRC_CKPT &
       }
       __builtin_amdgcn_sched_barrier(0);
       read_q(qa, qn, 0);
-      read_p(pu, pn, 0, 0);
+      read_p(pb[0], pn, 0, 0);
       if constexpr (kSpread) {
         lp.template part<0>(pc);
         lq.template part<0>(qc);
@@ -665,7 +842,7 @@ __global__ void __launch_bounds__(WP* WQ* kWave, ST == 2 && !(PSRC == SRC_CKPT &
         lp.end();
         lq.end();
       }
-      multiply(pl, qb, lower);
+      multiply(pb[1], qb, last);
       interleave<kReadsP + kReadsQ, H * TQ, kBetween ? kLoads : kPart>();
       ++t;
     };
@@ -712,10 +889,13 @@ __global__ void __launch_bounds__(WP* WQ* kWave, ST == 2 && !(PSRC == SRC_CKPT &
       }
     }
     phases(pe, qe, nullptr, nullptr, nullptr, nullptr, false, no_loads);
-    multiply(pl, qb, lower);
+    multiply(pb[1], qb, last);
   }
-  sync(upper);   // no direct load is on its way
-  __syncthreads();   // the stages' LDS is free
+  sync(none);   // no direct load is on its way, and the stages' LDS is free
+  // (what follows derives its places anew: kept through the loop, they would take its registers)
+  int late = lane;
+  asm volatile("" : "+v"(late));
+  const int c16 = late & 15, g = late >> 4;
 
   if constexpr (KIND == LIN_WGRAD) {
     if (g == 0)
@@ -729,42 +909,65 @@ __global__ void __launch_bounds__(WP* WQ* kWave, ST == 2 && !(PSRC == SRC_CKPT &
   uint4* mine = w < NW / 2 ? p0 + w * kPiece : p1 + (w - NW / 2) * kPiece;
   static_assert(NW / 2 * kPiece <= RP * 8);
   constexpr bool VEC = PSRC != SRC_ANY && QSRC != SRC_ANY;
-  constexpr int NI = 16 * CPR / kWave;
-  const int r0 = lane / CPR, k = lane % CPR, c = ip * RP + wp * TP * 16 + 8 * k;
+  constexpr int NI = 16 * CPR / kWave, kRows = kWave / CPR;   // items of a row of tiles, rows between them
+  constexpr int NB = KIND == LIN_FWD ? NI : 2;                 // items at a time (as many as fit the registers)
+  const int r0 = late / CPR, k = late % CPR, c = ip * RP + wp * TP * 16 + 8 * k;
+  TileEpilogue<KIND> te;
+  if (VEC) te.init(a, iq * RQ, c);
 #pragma unroll
   for (int j = 0; j < TQ; ++j) {
-    const int q_tile = wq * TQ + slot(j), q0r = iq * RQ + q_tile * 16 + r0;
-    Extra ex[NI];
-    if (VEC && !part)
-#pragma unroll
-      for (int it = 0; it < NI; ++it) ex[it] = request<KIND>(a, q0r + it * (kWave / CPR), c);
+    const int r_tile = (wq * TQ + slot(j)) * 16 + r0;   // row within the tile of this lane's first item
+    typename TileEpilogue<KIND>::Ask ask[NI];
+    if (VEC && !part) te.ask(a, r_tile, kRows, ask);
 #pragma unroll
     for (int i = 0; i < TP; ++i)
       mine[c16 * 4 * TP + ((4 * i + g) ^ c16)] = __builtin_bit_cast(uint4, acc[i][j]);
-    auto item = [&](int it, const Extra& e) {
-      const int r = it * (kWave / CPR) + r0, q = q0r + it * (kWave / CPR);
+    auto piece = [&](int it, float (&h)[8]) {
+      const int r = it * kRows + r0;
       const f32x4 lo = __builtin_bit_cast(f32x4, mine[r * 4 * TP + ((2 * k) ^ r)]);
       const f32x4 hi = __builtin_bit_cast(f32x4, mine[r * 4 * TP + ((2 * k + 1) ^ r)]);
-      const float qsum = KIND == LIN_WGRAD ? sums[q_tile * 16 + r] : 0.f;
-      if (part) {
-        // tile [RQ][RP] of split, tile, then its rows' sums
-        const size_t at = (size_t)split * rest + xcd_order(nth, rest);
-        float* to = a.part + (at * RQ + q_tile * 16 + r) * RP + wp * TP * 16 + 8 * k;
-        *(f32x4*)to = lo;
-        *(f32x4*)(to + 4) = hi;
-        if (KIND == LIN_WGRAD && wp == 0 && k == 0) a.part_sum[at * RQ + q_tile * 16 + r] = qsum;
-      } else {
-        float h[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        epilogue<KIND, VEC>(a, q, c, h, qsum, e);
-      }
-    };
-    if constexpr (VEC) {
 #pragma unroll
-      for (int it = 0; it < NI; ++it) item(it, ex[it]);
+      for (int i = 0; i < 4; ++i) { h[i] = lo[i]; h[4 + i] = hi[i]; }
+      return KIND == LIN_WGRAD ? sums[r_tile + it * kRows] : 0.f;
+    };
+    if (part) {
+      // tile [RQ][RP] of split, tile, then its rows' sums
+      const size_t at = (size_t)split * rest + xcd_order(nth, rest);
+#pragma unroll
+      for (int it = 0; it < NI; ++it) {
+        float h[8];
+        const int rt = r_tile + it * kRows;
+        const float qsum = piece(it, h);
+        float* to = a.part + (at * RQ + rt) * RP + wp * TP * 16 + 8 * k;
+        *(f32x4*)to = f32x4{h[0], h[1], h[2], h[3]};
+        *(f32x4*)(to + 4) = f32x4{h[4], h[5], h[6], h[7]};
+        if (KIND == LIN_WGRAD && wp == 0 && k == 0) a.part_sum[at * RQ + rt] = qsum;
+      }
+    } else if constexpr (VEC) {
+      auto group = [&](auto first) {
+        float h[NB][8], qsum[NB];
+#pragma unroll
+        for (int it = 0; it < NB; ++it) qsum[it] = piece(first.value + it, h[it]);
+        te.template rows<first.value>(a, r_tile + first.value * kRows, kRows, h, qsum, ask);
+      };
+      group(std::integral_constant<int, 0>{});
+      if constexpr (NI > NB) group(std::integral_constant<int, NB>{});
+      if constexpr (NI > 2 * NB) group(std::integral_constant<int, 2 * NB>{});
+      if constexpr (NI > 3 * NB) group(std::integral_constant<int, 3 * NB>{});
+      static_assert(NI <= 4 * NB);
     } else {
 #pragma unroll 1
-      for (int it = 0; it < NI; ++it) item(it, Extra{});
+      for (int it = 0; it < NI; ++it) {
+        float h[8];
+        const float qsum = piece(it, h);
+        epilogue<KIND, false>(a, iq * RQ + r_tile + it * kRows, c, h, qsum, Extra{});
+      }
     }
+  }
+  if constexpr (VEC && KIND == LIN_WGRAD) {   // (the other epilogue writes it with the row)
+    const int q = iq * RQ + threadIdx.x;
+    if (!part && ip == 0 && a.dbias && threadIdx.x < RQ && q < a.Q.extent)
+      a.dbias[q] = a.accumulate ? a.dbias[q] + sums[threadIdx.x] : sums[threadIdx.x];
   }
 }
 

@@ -174,21 +174,27 @@ __device__ __forceinline__ void ckpt_value4(uint32_t w, float two, float (&v)[4]
 }
 __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
-// Columns c .. c + 7 (c a multiple of 8) into a checkpoint row; four neighbouring lanes, all
-// of them active, hold one group of 32.  v is 0 from the last column on.
-__device__ __forceinline__ void ckpt_store8(const DCkpt& k, size_t row, int c, const float (&v)[8]) {
+// Eight values as bytes, and their group's scale: four neighbouring lanes, all of them active, hold one
+// group of 32.  Lanes with in = false hold padding.
+__device__ __forceinline__ u32x2 ckpt_of8(bool in, const float (&v)[8], uint32_t& s) {
   uint32_t m = abs_bits(v[0]);
 #pragma unroll
   for (int i = 1; i < 8; ++i) m = max(m, abs_bits(v[i]));
+  m = in ? m : 0;
   m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0xB1, 0xf, 0xf, false));   // lane ^ 1
   m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x4E, 0xf, 0xf, false));   // lane ^ 2
-  const uint32_t s = ckpt_scale(m);
+  s = ckpt_scale(m);
   const float inv = ckpt_inv(s);
-  uint2 w = {pack_bytes(ckpt_round(v[0], inv), ckpt_round(v[1], inv), ckpt_round(v[2], inv), ckpt_round(v[3], inv)),
-             pack_bytes(ckpt_round(v[4], inv), ckpt_round(v[5], inv), ckpt_round(v[6], inv), ckpt_round(v[7], inv))};
-  if (s == 255u) w = uint2{0, 0};
+  const u32x2 w = {pack_bytes(ckpt_round(v[0], inv), ckpt_round(v[1], inv), ckpt_round(v[2], inv), ckpt_round(v[3], inv)),
+                   pack_bytes(ckpt_round(v[4], inv), ckpt_round(v[5], inv), ckpt_round(v[6], inv), ckpt_round(v[7], inv))};
+  return in && s != 255u ? w : u32x2{0, 0};
+}
+// Columns c .. c + 7 (c a multiple of 8) into a checkpoint row; v is 0 from the last column on.
+__device__ __forceinline__ void ckpt_store8(const DCkpt& k, size_t row, int c, const float (&v)[8]) {
+  uint32_t s;
+  const u32x2 w = ckpt_of8(true, v, s);
   if (c < k.ld) {
-    *(uint2*)(k.q + row * k.ld + c) = w;
+    *(u32x2*)(k.q + row * k.ld + c) = w;
     if (c % kCkptGroup == 0) k.scale[row * (size_t)(k.ld / kCkptGroup) + c / kCkptGroup] = (uint8_t)s;
   }
 }
@@ -219,21 +225,26 @@ __device__ __forceinline__ void ckpt_load8(const DCkpt& k, size_t row, int c, fl
 // One exponential serves the value and the slope; erff() alone takes about three times as long,
 // and the epilogues that call this are as long as a quarter of their product.
 struct Normal {
-  float cdf, e;
+  float tail, e;   // 1 - Phi(|h|)
 };
 __device__ __forceinline__ Normal normal(float h) {
   const float e = __builtin_amdgcn_exp2f(h * h * -0.72134752044448170f);          // -log2(e) / 2
   const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(h), 0.23164189f, 1.0f));        // p / sqrt(2)
-  float q = fmaf(t, 1.061405429f, -1.453152027f);
-  q = fmaf(q, t, 1.421413741f);
-  q = fmaf(q, t, -0.284496736f);
-  q = fmaf(q, t, 0.254829592f);
-  const float tail = 0.5f * q * t * e;
-  return Normal{h >= 0.f ? 1.0f - tail : tail, e};
+  float q = fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
+  q = fmaf(q, t, 0.5f * 1.421413741f);
+  q = fmaf(q, t, 0.5f * -0.284496736f);
+  q = fmaf(q, t, 0.5f * 0.254829592f);
+  return Normal{q * t * e, e};
 }
-__device__ __forceinline__ float gelu_value(float h) { return h * normal(h).cdf; }
+// h Phi(h) = max(h, 0) - |h| (1 - Phi(|h|)); |h| is kept finite, for h = inf (NaN comes through the tail)
+__device__ __forceinline__ float gelu_value(float h, Normal n) {
+  return fmaf(-fminf(fabsf(h), 1e30f), n.tail, fmaxf(h, 0.f));
+}
+__device__ __forceinline__ float gelu_value(float h) { return gelu_value(h, normal(h)); }
 // d/dh (h Phi(h)) = Phi(h) + h phi(h)
-__device__ __forceinline__ float gelu_slope(float h, Normal n) { return fmaf(h, 0.39894228040143268f * n.e, n.cdf); }
+__device__ __forceinline__ float gelu_slope(float h, Normal n) {
+  return fmaf(h, 0.39894228040143268f * n.e, h >= 0.f ? 1.0f - n.tail : n.tail);
+}
 
 // ----------------------------------------------------------------- launchers
 

@@ -75,7 +75,8 @@ ad::DMat mat(const ad_mat* m, int32_t cols) {
   d.ld = m->ld;
   d.bf16 = m->dtype == AD_BF16;
   const uintptr_t p = (uintptr_t)m->data;
-  d.vec = p % 16 == 0 && m->ld % (d.bf16 ? 8 : 4) == 0 && cols % 8 == 0;
+  // (kernels of whole vectors address a tile's 256 rows in 31 bits)
+  d.vec = p % 16 == 0 && m->ld % (d.bf16 ? 8 : 4) == 0 && cols % 8 == 0 && m->ld <= (1 << 20);
   return d;
 }
 

@@ -33,22 +33,19 @@ class FeedForward:
         self.dnarrow = empty(max_rows, d, dt=torch.bfloat16)
         self.grads = [torch.zeros(p.shape, dtype=torch.float32, device=dev) for p in params]
         self.rows = None
-        self.workspace = empty(0, dt=torch.uint8)
+        # One workspace for every call, large enough for any number of rows up to max_rows (a captured
+        # pass keeps its address).  What a call needs changes with its rows at multiples of 64 only,
+        # and the LayerNorm's grows with them.
+        need = ad.layer_norm_backward_workspace_size(max_rows, d)
+        for rows in range(64, max_rows + 64, 64):
+            need = max(need, *(size(rows, *shape) for shape in ((d, f), (f, d)) for size in
+                               (ad.linear_workspace_size, ad.linear_dgrad_workspace_size,
+                                ad.linear_wgrad_workspace_size)))
+        self.workspace = empty(max(need, 1), dt=torch.uint8)
 
     def zero_grads(self):
         for g in self.grads:
             g.zero_()
-
-    def _space(self, rows: int):
-        """One workspace for every call of a pass over `rows` rows."""
-        d, f = self.d, self.f
-        need = max(ad.linear_workspace_size(rows, f, d), ad.linear_workspace_size(rows, d, f),
-                   ad.linear_dgrad_workspace_size(rows, d, f), ad.linear_dgrad_workspace_size(rows, f, d),
-                   ad.linear_wgrad_workspace_size(rows, d, f), ad.linear_wgrad_workspace_size(rows, f, d),
-                   ad.layer_norm_backward_workspace_size(rows, d))
-        if self.workspace.numel() < need:
-            self.workspace = torch.empty(need, dtype=torch.uint8, device=self.w1.device)
-        return self.workspace
 
     def _kept(self, rows: int):
         cut = lambda k: ad.Ckpt(k.q[:rows], k.scale[:rows], k.cols)  # noqa: E731
@@ -59,7 +56,7 @@ class FeedForward:
         rows = x.shape[0]
         if rows > self.max_rows:
             raise ValueError(f"{rows} rows: the buffers hold {self.max_rows}")
-        ws = self._space(rows)
+        ws = self.workspace
         xhat, pre = self._kept(rows)
         ad.layer_norm(x, self.gain, self.bias, self.narrow[:rows], self.mean[:rows], self.rstd[:rows], xhat)
         ad.linear(self.narrow[:rows], self.w1, self.b1, ad.ACT_GELU, None, self.wide[:rows], None, pre, ws)
@@ -72,7 +69,7 @@ class FeedForward:
         rows = dout.shape[0]
         if rows != self.rows:
             raise ValueError(f"{rows} rows, but the last forward pass had {self.rows}")
-        ws = self._space(rows)
+        ws = self.workspace
         xhat, pre = self._kept(rows)
         ggain, gbias, gw1, gb1, gw2, gb2 = self.grads
         dlow, act, dpre = self.dnarrow[:rows], self.wide[:rows], self.wide2[:rows]

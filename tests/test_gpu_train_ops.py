@@ -619,6 +619,110 @@ def test_feed_forward_gradient_against_differences():
     assert abs(got - want) < 0.05 * max(abs(want), scale)
 
 
+def test_feed_forward_in_place_any_number_of_rows_and_refusals():
+    """out may be x; passes of every size share the buffers and the workspace, which stays where it is."""
+    d, f, most = 128, 320, 700
+    params, x, dout = _sublayer(31, d, f, most)
+    dev = [p.cuda() for p in params]
+    ff = FeedForward(dev, most)
+    space = ff.workspace.data_ptr()
+    for rows in (700, 1, 0, 65, 129, 512):
+        X, D = x[:rows].cuda(), dout[:rows].cuda()
+        alone = FeedForward(dev, max(rows, 1))
+        want, dwant = torch.empty_like(X), torch.empty_like(X)
+        alone.forward(X, want)
+        alone.backward(D, dwant)
+        ff.zero_grads()
+        got, dgot = X.clone(), torch.empty_like(X)
+        ff.forward(got, got)
+        ff.backward(D, dgot)
+        assert torch.equal(got, want) and torch.equal(dgot, dwant)
+        assert all(torch.equal(a, b) for a, b in zip(ff.grads, alone.grads))
+    assert ff.workspace.data_ptr() == space
+    with pytest.raises(ValueError, match="rows"):
+        ff.forward(torch.zeros(701, d, device="cuda"), torch.zeros(701, d, device="cuda"))
+    with pytest.raises(ValueError, match="last forward"):
+        ff.backward(torch.zeros(3, d, device="cuda"), torch.zeros(3, d, device="cuda"))
+
+
+def test_two_streams_at_once():
+    """Passes of two objects on two streams, each with its own workspace, at the same time."""
+    shapes = ((300, 256, 512), (170, 128, 384))
+    made = [(_sublayer(s[0], s[1], s[2], s[0]), s) for s in shapes]
+    objs, ins, outs, want = [], [], [], []
+    for (params, x, dout), s in made:
+        ff = FeedForward([p.cuda() for p in params], s[0])
+        X, D = x.cuda(), dout.cuda()
+        o, g = torch.empty_like(X), torch.empty_like(X)
+        ff.forward(X, o)
+        ff.backward(D, g)
+        objs.append(ff)
+        ins.append((X, D))
+        outs.append((o, g))
+        want.append([t.clone() for t in (o, g, *ff.grads)])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in objs]
+    for _ in range(5):
+        for ff, (X, D), (o, g), st in zip(objs, ins, outs, streams):
+            with torch.cuda.stream(st):
+                ff.zero_grads()
+                ff.forward(X, o)
+                ff.backward(D, g)
+    torch.cuda.synchronize()
+    for ff, (o, g), w in zip(objs, outs, want):
+        assert all(torch.equal(a, b) for a, b in zip((o, g, *ff.grads), w))
+
+
+def test_binding_refuses_what_the_tensors_show():
+    x, w = torch.zeros(8, 64, dtype=BF16, device="cuda"), torch.zeros(32, 64, dtype=BF16, device="cuda")
+    y = torch.zeros(8, 32, device="cuda")
+    ok = lambda **o: ad.linear(o.get("x", x), o.get("w", w), o.get("bias"), 0, o.get("res"), o.get("y", y), None,  # noqa: E731
+                               o.get("keep"), _space(ad.linear_workspace_size(8, 32, 64)))
+    ok()
+    for bad in (dict(w=w[:, :32]), dict(y=y[:4]), dict(res=torch.zeros(8, 31, device="cuda")), dict(y=y.t()[:8]),
+                dict(y=torch.zeros(32, 8, device="cuda").t()), dict(y=y.half()), dict(bias=torch.zeros(31, device="cuda")),
+                dict(bias=torch.zeros(64, device="cuda")[::2]), dict(keep=ad.Ckpt.empty(8, 33)), dict(w=w.cpu())):
+        with pytest.raises(ValueError):
+            ok(**bad)
+    with pytest.raises(ad.ADError, match="AD_EUNSUPPORTED"):
+        ok(x=x.float())
+    with pytest.raises(ad.ADError, match="AD_EINVAL"):
+        ok(x=x[:1].expand(8, 64))                       # every row the same memory: ld 0
+    with pytest.raises(ad.ADError, match="AD_ENOSPACE|AD_EINVAL"):
+        ad.linear_wgrad(torch.zeros(4096, 128, dtype=BF16, device="cuda"), torch.zeros(4096, 64, dtype=BF16, device="cuda"),
+                        None, None, None, torch.zeros(128, 64, device="cuda"), None, None)
+    with pytest.raises(ValueError, match="same dtype"):
+        ad.layer_norm(y, torch.ones(32, device="cuda"), torch.ones(32, dtype=BF16, device="cuda"), y)
+    k = ad.Ckpt.empty(8, 64)
+    with pytest.raises(ad.ADError, match="AD_EINVAL"):
+        ad.ckpt_unpack(k, torch.zeros(8, 64, device="cuda"), act=7)
+
+
+def test_checkpoint_of_nan_and_infinity_through_the_products():
+    """A group of the pre-activation that holds a NaN or an infinity reads as NaN, and only it does."""
+    g = _gen(17)
+    rows, n, k = 40, 256, 64
+    x, w = _rand(g, rows, k, dtype=BF16), _rand(g, n, k, dtype=BF16)
+    w[70, 5] = float("inf")
+    bias = torch.zeros(n, dtype=BF16)
+    bias[200] = float("nan")
+    y, kept, v = torch.empty(rows, n, device="cuda"), ad.Ckpt.empty(rows, n), torch.empty(rows, n, device="cuda")
+    ad.linear(x.cuda(), w.cuda(), bias.cuda(), ad.ACT_NONE, None, y, None, kept, _space(ad.linear_workspace_size(rows, n, k)))
+    ad.ckpt_unpack(kept, v)
+    bad = torch.isnan(v).all(0).cpu()
+    want = torch.zeros(n, dtype=torch.bool)
+    want[64:96] = want[192:224] = True
+    assert torch.equal(bad, want) and torch.equal(torch.isnan(v).any(0).cpu(), want)
+    assert bool(torch.isnan(y[:, 200]).all()) and not bool(torch.isfinite(y[:, 70]).any())
+    dx = torch.empty(rows, n, device="cuda")
+    dy, w2 = _rand(g, rows, k, dtype=BF16), _rand(g, k, n, dtype=BF16)
+    ad.linear_dgrad(dy.cuda(), w2.cuda(), ad.ACT_GELU, None, kept, dx, None, _space(ad.linear_dgrad_workspace_size(rows, k, n)))
+    assert torch.equal(torch.isnan(dx).any(0).cpu(), want)
+    dw = torch.empty(k, n, device="cuda")
+    ad.linear_wgrad(dy.cuda(), None, kept, None, None, dw, None, _space(ad.linear_wgrad_workspace_size(rows, k, n)))
+    assert torch.equal(torch.isnan(dw).any(0).cpu(), want)
+
+
 def test_other_stream_and_graph_replays():
     rows, d, f = 130, 256, 512
     params, x, dout = _sublayer(21, d, f, rows)

@@ -301,25 +301,29 @@ def draft_input(model: Model, w_fuse, b_fuse, w_in, b_in, batch: int, taps, hidd
 # they agree with each other, lie on the current device and have their columns side by side.
 
 _DTYPE = {torch.float32: AD_F32, torch.bfloat16: AD_BF16}
+_byref = ctypes.byref
+
+
+_current_device = torch.cuda.current_device
 
 
 def _device(name: str, t) -> int:
     """The current GPU, where the call's tensors have to be."""
     if not t.is_cuda:
         raise ValueError(f"{name} is on {t.device}, not on the current GPU")
-    return torch.cuda.current_device()
+    return _current_device()
 
 
-def _on_device(name: str, t, dev: int):
-    if t.get_device() != dev:
-        raise ValueError(f"{name} is on {t.device}, not on the current GPU")
+def _elsewhere(name: str, t):
+    return ValueError(f"{name} is on {t.device}, not on the current GPU")
 
 
 def _mat(name: str, t, rows: int, cols: int, dev: int):
     """A [rows][cols] float32 or bf16 tensor with adjacent columns as an ad_mat (None for None)."""
     if t is None:
         return None
-    _on_device(name, t, dev)
+    if t.get_device() != dev:
+        raise _elsewhere(name, t)
     if t.shape != (rows, cols):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(rows, cols)}")
     dtype = _DTYPE.get(t.dtype)
@@ -328,21 +332,29 @@ def _mat(name: str, t, rows: int, cols: int, dev: int):
     ld, step = t.stride()
     if step != 1 and cols > 1:
         raise ValueError(f"{name}: the columns of a row must be adjacent")
-    return ctypes.byref(Mat(t.data_ptr(), cols if rows <= 1 else ld, dtype))
+    return _byref(Mat(t.data_ptr(), ld if rows > 1 else cols, dtype))
 
 
-def _vec(name: str, t, n: int, dev: int, dtypes=(torch.float32, torch.bfloat16)):
-    """The address of a contiguous [n] tensor (None for None)."""
+def _vec(name: str, t, n: int, dev: int):
+    """The address of a contiguous [n] float32 or bf16 tensor (None for None)."""
     if t is None:
         return None
-    _on_device(name, t, dev)
-    if t.shape != (n,) or t.dtype not in dtypes or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous [{n}] tensor of {' or '.join(map(str, dtypes))}")
+    if t.get_device() != dev:
+        raise _elsewhere(name, t)
+    if t.shape != (n,) or t.dtype not in _DTYPE or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous [{n}] tensor of float32 or bfloat16")
     return t.data_ptr()
 
 
 def _floats(name: str, t, n: int, dev: int):
-    return None if t is None else _vec(name, t, n, dev, (torch.float32,))
+    """The address of a contiguous [n] float32 tensor (None for None)."""
+    if t is None:
+        return None
+    if t.get_device() != dev:
+        raise _elsewhere(name, t)
+    if t.shape != (n,) or t.dtype is not torch.float32 or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous [{n}] tensor of float32")
+    return t.data_ptr()
 
 
 def _params(a_name: str, a, b_name: str, b, n: int, dev: int):
@@ -355,10 +367,11 @@ def _params(a_name: str, a, b_name: str, b, n: int, dev: int):
 def _space(workspace, dev: int):
     if workspace is None:
         return None, 0
-    _on_device("workspace", workspace, dev)
+    if workspace.get_device() != dev:
+        raise _elsewhere("workspace", workspace)
     if not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous")
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    return workspace.data_ptr(), workspace.nbytes
 
 
 class Ckpt:
@@ -368,9 +381,10 @@ class Ckpt:
     def __init__(self, q, scale, cols: int):
         ld = LIB.ad_ckpt_ld(cols)
         rows = q.shape[0]
-        for name, t, dtype, width in (("q", q, torch.int8, ld), ("scale", scale, torch.uint8, ld // 32)):
-            if tuple(t.shape) != (rows, width) or t.dtype != dtype or not t.is_contiguous() or not ld:
-                raise ValueError(f"a checkpoint's {name} must be a contiguous [{rows}][{width}] {dtype} tensor")
+        if not ld or q.shape != (rows, ld) or q.dtype is not torch.int8 or not q.is_contiguous():
+            raise ValueError(f"a checkpoint's q must be a contiguous [{rows}][{ld}] int8 tensor")
+        if scale.shape != (rows, ld // 32) or scale.dtype is not torch.uint8 or not scale.is_contiguous():
+            raise ValueError(f"a checkpoint's scale must be a contiguous [{rows}][{ld // 32}] uint8 tensor")
         self.q, self.scale, self.rows, self.cols = q, scale, rows, cols
 
     @classmethod
@@ -383,11 +397,12 @@ class Ckpt:
 def _ckpt(name: str, k, rows: int, cols: int, dev: int):
     if k is None:
         return None
-    _on_device(name, k.q, dev)
-    _on_device(name, k.scale, dev)
-    if (k.rows, k.cols) != (rows, cols):
+    q, scale = k.q, k.scale
+    if q.get_device() != dev or scale.get_device() != dev:
+        raise _elsewhere(name, q)
+    if k.rows != rows or k.cols != cols:
         raise ValueError(f"{name} holds {(k.rows, k.cols)}, expected {(rows, cols)}")
-    return ctypes.byref(CkptView(k.q.data_ptr(), k.scale.data_ptr()))
+    return _byref(CkptView(q.data_ptr(), scale.data_ptr()))
 
 
 def ckpt_pack(x, ckpt: Ckpt, stream=None):

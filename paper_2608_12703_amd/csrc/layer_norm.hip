@@ -4,6 +4,12 @@
 // at a time (16 bytes of bf16), a wave 512, so rows of up to 2048 columns live in one wave's
 // registers (J = 1 .. 4 pieces a lane) and need no LDS for their sums; wider rows, up to 8192
 // columns, are spread over the four waves of a workgroup.
+//
+// Measured against a large copy's 4.9 TB/s: LayerNorm of 14336 x 1280 float32 rows into bf16 and
+// the checkpoint 36 us (3.6 TB/s), its backward pass over 13331 such rows kept whole 61 us (4.5),
+// packing 14336 x 5120 bf16 45 us (4.9), reading them back 41 us (5.4).  Loads must be whole
+// vectors in one block each: as selects of a load and a zero they became eight loads of 4 bytes
+// with a branch each, and the same LayerNorm took 52 us.
 #include <algorithm>
 
 #include "train.h"

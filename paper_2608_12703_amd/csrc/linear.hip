@@ -11,8 +11,19 @@
 // so that 16-byte loads go straight from memory to LDS; KS fragments are transposed by the
 // LDS read itself (ds_read_b64_tr_b16: 16 lanes read four r of 16 columns, lane c gets column c's
 // four).  P is the matrix instruction's first operand: a lane's four accumulators are four
-// consecutive columns of one output row, so the epilogue moves 16 bytes of float32 at a time, and
-// two neighbouring tiles hold a whole 8-bit checkpoint group of 32 columns.
+// consecutive columns of one output row.  The epilogue takes them through LDS once more, a row of tiles
+// at a time, to have 8 columns a lane and whole rows side by side: 16-byte stores, and four
+// lanes hold a checkpoint's group of 32.  (Stored straight from the accumulators, with every choice
+// made for every value, the epilogue took as long as 20 stages of products.)
+//
+// What bounds it.  A tile of T x T needs T^2 products for 2 T loads, and a CU takes in 25 to 60 bytes a
+// clock: 128 x 128 tiles, two workgroups a CU, are bound by that (860 of 1060 us for 8192 cubed
+// without any product), 256 x 256 tiles, eight waves of 128 x 64, by the products (660 us without
+// loads) and what keeps the two from overlapping whole (794 us, 1385 TFLOP/s; the library's
+// product 1485).  Launches too small for 256 x 256 tiles on every CU are bound by the time a stage takes
+// one workgroup: they have a ring of four stages of 128 x 128 and one workgroup a CU.  Then there are
+// a round's first loads and its epilogue, which nothing overlaps with 256 x 256 tiles: 13 us of 45 for
+// 20 stages.  plan() weighs these by what was measured.
 //
 // LDS bank conflicts.  KC rows are 128 bytes: the 16-byte piece c of row r sits at place
 // c ^ (r / 2 % 8), so the 16 rows that are read together cover every bank.  KS rows are 256 or
@@ -74,7 +85,7 @@ __device__ __forceinline__ uint4 short_row(const uint16_t* row, int i, int n) {
 
 // The part of one operand's stage that a wave moves: R rows (KC) or columns (KS) x 64 of r in
 // pieces of 1 KB, NW waves.  Direct: memory to LDS; otherwise through registers (any
-// alignment, element by element; or a checkpoint's 8-bit values, dequantised on the way).
+// alignment; or a checkpoint's 8-bit values, which become bf16 on the way, exactly).
 template <int R, int NW, bool KS, int SRC>
 struct Loader {
   static constexpr int N = R / 8 / NW;   // pieces a wave
@@ -314,76 +325,46 @@ struct Reader {
   }
 };
 
-// What an epilogue reads from memory for 8 columns of a row, requested before it is needed (whole
-// vectors only): the residual, the pre-activation, or the gradient that is added to.
+// The epilogue where not every matrix and parameter allows whole vectors, of the joined tiles, and of few
+// rows.  Few rows ask for what it reads (the residual and the bias of 8 columns of a row) before
+// their product, and have whole vectors.
 struct Extra {
   u32x4 lo, hi;
-  uint32_t scale;
-  float bias[8];   // forward, few rows only
+  float bias[8];
 };
-__device__ __forceinline__ void request8(const DMat& m, size_t row, int c, Extra& e) {
-  if (m.bf16) {
-    e.lo = *(const u32x4*)((const uint16_t*)m.p + row * m.ld + c);
-  } else {
-    const float* p = (const float*)m.p + row * m.ld + c;
-    e.lo = *(const u32x4*)p;
-    e.hi = *(const u32x4*)(p + 4);
-  }
-}
-__device__ __forceinline__ void received8(const DMat& m, const Extra& e, float (&v)[8]) {
-  if (m.bf16) {
-    widen8(e.lo, v);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[i] = __uint_as_float(e.lo[i]);
-      v[4 + i] = __uint_as_float(e.hi[i]);
-    }
-  }
-}
-template <int KIND>
 __device__ __forceinline__ Extra request(const LinArgs& a, int q, int c) {
   Extra e{};
   if (q >= a.Q.extent || c >= a.P.extent) return e;
-  if constexpr (KIND == LIN_FWD) {
-    if (a.res.p) request8(a.res, q, c, e);
-  } else if constexpr (KIND == LIN_DGRAD) {
-    if (a.gelu) {
-      if (a.ck.q) {
-        const u32x2 w = *(const u32x2*)(a.ck.q + (size_t)q * a.ck.ld + c);
-        e.lo[0] = w[0];
-        e.lo[1] = w[1];
-        e.scale = a.ck.scale[(size_t)q * (a.ck.ld / kCkptGroup) + c / kCkptGroup];
-      } else {
-        request8(a.pre, q, c, e);
-      }
-    }
-  } else {
-    if (a.accumulate) request8(a.out, q, c, e);
+  if (a.res.p && a.res.bf16) {
+    e.lo = *(const u32x4*)((const uint16_t*)a.res.p + (size_t)q * a.res.ld + c);
+  } else if (a.res.p) {
+    const float* p = (const float*)a.res.p + (size_t)q * a.res.ld + c;
+    e.lo = *(const u32x4*)p;
+    e.hi = *(const u32x4*)(p + 4);
   }
+  if (a.bias.p) load_vec8<true>(a.bias, c, a.P.extent, e.bias);
   return e;
 }
 
 // Columns c .. c + 7 of output row q (four neighbouring lanes hold one checkpoint group of 32; every
-// lane of the wave calls this).  qsum: wgrad's sum of dy for row q.  VEC: every matrix and
-// parameter allows whole vectors, and `e` is what request() asked for.
-// FEW: the bias has been asked for too.
-template <int KIND, bool VEC, bool FEW = false>
-__device__ __forceinline__ void epilogue(const LinArgs& a, int q, int c, float (&h)[8], float qsum, const Extra& e) {
+// lane of the wave calls this).  qsum: wgrad's sum of dy for row q.  FEW: `e` is what request()
+// asked for.
+template <int KIND, bool FEW = false>
+__device__ __forceinline__ void epilogue(const LinArgs& a, int q, int c, float (&h)[8], float qsum, const Extra& e = {}) {
   const int cols = a.P.extent;
   const bool row = q < a.Q.extent;
   if constexpr (KIND == LIN_FWD) {
     float b[8];
     if (a.bias.p) {
-      if (!FEW) load_vec8<VEC>(a.bias, c, cols, b);
+      if (!FEW) load_vec8(a.bias, c, cols, b);
 #pragma unroll
       for (int i = 0; i < 8; ++i) h[i] += FEW ? e.bias[i] : b[i];
     }
-    if (a.pre.p && row) store8<VEC>(a.pre, q, c, cols, h);
-    if (a.ck.q) {
+    if (a.pre.p && row) store8<FEW>(a.pre, q, c, cols, h);
+    if (!FEW && a.ck.q) {
       float z[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) z[i] = c + (VEC ? 0 : i) < cols ? h[i] : 0.f;   // (padding is written as 0)
+      for (int i = 0; i < 8; ++i) z[i] = c + i < cols ? h[i] : 0.f;   // (padding is written as 0)
       ckpt_store8(a.ck, q, row ? c : a.ck.ld, z);
     }
     if (!row) return;
@@ -391,22 +372,29 @@ __device__ __forceinline__ void epilogue(const LinArgs& a, int q, int c, float (
 #pragma unroll
       for (int i = 0; i < 8; ++i) h[i] = gelu_value(h[i]);
     if (a.res.p) {
-      if (VEC) received8(a.res, e, b);
-      else load8(a.res, q, c, cols, b);
+      if (!FEW) {
+        load8(a.res, q, c, cols, b);
+      } else if (a.res.bf16) {
+        widen8(e.lo, b);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          b[i] = __uint_as_float(e.lo[i]);
+          b[4 + i] = __uint_as_float(e.hi[i]);
+        }
+      }
 #pragma unroll
       for (int i = 0; i < 8; ++i) h[i] += b[i];
     }
-    store8<VEC>(a.out, q, c, cols, h);
+    store8<FEW>(a.out, q, c, cols, h);
   } else if constexpr (KIND == LIN_DGRAD) {
     if (!row) return;
     if (a.gelu) {
       float x[8];
       if (a.ck.q) {
-        if (VEC) ckpt_value8(u32x2{e.lo[0], e.lo[1]}, e.scale, x);
-        else ckpt_load8(a.ck, q, c, x);
+        ckpt_load8(a.ck, q, c, x);
       } else {
-        if (VEC) received8(a.pre, e, x);
-        else load8(a.pre, q, c, cols, x);
+        load8(a.pre, q, c, cols, x);
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -414,26 +402,25 @@ __device__ __forceinline__ void epilogue(const LinArgs& a, int q, int c, float (
         h[i] *= gelu_slope(x[i], n);
         x[i] = gelu_value(x[i], n);
       }
-      if (a.act_out.p) store8<VEC>(a.act_out, q, c, cols, x);
+      if (a.act_out.p) store8(a.act_out, q, c, cols, x);
     }
-    store8<VEC>(a.out, q, c, cols, h);
+    store8(a.out, q, c, cols, h);
   } else {
     if (!row) return;
     if (a.gain.p) {
       float g[8], b[8];
-      load_vec8<VEC>(a.gain, c, cols, g);
-      load_vec8<VEC>(a.shift, c, cols, b);
+      load_vec8(a.gain, c, cols, g);
+      load_vec8(a.shift, c, cols, b);
 #pragma unroll
       for (int i = 0; i < 8; ++i) h[i] = fmaf(h[i], g[i], b[i] * qsum);
     }
     if (a.accumulate) {
       float o[8];
-      if (VEC) received8(a.out, e, o);
-      else load8(a.out, q, c, cols, o);
+      load8(a.out, q, c, cols, o);
 #pragma unroll
       for (int i = 0; i < 8; ++i) h[i] += o[i];
     }
-    store8<VEC>(a.out, q, c, cols, h);
+    store8(a.out, q, c, cols, h);
     if (a.dbias && c == 0) a.dbias[q] = a.accumulate ? a.dbias[q] + qsum : qsum;
   }
 }
@@ -660,9 +647,9 @@ __device__ __forceinline__ void interleave() {
 constexpr int wait_for(int n) { return (n & 15) | ((n >> 4) << 14) | 0x0070; }
 
 // WP x WQ waves of TP x TQ 16 x 16 tiles, a ring of ST LDS stages (2 or 4; 2 where an operand goes
-// through registers).  A stage is two 32-wide steps of two phases each (the upper and the lower
-// half of the wave's P tiles).  While a wave multiplies in one phase it reads the next one's
-// operands, so no product waits for LDS.  The barrier falls before the stage's last phase, when all
+// through registers).  A stage is two 32-wide steps of G phases each (a half or a quarter of the
+// wave's P tiles).  While a wave multiplies in one phase it reads the next one's operands, so no
+// product waits for LDS.  The barrier falls before the stage's last phase, when all
 // of it is in registers and its LDS is free: the loads of the stage ST later start there.
 template <int KIND, int WP, int WQ, int TP, int TQ, int ST, bool PKS, int PSRC, bool QKS, int QSRC>
 __global__ void __launch_bounds__(WP* WQ* kWave, ST == 2 && !(PSRC == SRC_CKPT && QSRC == SRC_ANY) ? 2 : 1) linear_kernel(LinArgs a) {
@@ -960,7 +947,7 @@ __global__ void __launch_bounds__(WP* WQ* kWave, ST == 2 && !(PSRC == SRC_CKPT &
       for (int it = 0; it < NI; ++it) {
         float h[8];
         const float qsum = piece(it, h);
-        epilogue<KIND, false>(a, iq * RQ + r_tile + it * kRows, c, h, qsum, Extra{});
+        epilogue<KIND>(a, iq * RQ + r_tile + it * kRows, c, h, qsum);
       }
     }
   }
@@ -997,7 +984,7 @@ __global__ void __launch_bounds__(256) linear_join_kernel(LinArgs a) {
     }
     if (KIND == LIN_WGRAD) qsum += a.part_sum[at];
   }
-  epilogue<KIND, false>(a, q, c, h, qsum, Extra{});
+  epilogue<KIND>(a, q, c, h, qsum);
 }
 
 // Forward product of at most 16 RT rows (single tokens, a decoding batch): the weight is read once and
@@ -1014,10 +1001,7 @@ __global__ void __launch_bounds__(kFewWaves* kWave) linear_few_kernel(LinArgs a)
   constexpr int kItems = RT * 16 * PC / 8;
   const int t = threadIdx.x, q = t / (PC / 8), c = p0 + t % (PC / 8) * 8;
   Extra e{};
-  if (t < kItems) {
-    e = request<LIN_FWD>(a, q, c);
-    if (a.bias.p) load_vec8<true>(a.bias, c, a.P.extent, e.bias);
-  }
+  if (t < kItems) e = request(a, q, c);
   const int all = (a.K + 31) / 32, each = (all + NW - 1) / NW;
   const int beg = w * each, end = min(all, beg + each);
   const uint16_t* pw = a.P.p + (size_t)min(p0 + c16 % PC, a.P.extent - 1) * a.P.ld + 8 * g;
@@ -1062,7 +1046,7 @@ __global__ void __launch_bounds__(kFewWaves* kWave) linear_few_kernel(LinArgs a)
         h[4 + i] += hi[i];
       }
     }
-    epilogue<LIN_FWD, true, true>(a, q, c, h, 0.f, e);
+    epilogue<LIN_FWD, true>(a, q, c, h, 0.f, e);
   }
 }
 
@@ -1079,7 +1063,8 @@ constexpr int kCUs = 256;
 
 // Workgroups at once, and measured microseconds: of a 64-wide step, and of a round of workgroups besides
 // (its first loads, its epilogues).  14336 rows, width 1280 to 5120 (20 steps) and 5120 to 1280 (80):
-// large 206 and 175, pairs 219 and 204, deep 276 and 215; 1536 rows, 1280 to 2560: 45, 27, 20.
+// large 185 and 174, pairs 202 and 204, deep 241 and 211; 1536 rows, 1280 to 2560: 45, 27, 23.  The
+// plan of least cost was within 0.6% of the best of the three over 147 products of 1 to 14336 rows.
 struct Shape {
   int tile;
   bool deep;

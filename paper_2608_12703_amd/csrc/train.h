@@ -29,7 +29,7 @@ struct DCkpt {
 constexpr int kCkptGroup = 32;
 inline int ckpt_ld(int cols) { return (cols + 127) / 128 * 128; }
 
-// Largest launch of a plain 1-D grid used here: the launchers check against it.
+// The widest row that a LayerNorm workgroup keeps in its registers.
 constexpr int kLnMaxCols = 8192;
 
 // ----------------------------------------------------------------- elements
@@ -241,9 +241,9 @@ __device__ __forceinline__ float gelu_value(float h, Normal n) {
   return fmaf(-fminf(fabsf(h), 1e30f), n.tail, fmaxf(h, 0.f));
 }
 __device__ __forceinline__ float gelu_value(float h) { return gelu_value(h, normal(h)); }
-// d/dh (h Phi(h)) = Phi(h) + h phi(h)
+// d/dh (h Phi(h)) = Phi(h) + h phi(h); h is kept finite likewise: 1 at infinity, 0 at -infinity
 __device__ __forceinline__ float gelu_slope(float h, Normal n) {
-  return fmaf(h, 0.39894228040143268f * n.e, h >= 0.f ? 1.0f - n.tail : n.tail);
+  return fmaf(__builtin_amdgcn_fmed3f(h, -1e30f, 1e30f), 0.39894228040143268f * n.e, h >= 0.f ? 1.0f - n.tail : n.tail);
 }
 
 // ----------------------------------------------------------------- launchers

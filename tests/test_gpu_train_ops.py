@@ -723,6 +723,26 @@ def test_checkpoint_of_nan_and_infinity_through_the_products():
     assert torch.equal(torch.isnan(dw).any(0).cpu(), want)
 
 
+@pytest.mark.parametrize("k", [64, 61])
+def test_gelu_of_infinities_and_large_values(k):
+    """GELU is 0 at -infinity, its slope 0 there and 1 at infinity; neither is NaN for any number."""
+    h = torch.tensor([float("inf"), -float("inf"), 3e38, -3e38, 1e20, -1e20, 50.0, -50.0], dtype=BF16)
+    pre = h.repeat(3, 8)[:, :k].contiguous()
+    up = (pre > 0).double()
+    dy = torch.ones(3, 16, dtype=BF16)
+    w = torch.full((16, k), 0.125, dtype=BF16)
+    dx, again = torch.empty(3, k, device="cuda"), torch.empty(3, k, dtype=BF16, device="cuda")
+    ad.linear_dgrad(dy.cuda(), w.cuda(), ad.ACT_GELU, pre.cuda(), None, dx, again, _space(ad.linear_dgrad_workspace_size(3, 16, k)))
+    assert torch.equal(dx.double().cpu(), 2 * up)
+    want = torch.where(pre > 0, pre, torch.zeros_like(pre))
+    assert torch.equal(again.cpu().float().abs(), want.float())
+    # the forward product: zeros times a weight, and the values as its bias
+    y = torch.empty(3, k, dtype=BF16, device="cuda")
+    ad.linear(torch.zeros(3, 16, dtype=BF16, device="cuda"), w.t().contiguous().cuda(), pre[0].cuda(), ad.ACT_GELU, None, y, None,
+              None, _space(ad.linear_workspace_size(3, k, 16)))
+    assert torch.equal(y.cpu().float().abs(), want.float())
+
+
 def test_other_stream_and_graph_replays():
     rows, d, f = 130, 256, 512
     params, x, dout = _sublayer(21, d, f, rows)

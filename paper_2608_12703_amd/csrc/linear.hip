@@ -468,7 +468,10 @@ struct TileRows {   // float32 or bf16 rows
     }
   }
 };
-template <int KIND>
+// What the input's gradient multiplies by: nothing, or the slope at a pre-activation of this kind.  (A choice
+// inside the kernel would keep the waits for it from being exact.)
+enum Slope : int { SLOPE_NONE = 0, SLOPE_BF16 = 1, SLOPE_CKPT = 2 };
+template <int KIND, int SLOPE>
 struct TileEpilogue {
   TileRows out, in, also;    // in: residual, pre-activation or old gradient; also: pre or act_out
   TileMat q, scale;          // the checkpoint
@@ -504,7 +507,7 @@ struct TileEpilogue {
   template <int N>
   __device__ __forceinline__ void ask(const LinArgs& a, int r, int step, Ask (&e)[N]) const {
     if constexpr (KIND == LIN_DGRAD) {
-      if (a.gelu && a.ck.q) {
+      if constexpr (SLOPE == SLOPE_CKPT) {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
           const auto w = __builtin_amdgcn_raw_buffer_load_b64(descriptor(q.base, q.size), q.at(r + n * step), 0, 0);
@@ -512,22 +515,21 @@ struct TileEpilogue {
           e[n].lo[1] = w[1];
           e[n].s = __builtin_amdgcn_raw_buffer_load_b8(descriptor(scale.base, scale.size), scale.at(r + n * step), 0, 0);
         }
-        return;
       }
-      if (!a.gelu) return;
+      if (SLOPE != SLOPE_BF16) return;
     } else if (KIND == LIN_FWD ? !a.res.p : !a.accumulate) {
       return;
     }
 #pragma unroll
     for (int n = 0; n < N; ++n) e[n].lo = in.m.get(in.m.at(r + n * step));
-    if (in.bf16) return;
+    if (KIND == LIN_DGRAD || in.bf16) return;   // (a kept pre-activation is bf16)
 #pragma unroll
     for (int n = 0; n < N; ++n) e[n].hi = in.m.get(in.m.at(r + n * step) + 16);
   }
   // (items I0 .. I0 + N - 1 of those asked for)
   template <int I0, int N, int M>
   __device__ __forceinline__ void received(const Ask (&e)[M], float (&v)[N][8]) const {
-    if (in.bf16) {
+    if (KIND == LIN_DGRAD || in.bf16) {
 #pragma unroll
       for (int n = 0; n < N; ++n) widen8(e[I0 + n].lo, v[n]);
     } else {
@@ -572,8 +574,8 @@ struct TileEpilogue {
           for (int i = 0; i < 8; ++i) h[n][i] += x[n][i];
       }
     } else if constexpr (KIND == LIN_DGRAD) {
-      if (a.gelu) {
-        if (a.ck.q) {
+      if constexpr (SLOPE != SLOPE_NONE) {
+        if constexpr (SLOPE == SLOPE_CKPT) {
 #pragma unroll
           for (int n = 0; n < N; ++n) ckpt_value8(u32x2{e[I0 + n].lo[0], e[I0 + n].lo[1]}, e[I0 + n].s, x[n]);
         } else {
@@ -651,7 +653,8 @@ constexpr int wait_for(int n) { return (n & 15) | ((n >> 4) << 14) | 0x0070; }
 // wave's P tiles).  While a wave multiplies in one phase it reads the next one's operands, so no
 // product waits for LDS.  The barrier falls before the stage's last phase, when all
 // of it is in registers and its LDS is free: the loads of the stage ST later start there.
-template <int KIND, int WP, int WQ, int TP, int TQ, int ST, bool PKS, int PSRC, bool QKS, int QSRC>
+// SLOPE: what the epilogue of direct operands reads (the other one sees for itself).
+template <int KIND, int WP, int WQ, int TP, int TQ, int ST, bool PKS, int PSRC, bool QKS, int QSRC, int SLOPE = SLOPE_NONE>
 __global__ void __launch_bounds__(WP* WQ* kWave, ST == 2 && !(PSRC == SRC_CKPT && QSRC == SRC_ANY) ? 2 : 1) linear_kernel(LinArgs a) {
   constexpr int NW = WP * WQ, RP = WP * TP * 16, RQ = WQ * TQ * 16, NS = TQ / WP;
   static_assert(TP % 2 == 0 && TQ % WP == 0);
@@ -899,16 +902,24 @@ __global__ void __launch_bounds__(WP* WQ* kWave, ST == 2 && !(PSRC == SRC_CKPT &
   constexpr int NI = 16 * CPR / kWave, kRows = kWave / CPR;   // items of a row of tiles, rows between them
   constexpr int NB = KIND == LIN_FWD ? NI : 2;                 // items at a time (as many as fit the registers)
   const int r0 = late / CPR, k = late % CPR, c = ip * RP + wp * TP * 16 + 8 * k;
-  TileEpilogue<KIND> te;
+  TileEpilogue<KIND, SLOPE> te;
   if (VEC) te.init(a, iq * RQ, c);
+  // What a row of tiles reads is asked for before the row's accumulators are moved; a pre-activation, which
+  // is small, while the row before it is worked on (251 against 267 us for 14336 rows of 1280 into
+  // 5120, slope and activation).
+  constexpr bool kAhead = SLOPE != SLOPE_NONE;
+  auto row_of = [&](int j) { return (wq * TQ + slot(j)) * 16 + r0; };   // of the tile: this lane's first item's
+  typename TileEpilogue<KIND, SLOPE>::Ask asked[kAhead ? 2 : 1][NI];
+  if (kAhead && !part) te.ask(a, row_of(0), kRows, asked[0]);
 #pragma unroll
   for (int j = 0; j < TQ; ++j) {
-    const int r_tile = (wq * TQ + slot(j)) * 16 + r0;   // row within the tile of this lane's first item
-    typename TileEpilogue<KIND>::Ask ask[NI];
-    if (VEC && !part) te.ask(a, r_tile, kRows, ask);
+    const int r_tile = row_of(j);
+    auto& ask = asked[kAhead ? j % 2 : 0];
+    if (VEC && !kAhead && !part) te.ask(a, r_tile, kRows, ask);
 #pragma unroll
     for (int i = 0; i < TP; ++i)
       mine[c16 * 4 * TP + ((4 * i + g) ^ c16)] = __builtin_bit_cast(uint4, acc[i][j]);
+    if (kAhead && !part && j + 1 < TQ) te.ask(a, row_of(j + 1), kRows, asked[kAhead ? (j + 1) % 2 : 0]);
     auto piece = [&](int it, float (&h)[8]) {
       const int r = it * kRows + r0;
       const f32x4 lo = __builtin_bit_cast(f32x4, mine[r * 4 * TP + ((2 * k) ^ r)]);
@@ -1119,21 +1130,21 @@ size_t part_floats(const Plan& r) {
   return r.S > 1 ? (size_t)r.S * (r.tiles_p * r.tiles_q - r.whole) * ((size_t)r.tile * r.tile + r.tile) : 0;
 }
 
-template <int KIND, bool PKS, int PSRC, bool QKS, int QSRC>
+template <int KIND, bool PKS, int PSRC, bool QKS, int QSRC, int SLOPE = SLOPE_NONE>
 void launch_one(const LinArgs& a, const Plan& r, hipStream_t st) {
   const unsigned rest = a.tiles_p * a.tiles_q - a.whole, grid = a.whole + rest * a.S;
   if (r.tile == 256) {
     if constexpr (PSRC != SRC_ANY && QSRC == SRC_DIRECT) {
-      linear_kernel<KIND, 2, 4, 8, 4, 2, PKS, PSRC, QKS, QSRC><<<grid, 512, 0, st>>>(a);
+      linear_kernel<KIND, 2, 4, 8, 4, 2, PKS, PSRC, QKS, QSRC, SLOPE><<<grid, 512, 0, st>>>(a);
       if (rest) linear_join_kernel<KIND, 256><<<rest * 32, 256, 0, st>>>(a);
     }
     return;
   }
   if constexpr (PSRC == SRC_DIRECT && QSRC == SRC_DIRECT) {
-    if (r.deep) linear_kernel<KIND, 2, 2, 4, 4, 4, PKS, PSRC, QKS, QSRC><<<grid, 256, 0, st>>>(a);
-    else linear_kernel<KIND, 2, 2, 4, 4, 2, PKS, PSRC, QKS, QSRC><<<grid, 256, 0, st>>>(a);
+    if (r.deep) linear_kernel<KIND, 2, 2, 4, 4, 4, PKS, PSRC, QKS, QSRC, SLOPE><<<grid, 256, 0, st>>>(a);
+    else linear_kernel<KIND, 2, 2, 4, 4, 2, PKS, PSRC, QKS, QSRC, SLOPE><<<grid, 256, 0, st>>>(a);
   } else {
-    linear_kernel<KIND, 2, 2, 4, 4, 2, PKS, PSRC, QKS, QSRC><<<grid, 256, 0, st>>>(a);
+    linear_kernel<KIND, 2, 2, 4, 4, 2, PKS, PSRC, QKS, QSRC, SLOPE><<<grid, 256, 0, st>>>(a);
   }
   if (rest) linear_join_kernel<KIND, 128><<<rest * 8, 256, 0, st>>>(a);
 }
@@ -1203,7 +1214,9 @@ void launch_linear(int kind, LinArgs a, hipStream_t st) {
     if (direct) launch_one<LIN_FWD, false, SRC_DIRECT, false, SRC_DIRECT>(a, r, st);
     else launch_one<LIN_FWD, false, SRC_ANY, false, SRC_ANY>(a, r, st);
   } else if (kind == LIN_DGRAD) {
-    if (direct) launch_one<LIN_DGRAD, true, SRC_DIRECT, false, SRC_DIRECT>(a, r, st);
+    if (direct && a.gelu && a.ck.q) launch_one<LIN_DGRAD, true, SRC_DIRECT, false, SRC_DIRECT, SLOPE_CKPT>(a, r, st);
+    else if (direct && a.gelu) launch_one<LIN_DGRAD, true, SRC_DIRECT, false, SRC_DIRECT, SLOPE_BF16>(a, r, st);
+    else if (direct) launch_one<LIN_DGRAD, true, SRC_DIRECT, false, SRC_DIRECT>(a, r, st);
     else launch_one<LIN_DGRAD, true, SRC_ANY, false, SRC_ANY>(a, r, st);
   } else if (!a.P.p) {
     if (direct) launch_one<LIN_WGRAD, true, SRC_CKPT, true, SRC_DIRECT>(a, r, st);

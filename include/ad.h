@@ -402,7 +402,7 @@ typedef struct {
 } ad_ckpt;
 
 /* Activations of the products below: none, or the decoder's GELU(h) = h Phi(h) (0 at -infinity),
- * with Phi from an approximation of erf that is good to 1.5e-7. */
+ * with Phi from approximations that are good to 1e-7. */
 typedef enum { AD_ACT_NONE = 0, AD_ACT_GELU = 1 } ad_act;
 
 int32_t ad_ckpt_ld(int32_t cols);

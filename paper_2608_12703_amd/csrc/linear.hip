@@ -1187,10 +1187,11 @@ void launch_few(const LinArgs& a, const FewPlan& f, hipStream_t st) {
   linear_few_kernel<RT, PC><<<f.grid, kFewWaves * kWave, 0, st>>>(a);
 }
 
-size_t lin_part_floats(int P, int Q, int K) {
+size_t lin_part_floats(int kind, int P, int Q, int K) {
   // (asked for before the operands are known)
-  return std::max({part_floats(plan(P, Q, K, true, false)), part_floats(plan(P, Q, K, true, true)),
-                   part_floats(plan(P, Q, K, false, false)), part_floats(plan(P, Q, K, false, true))});
+  const size_t n = std::max(part_floats(plan(P, Q, K, true, false)), part_floats(plan(P, Q, K, false, false)));
+  if (kind != LIN_WGRAD) return n;
+  return std::max({n, part_floats(plan(P, Q, K, true, true)), part_floats(plan(P, Q, K, false, true))});
 }
 
 void launch_linear(int kind, LinArgs a, hipStream_t st) {

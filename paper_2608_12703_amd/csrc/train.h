@@ -312,8 +312,8 @@ struct LinArgs {
   DCkpt ck;              // fwd: the pre-activation out; dgrad: in
   float* dbias;
 };
-// Floats of workspace of a product with these extents.
-size_t lin_part_floats(int P, int Q, int K);
+// Floats of workspace of a product of this kind with these extents.
+size_t lin_part_floats(int kind, int P, int Q, int K);
 void launch_linear(int kind, LinArgs a, hipStream_t st);
 
 }  // namespace ad

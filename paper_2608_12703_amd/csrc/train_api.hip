@@ -94,7 +94,7 @@ size_t ln_bwd_bytes(int32_t rows, int32_t cols) {
 size_t linear_bytes(int kind, int32_t rows, int32_t n, int32_t k) {
   const int P = kind == ad::LIN_FWD ? n : k, Q = kind == ad::LIN_WGRAD ? n : rows,
             K = kind == ad::LIN_FWD ? k : kind == ad::LIN_DGRAD ? n : rows;
-  return Q > 0 ? align256(4 * ad::lin_part_floats(P, Q, K)) : 0;
+  return Q > 0 ? align256(4 * ad::lin_part_floats(kind, P, Q, K)) : 0;
 }
 ad_status linear_space(int kind, int32_t rows, int32_t n, int32_t k, size_t* bytes) {
   if (!bytes) return bad("NULL argument");

@@ -6,7 +6,7 @@
 // columns, are spread over the four waves of a workgroup.
 //
 // Measured against a large copy's 4.9 TB/s: LayerNorm of 14336 x 1280 float32 rows into bf16 and
-// the checkpoint 36 us (3.6 TB/s), its backward pass over 13331 such rows kept whole 61 us (4.5),
+// the checkpoint 34 us (3.8 TB/s), its backward pass over 13331 such rows kept whole 60 us (4.5),
 // packing 14336 x 5120 bf16 45 us (4.9), reading them back 41 us (5.4).  Loads must be whole
 // vectors in one block each: as selects of a load and a zero they became eight loads of 4 bytes
 // with a branch each, and the same LayerNorm took 52 us.
@@ -43,48 +43,41 @@ __device__ __forceinline__ float row_total(float v, float* red) {
   return v;
 }
 
-// W: waves per row (1 or 4), R rows at a time, VEC: every matrix and parameter allows whole vectors.
-// The statistics are two passes over the registers: the mean, then the squared deviations from it
-// (no cancellation of large means).  Columns past the row's end hold 0 throughout: with whole
-// vectors a lane's piece is all in or all out, so it deviates from 0 instead of the mean.
-template <int J, int W, int R, bool VEC>
-__global__ void __launch_bounds__(256) ln_fwd_kernel(LnFwdArgs a) {
+// W: waves per row (1 or 4), VEC: every matrix and parameter allows whole vectors.  The statistics
+// are two passes over the registers: the mean, then the squared deviations from it (no
+// cancellation of large means).  Columns past the row's end hold 0 throughout: with whole vectors a
+// lane's piece is all in or all out, so it deviates from 0 instead of the mean.  A row a wave: two
+// at a time had more loads in flight but fewer waves, and took 28.3 us for 14336 x 1280 float32
+// into bf16, in place of 26.7.
+// (The bound keeps the element paths of J = 3 at four waves a SIMD: 38 in place of 42 us.)
+template <int J, int W, bool VEC>
+__global__ void __launch_bounds__(256, J == 3 ? 4 : 1) ln_fwd_kernel(LnFwdArgs a) {
   __shared__ float red[4];
   const int t = W == 1 ? threadIdx.x % kWave : threadIdx.x;
-  const int first = R * (W == 1 ? blockIdx.x * 4 + threadIdx.x / kWave : blockIdx.x);
-  const int stride = R * (W == 1 ? gridDim.x * 4 : gridDim.x);
+  const int first = W == 1 ? blockIdx.x * 4 + threadIdx.x / kWave : blockIdx.x;
+  const int stride = W == 1 ? gridDim.x * 4 : gridDim.x;
   constexpr int kStep = 8 * kWave * W;
   const float inv_n = 1.0f / (float)a.cols;
   // (with W == 4 every wave of the workgroup has the same rows, so the barriers are met by all)
-  for (int row0 = first; row0 < a.rows; row0 += stride) {
-    float x[R][J][8], mean[R], rstd[R];
+  for (int row = first; row < a.rows; row += stride) {
+    float x[J][8], s = 0.f, v = 0.f;
 #pragma unroll
-    for (int u = 0; u < R; ++u)
+    for (int j = 0; j < J; ++j) load8<VEC>(a.x, row, 8 * t + j * kStep, a.cols, x[j]);
 #pragma unroll
-      for (int j = 0; j < J; ++j) load8<VEC>(a.x, min(row0 + u, a.rows - 1), 8 * t + j * kStep, a.cols, x[u][j]);
+    for (int j = 0; j < J; ++j)
 #pragma unroll
-    for (int u = 0; u < R; ++u) {
-      float s = 0.f;
+      for (int i = 0; i < 8; ++i) s += x[j][i];
+    const float mean = row_total<W>(s, red) * inv_n;
 #pragma unroll
-      for (int j = 0; j < J; ++j)
+    for (int j = 0; j < J; ++j) {
+      const float m = 8 * t + j * kStep < a.cols ? mean : 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s += x[u][j][i];
-      mean[u] = row_total<W>(s, red) * inv_n;
-    }
-#pragma unroll
-    for (int u = 0; u < R; ++u) {
-      float v = 0.f;
-#pragma unroll
-      for (int j = 0; j < J; ++j) {
-        const float m = 8 * t + j * kStep < a.cols ? mean[u] : 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          x[u][j][i] = VEC || 8 * t + j * kStep + i < a.cols ? x[u][j][i] - m : 0.f;
-          v = fmaf(x[u][j][i], x[u][j][i], v);
-        }
+      for (int i = 0; i < 8; ++i) {
+        x[j][i] = VEC || 8 * t + j * kStep + i < a.cols ? x[j][i] - m : 0.f;
+        v = fmaf(x[j][i], x[j][i], v);
       }
-      rstd[u] = 1.0f / sqrtf(row_total<W>(v, red) * inv_n + kEps);
     }
+    const float rstd = 1.0f / sqrtf(row_total<W>(v, red) * inv_n + kEps);
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       const int c = 8 * t + j * kStep;
@@ -92,30 +85,22 @@ __global__ void __launch_bounds__(256) ln_fwd_kernel(LnFwdArgs a) {
       load_vec8<VEC>(a.gain, c, a.cols, g);
       load_vec8<VEC>(a.bias, c, a.cols, b);
 #pragma unroll
-      for (int u = 0; u < R; ++u) {
-        if (R > 1 && row0 + u >= a.rows) break;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          x[u][j][i] *= rstd[u];
-          y[i] = fmaf(x[u][j][i], g[i], b[i]);
-        }
-        if (!VEC && rstd[u] != rstd[u])   // a NaN row: its padding is 0 all the same
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[u][j][i] = c + i < a.cols ? x[u][j][i] : 0.f;
-        if (VEC && c >= a.cols)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[u][j][i] = 0.f;
-        store8<VEC>(a.y, row0 + u, c, a.cols, y);
-        if (a.xhat.q) ckpt_store8(a.xhat, row0 + u, c, x[u][j]);
+      for (int i = 0; i < 8; ++i) {
+        x[j][i] *= rstd;
+        y[i] = fmaf(x[j][i], g[i], b[i]);
       }
+      if (!VEC && rstd != rstd)   // a NaN row: its padding is 0 all the same
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[j][i] = c + i < a.cols ? x[j][i] : 0.f;
+      if (VEC && c >= a.cols)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[j][i] = 0.f;
+      store8<VEC>(a.y, row, c, a.cols, y);
+      if (a.xhat.q) ckpt_store8(a.xhat, row, c, x[j]);
     }
     if (t == 0) {
-#pragma unroll
-      for (int u = 0; u < R; ++u)
-        if (row0 + u < a.rows) {
-          if (a.mean) a.mean[row0 + u] = mean[u];
-          if (a.rstd) a.rstd[row0 + u] = rstd[u];
-        }
+      if (a.mean) a.mean[row] = mean;
+      if (a.rstd) a.rstd[row] = rstd;
     }
   }
 }
@@ -287,20 +272,13 @@ void by_width(int cols, A&&... args) {
 bool whole(const DMat& m) { return !m.p || m.vec; }
 bool whole(const DVec& v, int cols) { return v.vec && cols % 8 == 0; }
 
-constexpr int kTwoRows = 8192;   // rows from which a wave takes two at a time (with fewer, one keeps more waves busy)
-
 template <int J, int W>
 struct Fwd {
-  template <int R, bool VEC>
-  static void go(const LnFwdArgs& a, hipStream_t st) {
-    const int rows = (a.rows + R - 1) / R;
-    ln_fwd_kernel<J, W, R, VEC><<<grid_of(W == 1 ? (rows + 3) / 4 : rows), 256, 0, st>>>(a);
-  }
   static void run(const LnFwdArgs& a, hipStream_t st) {
     const bool vec = whole(a.x) && whole(a.y) && whole(a.gain, a.cols) && whole(a.bias, a.cols);
-    if (!vec) go<1, false>(a, st);
-    else if (W == 1 && a.rows >= kTwoRows) go<W == 1 ? 2 : 1, true>(a, st);
-    else go<1, true>(a, st);
+    const int grid = grid_of(W == 1 ? (a.rows + 3) / 4 : a.rows);
+    if (vec) ln_fwd_kernel<J, W, true><<<grid, 256, 0, st>>>(a);
+    else ln_fwd_kernel<J, W, false><<<grid, 256, 0, st>>>(a);
   }
 };
 template <int J, int W>

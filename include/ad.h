@@ -390,8 +390,9 @@ typedef struct {
  * s the smallest byte >= 1 with max |v| <= 127 * 2^(s - 127); a value is q * 2^(s - 127)
  * with q = v / 2^(s - 127) rounded to the nearest integer, ties to even.  So the error is at
  * most half a step, 2^(s - 128) < max |v| / 127 (2^-127 where s = 1), and every value is
- * exact in bf16: products read checkpoints without a further rounding.  A group that holds
- * a NaN or an infinity has s = 255 and reads as NaN throughout.  Rows are padded to
+ * exact in bf16: products read checkpoints without a further rounding.  (A value within half a step
+ * of 2^128 rounds to it, which reads as an infinity; its group's other values are not touched.)  A
+ * group that holds a NaN or an infinity has s = 255 and reads as NaN throughout.  Rows are padded to
  * ad_ckpt_ld(cols) = cols rounded up to 128: q is [rows][ld], scale [rows][ld / 32]; padding
  * is written as q = 0, s = 1.  q is 16-byte aligned and scale 4-byte aligned (AD_EINVAL
  * otherwise).

@@ -162,15 +162,12 @@ __device__ __forceinline__ uint32_t pack_bytes(uint32_t a, uint32_t b, uint32_t 
 }
 // (s = 255: infinity, and every q of the group is 0, so the product is NaN)
 __device__ __forceinline__ float ckpt_two(uint32_t s) { return __uint_as_float(s << 23); }
-// Four values q * two: the bytes with their sign bit turned are q + 128 unsigned, which converts
-// in one instruction, and (q + 128) two - 128 two is exact.
+// Four values q * two, exact up to float32's range (2^128 is an infinity).  A signed byte converts in one
+// instruction; as (q + 128 - 128) two from unsigned ones the weight gradient of 14336 rows from a checkpoint
+// took 240 us in place of 225.  (q + 128) two - 128 two has no place here: 128 two overflows from s = 248 on.
 __device__ __forceinline__ void ckpt_value4(uint32_t w, float two, float (&v)[4]) {
-  const uint32_t u = w ^ 0x80808080u;
-  const float low = -128.f * two;
-  v[0] = fmaf((float)(u & 0xffu), two, low);
-  v[1] = fmaf((float)((u >> 8) & 0xffu), two, low);
-  v[2] = fmaf((float)((u >> 16) & 0xffu), two, low);
-  v[3] = fmaf((float)(u >> 24), two, low);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = (float)(int8_t)(w >> (8 * i)) * two;
 }
 __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 

@@ -30,29 +30,42 @@ __device__ __forceinline__ float wave_total(float v) {
   return rows4_sum(v);
 }
 
-// Sum over the lanes that share a row: the wave, or the workgroup's four waves.
-template <int W>
-__device__ __forceinline__ float row_total(float v, float* red) {
-  v = wave_total(v);
+// Sums over the lanes that share a row: the wave, or the workgroup's four waves.
+template <int W, int N>
+__device__ __forceinline__ void row_totals(float (&v)[N], float (*red)[4]) {
+#pragma unroll
+  for (int n = 0; n < N; ++n) v[n] = wave_total(v[n]);
   if constexpr (W == 4) {
     __syncthreads();
-    if (threadIdx.x % kWave == 0) red[threadIdx.x / kWave] = v;
+    if (threadIdx.x % kWave == 0)
+#pragma unroll
+      for (int n = 0; n < N; ++n) red[n][threadIdx.x / kWave] = v[n];
     __syncthreads();
-    v = (red[0] + red[1]) + (red[2] + red[3]);
+#pragma unroll
+    for (int n = 0; n < N; ++n) v[n] = (red[n][0] + red[n][1]) + (red[n][2] + red[n][3]);
   }
-  return v;
+}
+template <int W>
+__device__ __forceinline__ float row_total(float v, float (*red)[4]) {
+  float one[1] = {v};
+  row_totals<W>(one, red);
+  return one[0];
 }
 
 // W: waves per row (1 or 4), VEC: every matrix and parameter allows whole vectors.  The statistics
-// are two passes over the registers: the mean, then the squared deviations from it (no
-// cancellation of large means).  Columns past the row's end hold 0 throughout: with whole vectors a
+// are two passes over the registers: the mean m, then the sum of the deviations from it and that of
+// their squares.  m is off by its roundings, which a large mean makes large beside the deviations (a row of
+// 1e5 came out as 1 instead of 0): the deviations' own mean c is that error, mean = m + c and
+// var = sum (x - m)^2 / n - c^2, where c^2 is as small as the roundings.  Columns past the row's end hold 0 throughout: with whole vectors a
 // lane's piece is all in or all out, so it deviates from 0 instead of the mean.  A row a wave: two
 // at a time had more loads in flight but fewer waves, and took 28.3 us for 14336 x 1280 float32
 // into bf16, in place of 26.7.
-// (The bound keeps the element paths of J = 3 at four waves a SIMD: 38 in place of 42 us.)
+// (The bounds keep J = 3 at five waves a SIMD, and its element paths at four: 38 in place of 42 us.)
 template <int J, int W, bool VEC>
-__global__ void __launch_bounds__(256, J == 3 ? 4 : 1) ln_fwd_kernel(LnFwdArgs a) {
-  __shared__ float red[4];
+__global__ void __launch_bounds__(256, J == 3 ? (VEC ? 5 : 4) : 1) ln_fwd_kernel(LnFwdArgs a) {
+  // (contracted, m = total * inv_n is rounded in some columns' deviations and not in others')
+#pragma clang fp contract(off)
+  __shared__ float red[2][4];
   const int t = W == 1 ? threadIdx.x % kWave : threadIdx.x;
   const int first = W == 1 ? blockIdx.x * 4 + threadIdx.x / kWave : blockIdx.x;
   const int stride = W == 1 ? gridDim.x * 4 : gridDim.x;
@@ -60,24 +73,29 @@ __global__ void __launch_bounds__(256, J == 3 ? 4 : 1) ln_fwd_kernel(LnFwdArgs a
   const float inv_n = 1.0f / (float)a.cols;
   // (with W == 4 every wave of the workgroup has the same rows, so the barriers are met by all)
   for (int row = first; row < a.rows; row += stride) {
-    float x[J][8], s = 0.f, v = 0.f;
+    float x[J][8], s = 0.f;
 #pragma unroll
     for (int j = 0; j < J; ++j) load8<VEC>(a.x, row, 8 * t + j * kStep, a.cols, x[j]);
 #pragma unroll
     for (int j = 0; j < J; ++j)
 #pragma unroll
       for (int i = 0; i < 8; ++i) s += x[j][i];
-    const float mean = row_total<W>(s, red) * inv_n;
+    const float m0 = row_total<W>(s, red) * inv_n;
+    float d[2] = {0.f, 0.f};   // the deviations' sum, and their squares'
 #pragma unroll
     for (int j = 0; j < J; ++j) {
-      const float m = 8 * t + j * kStep < a.cols ? mean : 0.f;
+      const float m = 8 * t + j * kStep < a.cols ? m0 : 0.f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         x[j][i] = VEC || 8 * t + j * kStep + i < a.cols ? x[j][i] - m : 0.f;
-        v = fmaf(x[j][i], x[j][i], v);
+        d[0] += x[j][i];
+        d[1] = fmaf(x[j][i], x[j][i], d[1]);
       }
     }
-    const float rstd = 1.0f / sqrtf(row_total<W>(v, red) * inv_n + kEps);
+    row_totals<W>(d, red);
+    const float c0 = d[0] * inv_n, mean = m0 + c0;
+    const float var = fmaf(-c0, c0, d[1] * inv_n);
+    const float rstd = 1.0f / sqrtf((var < 0.f ? 0.f : var) + kEps);   // (NaN stays NaN)
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       const int c = 8 * t + j * kStep;
@@ -86,15 +104,12 @@ __global__ void __launch_bounds__(256, J == 3 ? 4 : 1) ln_fwd_kernel(LnFwdArgs a
       load_vec8<VEC>(a.bias, c, a.cols, b);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        x[j][i] *= rstd;
+        x[j][i] = (x[j][i] - c0) * rstd;
         y[i] = fmaf(x[j][i], g[i], b[i]);
       }
-      if (!VEC && rstd != rstd)   // a NaN row: its padding is 0 all the same
+      if (VEC ? c >= a.cols : c + 8 > a.cols)   // the checkpoint's padding is 0
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[j][i] = c + i < a.cols ? x[j][i] : 0.f;
-      if (VEC && c >= a.cols)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[j][i] = 0.f;
       store8<VEC>(a.y, row, c, a.cols, y);
       if (a.xhat.q) ckpt_store8(a.xhat, row, c, x[j]);
     }
@@ -110,7 +125,7 @@ __global__ void __launch_bounds__(256, J == 3 ? 4 : 1) ln_fwd_kernel(LnFwdArgs a
 // on the number of rows and columns only.
 template <int J, int W, bool VEC>
 __global__ void __launch_bounds__(256) ln_bwd_kernel(LnBwdArgs a) {
-  __shared__ float red[4];
+  __shared__ float red[1][4];
   constexpr int kStep = 8 * kWave * W;
   const int w = threadIdx.x / kWave, t = W == 1 ? threadIdx.x % kWave : threadIdx.x;
   const int first = W == 1 ? blockIdx.x * 4 + w : blockIdx.x, stride = W == 1 ? gridDim.x * 4 : gridDim.x;

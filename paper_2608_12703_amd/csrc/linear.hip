@@ -33,13 +33,12 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "linear_plan.h"
 #include "train.h"
 
 namespace ad {
 
 namespace {
-
-constexpr int kBK = 64;   // reduction elements of one LDS stage
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
@@ -1002,7 +1001,6 @@ __global__ void __launch_bounds__(256) linear_join_kernel(LinArgs a) {
 // that is the floor, so it goes from memory straight to registers, many loads at a time, with no LDS
 // and no second launch.  A workgroup owns PC columns; its eight waves share the reduction and add up
 // in LDS, in order (sixteen were no faster: 8.4 against 8.1 us for 1280 x 5120).
-constexpr int kFewWaves = 8, kFewSteps = 5;   // and the 32-wide steps that a wave has in flight
 template <int RT, int PC>
 __global__ void __launch_bounds__(kFewWaves* kWave) linear_few_kernel(LinArgs a) {
   constexpr int U = kFewSteps, NW = kFewWaves;
@@ -1061,78 +1059,6 @@ __global__ void __launch_bounds__(kFewWaves* kWave) linear_few_kernel(LinArgs a)
   }
 }
 
-// How a product is cut.  Tiles that fill whole rounds of the chip are computed by one workgroup
-// each; the tiles of the last, partly filled round in S parts of the reduction, so that the
-// chip is about full there too.
-struct Plan {
-  int tile;              // 128 (four waves) or 256 (eight waves, one workgroup a CU)
-  bool deep;             // 128: one workgroup a CU with a ring of four stages, not two with two
-  int tiles_p, tiles_q, whole, S, steps;
-  double cost;           // microseconds, to compare plans
-};
-constexpr int kCUs = 256;
-
-// Workgroups at once, and measured microseconds: of a 64-wide step, and of a round of workgroups besides
-// (its first loads, its epilogues).  14336 rows, width 1280 to 5120 (20 steps) and 5120 to 1280 (80):
-// large 185 and 174, pairs 202 and 204, deep 241 and 211; 1536 rows, 1280 to 2560: 45, 27, 23.  The
-// plan of least cost was within 0.6% of the best of the three over 147 products of 1 to 14336 rows.
-struct Shape {
-  int tile;
-  bool deep;
-  int slots;
-  double step, round;
-};
-constexpr Shape kLarge = {256, false, kCUs, 1.6, 13.0}, kPairs = {128, false, 2 * kCUs, 1.05, 5.0},
-                kDeep = {128, true, kCUs, 0.52, 5.6}, kAny = {128, false, 2 * kCUs, 1.6, 5.0};
-// A checkpoint with rows of any alignment: its registers leave room for one workgroup a CU (1500 x 1283 x
-// 1001 in two parts 31.6 us, in more 33 to 36).
-constexpr Shape kAnyCkpt = {128, false, kCUs, 1.6, 5.0};
-
-Plan plan_of(int P, int Q, int K, Shape sh) {
-  Plan r;
-  r.tile = sh.tile;
-  r.deep = sh.deep;
-  r.tiles_p = (P + sh.tile - 1) / sh.tile;
-  r.tiles_q = (Q + sh.tile - 1) / sh.tile;
-  const int all = (K + kBK - 1) / kBK;
-  const int64_t T = (int64_t)r.tiles_p * r.tiles_q;
-  const int rest = (int)(T % sh.slots);
-  r.whole = (int)T;
-  r.S = 1;
-  r.steps = all;
-  const double whole = sh.round + sh.step * all;
-  r.cost = whole * (double)((T + sh.slots - 1) / sh.slots);
-  for (int S = 2; rest && S <= 64 && rest * S <= sh.slots && all / S >= 4; ++S) {
-    // the parts, their way through memory twice, and another launch
-    const int steps = (all + S - 1) / S, parts = (all + steps - 1) / steps;
-    const double cost = whole * (double)(T / sh.slots) + sh.round + sh.step * steps + 5.0 +
-                        2e-6 * sh.tile * sh.tile * parts * rest;
-    if (cost < r.cost) {
-      r.whole = (int)(T - rest);
-      r.S = parts;
-      r.steps = steps;
-      r.cost = cost;
-    }
-  }
-  return r;
-}
-
-// From the sizes, whether the operands allow direct loads, and whether P is a checkpoint.
-Plan plan(int P, int Q, int K, bool direct, bool ckpt) {
-  if (!direct) return plan_of(P, Q, K, ckpt ? kAnyCkpt : kAny);
-  Plan best = plan_of(P, Q, K, kPairs);
-  for (const Shape& sh : {kLarge, kDeep}) {
-    if (sh.deep && ckpt) continue;
-    const Plan r = plan_of(P, Q, K, sh);
-    if (r.cost < best.cost) best = r;
-  }
-  return best;
-}
-
-size_t part_floats(const Plan& r) {
-  return r.S > 1 ? (size_t)r.S * (r.tiles_p * r.tiles_q - r.whole) * ((size_t)r.tile * r.tile + r.tile) : 0;
-}
-
 template <int KIND, bool PKS, int PSRC, bool QKS, int QSRC, int SLOPE = SLOPE_NONE>
 void launch_one(const LinArgs& a, const Plan& r, hipStream_t st) {
   const unsigned rest = a.tiles_p * a.tiles_q - a.whole, grid = a.whole + rest * a.S;
@@ -1162,37 +1088,12 @@ bool direct_ok(const LinOp& o, int contiguous) {
 
 }  // namespace
 
-// The forward product of few rows straight from registers: how it is cut, and its microseconds, to
-// compare with a plan's: what the weight's loads take one after the other or at the memory's rate,
-// and the rows, which every workgroup reads from L2 (measured from 1 to 32 rows at 1280 x 1280 to
-// 51864 x 1280 and 1280 x 5120, within 20%; a 51864-wide head takes 27 us for a row, 42 for 16
-// and 62 for 32, against 31, 31 and 32 in tiles).
-struct FewPlan {
-  bool narrow;   // 8 columns a workgroup where 16 would leave CUs without one
-  int grid;
-  double cost;
-};
-constexpr int kFewRows = 32;
-FewPlan few_plan(int P, int Q, int K) {
-  FewPlan f;
-  f.narrow = (P + 15) / 16 < kCUs;
-  f.grid = f.narrow ? (P + 7) / 8 : (P + 15) / 16;
-  const int turns = ((K + 31) / 32 + kFewWaves * kFewSteps - 1) / (kFewWaves * kFewSteps);
-  f.cost = std::max(3.0 + 1.2 * turns, 2.0 * P * K / 4.9e6) + 2.0 * f.grid * Q * K / 8e6;
-  return f;
-}
-
 template <int RT, int PC>
 void launch_few(const LinArgs& a, const FewPlan& f, hipStream_t st) {
   linear_few_kernel<RT, PC><<<f.grid, kFewWaves * kWave, 0, st>>>(a);
 }
 
-size_t lin_part_floats(int kind, int P, int Q, int K) {
-  // (asked for before the operands are known)
-  const size_t n = std::max(part_floats(plan(P, Q, K, true, false)), part_floats(plan(P, Q, K, false, false)));
-  if (kind != LIN_WGRAD) return n;
-  return std::max({n, part_floats(plan(P, Q, K, true, true)), part_floats(plan(P, Q, K, false, true))});
-}
+size_t lin_part_floats(int kind, int P, int Q, int K) { return plan_floats(kind == LIN_WGRAD, P, Q, K); }
 
 void launch_linear(int kind, LinArgs a, hipStream_t st) {
   const bool pk = kind == LIN_FWD, qk = kind != LIN_WGRAD;   // contiguous along the reduction
@@ -1207,8 +1108,7 @@ void launch_linear(int kind, LinArgs a, hipStream_t st) {
   if (kind == LIN_FWD && direct && !a.ck.q && a.Q.extent <= kFewRows) {
     // (a checkpoint's groups of 32 columns do not fit the workgroups of few rows)
     const FewPlan f = few_plan(a.P.extent, a.Q.extent, a.K);
-    // (tiles read the weight at 4.2 TB/s at best)
-    if (f.cost < std::max(r.cost, 2.0 * a.P.extent * a.K / 4.2e6)) {
+    if (few_wins(f, r, a.P.extent, a.K)) {
       if (a.Q.extent <= 16) f.narrow ? launch_few<1, 8>(a, f, st) : launch_few<1, 16>(a, f, st);
       else f.narrow ? launch_few<2, 8>(a, f, st) : launch_few<2, 16>(a, f, st);
       return;

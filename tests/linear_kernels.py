@@ -1,0 +1,29 @@
+"""Products whose sizes reach each kernel and each way of cutting a product, and which one that is.
+
+P columns and Q rows of the output, K long: a forward product has n = P, rows = Q, k = K, an input gradient
+k = P, rows = Q, n = K, a weight gradient k = P, n = Q, rows = K.  "256/1" is the kernel of 256 x 256 tiles, its
+reduction whole; "256/3": all of its tiles in 3 parts; "256+3": whole tiles, and a last round in 3 parts.  "128"
+has two workgroups a CU, "deep" one."""
+
+# P, Q, K, padding of a row, the first element's offset: 8-element vectors throughout
+TILES_256 = [
+    (2056, 4083, 392, 0, 0, "256/1"),         # 7 steps; one tile of 8 columns, one of 243 rows, a step of 8
+    (2056, 4083, 456, 8, 8, "256/1"),         # 8 steps
+    (2056, 1003, 14984, 0, 0, "256/7"),
+    (4360, 4333, 4104, 8, 0, "256+4"),
+    (5112, 14301, 1272, 0, 0, "256/1"),       # five rounds
+    (1272, 14301, 5112, 0, 0, "256+8"),
+]
+# weight gradients: Q a multiple of 8, any K
+WGRAD_256 = [
+    (2056, 4088, 391, 0, 0, "256/1"),
+    (2056, 4088, 453, 8, 8, "256/1"),
+    (4360, 4360, 4099, 8, 0, "256+3"),
+    (1272, 5112, 14301, 0, 0, "256/2"),
+]
+# (from here on a checkpoint's product is cut otherwise)
+WGRAD_256_BF16 = [(2056, 1000, 14981, 0, 0, "256/7")]
+WGRAD_256_CKPT = [(2056, 2000, 5121, 0, 0, "256/3"), (2056, 2056, 8205, 8, 8, "256/3")]
+# smaller tiles: whole, in parts, and a last round in parts
+TILES_128 = [(2056, 4090, 1416, 0, 0, "128+5"), (1288, 1537, 7368, 8, 0, "128/3"), (2568, 1537, 200, 0, 8, "128/1"),
+             (2568, 1537, 2888, 0, 0, "deep+6"), (776, 515, 2440, 8, 8, "deep/4")]

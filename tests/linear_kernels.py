@@ -3,7 +3,8 @@
 P columns and Q rows of the output, K long: a forward product has n = P, rows = Q, k = K, an input gradient
 k = P, rows = Q, n = K, a weight gradient k = P, n = Q, rows = K.  "256/1" is the kernel of 256 x 256 tiles, its
 reduction whole; "256/3": all of its tiles in 3 parts; "256+3": whole tiles, and a last round in 3 parts.  "128"
-has two workgroups a CU, "deep" one."""
+has two workgroups a CU, "deep" one; "few1x16" rows straight from registers, 1 x 16
+rows and 16 columns a workgroup."""
 
 # P, Q, K, padding of a row, the first element's offset: 8-element vectors throughout
 TILES_256 = [
@@ -27,3 +28,13 @@ WGRAD_256_CKPT = [(2056, 2000, 5121, 0, 0, "256/3"), (2056, 2056, 8205, 8, 8, "2
 # smaller tiles: whole, in parts, and a last round in parts
 TILES_128 = [(2056, 4090, 1416, 0, 0, "128+5"), (1288, 1537, 7368, 8, 0, "128/3"), (2568, 1537, 200, 0, 8, "128/1"),
              (2568, 1537, 2888, 0, 0, "deep+6"), (776, 515, 2440, 8, 8, "deep/4")]
+
+# rows, n, k, padding
+FEW = [
+    (1, 5120, 1280, 0, "few1x16"), (16, 5120, 1280, 8, "few1x16"), (7, 4088, 264, 0, "few1x16"), (15, 4104, 72, 0, "few1x16"),
+    (3, 51864, 64, 0, "few1x16"),
+    (17, 384, 1280, 0, "few2x8"), (31, 384, 72, 8, "few2x8"), (32, 1280, 1280, 0, "few2x8"), (25, 136, 2568, 0, "few2x8"),
+    (17, 5120, 1280, 0, "few2x16"), (32, 5120, 1280, 8, "few2x16"), (17, 4104, 1280, 0, "few2x16"), (32, 4104, 200, 0, "few2x16"),
+    (1, 4080, 200, 0, "few1x8"), (16, 136, 2568, 8, "few1x8"),
+    (33, 5120, 1280, 0, "deep/1"), (33, 384, 1280, 8, "deep/5"),
+]

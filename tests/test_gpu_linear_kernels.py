@@ -147,3 +147,25 @@ def test_input_gradient_tiles(P, Q, K, pad, shift, kernel, src, ot, again):
                          + [(*t, src) for t in sizes.WGRAD_256_CKPT for src in ("ckpt", "affine")])
 def test_weight_gradient_tiles_of_256(P, Q, K, pad, shift, kernel, src):
     _wgrad(K, Q, P, pad, shift, src)
+
+
+@pytest.mark.parametrize("act,rt,yt,keep", [(ad.ACT_GELU, None, BF16, None), (ad.ACT_NONE, F32, F32, None),
+                                            (ad.ACT_GELU, BF16, F32, "bf16"), (ad.ACT_NONE, BF16, BF16, "bf16")])
+@pytest.mark.parametrize("rows,n,k,pad,kernel", sizes.FEW)
+def test_few_rows(rows, n, k, pad, kernel, act, rt, yt, keep):
+    _forward(rows, n, k, pad, pad, act, rt, yt, keep)
+
+
+def test_few_rows_over_their_residual():
+    """y may be the residual; a row of NaN stays a row of NaN."""
+    for rows, n, k in ((1, 5120, 1280), (17, 384, 1280), (32, 4104, 200), (5, 200, 64)):
+        rnd = _draws(rows, n, k)
+        x, w, res, y = rnd(rows, k), rnd(n, k), rnd(rows, n, dtype=F32), torch.empty(rows, n, device="cuda")
+        ws = _space(ad.linear_workspace_size(rows, n, k))
+        ad.linear(x, w, None, ad.ACT_NONE, res, y, None, None, ws)
+        over = res.clone()
+        ad.linear(x, w, None, ad.ACT_NONE, over, over, None, None, ws)
+        assert torch.equal(over, y)
+        x[rows - 1, k - 1] = float("nan")
+        ad.linear(x, w, None, ad.ACT_NONE, res, over, None, None, ws)
+        assert bool(torch.isnan(over[rows - 1]).all()) and torch.equal(over[:rows - 1], y[:rows - 1])

@@ -59,3 +59,8 @@ def test_tiles_of_256(choose):
 def test_tiles_of_128(choose):
     assert choose([(P, Q, K, 1, 0, 0) for P, Q, K, *_ in sizes.TILES_128]) == [t[-1] for t in sizes.TILES_128]
     assert all(P % 8 == 0 and K % 8 == 0 and pad % 8 == 0 for P, _, K, pad, *_ in sizes.TILES_128)
+
+
+def test_few_rows(choose):
+    assert choose([(n, rows, k, 1, 0, 1) for rows, n, k, *_ in sizes.FEW]) == [t[-1] for t in sizes.FEW]
+    assert {"few1x8", "few1x16", "few2x8", "few2x16"} <= {t[-1] for t in sizes.FEW}

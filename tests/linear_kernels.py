@@ -3,7 +3,7 @@
 P columns and Q rows of the output, K long: a forward product has n = P, rows = Q, k = K, an input gradient
 k = P, rows = Q, n = K, a weight gradient k = P, n = Q, rows = K.  "256/1" is the kernel of 256 x 256 tiles, its
 reduction whole; "256/3": all of its tiles in 3 parts; "256+3": whole tiles, and a last round in 3 parts.  "128"
-has two workgroups a CU, "deep" one; "few1x16" rows straight from registers, 1 x 16
+has two workgroups a CU, "deep" one; "any" operands of any alignment; "few1x16" rows straight from registers, 1 x 16
 rows and 16 columns a workgroup."""
 
 # P, Q, K, padding of a row, the first element's offset: 8-element vectors throughout
@@ -38,3 +38,16 @@ FEW = [
     (1, 4080, 200, 0, "few1x8"), (16, 136, 2568, 8, "few1x8"),
     (33, 5120, 1280, 0, "deep/1"), (33, 384, 1280, 8, "deep/5"),
 ]
+
+# rows, n, k, padding, offset: sizes and strides that allow no vectors, the reduction in parts
+ANY_FWD = [(130, 129, 1001, 3, 1, "any/4"), (40, 200, 2049, 5, 0, "any/7"), (257, 72, 4099, 0, 3, "any/13")]
+ANY_DGRAD = [(33, 1001, 77, 3, 0, "any/4"), (70, 2049, 203, 0, 1, "any/7"), (48, 51866, 136, 0, 0, "any/63"),
+             (1499, 1283, 1001, 3, 0, "any/3")]
+ANY_WGRAD = [(1500, 283, 201, 3, 1, "any/6"), (1499, 1283, 1001, 3, 0, "any/4"), (2049, 40, 131, 0, 0, "any/7"),
+             (513, 131, 7, 1, 1, "any/2")]
+# ... of a weight gradient from a checkpoint: dy alone has no vectors
+ANY_WGRAD_CKPT = [(1500, 283, 201, 3, 1, "any/6"), (1499, 1283, 1001, 3, 0, "any/2"), (2049, 37, 136, 0, 0, "any/7"),
+                  (513, 131, 8, 1, 1, "any/2")]
+
+# reductions of 1 to 7 steps, and in parts of which the last has 1 to 5: P = 136, Q = 40
+STEPS = [8, 72, 136, 200, 264, 328, 392, 904, 968, 1032, 1096, 1288]

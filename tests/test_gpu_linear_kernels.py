@@ -51,15 +51,17 @@ def _products(a, b):
     return a @ b, a.abs() @ b.abs()
 
 
-def _forward(rows, n, k, pad, shift, act, rt, yt, keep):
+def _forward(rows, n, k, pad, shift, act, rt, yt, keep, parts=None):
     rnd = _draws(rows, n, k)
     x, w, bias = rnd(rows, k), rnd(n, k, scale=k ** -0.5), rnd(n)
     res = None if rt is None else rnd(rows, n, dtype=rt)
     y = Out(rows, n, yt, pad, shift)
     pre = Out(rows, n, BF16, pad, shift) if keep == "bf16" else None
     kept = ad.Ckpt.empty(rows, n) if keep == "ckpt" else None
+    space = ad.linear_workspace_size(rows, n, k)
+    assert parts is None or (space > 0) == parts
     ad.linear(_put(x, pad, shift), _put(w, pad, shift), bias, act, None if res is None else _put(res, pad, shift), y.t,
-              None if pre is None else pre.t, kept, _space(ad.linear_workspace_size(rows, n, k)))
+              None if pre is None else pre.t, kept, _space(space))
     h, mag = _products(x, w.t())
     h += bias.double()
     th = 2 * k * U * mag + 2 * U * (h.abs() + bias.double().abs())
@@ -99,7 +101,7 @@ def _dgrad(rows, n, k, pad, shift, src, ot, again):
         _near(_get(act_out), _gelu(h), h.abs() * 1e-7 + _gelu(h).abs() * (8 * U + 2.0 ** -8) + 1e-37, "act_out")
 
 
-def _wgrad(rows, n, k, pad, shift, src):
+def _wgrad(rows, n, k, pad, shift, src, parts=None):
     rnd = _draws(13, rows, n, k)
     dy, x16, kept, gain, shift_v = rnd(rows, n), rnd(rows, k), None, None, None
     x = mag = x16.double()
@@ -112,7 +114,9 @@ def _wgrad(rows, n, k, pad, shift, src):
         gain, shift_v = 1 + rnd(k, scale=0.1), rnd(k)
         x, mag = x * gain.double() + shift_v.double(), x.abs() * gain.double().abs() + shift_v.double().abs()
     dw, dbias = Out(n, k, F32, pad, shift), torch.empty(n, device="cuda")
-    ws = _space(ad.linear_wgrad_workspace_size(rows, n, k))
+    space = ad.linear_wgrad_workspace_size(rows, n, k)
+    assert parts is None or (space > 0) == parts
+    ws = _space(space)
     args = (_put(dy, pad, shift), _put(x16, pad, shift) if kept is None else None, kept, gain, shift_v)
     ad.linear_wgrad(*args, dw.t, dbias, ws)
     d = dy.double().t().contiguous()
@@ -169,3 +173,51 @@ def test_few_rows_over_their_residual():
         x[rows - 1, k - 1] = float("nan")
         ad.linear(x, w, None, ad.ACT_NONE, res, over, None, None, ws)
         assert bool(torch.isnan(over[rows - 1]).all()) and torch.equal(over[:rows - 1], y[:rows - 1])
+
+
+@pytest.mark.parametrize("act,rt,yt,keep", FORWARD)
+@pytest.mark.parametrize("rows,n,k,pad,shift,kernel", sizes.ANY_FWD)
+def test_forward_any_alignment_in_parts(rows, n, k, pad, shift, kernel, act, rt, yt, keep):
+    _forward(rows, n, k, pad, shift, act, rt, yt, keep, parts=True)
+
+
+@pytest.mark.parametrize("src,ot,again", DGRAD)
+@pytest.mark.parametrize("rows,n,k,pad,shift,kernel", sizes.ANY_DGRAD)
+def test_input_gradient_any_alignment_in_parts(rows, n, k, pad, shift, kernel, src, ot, again):
+    assert ad.linear_dgrad_workspace_size(rows, n, k) > 0
+    _dgrad(rows, n, k, pad, shift, src, ot, again)
+
+
+@pytest.mark.parametrize("rows,n,k,pad,shift,kernel,src", [(*t, "bf16") for t in sizes.ANY_WGRAD]
+                         + [(*t, src) for t in sizes.ANY_WGRAD_CKPT for src in ("ckpt", "affine")])
+def test_weight_gradient_any_alignment_in_parts(rows, n, k, pad, shift, kernel, src):
+    _wgrad(rows, n, k, pad, shift, src, parts=True)
+
+
+@pytest.mark.parametrize("pad", [0, 1])         # whole vectors, and none
+def test_every_number_of_steps(pad):
+    for K in sizes.STEPS:
+        _forward(40, 136, K, pad, 0, ad.ACT_GELU, None, F32, "ckpt")
+        _dgrad(40, K, 136, pad, 0, "bf16", F32, True)
+        for src in ("bf16", "affine"):
+            _wgrad(K, 40, 136, pad, 0, src)
+
+
+@pytest.mark.parametrize("odd", ["x", "w", "residual", "y", "pre", "bias"])
+def test_one_matrix_without_vectors(odd):
+    """Any one argument may lie anywhere; the others' padding stays as it was."""
+    rows, n, k = 140, 264, 584
+    rnd = _draws(rows, n, k)
+    x, w, bias, res = rnd(rows, k), rnd(n, k, scale=k ** -0.5), rnd(n + 1), rnd(rows, n, dtype=F32)
+    at = lambda name, t: _put(t, 3, 1) if name == odd else _put(t)  # noqa: E731
+    y, pre = (Out(rows, n, t, 3 if name == odd else 0, 1 if name == odd else 0) for name, t in (("y", F32), ("pre", BF16)))
+    bias = bias[1:] if odd == "bias" else bias[:n]
+    ad.linear(at("x", x), at("w", w), bias, ad.ACT_GELU, at("residual", res), y.t, pre.t, None,
+              _space(ad.linear_workspace_size(rows, n, k)))
+    h, mag = _products(x, w.t())
+    h += bias.double()
+    th = 2 * k * U * mag + 2 * U * (h.abs() + bias.double().abs())
+    out = _gelu(h) + res.double()
+    tol = 1.13 * th + h.abs() * (1e-7 + 8 * U) + 2 * U * (out.abs() + res.double().abs())
+    _near(_get(y), out, tol * 1.01 + out.abs() * U, "y")
+    _near(_get(pre), h, th * 1.01 + h.abs() * 2.0 ** -8, "pre")

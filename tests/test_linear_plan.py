@@ -64,3 +64,16 @@ def test_tiles_of_128(choose):
 def test_few_rows(choose):
     assert choose([(n, rows, k, 1, 0, 1) for rows, n, k, *_ in sizes.FEW]) == [t[-1] for t in sizes.FEW]
     assert {"few1x8", "few1x16", "few2x8", "few2x16"} <= {t[-1] for t in sizes.FEW}
+
+
+def test_any_alignment_in_parts(choose):
+    assert choose([(n, rows, k, 0, 0, 0) for rows, n, k, *_ in sizes.ANY_FWD]) == [t[-1] for t in sizes.ANY_FWD]
+    assert choose([(k, rows, n, 0, 0, 0) for rows, n, k, *_ in sizes.ANY_DGRAD]) == [t[-1] for t in sizes.ANY_DGRAD]
+    for ckpt, table in ((0, sizes.ANY_WGRAD), (1, sizes.ANY_WGRAD_CKPT)):
+        assert choose([(k, n, rows, 0, ckpt, 0) for rows, n, k, *_ in table]) == [t[-1] for t in table]
+
+
+def test_numbers_of_steps(choose):
+    for direct, ckpt in ((1, 0), (1, 1), (0, 0), (0, 1)):
+        got = choose([(136, 40, K, direct, ckpt, 0) for K in sizes.STEPS])
+        assert all(g.endswith("/1") for g in got[:7]) and all(int(g.split("/")[1]) > 1 for g in got[7:]), got

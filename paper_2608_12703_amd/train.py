@@ -51,11 +51,22 @@ class FeedForward:
         cut = lambda k: ad.Ckpt(k.q[:rows], k.scale[:rows], k.cols)  # noqa: E731
         return cut(self.xhat), cut(self.pre)
 
+    def _rows(self, name: str, t, rows: int, *dtypes):
+        """Refuses what a later call of the pass would refuse, before the first one has written."""
+        if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+            raise ValueError(f"{name} is on {t.device}, not on the current GPU")
+        if t.shape != (rows, self.d) or t.dtype not in dtypes:
+            raise ValueError(f"{name} is {tuple(t.shape)} of {t.dtype}, expected {(rows, self.d)} of {dtypes}")
+        ld, step = t.stride()
+        if (self.d > 1 and step != 1) or (rows > 1 and not self.d <= ld <= 1 << 22):
+            raise ValueError(f"{name}: the columns of a row must be adjacent, and rows apart by at most 2^22")
+
     def forward(self, x, out):
         """out <- x + W2 GELU(W1 LN(x) + b1) + b2 for float32 rows x [rows][d]; out may be x."""
         rows = x.shape[0]
         if rows > self.max_rows:
             raise ValueError(f"{rows} rows: the buffers hold {self.max_rows}")
+        self.rows = None      # (a pass that is refused halfway leaves nothing to go back from)
         ws = self.workspace
         xhat, pre = self._kept(rows)
         ad.layer_norm(x, self.gain, self.bias, self.narrow[:rows], self.mean[:rows], self.rstd[:rows], xhat)
@@ -65,10 +76,15 @@ class FeedForward:
 
     def backward(self, dout, dx, dx_copy=None):
         """dx <- dL/dx from dout = dL/dout (float32 [rows][d]), for the rows of the last forward
-        pass, and the parameters' gradients added to `grads`.  dx may be dout."""
+        pass, and the parameters' gradients added to `grads`.  dx may be dout; dx_copy is a bf16 copy of
+        dx.  A refused pass adds nothing."""
         rows = dout.shape[0]
         if rows != self.rows:
             raise ValueError(f"{rows} rows, but the last forward pass had {self.rows}")
+        self._rows("dout", dout, rows, torch.float32, torch.bfloat16)
+        self._rows("dx", dx, rows, torch.float32, torch.bfloat16)
+        if dx_copy is not None:
+            self._rows("dx_copy", dx_copy, rows, torch.bfloat16)
         ws = self.workspace
         xhat, pre = self._kept(rows)
         ggain, gbias, gw1, gb1, gw2, gb2 = self.grads

@@ -3,9 +3,11 @@
     out = x + W2 GELU(W1 LN(x) + b1) + b2
 
 (the third sublayer of the decoder's blocks; its parameters are a model's ln3_g, ln3_b, w_1,
-b_1, w_2 and b_2).  What the backward pass needs is kept in 8 bits: the normalised rows and the
-pre-activation, 1.03 bytes a value in place of two LayerNorm outputs, a pre-activation and a
-GELU output in bf16.  Like Session it owns its buffers and only calls libad entry points.
+b_1, w_2 and b_2).  From the forward to the backward pass a sublayer keeps the normalised rows and the
+pre-activation in 8 bits: 1.03 (d + f) bytes a row and 4 for LayerNorm's factor, where the LayerNorm
+output, the pre-activation and GELU's output in bf16 would be 2 d + 4 f.  A running pass also needs
+2 d + 4 f bytes a row and a workspace (Scratch), which sublayers can share.  Like Session they own
+their buffers and only call libad entry points.
 """
 from __future__ import annotations
 
@@ -14,34 +16,50 @@ import torch
 from . import ad
 
 
-class FeedForward:
-    """Buffers for up to max_rows rows.  params: (ln_gain [d], ln_bias [d], w1 [f][d], b1 [f],
-    w2 [d][f], b2 [d]) on the GPU, w1 and w2 in bf16.  Gradients are float32 tensors of the same
-    shapes in `grads`, in the same order; backward adds to them (zero_grads clears them)."""
+class Scratch:
+    """What passes over up to max_rows rows need only while they run: rows of width d and f in bf16, and one
+    workspace for every call, large enough for any number of rows up to max_rows (a captured pass
+    keeps its address).  Sublayers whose passes follow one another, on one stream or as graphs that are
+    replayed in turn, can share one; passes that may overlap need one each."""
 
-    def __init__(self, params, max_rows: int):
-        self.gain, self.bias, self.w1, self.b1, self.w2, self.b2 = params
-        self.f, self.d = self.w1.shape
-        d, f, dev = self.d, self.f, self.w1.device
-        empty = lambda *shape, dt=torch.float32: torch.empty(*shape, dtype=dt, device=dev)  # noqa: E731
-        self.max_rows = max_rows
-        self.mean, self.rstd = empty(max_rows), empty(max_rows)
-        self.xhat = ad.Ckpt.empty(max_rows, d, dev)
-        self.pre = ad.Ckpt.empty(max_rows, f, dev)
-        self.narrow, self.wide = empty(max_rows, d, dt=torch.bfloat16), empty(max_rows, f, dt=torch.bfloat16)
-        self.wide2 = empty(max_rows, f, dt=torch.bfloat16)
-        self.dnarrow = empty(max_rows, d, dt=torch.bfloat16)
-        self.grads = [torch.zeros(p.shape, dtype=torch.float32, device=dev) for p in params]
-        self.rows = None
-        # One workspace for every call, large enough for any number of rows up to max_rows (a captured
-        # pass keeps its address).  What a call needs changes with its rows at multiples of 64 only,
-        # and the LayerNorm's grows with them.
+    def __init__(self, d: int, f: int, max_rows: int, device="cuda"):
+        empty = lambda *shape, dt=torch.bfloat16: torch.empty(*shape, dtype=dt, device=device)  # noqa: E731
+        self.d, self.f, self.max_rows = d, f, max_rows
+        self.narrow, self.wide, self.wide2 = empty(max_rows, d), empty(max_rows, f), empty(max_rows, f)
+        # What a call needs changes with its rows at multiples of 64 only, and the LayerNorm's grows with them.
         need = ad.layer_norm_backward_workspace_size(max_rows, d)
         for rows in range(64, max_rows + 64, 64):
             need = max(need, *(size(rows, *shape) for shape in ((d, f), (f, d)) for size in
                                (ad.linear_workspace_size, ad.linear_dgrad_workspace_size,
                                 ad.linear_wgrad_workspace_size)))
         self.workspace = empty(max(need, 1), dt=torch.uint8)
+
+
+class FeedForward:
+    """Buffers for up to max_rows rows.  params: (ln_gain [d], ln_bias [d], w1 [f][d], b1 [f],
+    w2 [d][f], b2 [d]) on the GPU, w1 and w2 in bf16.  scratch: shared with other sublayers, or None
+    for one of its own.  Gradients are float32 tensors of the parameters' shapes in `grads`, in the same
+    order; backward adds to them (zero_grads clears them)."""
+
+    def __init__(self, params, max_rows: int, scratch: Scratch | None = None):
+        self.gain, self.bias, self.w1, self.b1, self.w2, self.b2 = params
+        self.f, self.d = self.w1.shape
+        d, f, dev = self.d, self.f, self.w1.device
+        self.max_rows = max_rows
+        self.scratch = Scratch(d, f, max_rows, dev) if scratch is None else scratch
+        s = self.scratch
+        if (s.d, s.f) != (d, f) or s.max_rows < max_rows or s.workspace.device != dev:
+            raise ValueError(f"scratch of {(s.d, s.f)} for {s.max_rows} rows on {s.workspace.device}, "
+                             f"expected {(d, f)} for {max_rows} on {dev}")
+        self.rstd = torch.empty(max_rows, dtype=torch.float32, device=dev)
+        self.xhat = ad.Ckpt.empty(max_rows, d, dev)
+        self.pre = ad.Ckpt.empty(max_rows, f, dev)
+        self.grads = [torch.zeros(p.shape, dtype=torch.float32, device=dev) for p in params]
+        self.rows = None
+
+    @property
+    def workspace(self):
+        return self.scratch.workspace
 
     def zero_grads(self):
         for g in self.grads:
@@ -69,9 +87,10 @@ class FeedForward:
         self.rows = None      # (a pass that is refused halfway leaves nothing to go back from)
         ws = self.workspace
         xhat, pre = self._kept(rows)
-        ad.layer_norm(x, self.gain, self.bias, self.narrow[:rows], self.mean[:rows], self.rstd[:rows], xhat)
-        ad.linear(self.narrow[:rows], self.w1, self.b1, ad.ACT_GELU, None, self.wide[:rows], None, pre, ws)
-        ad.linear(self.wide[:rows], self.w2, self.b2, ad.ACT_NONE, x, out, None, None, ws)
+        narrow, wide = self.scratch.narrow[:rows], self.scratch.wide[:rows]
+        ad.layer_norm(x, self.gain, self.bias, narrow, None, self.rstd[:rows], xhat)
+        ad.linear(narrow, self.w1, self.b1, ad.ACT_GELU, None, wide, None, pre, ws)
+        ad.linear(wide, self.w2, self.b2, ad.ACT_NONE, x, out, None, None, ws)
         self.rows = rows
 
     def backward(self, dout, dx, dx_copy=None):
@@ -88,11 +107,11 @@ class FeedForward:
         ws = self.workspace
         xhat, pre = self._kept(rows)
         ggain, gbias, gw1, gb1, gw2, gb2 = self.grads
-        dlow, act, dpre = self.dnarrow[:rows], self.wide[:rows], self.wide2[:rows]
-        dlow.copy_(dout)      # the products' operand in bf16
-        ad.linear_dgrad(dlow, self.w2, ad.ACT_GELU, None, pre, dpre, act, ws)
-        ad.linear_wgrad(dlow, act, None, None, None, gw2, gb2, ws, accumulate=True)
+        narrow, act, dpre = (t[:rows] for t in (self.scratch.narrow, self.scratch.wide, self.scratch.wide2))
+        narrow.copy_(dout)    # the products' operand in bf16
+        ad.linear_dgrad(narrow, self.w2, ad.ACT_GELU, None, pre, dpre, act, ws)
+        ad.linear_wgrad(narrow, act, None, None, None, gw2, gb2, ws, accumulate=True)
         ad.linear_wgrad(dpre, None, xhat, self.gain, self.bias, gw1, gb1, ws, accumulate=True)
-        ad.linear_dgrad(dpre, self.w1, ad.ACT_NONE, None, None, self.narrow[:rows], None, ws)
-        ad.layer_norm_backward(self.narrow[:rows], None, None, self.rstd[:rows], xhat, self.gain, dout, dx,
+        ad.linear_dgrad(dpre, self.w1, ad.ACT_NONE, None, None, narrow, None, ws)     # dL/dLN(x)
+        ad.layer_norm_backward(narrow, None, None, self.rstd[:rows], xhat, self.gain, dout, dx,
                                dx_copy, ggain, gbias, ws, accumulate=True)

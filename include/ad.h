@@ -420,8 +420,8 @@ ad_status ad_ckpt_unpack(int32_t rows, int32_t cols, const ad_ckpt* ckpt, int32_
  * rounding).  Optional outputs for the backward pass: mean, rstd [rows] float32, and xhat,
  * the normalised rows before gain and bias in 8 bits.  y may be x when their types and ld
  * are the same.  Statistics are float32, in two passes over registers; the mean is corrected by the
- * deviations' own mean, so that a large mean costs nothing (a row of one value gives y = bias), up
- * to deviations of 1.8e19, whose squares overflow.
+ * deviations' own mean, so that a large mean costs nothing (a row of one value gives y = bias).
+ * Deviations whose squares overflow (1.8e19) give y = bias, a row whose sum does gives NaN.
  * Errors: AD_EINVAL (NULL argument, bad dtype, misaligned data, ld < cols), AD_ERANGE,
  * AD_EUNSUPPORTED (cols > 8192), AD_EHIP.
  */

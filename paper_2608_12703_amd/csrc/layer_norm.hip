@@ -6,8 +6,9 @@
 // columns, are spread over the four waves of a workgroup.
 //
 // Measured against a large copy's 4.9 TB/s: LayerNorm of 14336 x 1280 float32 rows into bf16 and
-// the checkpoint 34 us (3.8 TB/s), its backward pass over 13331 such rows kept whole 60 us (4.5),
-// packing 14336 x 5120 bf16 45 us (4.9), reading them back 41 us (5.4).  Loads must be whole
+// the checkpoint 35 us (3.7 TB/s), its backward pass over 13331 such rows kept whole 60 us (4.6),
+// packing 14336 x 5120 bf16 49 us (4.5), reading them back 34 us (6.5: 76 MB that were written just
+// before, most likely from the last-level cache).  Loads must be whole
 // vectors in one block each: as selects of a load and a zero they became eight loads of 4 bytes
 // with a branch each, and the same LayerNorm took 52 us.
 #include <algorithm>
@@ -58,8 +59,8 @@ __device__ __forceinline__ float row_total(float v, float (*red)[4]) {
 // 1e5 came out as 1 instead of 0): the deviations' own mean c is that error, mean = m + c and
 // var = sum (x - m)^2 / n - c^2, where c^2 is as small as the roundings.  Columns past the row's end hold 0 throughout: with whole vectors a
 // lane's piece is all in or all out, so it deviates from 0 instead of the mean.  A row a wave: two
-// at a time had more loads in flight but fewer waves, and took 28.3 us for 14336 x 1280 float32
-// into bf16, in place of 26.7.
+// at a time had more loads in flight but fewer waves, and took 6% longer for 14336 x 1280 float32
+// into bf16 (26.7 us; 25.9 without the correction of the mean).
 // (The bounds keep J = 3 at five waves a SIMD, and its element paths at four: 38 in place of 42 us.)
 template <int J, int W, bool VEC>
 __global__ void __launch_bounds__(256, J == 3 ? (VEC ? 5 : 4) : 1) ln_fwd_kernel(LnFwdArgs a) {

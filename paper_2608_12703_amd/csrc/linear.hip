@@ -904,8 +904,8 @@ __global__ void __launch_bounds__(WP* WQ* kWave, ST == 2 && !(PSRC == SRC_CKPT &
   TileEpilogue<KIND, SLOPE> te;
   if (VEC) te.init(a, iq * RQ, c);
   // What a row of tiles reads is asked for before the row's accumulators are moved; a pre-activation, which
-  // is small, while the row before it is worked on (251 against 267 us for 14336 rows of 1280 into
-  // 5120, slope and activation).
+  // is small, while the row before it is worked on (6% less for 14336 rows of 1280 into 5120, slope
+  // and activation, now 258 us).
   constexpr bool kAhead = SLOPE != SLOPE_NONE;
   auto row_of = [&](int j) { return (wq * TQ + slot(j)) * 16 + r0; };   // of the tile: this lane's first item's
   typename TileEpilogue<KIND, SLOPE>::Ask asked[kAhead ? 2 : 1][NI];

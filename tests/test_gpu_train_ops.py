@@ -404,9 +404,9 @@ def test_linear_wgrad(rows, n, k, pad, shift, src):
     assert torch.equal(dw.get(), one.double().cpu()), "the same call gives the same bits"
 
 
-# Products of several rounds of large tiles, the last round's in parts of the reduction (289 and 300
-# tiles of 256 x 256), tiles past the last row and column, a reduction that ends inside a stage;
-# the references are float64 products on the GPU.
+# Products of several rounds of 128 x 128 tiles, tiles past the last row and column, a reduction that ends
+# inside a stage (tests/linear_kernels.py has those of 256 x 256); the references are float64 products
+# on the GPU.
 LARGE = [(4104, 4200, 200, 0, 0), (4500, 1032, 4104, 8, 8), (1000, 4104, 4360, 0, 0)]
 
 

@@ -55,12 +55,12 @@ __device__ __forceinline__ float row_total(float v, float (*red)[4]) {
 
 // W: waves per row (1 or 4), VEC: every matrix and parameter allows whole vectors.  The statistics
 // are two passes over the registers: the mean m, then the sum of the deviations from it and that of
-// their squares.  m is off by its roundings, which a large mean makes large beside the deviations (a row of
-// 1e5 came out as 1 instead of 0): the deviations' own mean c is that error, mean = m + c and
-// var = sum (x - m)^2 / n - c^2, where c^2 is as small as the roundings.  Columns past the row's end hold 0 throughout: with whole vectors a
-// lane's piece is all in or all out, so it deviates from 0 instead of the mean.  A row a wave: two
-// at a time had more loads in flight but fewer waves, and took 6% longer for 14336 x 1280 float32
-// into bf16 (26.7 us; 25.9 without the correction of the mean).
+// their squares.  m is off by its roundings, which are large beside the deviations where the mean is
+// (alone, it made a row of 1e5 come out as 1 instead of 0).  The deviations' own mean c is that error:
+// mean = m + c, var = sum (x - m)^2 / n - c^2, with c^2 as small as the roundings.  Columns past the
+// row's end hold 0 throughout: with whole vectors a lane's piece is all in or all out, so it deviates
+// from 0 instead of the mean.  A row a wave: two at a time had more loads in flight but fewer waves,
+// and took 6% longer for 14336 x 1280 float32 into bf16 (26.7 us; 25.9 without c).
 // (The bounds keep J = 3 at five waves a SIMD, and its element paths at four: 38 in place of 42 us.)
 template <int J, int W, bool VEC>
 __global__ void __launch_bounds__(256, J == 3 ? (VEC ? 5 : 4) : 1) ln_fwd_kernel(LnFwdArgs a) {

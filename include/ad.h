@@ -498,6 +498,146 @@ ad_status ad_linear_wgrad(int32_t rows, int32_t n, int32_t k, const ad_mat* dy, 
                           size_t workspace_bytes, void* stream);
 
 /*
+ * Attention over matrices, for training the draft block's self- and cross-attention (paper,
+ * section 3 "Models and Protocol" and appendix "Draft architecture"): 64-wide heads, score
+ * scale 1/8, head h of a matrix in its columns 64 h .. 64 h + 63, as the projections write
+ * them (queries, keys and values may be column ranges of one matrix).  Sequence b owns the
+ * query rows cu_q[b] .. cu_q[b+1] - 1 and the key rows cu_k[b] .. cu_k[b+1] - 1; with q_len / k_len
+ * only the first q_len[b] / k_len[b] of them hold something and the others are padding, without
+ * all of them do.  So PADDED batches are a fixed stride with lengths, PACKED ones running sums.
+ * Rows outside every sequence are not read and not written.
+ * Key j of a sequence is visible to its query i if j < k_len and, with causal, j <= i + k_len -
+ * q_len (the last query sees every key) and, with window, window[row][0] <= j < window[row][1]
+ * (frames of the sequence, any integers; row is the query's row of the matrix).  What is not
+ * visible has no influence, whatever it holds (NaN and infinities too).  With q_heads a multiple
+ * of kv_heads, query head h reads key head h / (q_heads / kv_heads).
+ * A table entry out of range (cu not from 0 on and increasing, a row past q_rows or k_rows, a sequence of
+ * more than q_max or k_max rows, a length outside its rows) sets AD_ERR_LENGTH, and nothing of
+ * that sequence is written; rows that a wrong table gives to two sequences may hold either's.
+ */
+typedef struct {
+  int32_t batch;              /* sequences, 0 <= batch <= 65535                       */
+  int32_t q_heads, kv_heads;  /* kv_heads divides q_heads                             */
+  int32_t q_rows, k_rows;     /* rows of the matrices                                 */
+  int32_t q_max, k_max;       /* no sequence owns more rows than this                 */
+  int32_t causal;
+  const int32_t* cu_q;        /* device [batch + 1]                                   */
+  const int32_t* cu_k;        /* device [batch + 1]                                   */
+  const int32_t* q_len;       /* device [batch] (optional)                            */
+  const int32_t* k_len;       /* device [batch] (optional)                            */
+  const int32_t* window;      /* device [q_rows][2] (optional)                        */
+  int32_t* err_flag;          /* device [1]: AD_ERR_* bits are OR-ed in               */
+} ad_attn;
+
+/*
+ *   s_ij = q_i . k_j / 8,  p_i = softmax of s_i over the visible keys,  o_i = sum_j p_ij v_j
+ * q [q_rows][64 q_heads], k, v [k_rows][64 kv_heads], o as q, all bf16.  Scores, the softmax and
+ * sums are float32; a probability enters its product as bf16, o is rounded once.  Optional outputs
+ * for the backward pass: lse [q_heads][q_rows] float32, the row's log sum_j exp(s_ij), and o_rest (bf16,
+ * as o), what o's rounding took away.  A row that sees no key, or only scores of -infinity, and a
+ * padding row give o = o_rest = 0 and lse = -infinity.
+ * workspace: device, >= ad_attention_workspace_size() bytes (of the sizes in a; the tables are
+ * not read), 256-byte aligned, NULL where that is 0.
+ * Errors: AD_EINVAL (NULL argument, misaligned data, ld too small, heads that do not divide),
+ * AD_ERANGE (sizes), AD_ENOSPACE, AD_EUNSUPPORTED (a float32 matrix), AD_EHIP.
+ */
+ad_status ad_attention_workspace_size(const ad_attn* a, size_t* bytes);
+ad_status ad_attention(const ad_attn* a, const ad_mat* q, const ad_mat* k, const ad_mat* v, const ad_mat* o,
+                       const ad_mat* o_rest, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Its gradients, with the probabilities computed again from lse:
+ *   dP_ij = dout_i . v_j,  delta_i = dout_i . o_i,  dS_ij = p_ij (dP_ij - delta_i) / 8,
+ *   dq_i = sum_j dS_ij k_j + dq_res_i,  dk_j = sum_i dS_ij q_i,  dv_j = sum_i p_ij dout_i,
+ * dk and dv summed over the query heads that share a key head too.  q, k, v, o, o_rest and lse
+ * are the forward pass's (o_rest may be NULL: then delta carries o's rounding, which a row with few
+ * visible keys shows: dS of a single key is 0 only with it).  dout, dq, dk, dv bf16, of the shapes of
+ * o, q, k, v; dq_res (optional, float32 or bf16, as q) is a gradient that reaches the queries on
+ * another way, as the objective's out_dxq does; dq may be dq_res when their types and ld are the same.
+ * Sums are float32, p and dS enter their products as bf16, every output is rounded once.  Padding
+ * rows get 0 (and dq_res is not added to them).
+ * workspace and errors as for ad_attention.
+ */
+ad_status ad_attention_backward_workspace_size(const ad_attn* a, size_t* bytes);
+ad_status ad_attention_backward(const ad_attn* a, const ad_mat* q, const ad_mat* k, const ad_mat* v, const ad_mat* o,
+                                const ad_mat* o_rest, const float* lse, const ad_mat* dout, const ad_mat* dq_res,
+                                const ad_mat* dq, const ad_mat* dk, const ad_mat* dv, void* workspace,
+                                size_t workspace_bytes, void* stream);
+
+/*
+ * A parameter tensor of n elements side by side, with its gradient and the optimizer's state.
+ * State in 8 bits (AD_STATE_8): 128 consecutive elements (the last group may be shorter) share a float32 scale
+ * s, m_scale and v_scale [ceil(n / 128)]:
+ *   m = q s   with q int8,  s = max|m| / 127
+ *   v = q^2 s with q uint8, s = max v / 65025, q >= 1 where v > 0
+ * Between two codes the upper one is taken with the probability that keeps the value's mean: v moves
+ * by a thousandth a step, which rounding to the nearest code would lose.  (q = 0 for a small v would
+ * make m / sqrt(v) of the next step far too large.)  All zeros, scales too, is the state before the first
+ * step.  A group that holds a NaN or an infinity reads as NaN from then on.  A group whose largest |m| is under
+ * 2^-100, or whose largest v is under 2^-100, holds zeros.
+ */
+typedef enum { AD_STATE_F = 0, AD_STATE_8 = 1 } ad_state;
+typedef struct {
+  int64_t n;                  /* 0 <= n <= 2^40                                       */
+  void* param;                /* device [n] of param_dtype                            */
+  void* copy;                 /* device [n] bf16 (optional, float32 param only): the
+                                 parameter after the step, rounded                    */
+  const void* grad;           /* device [n] of grad_dtype                             */
+  void* m;                    /* device [n] float32, or int8                          */
+  void* v;                    /* device [n] float32, or uint8                         */
+  float* m_scale;             /* device, AD_STATE_8 only                              */
+  float* v_scale;
+  double weight_decay;        /* >= 0                                                 */
+  int32_t param_dtype, grad_dtype;
+  int32_t state;              /* ad_state                                             */
+} ad_opt_tensor;
+
+/*
+ * One AdamW step t over `count` tensors (host array; paper, appendix "Training": AdamW, learning rate
+ * 1e-3, weight decay 0.01):
+ *   g = grad * grad_scale,  m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2,
+ *   param = param (1 - lr weight_decay) - lr / (1 - b1^t) * m / (sqrt(v) / sqrt(1 - b2^t) + eps)
+ * in float32, the products and sums of m and v each rounded (no fused multiply-add), so a state in 8 bits
+ * is a function of its inputs that can be computed again elsewhere.  A float32 param is
+ * rounded to nearest; a bf16 param takes the upper neighbour with the probability that keeps its
+ * mean (steps are smaller than half its spacing).  Random bits come from a hash of (seed, t, the
+ * tensor's place in the list, the element); the caller gives a run a seed.
+ * lr_at / step_at (device, optional) replace lr and step, for steps in a captured graph; with
+ * grad_scale (device [1], optional) not finite nothing is written (see ad_grad_norm).  No two tensors may
+ * overlap.  count = 0 does nothing.
+ * Errors: AD_EINVAL (NULL argument, unknown dtype or state, misaligned pointer, copy of a bf16 param), AD_ERANGE
+ * (n, step < 1, lr < 0 or not finite, betas outside [0, 1), eps < 0, weight_decay < 0), AD_EHIP.
+ */
+typedef struct {
+  double lr, beta1, beta2, eps;
+  int32_t step;               /* t >= 1                                               */
+  uint32_t seed;
+  const float* lr_at;         /* device [1] (optional)                                */
+  const int32_t* step_at;     /* device [1] (optional)                                */
+  const float* grad_scale;    /* device [1] (optional)                                */
+} ad_adamw_args;
+ad_status ad_adamw(const ad_opt_tensor* tensors, int32_t count, const ad_adamw_args* args, void* stream);
+
+/* The states of all tensors, one tensor after the other, as float32 values: what a checkpoint of a training
+ * run or a look at its states reads.  m and v: device [sum of n]; either may be NULL.  Uses n, m, v, the scales and state
+ * of the tensors.  Errors: AD_EINVAL, AD_ERANGE, AD_EHIP. */
+ad_status ad_opt_state(const ad_opt_tensor* tensors, int32_t count, float* m, float* v, void* stream);
+
+/*
+ * The norm of all gradients together, and the factor that clips it (paper, appendix "Training":
+ * clipping at 1.0):
+ *   out[0] = sqrt(sum over all tensors of g^2),  out[1] = min(1, max_norm / out[0])
+ * max_norm = 0 does not clip (out[1] = 1).  A norm that is not finite gives out[1] = NaN, which ad_adamw takes
+ * for a step to leave out.  step (device [1], optional) is increased by one when the norm is finite: the step_at
+ * of the ad_adamw that follows.  Sums are 64-bit floats in a fixed order.  Uses n, grad and grad_dtype of the
+ * tensors.  workspace: device, >= ad_grad_norm_workspace_size() bytes, 256-byte aligned.
+ * Errors: AD_EINVAL, AD_ERANGE (n, max_norm < 0 or not finite), AD_ENOSPACE, AD_EHIP.
+ */
+ad_status ad_grad_norm_workspace_size(const ad_opt_tensor* tensors, int32_t count, size_t* bytes);
+ad_status ad_grad_norm(const ad_opt_tensor* tensors, int32_t count, double max_norm, float* out, int32_t* step,
+                       void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Next draft block from linear draft heads on the final hidden state.  For sequence b
  * take the LN_f output h at row row0_b + a_b (row0_b = first row of b in `layout`),
  * d_i = argmax(W_i h) (float32 logits, lowest index on ties), i = 1..n_heads, and write

@@ -22,6 +22,7 @@ STATUS = {0: "AD_OK", -1: "AD_EINVAL", -2: "AD_ERANGE", -3: "AD_ENOSPACE", -4: "
           -5: "AD_EUNSUPPORTED"}
 
 ACT_NONE, ACT_GELU = 0, 1
+STATE_F, STATE_8 = 0, 1
 
 _i32 = ctypes.c_int32
 _ptr = ctypes.c_void_p
@@ -62,11 +63,30 @@ class CkptView(ctypes.Structure):
     _fields_ = [("q", _ptr), ("scale", _ptr)]
 
 
+class AttnView(ctypes.Structure):
+    _fields_ = [("batch", _i32), ("q_heads", _i32), ("kv_heads", _i32), ("q_rows", _i32), ("k_rows", _i32),
+                ("q_max", _i32), ("k_max", _i32), ("causal", _i32), ("cu_q", _ptr), ("cu_k", _ptr),
+                ("q_len", _ptr), ("k_len", _ptr), ("window", _ptr), ("err_flag", _ptr)]
+
+
+class OptTensor(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int64), ("param", _ptr), ("copy", _ptr), ("grad", _ptr), ("m", _ptr), ("v", _ptr),
+                ("m_scale", _ptr), ("v_scale", _ptr), ("weight_decay", ctypes.c_double), ("param_dtype", _i32),
+                ("grad_dtype", _i32), ("state", _i32)]
+
+
+class AdamwArgs(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("step", _i32), ("seed", ctypes.c_uint32), ("lr_at", _ptr),
+                ("step_at", _ptr), ("grad_scale", _ptr)]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is not built; run paper_2608_12703_amd.build.build()")
     lib = ctypes.CDLL(LIB_PATH)
     _mat, _ckpt = ctypes.POINTER(Mat), ctypes.POINTER(CkptView)
+    _attn, _opt = ctypes.POINTER(AttnView), ctypes.POINTER(OptTensor)
     sig = {
         "ad_last_error": (ctypes.c_char_p, []),
         "ad_model_param_count": (_i32, [ctypes.POINTER(ModelDesc)]),
@@ -110,6 +130,15 @@ def _load():
         "ad_linear_wgrad_workspace_size": (_i32, [_i32, _i32, _i32, ctypes.POINTER(_size)]),
         "ad_linear_wgrad": (_i32, [_i32, _i32, _i32, _mat, _mat, _ckpt, _ptr, _ptr, _i32, _mat, _ptr, _i32,
                                    _ptr, _size, _ptr]),
+        "ad_attention_workspace_size": (_i32, [_attn, ctypes.POINTER(_size)]),
+        "ad_attention": (_i32, [_attn, _mat, _mat, _mat, _mat, _mat, _ptr, _ptr, _size, _ptr]),
+        "ad_attention_backward_workspace_size": (_i32, [_attn, ctypes.POINTER(_size)]),
+        "ad_attention_backward": (_i32, [_attn, _mat, _mat, _mat, _mat, _mat, _ptr, _mat, _mat, _mat, _mat, _mat,
+                                         _ptr, _size, _ptr]),
+        "ad_adamw": (_i32, [_opt, _i32, ctypes.POINTER(AdamwArgs), _ptr]),
+        "ad_opt_state": (_i32, [_opt, _i32, _ptr, _ptr, _ptr]),
+        "ad_grad_norm_workspace_size": (_i32, [_opt, _i32, ctypes.POINTER(_size)]),
+        "ad_grad_norm": (_i32, [_opt, _i32, ctypes.c_double, _ptr, _ptr, _ptr, _size, _ptr]),
         "ad_profile_enable": (_i32, [_ptr, _i32, _i32]),
         "ad_profile_read": (_i32, [_ptr, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(_i32)]),
     }
@@ -131,6 +160,8 @@ EXPORTS = ("ad_last_error", "ad_model_param_count", "ad_model_create", "ad_model
            "ad_layer_norm_backward_workspace_size", "ad_layer_norm_backward",
            "ad_linear_workspace_size", "ad_linear", "ad_linear_dgrad_workspace_size", "ad_linear_dgrad",
            "ad_linear_wgrad_workspace_size", "ad_linear_wgrad",
+           "ad_attention_workspace_size", "ad_attention", "ad_attention_backward_workspace_size",
+           "ad_attention_backward", "ad_adamw", "ad_opt_state", "ad_grad_norm_workspace_size", "ad_grad_norm",
            "ad_profile_enable", "ad_profile_read")
 PROF_CROSS_ATTN, PROF_SELF_ATTN, PROF_GEMM, PROF_LM_HEAD, PROF_XQ_CROSS, PROF_XQ, PROF_ANCHOR = 1, 2, 3, 4, 5, 6, 7
 
@@ -504,6 +535,216 @@ def linear_wgrad(dy, x, x_ckpt, gain, shift, dw, dbias, workspace, accumulate: b
                               _ckpt("x_ckpt", x_ckpt, rows, k, dev), g, s, dt, _mat("dw", dw, n, k, dev),
                               _floats("dbias", dbias, n, dev), int(accumulate), ws, ws_bytes, _stream(stream, dev)),
           "ad_linear_wgrad")
+
+
+def _ints(name: str, t, shape, dev: int):
+    """The address of a contiguous int32 tensor of this shape (None for None)."""
+    if t is None:
+        return None
+    if t.get_device() != dev:
+        raise _elsewhere(name, t)
+    if tuple(t.shape) != shape or t.dtype is not torch.int32 or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {list(shape)} tensor of int32")
+    return t.data_ptr()
+
+
+class Attention:
+    """What an attention call knows of its batch (ad.h: ad_attn), kept from one call to the next: heads,
+    the tables of the sequences' rows (int32 tensors, read when the kernels run) and which keys are visible.
+    q_max and k_max bound the rows of a sequence.  err_flag (int32 [1]) collects AD_ERR_* bits; without
+    one the object has its own, `err_flag`."""
+
+    def __init__(self, q_heads: int, kv_heads: int, cu_q, cu_k, q_max: int, k_max: int, q_len=None, k_len=None,
+                 causal: bool = False, window=None, err_flag=None):
+        self.batch = cu_q.shape[0] - 1
+        if self.batch < 0:
+            raise ValueError("cu_q needs at least one entry")
+        dev = cu_q.get_device()
+        if err_flag is None:
+            err_flag = torch.zeros(1, dtype=torch.int32, device=cu_q.device)
+        self.q_heads, self.kv_heads, self.window, self.err_flag = q_heads, kv_heads, window, err_flag
+        self._dev, self._tables = dev, (cu_q, cu_k, q_len, k_len)
+        window_rows = 0 if window is None else window.shape[0]
+        self._fields = (_ints("cu_q", cu_q, (self.batch + 1,), dev), _ints("cu_k", cu_k, (self.batch + 1,), dev),
+                        _ints("q_len", q_len, (self.batch,), dev), _ints("k_len", k_len, (self.batch,), dev),
+                        _ints("window", window, (window_rows, 2), dev), _ints("err_flag", err_flag, (1,), dev))
+        self._sizes = (q_max, k_max, int(causal))
+        self._view = None
+
+    def view(self, q_rows: int, k_rows: int):
+        """The ad_attn of matrices with these rows."""
+        kept = self._view
+        if kept is None or kept[0] != (q_rows, k_rows):
+            if self.window is not None and self.window.shape[0] != q_rows:
+                raise ValueError(f"window has {self.window.shape[0]} rows, expected {q_rows}")
+            s = AttnView(self.batch, self.q_heads, self.kv_heads, q_rows, k_rows, *self._sizes, *self._fields)
+            kept = self._view = ((q_rows, k_rows), _byref(s))
+        return kept[1]
+
+    def on(self, dev: int):
+        if self._dev != dev:
+            raise ValueError(f"the batch's tables are on GPU {self._dev}, not on the current one")
+        return dev
+
+
+def _attn_space(name: str, at: Attention, q_rows: int, k_rows: int) -> int:
+    n = _size()
+    check(getattr(LIB, name)(at.view(q_rows, k_rows), ctypes.byref(n)), name)
+    return n.value
+
+
+def attention_workspace_size(at: Attention, q_rows: int, k_rows: int) -> int:
+    return _attn_space("ad_attention_workspace_size", at, q_rows, k_rows)
+
+
+def attention(at: Attention, q, k, v, o, lse=None, o_rest=None, workspace=None, stream=None):
+    """o = softmax(q k^T / 8) v over the visible keys (ad.h: ad_attention); lse [q_heads][rows] and o_rest are
+    kept for the backward pass when given."""
+    rows, k_rows, dev = q.shape[0], k.shape[0], at.on(_device("q", q))
+    wq, wk = 64 * at.q_heads, 64 * at.kv_heads
+    ws, ws_bytes = _space(workspace, dev)
+    check(LIB.ad_attention(at.view(rows, k_rows), _mat("q", q, rows, wq, dev), _mat("k", k, k_rows, wk, dev),
+                           _mat("v", v, k_rows, wk, dev), _mat("o", o, rows, wq, dev),
+                           _mat("o_rest", o_rest, rows, wq, dev), _table("lse", lse, at.q_heads, rows, dev), ws, ws_bytes,
+                           _stream(stream, dev)), "ad_attention")
+
+
+def _table(name: str, t, a: int, b: int, dev: int):
+    """The address of a contiguous [a][b] float32 tensor (None for None)."""
+    if t is None:
+        return None
+    if t.get_device() != dev:
+        raise _elsewhere(name, t)
+    if t.shape != (a, b) or t.dtype is not torch.float32 or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous [{a}][{b}] tensor of float32")
+    return t.data_ptr()
+
+
+def attention_backward_workspace_size(at: Attention, q_rows: int, k_rows: int) -> int:
+    return _attn_space("ad_attention_backward_workspace_size", at, q_rows, k_rows)
+
+
+def attention_backward(at: Attention, q, k, v, o, o_rest, lse, dout, dq_res, dq, dk, dv, workspace, stream=None):
+    """The gradients dq (+ dq_res), dk and dv (ad.h: ad_attention_backward) from the forward pass's inputs, o,
+    o_rest (or None) and lse; dq_res may be None."""
+    rows, k_rows, dev = q.shape[0], k.shape[0], at.on(_device("q", q))
+    wq, wk = 64 * at.q_heads, 64 * at.kv_heads
+    ws, ws_bytes = _space(workspace, dev)
+    if lse is None:
+        raise ValueError("lse of the forward pass is needed")
+    check(LIB.ad_attention_backward(
+        at.view(rows, k_rows), _mat("q", q, rows, wq, dev), _mat("k", k, k_rows, wk, dev),
+        _mat("v", v, k_rows, wk, dev), _mat("o", o, rows, wq, dev), _mat("o_rest", o_rest, rows, wq, dev),
+        _table("lse", lse, at.q_heads, rows, dev), _mat("dout", dout, rows, wq, dev),
+        _mat("dq_res", dq_res, rows, wq, dev), _mat("dq", dq, rows, wq, dev), _mat("dk", dk, k_rows, wk, dev),
+        _mat("dv", dv, k_rows, wk, dev), ws, ws_bytes, _stream(stream, dev)), "ad_attention_backward")
+
+
+class OptTensors:
+    """Parameters with their gradients and optimizer states (ad.h: ad_opt_tensor), kept from one step to the
+    next: lists of contiguous tensors of equal sizes on one GPU.  m and v are float32, or int8 and uint8 with the
+    scales m_scale and v_scale of every 128 elements; copies (bf16) and any list that a call does not use may
+    be None; weight_decay is one number or a list."""
+
+    def __init__(self, params=None, grads=None, m=None, v=None, m_scale=None, v_scale=None, copies=None,
+                 weight_decay=0.0):
+        lists = dict(params=params, grads=grads, m=m, v=v, m_scale=m_scale, v_scale=v_scale, copies=copies)
+        given = [x for x in (grads, params, m) if x is not None]
+        if not given:
+            raise ValueError("no tensors given")
+        self.count = len(given[0])
+        for name, x in lists.items():
+            if x is not None and len(x) != self.count:
+                raise ValueError(f"{name} has {len(x)} tensors, expected {self.count}")
+        if not isinstance(weight_decay, (list, tuple)):
+            weight_decay = [weight_decay] * self.count
+        elif len(weight_decay) != self.count:
+            raise ValueError(f"weight_decay has {len(weight_decay)} numbers, expected {self.count}")
+        self.tensors = lists
+        self.device = given[0][0].get_device() if self.count else None
+        self.numel = sum(t.numel() for t in given[0])
+        self.array = (OptTensor * self.count)()
+        self.steps = (params is not None and grads is not None and m is not None and v is not None)
+        pick = lambda x, i: None if x is None else x[i]  # noqa: E731
+        for i in range(self.count):
+            e, n = self.array[i], given[0][i].numel()
+            e.n, e.weight_decay = n, weight_decay[i]
+            e.param = self._at("param", pick(params, i), n, torch.float32, torch.bfloat16)
+            e.grad = self._at("grad", pick(grads, i), n, torch.float32, torch.bfloat16)
+            e.copy = self._at("copy", pick(copies, i), n, torch.bfloat16)
+            e.param_dtype = AD_F32 if params is None else _DTYPE[params[i].dtype]
+            e.grad_dtype = AD_F32 if grads is None else _DTYPE[grads[i].dtype]
+            eight = m is not None and m[i].dtype is torch.int8
+            e.state = STATE_8 if eight else STATE_F
+            e.m = self._at("m", pick(m, i), n, torch.int8 if eight else torch.float32)
+            e.v = self._at("v", pick(v, i), n, torch.uint8 if eight else torch.float32)
+            if eight:
+                groups = -(-n // 128)
+                if m_scale is None or v_scale is None:
+                    raise ValueError("8-bit states need m_scale and v_scale")
+                e.m_scale = self._at("m_scale", m_scale[i], groups, torch.float32)
+                e.v_scale = self._at("v_scale", v_scale[i], groups, torch.float32)
+
+    def _at(self, name: str, t, n: int, *dtypes):
+        if t is None:
+            return None
+        if t.get_device() != self.device:
+            raise ValueError(f"{name} is on {t.device}, not on the other tensors' GPU")
+        if t.numel() != n or t.dtype not in dtypes or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous tensor of {n} elements of {' or '.join(map(str, dtypes))}")
+        return t.data_ptr()
+
+    def on(self):
+        """The current GPU, where the tensors have to be."""
+        dev = _current_device() if self.count else torch.cuda.current_device()
+        if self.count and self.device != dev:
+            raise ValueError(f"the tensors are on GPU {self.device}, not on the current one")
+        return dev
+
+
+def _scalar(name: str, t, dtype, dev: int):
+    if t is None:
+        return None
+    if t.get_device() != dev:
+        raise _elsewhere(name, t)
+    if t.numel() != 1 or t.dtype is not dtype:
+        raise ValueError(f"{name} must be one number of {dtype}")
+    return t.data_ptr()
+
+
+def adamw(opt: OptTensors, lr, step, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, seed: int = 0,
+          grad_scale=None, stream=None):
+    """One AdamW step (ad.h: ad_adamw).  lr and step are numbers, or tensors on the GPU (float32 [1], int32
+    [1]) for a captured step; grad_scale is a float32 [1] on the GPU, or None."""
+    dev = opt.on()
+    if not opt.steps:
+        raise ValueError("a step needs params, grads, m and v")
+    lr_at = _scalar("lr", lr, torch.float32, dev) if isinstance(lr, torch.Tensor) else None
+    step_at = _scalar("step", step, torch.int32, dev) if isinstance(step, torch.Tensor) else None
+    a = AdamwArgs(0.0 if lr_at else lr, beta1, beta2, eps, 0 if step_at else step, seed & 0xFFFFFFFF, lr_at, step_at,
+                  _scalar("grad_scale", grad_scale, torch.float32, dev))
+    check(LIB.ad_adamw(opt.array, opt.count, _byref(a), _stream(stream, dev)), "ad_adamw")
+
+
+def opt_state(opt: OptTensors, m, v, stream=None):
+    """The states' values in float32, one tensor after the other, into m and v [sum of sizes] (either may
+    be None; ad.h: ad_opt_state)."""
+    dev = opt.on()
+    check(LIB.ad_opt_state(opt.array, opt.count, _floats("m", m, opt.numel, dev), _floats("v", v, opt.numel, dev),
+                           _stream(stream, dev)), "ad_opt_state")
+
+
+def grad_norm_workspace_size(opt: OptTensors) -> int:
+    return _workspace_size("ad_grad_norm_workspace_size", opt.array, opt.count)
+
+
+def grad_norm(opt: OptTensors, max_norm: float, out, workspace, step=None, stream=None):
+    """out[0] = the norm of all gradients, out[1] = the factor that clips it to max_norm (0: none); step (int32
+    [1]) counts the finite ones (ad.h: ad_grad_norm)."""
+    dev = opt.on()
+    ws, ws_bytes = _space(workspace, dev)
+    check(LIB.ad_grad_norm(opt.array, opt.count, max_norm, _floats("out", out, 2, dev),
+                           _scalar("step", step, torch.int32, dev), ws, ws_bytes, _stream(stream, dev)), "ad_grad_norm")
 
 
 def kv_import(model: Model, kv: KV, b: int, src, n: int, err_flag, stream=None):

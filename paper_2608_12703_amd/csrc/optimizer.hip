@@ -1,0 +1,362 @@
+// AdamW over many tensors in one launch, 8-bit states, and the gradients' norm.
+//
+// All of it streams each tensor once: the floor is HBM traffic.  A workgroup takes kChunk elements of
+// one tensor (the tensors of a launch are kernel arguments, found by their first workgroup), a
+// lane 8 consecutive elements at a time: 16-byte accesses of every type.
+#include <algorithm>
+
+#include "train.h"
+#include "top2.h"
+
+namespace ad {
+
+namespace {
+
+constexpr int kPass = 2048, kChunk = 4 * kPass;   // elements that a workgroup has at once, and in all
+constexpr int kGroup = 128;                       // elements that share a scale: 16 lanes
+
+// ----------------------------------------------------------------- elements of any alignment
+
+__device__ __forceinline__ void get8(const float* p, int n, float (&v)[8]) {
+  if (n >= 8) {
+    __builtin_memcpy(v, p, 32);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.f;
+  }
+}
+__device__ __forceinline__ void put8(float* p, int n, const float (&v)[8]) {
+  if (n >= 8) {
+    __builtin_memcpy(p, v, 32);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) p[i] = v[i];
+  }
+}
+__device__ __forceinline__ void get8(const uint16_t* p, int n, float (&v)[8]) {
+  if (n >= 8) {
+    u32x4 u;
+    __builtin_memcpy(&u, p, 16);
+    widen8(u, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < n ? bf16_to_f32(p[i]) : 0.f;
+  }
+}
+__device__ __forceinline__ void put8(uint16_t* p, int n, u32x4 u) {
+  if (n >= 8) {
+    __builtin_memcpy(p, &u, 16);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) p[i] = (uint16_t)(u[i / 2] >> (16 * (i % 2)));
+  }
+}
+__device__ __forceinline__ u32x4 narrow8(const float (&v)[8]) {
+  return u32x4{f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]), f32x2_to_bf16x2(v[4], v[5]),
+               f32x2_to_bf16x2(v[6], v[7])};
+}
+__device__ __forceinline__ u32x2 get_bytes(const void* p, int n) {
+  u32x2 u = {0, 0};
+  if (n >= 8) {
+    __builtin_memcpy(&u, p, 8);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) u[i / 4] |= (uint32_t)((const uint8_t*)p)[i] << (8 * (i % 4));
+  }
+  return u;
+}
+__device__ __forceinline__ void put_bytes(void* p, int n, u32x2 u) {
+  if (n >= 8) {
+    __builtin_memcpy(p, &u, 8);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) ((uint8_t*)p)[i] = (uint8_t)(u[i / 4] >> (8 * (i % 4)));
+  }
+}
+
+// ----------------------------------------------------------------- 8-bit states
+
+// 32 random bits of 32: exclusive-ors of shifts between products with odd constants (the fractions of
+// the square roots of 2 and 3); elements are the golden ratio's fraction apart.
+constexpr uint32_t kGolden = 0x9E3779B9u;
+__host__ __device__ __forceinline__ uint32_t mix(uint32_t x) {
+  x ^= x >> 16;
+  x *= 0x6A09E667u;
+  x ^= x >> 15;
+  x *= 0xBB67AE85u;
+  return x ^ (x >> 16);
+}
+// 16 bits as a threshold inside (0, 1); exact
+__device__ __forceinline__ float threshold(uint32_t bits) { return ((float)bits + 0.5f) * (1.0f / 65536.0f); }
+
+// Largest of 16 lanes, as the bits of magnitudes (a NaN is larger than an infinity).
+__device__ __forceinline__ uint32_t group_max(uint32_t m) {
+  m = max(m, (uint32_t)ror16<8>((int)m));
+  m = max(m, (uint32_t)ror16<4>((int)m));
+  m = max(m, (uint32_t)ror16<2>((int)m));
+  return max(m, (uint32_t)ror16<1>((int)m));
+}
+constexpr uint32_t kTiny = 0x0d800000u;           // 2^-100
+constexpr uint32_t kInf = 0x7f800000u;
+
+// scale = top / unit and its inverse, of a group whose largest magnitude has the bits `top`; a group under
+// 2^-100 is all zeros (scale 0), one that is not finite reads as NaN.
+__device__ __forceinline__ void scale_of(uint32_t top, float unit, float& scale, float& inv) {
+  const bool none = top < kTiny, bad = top >= kInf;
+  const float t = __uint_as_float(none || bad ? 0x3f800000u : top);
+  scale = none ? 0.f : bad ? __uint_as_float(0x7fc00000u) : t / unit;
+  inv = none || bad ? 0.f : unit / t;
+}
+
+__device__ __forceinline__ int code_m(float m, float inv, float r) {
+#pragma clang fp contract(off)
+  const float x = m * inv, low = floorf(x);
+  const float q = low + (x - low > r ? 1.f : 0.f);
+  return (int)__builtin_amdgcn_fmed3f(q, -127.f, 127.f);
+}
+// x = v inv in [0, 65025]: the root's whole part by an approximate root and one comparison each way
+// (squares of whole numbers up to 256 are exact)
+__device__ __forceinline__ int code_v(float v, float inv, float r) {
+#pragma clang fp contract(off)
+  const float x = v * inv;
+  float low = floorf(__builtin_amdgcn_sqrtf(x));
+  if (low * low > x) low -= 1.f;
+  if ((low + 1.f) * (low + 1.f) <= x) low += 1.f;
+  const float q = low + (x - low * low > r * (2.f * low + 1.f) ? 1.f : 0.f);
+  return (int)__builtin_amdgcn_fmed3f(q, v > 0.f && inv > 0.f ? 1.f : 0.f, 255.f);
+}
+__device__ __forceinline__ void value_m(u32x2 q, float s, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = (float)(int8_t)(q[i / 4] >> (8 * (i % 4))) * s;
+}
+__device__ __forceinline__ void value_v(u32x2 q, float s, float (&v)[8]) {
+#pragma clang fp contract(off)
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float r = (float)(uint8_t)(q[i / 4] >> (8 * (i % 4)));
+    v[i] = r * r * s;
+  }
+}
+
+// ----------------------------------------------------------------- the step
+
+// The tensor that a workgroup works on, and its place in it.
+__device__ __forceinline__ int find(const OptList& l, int block) {
+  int lo = 0;
+  for (int i = 1; i < l.count; ++i)
+    if (block >= l.first[i]) lo = i;
+  return lo;
+}
+
+struct Hyper {
+  float root, rate;
+  uint32_t key;
+  float lr;
+};
+
+template <bool STATE8>
+__device__ __forceinline__ void adamw_pass(const OptTensor& t, const AdamwArgs& a, const Hyper& y, float keep, float gs,
+                                           uint32_t key, int64_t i) {
+#pragma clang fp contract(off)
+  const int n = (int)min(t.n - i, (int64_t)8);          // may be <= 0: the lane only takes part in its group
+  float p[8] = {}, g[8] = {}, m[8] = {}, v[8] = {};
+  if (n > 0) {
+    if (t.kinds & OPT_GRAD16) get8((const uint16_t*)t.grad + i, n, g);
+    else get8((const float*)t.grad + i, n, g);
+    if (STATE8) {
+      value_m(get_bytes((const int8_t*)t.m + i, n), t.m_scale[i / kGroup], m);
+      value_v(get_bytes((const uint8_t*)t.v + i, n), t.v_scale[i / kGroup], v);
+    } else {
+      get8((const float*)t.m + i, n, m);
+      get8((const float*)t.v + i, n, v);
+    }
+    if (t.kinds & OPT_PARAM16) get8((const uint16_t*)t.param + i, n, p);
+    else get8((const float*)t.param + i, n, p);
+  }
+  uint32_t bits[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) bits[e] = mix(key + (uint32_t)(i + e) * kGolden);
+  uint32_t top_m = 0, top_v = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float ge = g[e] * gs;
+    m[e] = m[e] * a.b1 + ge * a.ob1;
+    v[e] = v[e] * a.b2 + ge * ge * a.ob2;
+    const float den = __builtin_amdgcn_sqrtf(v[e]) * y.root + a.eps;
+    p[e] = p[e] * keep - m[e] * __builtin_amdgcn_rcpf(den) * y.rate;
+    if (STATE8) {
+      top_m = max(top_m, e < n ? abs_bits(m[e]) : 0u);
+      top_v = max(top_v, e < n ? abs_bits(v[e]) : 0u);
+    }
+  }
+  if (n > 0) {
+    if (t.kinds & OPT_PARAM16) {
+      u32x4 u = {0, 0, 0, 0};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t b = __float_as_uint(p[e]);
+        const uint32_t up = (b & kInf) == kInf ? (uint32_t)f32_to_bf16(p[e]) : (b + (mix(bits[e] + kGolden) & 0xffffu)) >> 16;
+        u[e / 2] |= up << (16 * (e % 2));
+      }
+      put8((uint16_t*)t.param + i, n, u);
+    } else {
+      put8((float*)t.param + i, n, p);
+      if (t.copy) put8((uint16_t*)t.copy + i, n, narrow8(p));
+    }
+    if (!STATE8) {
+      put8((float*)t.m + i, n, m);
+      put8((float*)t.v + i, n, v);
+    }
+  }
+  if (STATE8) {
+    float ms, mi, vs, vi;
+    scale_of(group_max(top_m), 127.f, ms, mi);
+    scale_of(group_max(top_v), 65025.f, vs, vi);
+    if (n > 0) {
+      u32x2 qm, qv;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t cm[4], cv[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          cm[e] = (uint32_t)code_m(m[4 * h + e], mi, threshold(bits[4 * h + e] & 0xffffu));
+          cv[e] = (uint32_t)code_v(v[4 * h + e], vi, threshold(bits[4 * h + e] >> 16));
+        }
+        qm[h] = pack_bytes(cm[0], cm[1], cm[2], cm[3]);
+        qv[h] = pack_bytes(cv[0], cv[1], cv[2], cv[3]);
+      }
+      put_bytes((int8_t*)t.m + i, n, qm);
+      put_bytes((uint8_t*)t.v + i, n, qv);
+      if (i % kGroup == 0) {
+        t.m_scale[i / kGroup] = ms;
+        t.v_scale[i / kGroup] = vs;
+      }
+    }
+  }
+}
+
+__global__ void __launch_bounds__(256) adamw_kernel(OptList l, AdamwArgs a) {
+  __shared__ Hyper shared;
+  const OptTensor& t = l.t[find(l, blockIdx.x)];
+  Hyper y = {a.root, a.rate, a.key, 0.f};
+  float keep = t.keep;
+  if (a.lr_at || a.step_at) {
+    if (threadIdx.x == 0) {
+      const int step = a.step_at ? *a.step_at : a.step;
+      const double lr = a.lr_at ? (double)*a.lr_at : a.lr;
+      shared.root = (float)(1.0 / sqrt(-expm1(step * log(a.beta2))));
+      shared.rate = (float)(lr / -expm1(step * log(a.beta1)));
+      shared.key = mix(a.seed + kGolden * (uint32_t)step);
+      shared.lr = (float)lr;
+    }
+    __syncthreads();
+    y = shared;
+    keep = (float)(1.0 - (double)y.lr * (double)t.decay);
+  }
+  const float gs = a.scale ? *a.scale : 1.f;
+  if (!(fabsf(gs) < INFINITY)) return;
+  const uint32_t key = mix(t.key + y.key);
+  const int64_t base = (int64_t)(blockIdx.x - l.first[&t - l.t]) * kChunk;
+  for (int c = 0; c < kChunk; c += kPass) {
+    const int64_t i = base + c + 8 * threadIdx.x;
+    if (base + c >= t.n) break;
+    if (t.kinds & OPT_STATE8) adamw_pass<true>(t, a, y, keep, gs, key, i);
+    else adamw_pass<false>(t, a, y, keep, gs, key, i);
+  }
+}
+
+struct StateAt {
+  int64_t at[kOptTensors];     // where a tensor's values begin in m and v
+};
+__global__ void __launch_bounds__(256) opt_state_kernel(OptList l, StateAt s, float* m, float* v) {
+  const int k = find(l, blockIdx.x);
+  const OptTensor& t = l.t[k];
+  const int64_t base = (int64_t)(blockIdx.x - l.first[k]) * kChunk;
+  for (int c = 0; c < kChunk; c += kPass) {
+    const int64_t i = base + c + 8 * threadIdx.x;
+    const int n = (int)min(t.n - i, (int64_t)8);
+    if (n <= 0) break;
+    float x[8];
+    if (m) {
+      if (t.kinds & OPT_STATE8) value_m(get_bytes((const int8_t*)t.m + i, n), t.m_scale[i / kGroup], x);
+      else get8((const float*)t.m + i, n, x);
+      put8(m + s.at[k] + i, n, x);
+    }
+    if (v) {
+      if (t.kinds & OPT_STATE8) value_v(get_bytes((const uint8_t*)t.v + i, n), t.v_scale[i / kGroup], x);
+      else get8((const float*)t.v + i, n, x);
+      put8(v + s.at[k] + i, n, x);
+    }
+  }
+}
+
+// ----------------------------------------------------------------- the norm
+
+__device__ __forceinline__ double block_total(double s, double* red) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) s += __shfl_xor(s, o, kWave);
+  if (threadIdx.x % kWave == 0) red[threadIdx.x / kWave] = s;
+  __syncthreads();
+  return (red[0] + red[1]) + (red[2] + red[3]);
+}
+
+__global__ void __launch_bounds__(256) grad_squares_kernel(OptList l, double* part) {
+  __shared__ double red[4];
+  const int k = find(l, blockIdx.x);
+  const OptTensor& t = l.t[k];
+  const int64_t base = (int64_t)(blockIdx.x - l.first[k]) * kChunk;
+  double s = 0.0;
+  for (int c = 0; c < kChunk; c += kPass) {
+    const int64_t i = base + c + 8 * threadIdx.x;
+    const int n = (int)min(t.n - i, (int64_t)8);
+    if (n <= 0) break;
+    float g[8];
+    if (t.kinds & OPT_GRAD16) get8((const uint16_t*)t.grad + i, n, g);
+    else get8((const float*)t.grad + i, n, g);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s = fma((double)g[e], (double)g[e], s);
+  }
+  s = block_total(s, red);
+  if (threadIdx.x == 0) part[blockIdx.x] = s;
+}
+
+__global__ void __launch_bounds__(256) grad_norm_kernel(const double* part, int64_t parts, double max_norm, float* out,
+                                                        int* step) {
+  __shared__ double red[4];
+  double s = 0.0;
+  for (int64_t i = threadIdx.x; i < parts; i += 256) s += part[i];
+  s = block_total(s, red);
+  if (threadIdx.x == 0) {
+    const double norm = sqrt(s);
+    out[0] = (float)norm;
+    const bool fine = (float)norm < INFINITY;           // (NaN is not)
+    out[1] = !fine ? __uint_as_float(0x7fc00000u) : max_norm > 0.0 && norm > max_norm ? (float)(max_norm / norm) : 1.f;
+    if (step && fine) *step += 1;
+  }
+}
+
+}  // namespace
+
+int64_t opt_groups(int64_t n) { return (n + kChunk - 1) / kChunk; }
+
+void launch_adamw(const OptList& l, AdamwArgs a, hipStream_t st) {
+  a.key = mix(a.seed + kGolden * (uint32_t)a.step);
+  if (l.first[l.count]) adamw_kernel<<<l.first[l.count], 256, 0, st>>>(l, a);
+}
+void launch_opt_state(const OptList& l, float* m, float* v, const int64_t* at, hipStream_t st) {
+  StateAt s{};
+  for (int i = 0; i < l.count; ++i) s.at[i] = at[i];
+  if (l.first[l.count]) opt_state_kernel<<<l.first[l.count], 256, 0, st>>>(l, s, m, v);
+}
+void launch_grad_squares(const OptList& l, double* part, hipStream_t st) {
+  if (l.first[l.count]) grad_squares_kernel<<<l.first[l.count], 256, 0, st>>>(l, part);
+}
+void launch_grad_norm(const double* part, int64_t parts, double max_norm, float* out, int* step, hipStream_t st) {
+  grad_norm_kernel<<<1, 256, 0, st>>>(part, parts, max_norm, out, step);
+}
+
+}  // namespace ad

@@ -3,6 +3,7 @@
 #pragma once
 
 #include "common.h"
+#include "../../include/ad.h"
 
 namespace ad {
 
@@ -312,5 +313,77 @@ struct LinArgs {
 // Floats of workspace of a product of this kind with these extents.
 size_t lin_part_floats(int kind, int P, int Q, int K);
 void launch_linear(int kind, LinArgs a, hipStream_t st);
+
+// ----------------------------------------------------------------- attention
+
+// A strided bf16 matrix; vec: rows of 8 elements at a multiple of 8 are 16-byte aligned.
+struct HMat {
+  uint16_t* p;
+  int64_t ld;
+  int vec;
+};
+
+// What both passes know of a batch (ad_attn).
+struct AttnBatch {
+  int batch, heads, kv_heads, q_rows, k_rows, q_max, k_max, causal;
+  const int *cu_q, *cu_k, *q_len, *k_len, *window;
+  int* err;
+};
+struct AttnFwdArgs {
+  AttnBatch b;
+  HMat q, k, v, o, rest;   // rest.p NULL: not kept
+  float* lse;              // or NULL
+  float* part;
+};
+struct AttnBwdArgs {
+  AttnBatch b;
+  HMat q, k, v, o, rest, dout, dq, dk, dv;
+  DMat res;                // p NULL: none
+  const float* lse;
+  float* delta;            // [heads][q_rows]
+};
+size_t attn_fwd_bytes(const AttnBatch& b);
+size_t attn_bwd_bytes(const AttnBatch& b);
+// workgroups of the largest launch, to be held under 2^31
+int64_t attn_groups(const AttnBatch& b);
+void launch_attention(const AttnFwdArgs& a, hipStream_t st);
+void launch_attention_backward(const AttnBwdArgs& a, hipStream_t st);
+
+// ----------------------------------------------------------------- optimizer
+
+struct OptTensor {
+  int64_t n;
+  void *param, *copy;
+  const void* grad;
+  void *m, *v;
+  float *m_scale, *v_scale;
+  float keep;              // 1 - lr weight_decay
+  float decay;             // weight_decay (where lr is on the device)
+  uint32_t key;            // place in the list
+  int kinds;               // OPT_*
+};
+enum : int { OPT_PARAM16 = 1, OPT_GRAD16 = 2, OPT_STATE8 = 4 };
+// Tensors of one launch: kernel arguments hold 4 KB.
+constexpr int kOptTensors = 40;
+struct OptList {
+  int count;
+  int first[kOptTensors + 1];   // first workgroup of each tensor
+  OptTensor t[kOptTensors];
+};
+struct AdamwArgs {
+  float b1, ob1, b2, ob2, root, eps, rate;   // root = 1 / sqrt(1 - b2^t), rate = lr / (1 - b1^t)
+  uint32_t key;
+  // where step or learning rate are on the device
+  double beta1, beta2, lr;
+  int step;
+  uint32_t seed;
+  const float *lr_at, *scale;
+  const int* step_at;
+};
+int64_t opt_groups(int64_t n);   // workgroups of a tensor
+void launch_adamw(const OptList& l, AdamwArgs a, hipStream_t st);
+void launch_opt_state(const OptList& l, float* m, float* v, const int64_t* at, hipStream_t st);
+void launch_grad_squares(const OptList& l, double* part, hipStream_t st);
+void launch_grad_norm(const double* part, int64_t parts, double max_norm, float* out, int* step, hipStream_t st);
 
 }  // namespace ad

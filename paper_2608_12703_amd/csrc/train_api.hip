@@ -1,5 +1,6 @@
 // C-ABI entry points of the draft block's training operators: argument validation and the
 // description of the operands handed to the launchers.
+#include <cmath>
 #include <cstdint>
 #include <string>
 
@@ -104,6 +105,129 @@ ad_status linear_space(int kind, int32_t rows, int32_t n, int32_t k, size_t* byt
 }
 
 ad::LinOp op(const ad_mat* m, int extent) { return ad::LinOp{(const uint16_t*)m->data, m->ld, {}, extent}; }
+
+// ----------------------------------------------------------------- attention
+
+constexpr int32_t kMaxHeads = 1 << 14;    // 64 kMaxHeads = kMaxCols
+
+ad_status attn_ok(const ad_attn* a) {
+  if (!a) return bad("NULL argument");
+  if (a->batch < 0 || a->batch > 65535) return fail(AD_ERANGE, "batch must be in [0, 65535]");
+  if (a->q_heads < 1 || a->q_heads > kMaxHeads || a->kv_heads < 1 || a->kv_heads > kMaxHeads)
+    return fail(AD_ERANGE, "heads must be in [1, 2^14]");
+  if (a->q_heads % a->kv_heads) return bad("kv_heads must divide q_heads");
+  if (a->q_rows < 0 || a->q_rows > kMaxRows || a->k_rows < 0 || a->k_rows > kMaxRows)
+    return fail(AD_ERANGE, "rows must be in [0, 2^24]");
+  if (a->q_max < 0 || a->q_max > kMaxRows || a->k_max < 0 || a->k_max > kMaxRows)
+    return fail(AD_ERANGE, "q_max and k_max must be in [0, 2^24]");
+  return AD_OK;
+}
+
+ad::AttnBatch attn_batch(const ad_attn* a) {
+  ad::AttnBatch b{};
+  b.batch = a->batch; b.heads = a->q_heads; b.kv_heads = a->kv_heads;
+  b.q_rows = a->q_rows; b.k_rows = a->k_rows;
+  // (no sequence can have more rows than there are)
+  b.q_max = a->q_max < a->q_rows ? a->q_max : a->q_rows;
+  b.k_max = a->k_max < a->k_rows ? a->k_max : a->k_rows;
+  b.causal = a->causal != 0;
+  b.cu_q = a->cu_q; b.cu_k = a->cu_k; b.q_len = a->q_len; b.k_len = a->k_len; b.window = a->window;
+  b.err = a->err_flag;
+  return b;
+}
+
+// The sizes, the tables and that every launch's workgroups can be counted.
+ad_status attn_call_ok(const ad_attn* a) {
+  AD_TRY(attn_ok(a));
+  if (!a->cu_q || !a->cu_k || !a->err_flag) return bad("NULL argument: cu_q, cu_k or err_flag");
+  const void* tables[] = {a->cu_q, a->cu_k, a->q_len, a->k_len, a->window, a->err_flag};
+  for (const void* t : tables)
+    if ((uintptr_t)t % 4) return bad("misaligned table");
+  if (ad::attn_groups(attn_batch(a)) >= INT32_MAX) return fail(AD_ERANGE, "batch * heads * rows is too large");
+  return AD_OK;
+}
+
+ad::HMat hmat(const ad_mat* m) {
+  ad::HMat d{};
+  if (!m) return d;
+  d.p = (uint16_t*)m->data;
+  d.ld = m->ld;
+  d.vec = (uintptr_t)m->data % 16 == 0 && m->ld % 8 == 0;
+  return d;
+}
+
+// ----------------------------------------------------------------- optimizer
+
+ad_status tensors_ok(const ad_opt_tensor* t, int32_t count) {
+  if (count < 0) return fail(AD_ERANGE, "count must not be negative");
+  if (count > 0 && !t) return bad("NULL argument: tensors");
+  for (int32_t i = 0; i < count; ++i)
+    if (t[i].n < 0 || t[i].n > ((int64_t)1 << 40)) return fail(AD_ERANGE, "n must be in [0, 2^40]");
+  return AD_OK;
+}
+ad_status array_ok(const char* name, const void* p, int size) {
+  if (!p) return bad(std::string("NULL argument: ") + name);
+  return (uintptr_t)p % size ? bad(std::string("misaligned: ") + name) : AD_OK;
+}
+int width(int32_t dtype) { return dtype == AD_BF16 ? 2 : 4; }
+
+ad_status grad_ok(const ad_opt_tensor& t) {
+  if (!dtype_ok(t.grad_dtype)) return bad("unknown dtype: grad");
+  return t.n ? array_ok("grad", t.grad, width(t.grad_dtype)) : AD_OK;
+}
+ad_status state_ok(const ad_opt_tensor& t) {
+  if (t.state != AD_STATE_F && t.state != AD_STATE_8) return bad("unknown state");
+  if (!t.n) return AD_OK;
+  const int size = t.state == AD_STATE_8 ? 1 : 4;
+  AD_TRY(array_ok("m", t.m, size));
+  AD_TRY(array_ok("v", t.v, size));
+  if (t.state == AD_STATE_8) {
+    AD_TRY(array_ok("m_scale", t.m_scale, 4));
+    AD_TRY(array_ok("v_scale", t.v_scale, 4));
+  }
+  return AD_OK;
+}
+
+// Hands the tensors that hold something to `go`, a launch's worth at a time: the list and the tensors' places.
+// Returns false where a launch would have too many workgroups.
+template <class F>
+bool by_launch(const ad_opt_tensor* t, int32_t count, double lr, F&& go) {
+  ad::OptList l;
+  int at[ad::kOptTensors];
+  int64_t groups = 0;
+  l.count = 0;
+  l.first[0] = 0;
+  const auto flush = [&] {
+    if (l.count) go(l, at);
+    l.count = 0;
+    groups = 0;
+  };
+  for (int32_t i = 0; i < count; ++i) {
+    const int64_t more = ad::opt_groups(t[i].n);
+    if (!more) continue;
+    if (more >= INT32_MAX) return false;
+    if (l.count == ad::kOptTensors || groups + more >= INT32_MAX) flush();
+    ad::OptTensor& d = l.t[l.count];
+    d.n = t[i].n;
+    d.param = t[i].param; d.copy = t[i].copy; d.grad = t[i].grad;
+    d.m = t[i].m; d.v = t[i].v; d.m_scale = t[i].m_scale; d.v_scale = t[i].v_scale;
+    d.keep = (float)(1.0 - lr * t[i].weight_decay);
+    d.decay = (float)t[i].weight_decay;
+    d.key = (uint32_t)i;
+    d.kinds = (t[i].param_dtype == AD_BF16 ? ad::OPT_PARAM16 : 0) | (t[i].grad_dtype == AD_BF16 ? ad::OPT_GRAD16 : 0) |
+              (t[i].state == AD_STATE_8 ? ad::OPT_STATE8 : 0);
+    at[l.count] = i;
+    groups += more;
+    l.first[++l.count] = (int)groups;
+  }
+  flush();
+  return true;
+}
+int64_t norm_parts(const ad_opt_tensor* t, int32_t count) {
+  int64_t parts = 0;
+  for (int32_t i = 0; i < count; ++i) parts += ad::opt_groups(t[i].n);
+  return parts;
+}
 
 }  // namespace
 
@@ -297,6 +421,162 @@ ad_status ad_linear_wgrad(int32_t rows, int32_t n, int32_t k, const ad_mat* dy, 
   (void)hipGetLastError();
   ad::launch_linear(ad::LIN_WGRAD, a, (hipStream_t)stream);
   return check_hip("ad_linear_wgrad");
+}
+
+ad_status ad_attention_workspace_size(const ad_attn* a, size_t* bytes) {
+  if (!bytes) return bad("NULL argument");
+  AD_TRY(attn_ok(a));
+  *bytes = align256(ad::attn_fwd_bytes(attn_batch(a)));
+  return AD_OK;
+}
+
+ad_status ad_attention(const ad_attn* a, const ad_mat* q, const ad_mat* k, const ad_mat* v, const ad_mat* o,
+                       const ad_mat* o_rest, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  AD_TRY(attn_call_ok(a));
+  const int32_t wq = 64 * a->q_heads, wk = 64 * a->kv_heads;
+  AD_TRY(mat_ok("q", q, a->q_rows, wq, true));
+  AD_TRY(mat_ok("k", k, a->k_rows, wk, true));
+  AD_TRY(mat_ok("v", v, a->k_rows, wk, true));
+  AD_TRY(mat_ok("o", o, a->q_rows, wq, true));
+  if (o_rest) AD_TRY(mat_ok("o_rest", o_rest, a->q_rows, wq, true));
+  AD_TRY(floats_ok("lse", lse));
+  ad::AttnFwdArgs f{};
+  f.b = attn_batch(a);
+  AD_TRY(space_ok(workspace, workspace_bytes, align256(ad::attn_fwd_bytes(f.b))));
+  f.q = hmat(q); f.k = hmat(k); f.v = hmat(v); f.o = hmat(o); f.rest = hmat(o_rest);
+  f.lse = lse;
+  f.part = (float*)workspace;
+  (void)hipGetLastError();
+  ad::launch_attention(f, (hipStream_t)stream);
+  return check_hip("ad_attention");
+}
+
+ad_status ad_attention_backward_workspace_size(const ad_attn* a, size_t* bytes) {
+  if (!bytes) return bad("NULL argument");
+  AD_TRY(attn_ok(a));
+  *bytes = align256(ad::attn_bwd_bytes(attn_batch(a)));
+  return AD_OK;
+}
+
+ad_status ad_attention_backward(const ad_attn* a, const ad_mat* q, const ad_mat* k, const ad_mat* v, const ad_mat* o,
+                                const ad_mat* o_rest, const float* lse, const ad_mat* dout, const ad_mat* dq_res,
+                                const ad_mat* dq, const ad_mat* dk, const ad_mat* dv, void* workspace,
+                                size_t workspace_bytes, void* stream) {
+  AD_TRY(attn_call_ok(a));
+  const int32_t wq = 64 * a->q_heads, wk = 64 * a->kv_heads;
+  AD_TRY(mat_ok("q", q, a->q_rows, wq, true));
+  AD_TRY(mat_ok("k", k, a->k_rows, wk, true));
+  AD_TRY(mat_ok("v", v, a->k_rows, wk, true));
+  AD_TRY(mat_ok("o", o, a->q_rows, wq, true));
+  if (o_rest) AD_TRY(mat_ok("o_rest", o_rest, a->q_rows, wq, true));
+  AD_TRY(mat_ok("dout", dout, a->q_rows, wq, true));
+  if (dq_res) AD_TRY(mat_ok("dq_res", dq_res, a->q_rows, wq));
+  AD_TRY(mat_ok("dq", dq, a->q_rows, wq, true));
+  AD_TRY(mat_ok("dk", dk, a->k_rows, wk, true));
+  AD_TRY(mat_ok("dv", dv, a->k_rows, wk, true));
+  if (a->q_rows > 0 && !lse) return bad("NULL argument: lse");
+  AD_TRY(floats_ok("lse", lse));
+  ad::AttnBwdArgs f{};
+  f.b = attn_batch(a);
+  AD_TRY(space_ok(workspace, workspace_bytes, align256(ad::attn_bwd_bytes(f.b))));
+  f.q = hmat(q); f.k = hmat(k); f.v = hmat(v); f.o = hmat(o); f.rest = hmat(o_rest); f.dout = hmat(dout);
+  f.dq = hmat(dq); f.dk = hmat(dk); f.dv = hmat(dv);
+  f.res = mat(dq_res, wq);
+  f.lse = lse;
+  f.delta = (float*)workspace;
+  (void)hipGetLastError();
+  ad::launch_attention_backward(f, (hipStream_t)stream);
+  return check_hip("ad_attention_backward");
+}
+
+ad_status ad_adamw(const ad_opt_tensor* tensors, int32_t count, const ad_adamw_args* args, void* stream) {
+  AD_TRY(tensors_ok(tensors, count));
+  if (!args) return bad("NULL argument: args");
+  const ad_adamw_args& h = *args;
+  if (!h.step_at && h.step < 1) return fail(AD_ERANGE, "step must be at least 1");
+  if (!h.lr_at && !(h.lr >= 0 && std::isfinite(h.lr))) return fail(AD_ERANGE, "lr must be finite and not negative");
+  if (!(h.beta1 >= 0 && h.beta1 < 1 && h.beta2 >= 0 && h.beta2 < 1)) return fail(AD_ERANGE, "betas must be in [0, 1)");
+  if (!(h.eps >= 0 && std::isfinite(h.eps))) return fail(AD_ERANGE, "eps must be finite and not negative");
+  const void* scalars[] = {h.lr_at, h.step_at, h.grad_scale};
+  for (const void* p : scalars)
+    if ((uintptr_t)p % 4) return bad("misaligned: lr_at, step_at or grad_scale");
+  for (int32_t i = 0; i < count; ++i) {
+    const ad_opt_tensor& t = tensors[i];
+    if (!dtype_ok(t.param_dtype)) return bad("unknown dtype: param");
+    if (!(t.weight_decay >= 0 && std::isfinite(t.weight_decay)))
+      return fail(AD_ERANGE, "weight_decay must be finite and not negative");
+    AD_TRY(grad_ok(t));
+    AD_TRY(state_ok(t));
+    if (t.copy && t.param_dtype == AD_BF16) return bad("copy goes with a float32 param");
+    if ((uintptr_t)t.copy % 2) return bad("misaligned: copy");
+    if (t.n) AD_TRY(array_ok("param", t.param, width(t.param_dtype)));
+    if (ad::opt_groups(t.n) >= INT32_MAX) return fail(AD_ERANGE, "n is too large");
+  }
+  ad::AdamwArgs a{};
+  a.b1 = (float)h.beta1; a.ob1 = (float)(1.0 - h.beta1);
+  a.b2 = (float)h.beta2; a.ob2 = (float)(1.0 - h.beta2);
+  const int step = h.step_at ? 1 : h.step;       // (not used where it is on the device)
+  a.root = (float)(1.0 / std::sqrt(1.0 - std::pow(h.beta2, step)));
+  a.rate = (float)(h.lr / (1.0 - std::pow(h.beta1, step)));
+  a.eps = (float)h.eps;
+  a.beta1 = h.beta1; a.beta2 = h.beta2; a.lr = h.lr;
+  a.step = step; a.seed = h.seed;
+  a.lr_at = h.lr_at; a.step_at = h.step_at; a.scale = h.grad_scale;
+  (void)hipGetLastError();
+  by_launch(tensors, count, h.lr_at ? 0.0 : h.lr,
+            [&](const ad::OptList& l, const int*) { ad::launch_adamw(l, a, (hipStream_t)stream); });
+  return check_hip("ad_adamw");
+}
+
+ad_status ad_opt_state(const ad_opt_tensor* tensors, int32_t count, float* m, float* v, void* stream) {
+  AD_TRY(tensors_ok(tensors, count));
+  AD_TRY(floats_ok("m", m));
+  AD_TRY(floats_ok("v", v));
+  for (int32_t i = 0; i < count; ++i) {
+    AD_TRY(state_ok(tensors[i]));
+    if (ad::opt_groups(tensors[i].n) >= INT32_MAX) return fail(AD_ERANGE, "n is too large");
+  }
+  (void)hipGetLastError();
+  int64_t at = 0;
+  int32_t done = 0;
+  by_launch(tensors, count, 0.0, [&](const ad::OptList& l, const int* places) {
+    int64_t first[ad::kOptTensors];
+    for (int i = 0; i < l.count; ++i) {
+      for (; done < places[i]; ++done) at += tensors[done].n;
+      first[i] = at;
+    }
+    ad::launch_opt_state(l, m, v, first, (hipStream_t)stream);
+  });
+  return check_hip("ad_opt_state");
+}
+
+ad_status ad_grad_norm_workspace_size(const ad_opt_tensor* tensors, int32_t count, size_t* bytes) {
+  if (!bytes) return bad("NULL argument");
+  AD_TRY(tensors_ok(tensors, count));
+  *bytes = align256(8 * (size_t)norm_parts(tensors, count));
+  return AD_OK;
+}
+
+ad_status ad_grad_norm(const ad_opt_tensor* tensors, int32_t count, double max_norm, float* out, int32_t* step,
+                       void* workspace, size_t workspace_bytes, void* stream) {
+  AD_TRY(tensors_ok(tensors, count));
+  if (!(max_norm >= 0 && std::isfinite(max_norm))) return fail(AD_ERANGE, "max_norm must be finite and not negative");
+  AD_TRY(array_ok("out", out, 4));
+  if ((uintptr_t)step % 4) return bad("misaligned: step");
+  for (int32_t i = 0; i < count; ++i) {
+    AD_TRY(grad_ok(tensors[i]));
+    if (ad::opt_groups(tensors[i].n) >= INT32_MAX) return fail(AD_ERANGE, "n is too large");
+  }
+  const int64_t parts = norm_parts(tensors, count);
+  AD_TRY(space_ok(workspace, workspace_bytes, align256(8 * (size_t)parts)));
+  (void)hipGetLastError();
+  double* part = (double*)workspace;
+  by_launch(tensors, count, 0.0, [&](const ad::OptList& l, const int*) {
+    ad::launch_grad_squares(l, part, (hipStream_t)stream);
+    part += l.first[l.count];
+  });
+  ad::launch_grad_norm((const double*)workspace, parts, max_norm, out, step, (hipStream_t)stream);
+  return check_hip("ad_grad_norm");
 }
 
 }  // extern "C"

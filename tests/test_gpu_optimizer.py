@@ -1,0 +1,335 @@
+"""AdamW, 8-bit states and the gradients' norm against their definitions.
+
+Tolerances.  u = 2^-24.  m and v are products and sums rounded one by one: 3 u of the sum of magnitudes.  The root and the
+reciprocal are good to 1.5 u each (the hardware's, 1 ulp), the scalars to u: the step is off by 12 u of itself, the
+parameter by 3 u of itself on top.  Codes of 8-bit states are functions of their float32 inputs and have to be equal.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2608_12703_amd import ad
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+F32, BF16 = torch.float32, torch.bfloat16
+SIZES = [1, 7, 8, 127, 128, 129, 640, 2048, 2049, 8192, 8193, 0, 30001]
+
+
+def _gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def _cut(flat, sizes, gap=0):
+    """Tensors of these sizes inside one buffer, `gap` elements apart."""
+    out, at = [], 0
+    for n in sizes:
+        out.append(flat[at:at + n])
+        at += n + gap
+    return out
+
+
+def _mix(x):
+    x = x.astype(np.uint32)
+    x = x ^ (x >> np.uint32(16))
+    x = x * np.uint32(0x6A09E667)
+    x = x ^ (x >> np.uint32(15))
+    x = x * np.uint32(0xBB67AE85)
+    return x ^ (x >> np.uint32(16))
+
+
+GOLDEN = np.uint32(0x9E3779B9)
+
+
+def _bits(n, seed, step, place):
+    with np.errstate(over="ignore"):
+        key = _mix(np.array([seed], np.uint32) + GOLDEN * np.uint32(step))
+        key = _mix(key + np.uint32(place))
+        return _mix(key + np.arange(n, dtype=np.uint64).astype(np.uint32) * GOLDEN)
+
+
+def _groups(x):
+    n = -(-len(x) // 128) * 128
+    w = np.zeros(n, x.dtype)
+    w[:len(x)] = x
+    return w.reshape(-1, 128)
+
+
+def _pack(m, v, bits):
+    """(codes of m, scales, codes of v, scales) of float32 states, each operation rounded to float32."""
+    f = np.float32
+    with np.errstate(all="ignore"):
+        def scaled(x, unit):
+            top = np.abs(_groups(x)).max(1)
+            finite, none = np.isfinite(_groups(x)).all(1), top < f(2.0 ** -100)
+            t = np.where(none | ~finite, f(1), top)
+            scale = np.where(~finite, f(np.nan), np.where(none, f(0), t / f(unit))).astype(f)
+            return scale, np.repeat(np.where(none | ~finite, f(0), f(unit) / t).astype(f), 128)[:len(x)]
+        ms, mi = scaled(m, 127)
+        vs, vi = scaled(v, 65025)
+        up = lambda b: ((b.astype(np.float64) + 0.5) / 65536).astype(f)  # noqa: E731
+        x = m * mi
+        low = np.floor(x)
+        qm = np.clip(low + (x - low > up(bits & np.uint32(0xffff))), -127, 127)
+        y = v * vi
+        low = np.floor(np.sqrt(y.astype(np.float64))).astype(f)
+        qv = low + (y - low * low > up(bits >> np.uint32(16)) * (f(2) * low + f(1)))
+        qv = np.clip(qv, np.where((v > 0) & (vi > 0), 1, 0), 255)
+    return qm, ms, qv, vs
+
+
+def _unpack(qm, ms, qv, vs):
+    rep = lambda s, q: np.repeat(s, 128)[:len(q)]  # noqa: E731
+    f = np.float32
+    return qm.astype(f) * rep(ms, qm), qv.astype(f) * qv.astype(f) * rep(vs, qv)
+
+
+class Made:
+    """Tensors of SIZES on the GPU, at odd places in their buffers, and copies on the host."""
+
+    def __init__(self, state, param, grad, copy, seed=0, sizes=SIZES, gap=0, shift=0):
+        g = _gen(seed)
+        self.sizes, n = sizes, sum(sizes) + gap * len(sizes) + shift
+        rand = lambda scale, dt=F32: (torch.randn(n, generator=g) * scale).to(dt)  # noqa: E731
+        cut = lambda x: _cut(x[shift:], sizes, gap)  # noqa: E731
+        self.flat = dict(p=rand(0.02, param), g=rand(1e-2, grad))
+        if state == "f32":
+            self.flat.update(m=rand(1e-3), v=rand(1e-3).square())
+        else:
+            groups = [-(-z // 128) for z in sizes]
+            self.flat.update(m=rand(45.0).round().clamp(-127, 127).to(torch.int8),
+                             v=rand(90.0).abs().round().clamp(0, 255).to(torch.uint8))
+            sc = torch.rand(sum(groups), generator=g) + 0.1
+            self.scales = dict(m_scale=sc * 1e-5, v_scale=sc * 1e-9)
+        if copy:
+            self.flat["c"] = torch.full((n,), -77.0).to(BF16)
+        self.gpu = {k: x.cuda() for k, x in self.flat.items()}
+        self.host = {k: cut(x) for k, x in self.flat.items()}
+        self.dev = {k: cut(x) for k, x in self.gpu.items()}
+        self.state = state
+        more = {}
+        if state != "f32":
+            self.gpu_scales = {k: x.cuda() for k, x in self.scales.items()}
+            more = {k: _cut(x, groups) for k, x in self.gpu_scales.items()}
+            self.host_scales = {k: _cut(x, groups) for k, x in self.scales.items()}
+            self.dev_scales = more
+        self.decay = [0.01 * (i % 3) for i in range(len(sizes))]
+        self.opt = ad.OptTensors(params=self.dev["p"], grads=self.dev["g"], m=self.dev["m"], v=self.dev["v"],
+                                 copies=self.dev.get("c"), weight_decay=self.decay, **more)
+
+    def states(self, i):
+        """float32 states of tensor i on the host before the step."""
+        m, v = self.host["m"][i].numpy(), self.host["v"][i].numpy()
+        if self.state == "f32":
+            return m, v
+        return _unpack(m, self.host_scales["m_scale"][i].numpy(), v, self.host_scales["v_scale"][i].numpy())
+
+
+@pytest.mark.parametrize("gap,shift", [(0, 0), (8, 0), (3, 1)])
+@pytest.mark.parametrize("state", ["f32", "8bit"])
+@pytest.mark.parametrize("param,grad,copy,scale,step", [
+    (F32, F32, True, 0.37, 1), (F32, BF16, False, None, 17), (BF16, F32, False, None, 1000), (BF16, BF16, False, 0.5, 3)])
+def test_step(state, param, grad, copy, scale, step, gap, shift):
+    t = Made(state, param, grad, copy, seed=step, gap=gap, shift=shift)
+    lr, b1, b2, eps, seed = 1e-3, 0.9, 0.999, 1e-8, 12345 + step
+    gs = None if scale is None else torch.tensor([scale], device="cuda")
+    ad.adamw(t.opt, lr, step, beta1=b1, beta2=b2, eps=eps, seed=seed, grad_scale=gs)
+    f = np.float32
+    for i, n in enumerate(t.sizes):
+        if not n:
+            continue
+        m0, v0 = t.states(i)
+        g32 = t.host["g"][i].float().numpy() * f(1.0 if scale is None else scale)
+        m = m0 * f(b1) + g32 * f(1 - b1)
+        v = v0 * f(b2) + (g32 * g32) * f(1 - b2)
+        # in 64 bits, from the states before the step
+        G = t.host["g"][i].double().numpy() * float(f(1.0 if scale is None else scale))
+        M, V = b1 * m0.astype(float) + (1 - b1) * G, b2 * v0.astype(float) + (1 - b2) * G * G
+        P0 = t.host["p"][i].double().numpy()
+        move = lr / (1 - b1 ** step) * M / (np.sqrt(V / (1 - b2 ** step)) + eps)
+        P = P0 * (1 - lr * t.decay[i]) - move
+        # m may come from terms that cancel: their magnitudes bound its error
+        lost = lr / (1 - b1 ** step) * (np.abs(b1 * m0) + (1 - b1) * np.abs(G)) / (np.sqrt(V / (1 - b2 ** step)) + eps)
+        tol = 16 * U * lost + 3 * U * (np.abs(P0) + np.abs(P))
+        p = t.dev["p"][i].double().cpu().numpy()
+        if param == F32:
+            assert (np.abs(p - P) <= tol).all(), (i, n, np.abs(p - P).max())
+            if copy:
+                assert torch.equal(t.dev["c"][i].cpu(), t.dev["p"][i].cpu().to(BF16))
+        else:       # one of the two neighbours, and the bits of the rule for nearly all
+            step_of = 2.0 ** (np.floor(np.log2(np.maximum(np.abs(P), 1e-30))) - 7)
+            assert (np.abs(p - P) < step_of + tol).all()
+            more = _mix(_bits(n, seed, step, i) + GOLDEN) & np.uint32(0xffff)
+            want = ((P.astype(f).view(np.uint32) + more) & np.uint32(0xffff0000)).view(f)
+            sure = np.abs(((P.astype(f).view(np.uint32) + more) & np.uint32(0xffff)).astype(int) - 32768) < 32768 - 64
+            assert (p == want)[sure].all()
+        if state == "f32":
+            np.testing.assert_array_equal(t.dev["m"][i].cpu().numpy(), m)
+            np.testing.assert_array_equal(t.dev["v"][i].cpu().numpy(), v)
+        else:
+            qm, ms, qv, vs = _pack(m, v, _bits(n, seed, step, i))
+            np.testing.assert_array_equal(t.dev_scales["m_scale"][i].cpu().numpy(), ms)
+            np.testing.assert_array_equal(t.dev_scales["v_scale"][i].cpu().numpy(), vs)
+            np.testing.assert_array_equal(t.dev["m"][i].cpu().numpy(), qm)
+            np.testing.assert_array_equal(t.dev["v"][i].cpu().numpy(), qv)
+    # nothing between the tensors was written
+    if gap or shift:
+        for k, x in t.gpu.items():
+            inside = torch.zeros(len(x), dtype=torch.bool)
+            for part in _cut(inside[shift:], t.sizes, gap):
+                part.fill_(True)
+            assert torch.equal(x.cpu()[~inside], t.flat[k][~inside]), k
+
+
+@pytest.mark.parametrize("state", ["f32", "8bit"])
+def test_state_values(state):
+    t = Made(state, F32, F32, False, seed=4, gap=3, shift=1)
+    n = sum(t.sizes)
+    m, v = torch.full((n + 8,), -77.0, device="cuda"), torch.full((n + 8,), -77.0, device="cuda")
+    ad.opt_state(t.opt, m[:n], v[:n])
+    at = 0
+    for i, z in enumerate(t.sizes):
+        wm, wv = t.states(i)
+        np.testing.assert_array_equal(m[at:at + z].cpu().numpy(), wm)
+        np.testing.assert_array_equal(v[at:at + z].cpu().numpy(), wv)
+        at += z
+    assert bool((m[n:] == -77).all()) and bool((v[n:] == -77).all())
+    ad.opt_state(t.opt, None, v[:n])
+    ad.opt_state(t.opt, m[:n], None)
+
+
+def test_8bit_states_keep_the_mean():
+    """An average that decays by a thousandth a step moves in codes on the mean: 400 steps of equal
+    gradients and then none, against the float32 state.  Each code is off by at most one spacing s of its value's
+    neighbourhood a step, independently: the mean over n elements of what K steps add is within 5 s sqrt(K / n)."""
+    n, K = 65536, 400
+    g = torch.randn(n, generator=_gen(6)).cuda() * 1e-3
+    z = lambda dt: torch.zeros(n, dtype=dt, device="cuda")  # noqa: E731
+    p8, p32, m32, v32 = z(F32), z(F32), z(F32), z(F32)
+    q = dict(m=[z(torch.int8)], v=[z(torch.uint8)], m_scale=[torch.zeros(n // 128, device="cuda")],
+             v_scale=[torch.zeros(n // 128, device="cuda")])
+    o8 = ad.OptTensors(params=[p8], grads=[g], **q)
+    o32 = ad.OptTensors(params=[p32], grads=[g], m=[m32], v=[v32])
+    for t in range(1, K + 1):
+        if t == K // 2:
+            g.zero_()
+        ad.adamw(o8, 1e-3, t, seed=77)
+        ad.adamw(o32, 1e-3, t)
+    m, v = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+    ad.opt_state(o8, m, v)
+    # values whose code is at least 16: rounding up to code 1 has no part in them
+    big = v32 > (32.0 / 255) ** 2 * v32.view(-1, 128).amax(1).repeat_interleave(128)
+    spacing = float((2 * v32.sqrt() / 255 * v32.view(-1, 128).amax(1).sqrt().repeat_interleave(128))[big].max())
+    assert abs(float((v - v32)[big].double().mean())) <= 5 * spacing * math.sqrt(K / int(big.sum()))
+    assert float(v[big].double().sum() / v32[big].double().sum()) == pytest.approx(1.0, abs=0.02)
+
+
+def test_groups_that_are_not_finite_or_tiny():
+    n = 128 * 5 + 20
+    g = torch.randn(n, generator=_gen(8)) * 1e-2
+    g[130], g[300], g[128 * 3:128 * 4] = math.nan, math.inf, 0.0
+    g[128 * 4:128 * 5] *= 1e-25          # m about 1e-28, over 2^-100 = 8e-31; v about 1e-57, under it
+    x = dict(params=[torch.zeros(n).cuda()], grads=[g.cuda()], m=[torch.zeros(n, dtype=torch.int8).cuda()],
+             v=[torch.zeros(n, dtype=torch.uint8).cuda()], m_scale=[torch.zeros(6).cuda()], v_scale=[torch.zeros(6).cuda()])
+    opt = ad.OptTensors(**x)
+    ad.adamw(opt, 1e-3, 1)
+    m, v = torch.empty(n).cuda(), torch.empty(n).cuda()
+    ad.opt_state(opt, m, v)
+    for y in (m.cpu(), v.cpu()):
+        bad = torch.isnan(y)
+        assert bool(bad[128:384].all()) and not bool(bad[:128].any()) and not bool(bad[384:].any())
+        assert not bool(y[384:512].any()) and bool(y[640:].any())
+    assert bool(m[512:640].any()) and not bool(v[512:640].any())
+    g2 = torch.full((128,), 1e-31, device="cuda")            # m = 1e-32
+    opt = ad.OptTensors(params=[torch.zeros(128).cuda()], grads=[g2], m=[torch.ones(128, dtype=torch.int8).cuda()],
+                        v=[torch.ones(128, dtype=torch.uint8).cuda()], m_scale=[torch.zeros(1).cuda()],
+                        v_scale=[torch.zeros(1).cuda()])
+    ad.adamw(opt, 1e-3, 1)
+    assert not bool(opt.tensors["m"][0].any()) and not bool(opt.tensors["v"][0].any())
+    assert not bool(opt.tensors["m_scale"][0].any())
+    p = x["params"][0].cpu()
+    assert bool(torch.isnan(p[130])) and int(torch.isnan(p).sum()) <= 2 and not bool(p[384:512].any())
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_a_scale_that_is_not_finite_leaves_everything(bad):
+    t = Made("8bit", F32, F32, True, seed=9)
+    ad.adamw(t.opt, 1e-3, 5, grad_scale=torch.tensor([bad], device="cuda"))
+    for k, x in t.gpu.items():
+        assert torch.equal(x.cpu(), t.flat[k])
+    for k, x in t.gpu_scales.items():
+        assert torch.equal(x.cpu(), t.scales[k])
+
+
+@pytest.mark.parametrize("state", ["f32", "8bit"])
+def test_step_and_rate_on_the_device(state):
+    """The same bits from numbers in device memory: the scalars are computed in 64 bits on both sides."""
+    a, b = Made(state, F32, F32, True, seed=10), Made(state, F32, F32, True, seed=10)
+    lr = float(np.float32(3e-4))
+    ad.adamw(a.opt, lr, 1234, seed=5)
+    ad.adamw(b.opt, torch.tensor([lr], device="cuda"), torch.tensor([1234], dtype=torch.int32, device="cuda"), seed=5)
+    for k in a.gpu:
+        x, y = a.gpu[k].double().cpu(), b.gpu[k].double().cpu()
+        if k == "p":      # 1 - lr decay: the decay is float32 there
+            assert bool(((x - y).abs() <= 8 * U * x.abs() + 1e-9 * U).all())
+        elif k != "c":
+            assert torch.equal(x, y), k
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("max_norm", [0.0, 1e-3, 1e9])
+def test_grad_norm(dtype, max_norm):
+    g = [(torch.randn(n, generator=_gen(n)) * 0.1).to(dtype) for n in SIZES]
+    opt = ad.OptTensors(grads=[x.cuda() for x in g])
+    ws = torch.empty(ad.grad_norm_workspace_size(opt), dtype=torch.uint8, device="cuda")
+    out, step = torch.full((2,), -1.0, device="cuda"), torch.tensor([41], dtype=torch.int32, device="cuda")
+    ad.grad_norm(opt, max_norm, out, ws, step=step)
+    want = math.sqrt(sum(float(x.double().square().sum()) for x in g))
+    assert abs(float(out[0]) - want) <= 2 * U * want
+    scale = 1.0 if max_norm == 0.0 else min(1.0, max_norm / want)
+    assert abs(float(out[1]) - scale) <= 2 * U * scale and int(step) == 42
+
+
+def test_grad_norm_range_and_what_is_not_finite():
+    def norm(x, max_norm=1.0):
+        opt = ad.OptTensors(grads=[x.cuda()])
+        ws = torch.empty(ad.grad_norm_workspace_size(opt), dtype=torch.uint8, device="cuda")
+        out, step = torch.empty(2, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+        ad.grad_norm(opt, max_norm, out, ws, step=step)
+        return float(out[0]), float(out[1]), int(step)
+
+    assert norm(torch.full((4,), 1e30))[0] == pytest.approx(2e30, rel=1e-6)        # squares past float32's range
+    assert norm(torch.full((4,), 1e-30))[0] == pytest.approx(2e-30, rel=1e-6)
+    assert norm(torch.zeros(5)) == (0.0, 1.0, 1)
+    assert norm(torch.zeros(0)) == (0.0, 1.0, 1)
+    for bad in (math.nan, math.inf, -math.inf):
+        x = torch.ones(3000)
+        x[2999] = bad
+        n, s, step = norm(x)
+        assert not math.isfinite(n) and math.isnan(s) and step == 0
+    n, s, step = norm(torch.full((4,), 3e38))                                       # finite, but its float32 is not
+    assert n == math.inf and math.isnan(s) and step == 0
+
+
+def test_more_tensors_than_a_launch_holds():
+    n = 100
+    g = [torch.full((5 + i,), float(i)) for i in range(n)]
+    x = dict(params=[torch.zeros(5 + i).cuda() for i in range(n)], grads=[y.cuda() for y in g],
+             m=[torch.zeros(5 + i).cuda() for i in range(n)], v=[torch.zeros(5 + i).cuda() for i in range(n)])
+    opt = ad.OptTensors(**x, weight_decay=0.1)
+    ws = torch.empty(ad.grad_norm_workspace_size(opt), dtype=torch.uint8, device="cuda")
+    out = torch.empty(2, device="cuda")
+    ad.grad_norm(opt, 0.0, out, ws)
+    want = math.sqrt(sum((5 + i) * i * i for i in range(n)))
+    assert abs(float(out[0]) - want) <= 2 * U * want
+    ad.adamw(opt, 1e-2, 1)
+    for i in range(n):          # the first step moves by the rate
+        assert float((x["params"][i] + (1e-2 if i else 0.0)).abs().max()) <= 1e-7
+        assert bool((x["m"][i] == torch.tensor(float(i)) * torch.tensor(1 - 0.9)).all())
+    total = sum(5 + i for i in range(n))
+    m = torch.empty(total, device="cuda")
+    ad.opt_state(opt, m, None)
+    assert torch.equal(m, torch.cat(x["m"]))

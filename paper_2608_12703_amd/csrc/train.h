@@ -316,11 +316,10 @@ void launch_linear(int kind, LinArgs a, hipStream_t st);
 
 // ----------------------------------------------------------------- attention
 
-// A strided bf16 matrix; vec: rows of 8 elements at a multiple of 8 are 16-byte aligned.
+// A strided bf16 matrix, of any alignment.
 struct HMat {
   uint16_t* p;
   int64_t ld;
-  int vec;
 };
 
 // What both passes know of a batch (ad_attn).

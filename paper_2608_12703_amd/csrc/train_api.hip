@@ -152,7 +152,6 @@ ad::HMat hmat(const ad_mat* m) {
   if (!m) return d;
   d.p = (uint16_t*)m->data;
   d.ld = m->ld;
-  d.vec = (uintptr_t)m->data % 16 == 0 && m->ld % 8 == 0;
   return d;
 }
 

@@ -213,6 +213,35 @@ struct Stage {
   }
 };
 
+// A wave's transposed 64 x 32 result (columns l.n) as rows: out(row, c, v) with columns 8 c .. + 7 of row, eight lanes a
+// row, so that memory is accessed in whole rows.  buf: 8 KB of the wave's own; a row's 16-byte pieces p are at p ^ (row % 16).
+template <class F>
+__device__ __forceinline__ void by_rows(char* buf, const Lane& l, const f32x16 (&v)[2], F&& out) {
+#pragma unroll
+  for (int d = 0; d < 2; ++d)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      *(f32x4*)(buf + l.n * 256 + (((8 * d + 2 * e + l.h) ^ (l.n & 15)) << 4)) =
+          f32x4{v[d][4 * e], v[d][4 * e + 1], v[d][4 * e + 2], v[d][4 * e + 3]};
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int row = 8 * j + threadIdx.x % kWave / 8, c = threadIdx.x % 8;
+    const f32x4 x = *(const f32x4*)(buf + row * 256 + (((2 * c) ^ (row & 15)) << 4));
+    const f32x4 y = *(const f32x4*)(buf + row * 256 + (((2 * c + 1) ^ (row & 15)) << 4));
+    const float r[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+    out(row, c, r);
+  }
+}
+__device__ __forceinline__ uint4 narrow8(const float (&v)[8]) {
+  return make_uint4(f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]), f32x2_to_bf16x2(v[4], v[5]),
+                    f32x2_to_bf16x2(v[6], v[7]));
+}
+// columns 8 c .. + 7 of head h of a row
+__device__ __forceinline__ void store_piece(const HMat& m, int64_t row, int h, int c, uint4 u) {
+  __builtin_memcpy(m.p + row * m.ld + 64 * h + 8 * c, &u, 16);
+}
+
 // The tiles of one (sequence, head) follow each other on one of the eight XCDs, whose L2 then has its
 // keys: workgroup id i runs on XCD i % 8.
 struct Place {
@@ -264,7 +293,7 @@ __device__ __forceinline__ Range range_of(const Keys& k, bool in) {
 constexpr float kLazy = 8.f;
 
 template <int QW>
-__global__ void __launch_bounds__(256) attn_fwd_kernel(AttnFwdArgs a, int tiles, int splits, int chunk) {
+__global__ void __launch_bounds__(256, 2) attn_fwd_kernel(AttnFwdArgs a, int tiles, int splits, int chunk) {
   constexpr int TK = QW == 4 ? 64 : 128, NB = QW == 4 ? 2 : 1, kTileBytes = TK * kRowBytes;
   __shared__ __attribute__((aligned(16))) char lds[4 * kTileBytes];   // two stages of keys and values
   __shared__ int ends[8];
@@ -388,8 +417,6 @@ __global__ void __launch_bounds__(256) attn_fwd_kernel(AttnFwdArgs a, int tiles,
   sum += other_half(sum);
 
   if constexpr (QW == 4) {
-    // out through LDS, a row's 64 columns side by side; rows 136 bytes apart: columns of 32 rows in
-    // different banks
     const float inv = sum == 0.f || !in ? 0.f : 1.f / sum;
     bool bad = false;
 #pragma unroll
@@ -398,32 +425,19 @@ __global__ void __launch_bounds__(256) attn_fwd_kernel(AttnFwdArgs a, int tiles,
       for (int e = 0; e < 16; ++e) {
         o[d][e] = inv == 0.f && sum == 0.f ? 0.f : o[d][e] * inv;
         bad |= !(fabsf(o[d][e]) < INFINITY);
+        o[d][e] = in ? o[d][e] : 0.f;
       }
-    char* buf = lds + w * 32 * 136;
-    const auto put = [&](const HMat& m, bool rest) {
+    by_rows(lds + w * 32 * 256, l, o, [&](int row, int c, const float(&v)[8]) {
+      if (q0 + row >= s.oq) return;
+      const uint4 u = narrow8(v);
+      store_piece(a.o, s.q0 + (int64_t)(q0 + row), h, c, u);
+      if (!a.rest.p) return;
+      const uint32_t hi[4] = {u.x, u.y, u.z, u.w};
+      float low[8];
 #pragma unroll
-      for (int d = 0; d < 2; ++d)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float v[4];
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            v[c] = in ? o[d][4 * e + c] : 0.f;
-            if (rest) v[c] -= bf16_to_f32(f32_to_bf16(v[c]));
-          }
-          *(uint2*)(buf + l.n * 136 + 64 * d + 16 * e + 8 * l.h) = make_uint2(f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]));
-        }
-      __builtin_amdgcn_wave_barrier();
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int row = 8 * j + threadIdx.x % kWave / 8, c = threadIdx.x % 8;
-        uint2 u[2] = {*(const uint2*)(buf + row * 136 + 16 * c), *(const uint2*)(buf + row * 136 + 16 * c + 8)};
-        if (q0 + row < s.oq) __builtin_memcpy(m.p + (s.q0 + (int64_t)(q0 + row)) * m.ld + 64 * h + 8 * c, u, 16);
-      }
-      __builtin_amdgcn_wave_barrier();
-    };
-    put(a.o, false);
-    if (a.rest.p) put(a.rest, true);
+      for (int e = 0; e < 8; ++e) low[e] = v[e] - bf16_to_f32((uint16_t)(hi[e / 2] >> (16 * (e % 2))));
+      store_piece(a.rest, s.q0 + (int64_t)(q0 + row), h, c, narrow8(low));
+    });
     if (a.lse && l.h == 0 && i < s.oq)
       a.lse[(size_t)h * a.b.q_rows + s.q0 + i] = sum == 0.f || !in ? -INFINITY : (m + __log2f(sum)) * kLn2;
     // what is not finite may come from keys that this row does not see
@@ -524,22 +538,373 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnFwdArgs a, int tiles
   if (a.lse && d == 0) a.lse[at] = total == 0.f ? -INFINITY : (top + __log2f(total)) * kLn2;
 }
 
-__global__ void __launch_bounds__(256) attn_dq_rows_kernel(AttnBwdArgs a, int tiles) {
-  const int tile = blockIdx.x % tiles, h = blockIdx.x / tiles % a.b.heads, b = blockIdx.x / tiles / a.b.heads;
-  const Span s = span_of(a.b, b);
+// ----------------------------------------------------------------- backward
+
+// dq.  As the forward kernel, with p from lse and two products more: dP^T = V dO^T and, from dS, dQ^T =
+// K^T dS^T.  It leaves delta and what 32 queries see together for the second kernel.
+template <int QW>
+__global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnBwdArgs a, int tiles) {
+  constexpr int TK = QW == 4 ? 64 : 128, NB = QW == 4 ? 2 : 1, kTileBytes = TK * kRowBytes;
+  __shared__ __attribute__((aligned(16))) char lds[4 * kTileBytes];
+  __shared__ int ends[8];
+  const Place at = place_of(tiles, a.b.heads, a.b.batch, a.b.causal);
+  if (!at.in) return;
+  const int h = at.h;
+  const Span s = span_of(a.b, at.b);
   if (!s.ok) {
     if (threadIdx.x == 0) atomicOr(a.b.err, AD_ERR_LENGTH);
     return;
   }
-  const int i = tile * 4 + threadIdx.x / kWave;
-  if (i < s.oq) dq_row(a, s, h, i);
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), g = h / (a.b.heads / a.b.kv_heads);
+  const Lane l(threadIdx.x % kWave);
+  const int q0 = at.tile * 32 * QW + (QW == 4 ? 32 * w : 0), i = q0 + l.n;
+  if (at.tile * 32 * QW >= s.oq) return;
+  const bool in = i < s.nq;
+  const int64_t row = s.q0 + (int64_t)i;
+  const size_t stat = (size_t)h * a.b.q_rows + row;
+
+  bf16x8 q[4], go[4];
+  float delta = 0.f, lse = 0.f;
+  Keys keys = {0, s.nk};
+  if (in) {
+    keys = keys_of(a.b, s, i);
+    lse = a.lse[stat] * kLog2e;
+    if (lse == -INFINITY) keys.hi = keys.lo;
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    uint4 uq = make_uint4(0, 0, 0, 0), ud = uq, uo = uq, ur = uq;
+    if (in) {
+      const int c = 64 * h + 16 * k + 8 * l.h;
+      uq = load16(a.q.p + row * a.q.ld + c);
+      ud = load16(a.dout.p + row * a.dout.ld + c);
+      uo = load16(a.o.p + row * a.o.ld + c);
+      if (a.rest.p) ur = load16(a.rest.p + row * a.rest.ld + c);
+    }
+    q[k] = as_bf16x8(uq);
+    go[k] = as_bf16x8(ud);
+    float d[8], o[8], r[8];
+    widen8(__builtin_bit_cast(u32x4, ud), d);
+    widen8(__builtin_bit_cast(u32x4, uo), o);
+    widen8(__builtin_bit_cast(u32x4, ur), r);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) delta = fmaf(d[e], o[e] + r[e], delta);
+  }
+  delta += other_half(delta);
+  const Range r = range_of(keys, in);
+  if (QW == 4 || w == 0) {
+    if (in && l.h == 0) a.delta[stat] = delta;
+    if (h == 0 && threadIdx.x % kWave == 0 && q0 < s.nq)
+      a.ranges[(size_t)at.b * a.blocks + q0 / 32] = make_int4(r.lo, r.hi, r.all_lo, r.all_hi);
+  }
+
+  int first = r.lo, last = r.hi;
+  if (QW == 4) {
+    if (threadIdx.x % kWave == 0) {
+      ends[w] = r.lo;
+      ends[4 + w] = r.hi;
+    }
+    __syncthreads();
+    first = min(min(ends[0], ends[1]), min(ends[2], ends[3]));
+    last = max(max(ends[4], ends[5]), max(ends[6], ends[7]));
+  }
+  first = first / TK * TK;
+
+  f32x16 dq[2] = {zeros(), zeros()};
+  Stage<TK> ks, vs;
+  if (first < last) {
+    ks.load(a.k, s.k0, s.nk, 64 * g, first);
+    vs.load(a.v, s.k0, s.nk, 64 * g, first);
+    ks.store(lds);
+    vs.store(lds + kTileBytes);
+  }
+  __syncthreads();
+  for (int k0 = first, buf = 0; k0 < last; k0 += TK, buf ^= 2 * kTileBytes) {
+    const bool more = k0 + TK < last;
+    if (more) {
+      ks.load(a.k, s.k0, s.nk, 64 * g, k0 + TK);
+      vs.load(a.v, s.k0, s.nk, 64 * g, k0 + TK);
+    }
+    const int mine = QW == 4 ? k0 : k0 + 32 * w;
+    if (mine < r.hi && mine + 32 * NB > r.lo) {
+      const char* kt = lds + buf + (QW == 4 ? 0 : w * 32 * kRowBytes);
+      const char* vt = kt + kTileBytes;
+      const bool cut = mine < r.all_lo || mine + 32 * NB > r.all_hi;
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+        f32x16 x = zeros(), y = zeros();
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x = mfma32(read_rows(kt, l, n, k), q[k], x);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) y = mfma32(read_rows(vt, l, n, k), go[k], y);
+        if (cut) {
+          const int lo = keys.lo - mine - 4 * l.h;
+          const unsigned len = max(keys.hi - keys.lo, 0);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const bool seen = (unsigned)(32 * n + 8 * (e / 4) + e % 4 - lo) < len;
+            x[e] = seen ? x[e] : -INFINITY;
+            y[e] = seen ? y[e] : 0.f;
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] = __builtin_amdgcn_exp2f(fmaf(x[e], kScale2, -lse)) * (y[e] - delta);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const bf16x8 ds = narrow(x, 8 * c);
+#pragma unroll
+          for (int d = 0; d < 2; ++d) dq[d] = mfma32(read_cols(kt, l, d, 2 * n + c), ds, dq[d]);
+        }
+      }
+    }
+    if (more) {
+      ks.store(lds + (buf ^ (2 * kTileBytes)));
+      vs.store(lds + (buf ^ (2 * kTileBytes)) + kTileBytes);
+    }
+    __syncthreads();
+  }
+
+  if constexpr (QW == 1) {
+    // the other waves' sums to the first one, which goes on alone
+    float* part = (float*)lds;
+    if (w > 0)
+#pragma unroll
+      for (int d = 0; d < 2; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) part[((w - 1) * 32 + 16 * d + e) * 64 + threadIdx.x % kWave] = dq[d][e];
+    __syncthreads();
+    if (w > 0) return;
+#pragma unroll
+    for (int d = 0; d < 2; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+#pragma unroll
+        for (int u = 0; u < 3; ++u) dq[d][e] += part[(u * 32 + 16 * d + e) * 64 + threadIdx.x];
+  }
+  bool bad = false;
+#pragma unroll
+  for (int d = 0; d < 2; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      dq[d][e] = in ? dq[d][e] * kScale : 0.f;
+      bad |= !(fabsf(dq[d][e]) < INFINITY);
+    }
+  by_rows(lds + (QW == 1 ? 0 : w * 32 * 256), l, dq, [&](int n, int c, const float(&v)[8]) {
+    if (q0 + n >= s.oq) return;
+    const int64_t to = s.q0 + (int64_t)(q0 + n);
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = v[e];
+    if (a.res.p && q0 + n < s.nq) {
+      float more[8];
+      load8(a.res, to, 64 * h + 8 * c, 64 * a.b.heads, more);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] += more[e];
+    }
+    store_piece(a.dq, to, h, c, narrow8(x));
+  });
+  // what is not finite may come from keys that the row does not see
+  uint64_t again = __ballot(bad);
+  again = (again | again >> 32) & 0xffffffffu;
+  if (again) __threadfence_block();
+  for (; again; again &= again - 1) dq_row(a, s, h, q0 + __builtin_ctzll(again));
 }
-__global__ void __launch_bounds__(256) attn_dkv_rows_kernel(AttnBwdArgs a, int tiles) {
-  const int tile = blockIdx.x % tiles, g = blockIdx.x / tiles % a.b.kv_heads, b = blockIdx.x / tiles / a.b.kv_heads;
-  const Span s = span_of(a.b, b);
-  if (!s.ok) return;
-  const int j = tile * 4 + threadIdx.x / kWave;
-  if (j < s.ok_) dkv_row(a, s, g, j);
+
+// dk and dv: the same with the queries on the rows (S = Q K^T), a wave 32 keys and all of the queries that
+// see them, of every head that shares them.  KW waves of 32 keys each share tiles of 64 queries, or four
+// waves take a quarter of the queries each.
+template <int KW>
+__global__ void __launch_bounds__(256, 2) attn_dkv_kernel(AttnBwdArgs a, int tiles) {
+  constexpr int TQ = KW == 4 ? 64 : 128, NB = KW == 4 ? 2 : 1, kTileBytes = TQ * kRowBytes;
+  constexpr int kStatBytes = 4 * TQ * 4, kStageBytes = 2 * kTileBytes + kStatBytes;
+  __shared__ __attribute__((aligned(16))) char lds[2 * kStageBytes];
+  const Place at = place_of(tiles, a.b.kv_heads, a.b.batch, false);
+  if (!at.in) return;
+  const int g = at.h;
+  const Span s = span_of(a.b, at.b);
+  if (!s.ok) {
+    if (threadIdx.x == 0) atomicOr(a.b.err, AD_ERR_LENGTH);
+    return;
+  }
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const Lane l(threadIdx.x % kWave);
+  const int j0 = at.tile * 32 * KW + (KW == 4 ? 32 * w : 0), j = j0 + l.n;
+  if (at.tile * 32 * KW >= s.ok_) return;
+  const bool in = j < s.nk;
+  bf16x8 k[4], v[4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    uint4 uk = make_uint4(0, 0, 0, 0), uv = uk;
+    if (in) {
+      const int64_t row = s.k0 + (int64_t)j;
+      uk = load16(a.k.p + row * a.k.ld + 64 * g + 16 * c + 8 * l.h);
+      uv = load16(a.v.p + row * a.v.ld + 64 * g + 16 * c + 8 * l.h);
+    }
+    k[c] = as_bf16x8(uk);
+    v[c] = as_bf16x8(uv);
+  }
+  const int group = a.b.heads / a.b.kv_heads, blocks = (s.nq + TQ - 1) / TQ;
+  const int tile0 = at.tile * 32 * KW, tile1 = min(tile0 + 32 * KW, s.nk);     // the workgroup's keys
+  const int4* ranges = a.ranges + (size_t)at.b * a.blocks;
+
+  // steps: TQ queries of one head, those that some key of the workgroup is seen by
+  const auto wanted = [&](int t) {
+    for (int u = t * (TQ / 32); u < min((t + 1) * (TQ / 32), (s.nq + 31) / 32); ++u) {
+      const int4 r = ranges[u];
+      if (r.x < tile1 && r.y > tile0) return true;
+    }
+    return false;
+  };
+  // (causal: the queries before i see none of the keys from i + nk - nq + 1 on)
+  const int start = a.b.causal ? min(max(tile0 - (s.nk - s.nq), 0) / TQ, blocks) : 0;
+  int t = start, hq = g * group;
+  const auto settle = [&] {
+    while (hq < (g + 1) * group) {
+      while (t < blocks && !wanted(t)) ++t;
+      if (t < blocks) return true;
+      t = start;
+      ++hq;
+    }
+    return false;
+  };
+
+  Stage<TQ> qs, gs;
+  float st_lse, st_delta;
+  int st_lo, st_hi;
+  const auto load = [&] {
+    qs.load(a.q, s.q0, s.nq, 64 * hq, t * TQ);
+    gs.load(a.dout, s.q0, s.nq, 64 * hq, t * TQ);
+    st_lse = st_delta = 0.f;
+    st_lo = st_hi = 0;
+    const int i = t * TQ + (int)threadIdx.x;
+    if (threadIdx.x < TQ && i < s.nq) {
+      const size_t stat = (size_t)hq * a.b.q_rows + s.q0 + i;
+      st_lse = a.lse[stat] * kLog2e;
+      st_delta = a.delta[stat];
+      const Keys r = keys_of(a.b, s, i);
+      st_lo = r.lo;
+      st_hi = st_lse == -INFINITY ? r.lo : max(r.hi, r.lo);
+      if (st_lse == -INFINITY) st_lse = 0.f;
+    }
+  };
+  const auto store = [&](char* to) {
+    qs.store(to);
+    gs.store(to + kTileBytes);
+    if (threadIdx.x < TQ) {
+      float* f = (float*)(to + 2 * kTileBytes) + threadIdx.x;
+      f[0] = st_lse;
+      f[TQ] = st_delta;
+      ((int*)f)[2 * TQ] = st_lo;
+      ((int*)f)[3 * TQ] = st_hi;
+    }
+  };
+
+  f32x16 dk[2] = {zeros(), zeros()}, dv[2] = {zeros(), zeros()};
+  bool some = settle();
+  if (some) {
+    load();
+    store(lds);
+  }
+  __syncthreads();
+  for (int buf = 0; some; buf ^= kStageBytes) {
+    const int now = t;
+    ++t;
+    some = settle();
+    if (some) load();
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+      const int u = KW == 4 ? n : w, block = now * (TQ / 32) + u;
+      if (block * 32 >= s.nq) continue;
+      const int4 r = ranges[block];
+      if (r.x >= j0 + 32 || r.y <= j0) continue;
+      const char* qt = lds + buf + u * 32 * kRowBytes;
+      const char* gt = qt + kTileBytes;
+      const float* stat = (const float*)(lds + buf + 2 * kTileBytes) + 32 * u + 4 * l.h;
+      f32x16 x = zeros(), y = zeros();
+#pragma unroll
+      for (int c = 0; c < 4; ++c) x = mfma32(read_rows(qt, l, 0, c), k[c], x);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) y = mfma32(read_rows(gt, l, 0, c), v[c], y);
+      if (j0 < r.z || min(j0 + 32, s.nk) > r.w) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int4 lo = *(const int4*)(stat + 2 * TQ + 8 * e), hi = *(const int4*)(stat + 3 * TQ + 8 * e);
+          const int los[4] = {lo.x, lo.y, lo.z, lo.w}, his[4] = {hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const bool seen = j >= los[c] && j < his[c];
+            x[4 * e + c] = seen ? x[4 * e + c] : -INFINITY;
+            y[4 * e + c] = seen ? y[4 * e + c] : 0.f;
+          }
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const f32x4 lse = *(const f32x4*)(stat + 8 * e), delta = *(const f32x4*)(stat + TQ + 8 * e);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          x[4 * e + c] = __builtin_amdgcn_exp2f(fmaf(x[4 * e + c], kScale2, -lse[c]));
+          y[4 * e + c] = x[4 * e + c] * (y[4 * e + c] - delta[c]);
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const bf16x8 p = narrow(x, 8 * c), ds = narrow(y, 8 * c);
+#pragma unroll
+        for (int d = 0; d < 2; ++d) {
+          dv[d] = mfma32(read_cols(gt, l, d, c), p, dv[d]);
+          dk[d] = mfma32(read_cols(qt, l, d, c), ds, dk[d]);
+        }
+      }
+    }
+    if (some) store(lds + (buf ^ kStageBytes));
+    __syncthreads();
+  }
+
+  if constexpr (KW == 1) {
+    float* part = (float*)lds;
+    // (dk and dv of three waves are 48 KB)
+    if (w > 0)
+#pragma unroll
+      for (int d = 0; d < 2; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          part[((w - 1) * 64 + 16 * d + e) * 64 + threadIdx.x % kWave] = dk[d][e];
+          part[((w - 1) * 64 + 32 + 16 * d + e) * 64 + threadIdx.x % kWave] = dv[d][e];
+        }
+    __syncthreads();
+    if (w > 0) return;
+#pragma unroll
+    for (int d = 0; d < 2; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+#pragma unroll
+        for (int u = 0; u < 3; ++u) {
+          dk[d][e] += part[(u * 64 + 16 * d + e) * 64 + threadIdx.x];
+          dv[d][e] += part[(u * 64 + 32 + 16 * d + e) * 64 + threadIdx.x];
+        }
+  }
+  bool bad = false;
+#pragma unroll
+  for (int d = 0; d < 2; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      dk[d][e] = in ? dk[d][e] * kScale : 0.f;
+      dv[d][e] = in ? dv[d][e] : 0.f;
+      bad |= !(fabsf(dk[d][e]) < INFINITY) || !(fabsf(dv[d][e]) < INFINITY);
+    }
+  char* mine = lds + (KW == 1 ? 0 : w * 32 * 256);
+  by_rows(mine, l, dk, [&](int n, int c, const float(&x)[8]) {
+    if (j0 + n < s.ok_) store_piece(a.dk, s.k0 + (int64_t)(j0 + n), g, c, narrow8(x));
+  });
+  __builtin_amdgcn_wave_barrier();
+  by_rows(mine, l, dv, [&](int n, int c, const float(&x)[8]) {
+    if (j0 + n < s.ok_) store_piece(a.dv, s.k0 + (int64_t)(j0 + n), g, c, narrow8(x));
+  });
+  uint64_t again = __ballot(bad);
+  again = (again | again >> 32) & 0xffffffffu;
+  if (again) __threadfence_block();
+  for (; again; again &= again - 1) dkv_row(a, s, g, j0 + __builtin_ctzll(again));
 }
 
 }  // namespace
@@ -570,9 +935,15 @@ size_t attn_fwd_bytes(const AttnBatch& b) {
   const FwdPlan p = fwd_plan(b);
   return p.splits > 1 ? 4ull * 66 * p.splits * b.heads * b.q_rows : 0;
 }
-size_t attn_bwd_bytes(const AttnBatch& b) { return 4ull * b.heads * b.q_rows; }
+// delta [heads][q_rows], then what 32 queries of a sequence see together [batch][blocks]
+size_t attn_bwd_delta_bytes(const AttnBatch& b) { return (4ull * b.heads * b.q_rows + 255) / 256 * 256; }
+size_t attn_bwd_bytes(const AttnBatch& b) {
+  return attn_bwd_delta_bytes(b) + 16ull * b.batch * ((b.q_max + 31) / 32);
+}
 int64_t attn_groups(const AttnBatch& b) {
-  return std::max((int64_t)((b.q_max + 3) / 4) * b.heads, (int64_t)((b.k_max + 3) / 4) * b.kv_heads) * b.batch;
+  const FwdPlan p = fwd_plan(b);
+  return std::max({places(p.tiles, b.heads, b.batch) * p.splits, (int64_t)((b.q_max + 3) / 4) * b.heads * b.batch,
+                   places((b.q_max + 31) / 32, b.heads, b.batch), places((b.k_max + 31) / 32, b.kv_heads, b.batch)});
 }
 
 void launch_attention(const AttnFwdArgs& a, hipStream_t st) {
@@ -587,11 +958,27 @@ void launch_attention(const AttnFwdArgs& a, hipStream_t st) {
   }
 }
 
-void launch_attention_backward(const AttnBwdArgs& a, hipStream_t st) {
-  const int tiles = (a.b.q_max + 3) / 4, grid = tiles * a.b.heads * a.b.batch;
-  if (grid) attn_dq_rows_kernel<<<grid, 256, 0, st>>>(a, tiles);
-  const int ktiles = (a.b.k_max + 3) / 4, kgrid = ktiles * a.b.kv_heads * a.b.batch;
-  if (kgrid) attn_dkv_rows_kernel<<<kgrid, 256, 0, st>>>(a, ktiles);
+void launch_attention_backward(const AttnBwdArgs& args, hipStream_t st) {
+  AttnBwdArgs a = args;
+  const AttnBatch& b = a.b;
+  if (!b.batch) return;
+  a.blocks = (b.q_max + 31) / 32;
+  a.ranges = (int4*)((char*)a.delta + attn_bwd_delta_bytes(b));
+  // a tile a workgroup where that gives every CU two of them, else a quarter
+  const int wide_q = (b.q_max + 127) / 128, wide_k = (b.k_max + 127) / 128;
+  if (b.q_max > 0) {
+    if ((int64_t)wide_q * b.heads * b.batch >= 512 && b.q_max > 32)
+      attn_dq_kernel<4><<<places(wide_q, b.heads, b.batch), 256, 0, st>>>(a, wide_q);
+    else
+      attn_dq_kernel<1><<<places(a.blocks, b.heads, b.batch), 256, 0, st>>>(a, a.blocks);
+  }
+  if (b.k_max > 0) {
+    const int few_k = (b.k_max + 31) / 32;
+    if ((int64_t)wide_k * b.kv_heads * b.batch >= 512 && b.k_max > 32)
+      attn_dkv_kernel<4><<<places(wide_k, b.kv_heads, b.batch), 256, 0, st>>>(a, wide_k);
+    else
+      attn_dkv_kernel<1><<<places(few_k, b.kv_heads, b.batch), 256, 0, st>>>(a, few_k);
+  }
 }
 
 }  // namespace ad

@@ -340,6 +340,9 @@ struct AttnBwdArgs {
   DMat res;                // p NULL: none
   const float* lse;
   float* delta;            // [heads][q_rows]
+  // set by the launcher: of every 32 queries of a sequence, the keys that some and that all of them see
+  int4* ranges;            // [batch][blocks]
+  int blocks;
 };
 size_t attn_fwd_bytes(const AttnBatch& b);
 size_t attn_bwd_bytes(const AttnBatch& b);

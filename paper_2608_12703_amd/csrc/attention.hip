@@ -1,5 +1,6 @@
 // Attention over matrices and its gradients (the draft block's training), 64-wide heads.
 #include <algorithm>
+#include <type_traits>
 
 #include "train.h"
 
@@ -138,9 +139,11 @@ __device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
 
-// Tiles of 64-wide rows in LDS: 128 bytes a row, its 16-byte pieces c at c ^ (row % 8), so that eight rows'
-// same piece lies in different banks.
+// Tiles of 64-wide rows in LDS: 128 bytes a row, 16-byte piece c of row r at c ^ turn(r).  LDS has 64
+// banks of 4 bytes: 16 rows' same piece (16 lanes of a 16-byte read) lie in different banks, and so do four
+// rows' same 64 bytes (32 lanes of a transposing read).  With c ^ (r % 8) a third of LDS' cycles were conflicts.
 constexpr int kRowBytes = 128;
+__device__ __forceinline__ int turn(int r) { return (r << 1 & 4) | (r >> 1 & 2) | (r >> 3 & 1); }
 
 // A lane's place in a tile, as the A operand whose rows are the tile's rows (`row`: piece 2 s + h of row
 // l % 32), and as the one whose rows are the tile's columns (`col`: 16 lanes read 4 rows of 16 columns).
@@ -150,21 +153,21 @@ struct Lane {
   __device__ __forceinline__ explicit Lane(int l) {
     h = l >> 5;
     n = l & 31;
-    row = n * kRowBytes + ((h ^ (n & 7)) << 4);
+    row = n * kRowBytes + ((h ^ turn(n)) << 4);
     const int c16 = l & 15, r = 4 * h + (c16 >> 2), piece = 2 * ((l >> 4) & 1) + ((c16 & 3) >> 1);
-    col = r * kRowBytes + ((piece ^ r) << 4) + (c16 & 1) * 8;
+    col = r * kRowBytes + ((piece ^ turn(r)) << 4) + (c16 & 1) * 8;
   }
 };
 // rows 32 b .. + 31, columns 16 s .. + 15 as the reduction
 __device__ __forceinline__ bf16x8 read_rows(const char* tile, const Lane& l, int b, int s) {
   return as_bf16x8(*(const uint4*)(tile + b * 32 * kRowBytes + (l.row ^ (s * 32))));
 }
-// columns 32 b .. + 31, rows 16 c .. + 15 as the reduction (in the order above)
+// columns 32 b .. + 31, rows 16 c .. + 15 as the reduction (in the order above); 8 rows on, turn() differs by 1
 __device__ __forceinline__ bf16x8 read_cols(const char* tile, const Lane& l, int b, int c) {
   typedef __attribute__((address_space(3))) s16x4* lp;
-  const char* p = tile + c * 16 * kRowBytes + (l.col ^ (b * 64));
-  const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)p);
-  const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(p + 8 * kRowBytes));
+  const char* p = tile + c * 16 * kRowBytes;
+  const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(p + (l.col ^ (b * 64))));
+  const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(p + 8 * kRowBytes + (l.col ^ (b * 64) ^ 16)));
   return __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 // eight values of a lane's column as an operand
@@ -185,33 +188,121 @@ __device__ __forceinline__ f32x16 zeros() {
 }
 
 // 16 bytes of a row, whatever their alignment
-__device__ __forceinline__ uint4 load16(const uint16_t* p) {
+__device__ __forceinline__ uint4 load16(const void* p) {
   uint4 u;
   __builtin_memcpy(&u, p, 16);
   return u;
 }
+// Waits here for what was loaded into these registers, and not where a loop first uses them: there the wait
+// would be for every load in flight, each time round.
+__device__ __forceinline__ void settled(bf16x8 (&v)[4]) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) asm volatile("" : "+v"(v[k]));
+}
 
 // A tile of TR rows on its way from memory to LDS: thread t of 256 takes 16-byte piece t % 8 of rows
-// t / 8 + 32 j.  Rows from n on (counted from the first of the sequence) become zeros.
+// t / 8 + 32 j.  Rows past the sequence's last one become zeros.  A scalar base and a 32-bit offset a lane.
 template <int TR>
 struct Stage {
   static constexpr int N = TR / 32;
   uint4 reg[N];
-  __device__ __forceinline__ void load(const HMat& m, int first, int n, int col, int r0) {
-    const int t = threadIdx.x, r = r0 + t / 8;
-    const uint16_t* p = m.p + (first + (int64_t)r) * m.ld + col + (t % 8) * 8;
+  const char* base;   // the sequence's first row
+  int64_t pitch;      // bytes between rows
+  int n, from;        // the sequence's rows, and the tile's first one
+  __device__ __forceinline__ void init(const HMat& m, int first, int rows, int col) {
+    base = (const char*)(m.p + first * m.ld + col);
+    pitch = 2 * m.ld;
+    n = rows;
+  }
+  __device__ __forceinline__ void load(int r0) {
+    const char* p = base + r0 * pitch;
+    const uint32_t t = threadIdx.x, c = (t % 8) * 16;
+    from = r0;
+    if (r0 + TR <= n) {
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      reg[j] = make_uint4(0, 0, 0, 0);
-      if (r + 32 * j < n) reg[j] = load16(p + (int64_t)(32 * j) * m.ld);
+      for (int j = 0; j < N; ++j) reg[j] = load16(p + (uint32_t)((t / 8 + 32 * j) * (uint32_t)pitch + c));
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        reg[j] = load16(p + (uint32_t)(min((int)t / 8 + 32 * j, n - 1 - r0) * (uint32_t)pitch + c));
     }
   }
-  __device__ __forceinline__ void store(char* tile) const {
+  __device__ __forceinline__ void store(char* tile) {
     const int t = threadIdx.x, r = t / 8;
+    if (from + TR > n)
 #pragma unroll
-    for (int j = 0; j < N; ++j) *(uint4*)(tile + (r + 32 * j) * kRowBytes + (((t % 8) ^ (r & 7)) << 4)) = reg[j];
+      for (int j = 0; j < N; ++j)
+        if (from + r + 32 * j >= n) reg[j] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int j = 0; j < N; ++j) *(uint4*)(tile + (r + 32 * j) * kRowBytes + (((t % 8) ^ turn(r)) << 4)) = reg[j];
   }
 };
+
+// A tile of 64 rows to LDS by four waves, the loads in flight while the tile before is worked on.  DIRECT:
+// straight into LDS through a buffer descriptor, whose end makes zeros of the rows past the sequence's
+// last one (rows 16-byte aligned); a lane's 16 bytes land at its place in the wave's kilobyte, so it
+// loads the piece that belongs there.  Else through registers.
+constexpr uint32_t kBufferFlags = 0x00020000;   // raw buffer of 32-bit elements
+constexpr uint32_t kPastEnd = 0x80000000u;      // further than any offset in a tile: 64 * 2^23 bytes
+
+template <bool DIRECT>
+struct Loads {
+  const char* base;   // the sequence's first row
+  int64_t pitch;      // bytes between rows
+  int n, from;        // the sequence's rows, and the first one of the tile in registers
+  uint32_t off[2];
+  uint4 reg[DIRECT ? 1 : 2];
+  // thread t takes piece t % 8 of rows t / 8 + 8 (t / 64) + 8 j: those of its wave side by side
+  static __device__ __forceinline__ int row(int j) { return (threadIdx.x >> 6) * 16 + j * 8 + (threadIdx.x & 63) / 8; }
+  __device__ __forceinline__ void init(const HMat& m, int first, int rows, int col) {
+    base = (const char*)(m.p + first * m.ld + col);
+    pitch = 2 * m.ld;
+    n = rows;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) off[j] = row(j) * (uint32_t)pitch + (((threadIdx.x % 8) ^ turn(row(j))) << 4);
+  }
+  // (more: bytes further along the row)
+  __device__ __forceinline__ void issue(int r0, uint4* tile, int more = 0) {
+    const char* p = base + r0 * pitch + more;
+    if constexpr (DIRECT) {
+      const int64_t left = r0 < n ? (n - 1 - r0) * pitch + kRowBytes : 0;
+      const auto d = __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, (uint32_t)min(left, (int64_t)kPastEnd), kBufferFlags);
+      const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(d, (__attribute__((address_space(3))) void*)(tile + (2 * w + j) * 64), 16, off[j], 0, 0, 0);
+    } else {
+      from = r0;
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        if (r0 < n) reg[j] = load16(p + off[j] - (uint32_t)max(r0 + row(j) - (n - 1), 0) * (uint32_t)pitch);
+    }
+  }
+  // before the barrier after which the tile is read
+  __device__ __forceinline__ void arrive(uint4* tile) {
+    if constexpr (!DIRECT) {
+      const int w = threadIdx.x / kWave;
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        tile[(2 * w + j) * 64 + threadIdx.x % kWave] = from + row(j) < n ? reg[j] : make_uint4(0, 0, 0, 0);
+    }
+  }
+};
+// Every load of the wave has landed, every LDS access is done; then all waves meet.
+__device__ __forceinline__ void landed() {
+  __builtin_amdgcn_s_waitcnt(0x0070);
+  __builtin_amdgcn_s_barrier();
+}
+// One product, and VALU instructions that run beside it, N times.
+template <int N, int READS, int VALU>
+__device__ __forceinline__ void interleave() {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x402, VALU, 0);
+  }
+}
 
 // A wave's transposed 64 x 32 result (columns l.n) as rows: out(row, c, v) with columns 8 c .. + 7 of row, eight lanes a
 // row, so that memory is accessed in whole rows.  buf: 8 KB of the wave's own; a row's 16-byte pieces p are at p ^ (row % 16).
@@ -286,17 +377,14 @@ __device__ __forceinline__ Range range_of(const Keys& k, bool in) {
 
 // ----------------------------------------------------------------- forward
 
-// QW waves of 32 queries each share tiles of keys (QW = 4), or four waves share 32 queries and take a
-// quarter of each tile (QW = 1), where there are few queries.  One pass over the keys with the running
-// maximum m and sum l; the maximum that is taken off is only moved when a score exceeds it by 8 (in
-// powers of two), which keeps p under 256.
+// 32 queries, the four waves a quarter of each tile of 128 keys: where there are few queries.  One pass over the
+// keys with the running maximum m and sum l; the maximum that is taken off is only moved when a score exceeds
+// it by 8 (in powers of two), which keeps p under 256.
 constexpr float kLazy = 8.f;
 
-template <int QW>
-__global__ void __launch_bounds__(256, 2) attn_fwd_kernel(AttnFwdArgs a, int tiles, int splits, int chunk) {
-  constexpr int TK = QW == 4 ? 64 : 128, NB = QW == 4 ? 2 : 1, kTileBytes = TK * kRowBytes;
+__global__ void __launch_bounds__(256, 2) attn_fwd_few_kernel(AttnFwdArgs a, int tiles, int splits, int chunk) {
+  constexpr int TK = 128, kTileBytes = TK * kRowBytes;
   __shared__ __attribute__((aligned(16))) char lds[4 * kTileBytes];   // two stages of keys and values
-  __shared__ int ends[8];
   const int split = blockIdx.x % splits;
   const int slot = blockIdx.x / splits / 8, pair = slot / tiles * 8 + blockIdx.x / splits % 8;
   const int b = pair / a.b.heads, h = pair % a.b.heads;
@@ -309,8 +397,8 @@ __global__ void __launch_bounds__(256, 2) attn_fwd_kernel(AttnFwdArgs a, int til
   }
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), g = h / (a.b.heads / a.b.kv_heads);
   const Lane l(threadIdx.x % kWave);
-  const int q0 = tile * 32 * QW + (QW == 4 ? 32 * w : 0), i = q0 + l.n;
-  if (tile * 32 * QW >= s.oq) return;
+  const int q0 = tile * 32, i = q0 + l.n;
+  if (q0 >= s.oq) return;
   const bool in = i < s.nq;
   Keys keys = {0, s.nk};
   if (in) keys = keys_of(a.b, s, i);
@@ -327,25 +415,17 @@ __global__ void __launch_bounds__(256, 2) attn_fwd_kernel(AttnFwdArgs a, int til
     if (in) u = load16(a.q.p + (s.q0 + (int64_t)i) * a.q.ld + 64 * h + 16 * k + 8 * l.h);
     q[k] = as_bf16x8(u);
   }
+  settled(q);
 
-  int first = r.lo, last = r.hi;
-  if (QW == 4) {
-    if (threadIdx.x % kWave == 0) {
-      ends[w] = r.lo;
-      ends[4 + w] = r.hi;
-    }
-    __syncthreads();
-    first = min(min(ends[0], ends[1]), min(ends[2], ends[3]));
-    last = max(max(ends[4], ends[5]), max(ends[6], ends[7]));
-  }
-  first = first / TK * TK;
-
+  const int first = r.lo / TK * TK, last = r.hi;
   float m = -INFINITY, sum = 0.f;
   f32x16 o[2] = {zeros(), zeros()};
   Stage<TK> ks, vs;
+  ks.init(a.k, s.k0, s.nk, 64 * g);
+  vs.init(a.v, s.k0, s.nk, 64 * g);
   if (first < last) {
-    ks.load(a.k, s.k0, s.nk, 64 * g, first);
-    vs.load(a.v, s.k0, s.nk, 64 * g, first);
+    ks.load(first);
+    vs.load(first);
     ks.store(lds);
     vs.store(lds + kTileBytes);
   }
@@ -353,32 +433,188 @@ __global__ void __launch_bounds__(256, 2) attn_fwd_kernel(AttnFwdArgs a, int til
   for (int k0 = first, at = 0; k0 < last; k0 += TK, at ^= 2 * kTileBytes) {
     const bool more = k0 + TK < last;
     if (more) {
-      ks.load(a.k, s.k0, s.nk, 64 * g, k0 + TK);
-      vs.load(a.v, s.k0, s.nk, 64 * g, k0 + TK);
+      ks.load(k0 + TK);
+      vs.load(k0 + TK);
     }
-    const int mine = QW == 4 ? k0 : k0 + 32 * w;            // this wave's first key
-    if (mine < r.hi && mine + 32 * NB > r.lo) {
-      const char* kt = lds + at + (QW == 4 ? 0 : w * 32 * kRowBytes);
+    const int mine = k0 + 32 * w;            // this wave's first key
+    if (mine < r.hi && mine + 32 > r.lo) {
+      const char* kt = lds + at + w * 32 * kRowBytes;
       const char* vt = kt + kTileBytes;
-      f32x16 x[NB];
+      f32x16 x = zeros();
 #pragma unroll
-      for (int n = 0; n < NB; ++n) {
-        x[n] = zeros();
-#pragma unroll
-        for (int k = 0; k < 4; ++k) x[n] = mfma32(read_rows(kt, l, n, k), q[k], x[n]);
-      }
-      if (mine < r.all_lo || mine + 32 * NB > r.all_hi) {
+      for (int k = 0; k < 4; ++k) x = mfma32(read_rows(kt, l, 0, k), q[k], x);
+      if (mine < r.all_lo || mine + 32 > r.all_hi) {
         const int lo = keys.lo - mine - 4 * l.h;
         const unsigned len = max(keys.hi - keys.lo, 0);
 #pragma unroll
-        for (int n = 0; n < NB; ++n)
+        for (int e = 0; e < 16; ++e) x[e] = (unsigned)(8 * (e / 4) + e % 4 - lo) < len ? x[e] : -INFINITY;
+      }
+      float top = x[0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) top = fmaxf(top, x[e]);
+      top = fmaxf(top, other_half(top)) * kScale2;
+      if (__any(top > m + kLazy)) {
+        const float now = fmaxf(m, top), old = __builtin_amdgcn_exp2f(m - (now == -INFINITY ? 0.f : now));
+        m = now;
+        sum *= old;
+#pragma unroll
+        for (int d = 0; d < 2; ++d)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[d][e] *= old;
+      }
+      const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        x[e] = __builtin_amdgcn_exp2f(fmaf(x[e], kScale2, -base));
+        sum += x[e];
+      }
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const bf16x8 p = narrow(x, 8 * c);
+#pragma unroll
+        for (int d = 0; d < 2; ++d) o[d] = mfma32(read_cols(vt, l, d, c), p, o[d]);
+      }
+    }
+    if (more) {
+      ks.store(lds + (at ^ (2 * kTileBytes)));
+      vs.store(lds + (at ^ (2 * kTileBytes)) + kTileBytes);
+    }
+    __syncthreads();
+  }
+  sum += other_half(sum);
+
+  // the four waves' sums joined: [wave][dimension][query], and every thread 8 dimensions of a query
+  float* part = (float*)lds;
+  __shared__ float stat[4][2][32];
+  __shared__ int bad[32];
+#pragma unroll
+  for (int d = 0; d < 2; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) part[(w * 64 + 32 * d + 8 * (e / 4) + 4 * l.h + e % 4) * 32 + l.n] = o[d][e];
+  if (l.h == 0) {
+    stat[w][0][l.n] = m;
+    stat[w][1][l.n] = sum;
+  }
+  if (threadIdx.x < 32) bad[threadIdx.x] = 0;
+  __syncthreads();
+  const int n = threadIdx.x % 32, d0 = threadIdx.x / 32 * 8, row = q0 + n;
+  const float top = fmaxf(fmaxf(stat[0][0][n], stat[1][0][n]), fmaxf(stat[2][0][n], stat[3][0][n]));
+  const float base = top == -INFINITY ? 0.f : top;
+  float v[8] = {}, total = 0.f;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const float f = __builtin_amdgcn_exp2f(stat[u][0][n] - base);
+    total = fmaf(stat[u][1][n], f, total);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = fmaf(part[(u * 64 + d0 + e) * 32 + n], f, v[e]);
+  }
+  const bool live = row < s.oq, some = row < s.nq && total != 0.f;
+  if (splits > 1) {
+    if (!live) return;
+    const size_t at = ((size_t)split * a.b.heads + h) * a.b.q_rows + s.q0 + row;
+    const size_t rows = (size_t)splits * a.b.heads * a.b.q_rows;
+    *(f32x4*)(a.part + at * 64 + d0) = f32x4{v[0], v[1], v[2], v[3]};
+    *(f32x4*)(a.part + at * 64 + d0 + 4) = f32x4{v[4], v[5], v[6], v[7]};
+    if (d0 == 0) {
+      a.part[rows * 64 + at] = some ? top : -INFINITY;
+      a.part[rows * 65 + at] = some ? total : 0.f;
+    }
+    return;
+  }
+  const float inv = some ? 1.f / total : 0.f;
+  uint32_t hi[4], low[4];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    v[e] = some ? v[e] * inv : 0.f;
+    if (!(fabsf(v[e]) < INFINITY)) bad[n] = 1;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    hi[e] = f32x2_to_bf16x2(v[2 * e], v[2 * e + 1]);
+    low[e] = f32x2_to_bf16x2(v[2 * e] - bf16_to_f32(hi[e] & 0xffff), v[2 * e + 1] - bf16_to_f32(hi[e] >> 16));
+  }
+  __syncthreads();
+  const bool again = live && bad[n];
+  if (live && !again) {
+    const int64_t qr = s.q0 + (int64_t)row;
+    __builtin_memcpy(a.o.p + qr * a.o.ld + 64 * h + d0, hi, 16);
+    if (a.rest.p) __builtin_memcpy(a.rest.p + qr * a.rest.ld + 64 * h + d0, low, 16);
+    if (a.lse && d0 == 0) a.lse[(size_t)h * a.b.q_rows + qr] = some ? (top + __log2f(total)) * kLn2 : -INFINITY;
+  }
+  // what is not finite may come from keys that the row does not see
+  for (uint32_t rows = (uint32_t)__ballot(again); rows; rows &= rows - 1)
+    if (__builtin_ctz(rows) % 4 == w) fwd_row(a, s, h, q0 + __builtin_ctz(rows));
+}
+
+// Four waves of 32 queries share tiles of 64 keys.
+template <bool DIRECT>
+__global__ void __launch_bounds__(256, DIRECT ? 4 : 2) attn_fwd_wide_kernel(AttnFwdArgs a, int tiles) {
+  constexpr int TK = 64;
+  // (distinct objects, so that the compiler can tell a read of one tile from the loads that fill another)
+  __shared__ uint4 key0[512], key1[512], val0[512], val1[512];
+  __shared__ int ends[8];
+  const Place at = place_of(tiles, a.b.heads, a.b.batch, a.b.causal);
+  if (!at.in) return;
+  const int h = at.h;
+  const Span s = span_of(a.b, at.b);
+  if (!s.ok) {
+    if (threadIdx.x == 0) atomicOr(a.b.err, AD_ERR_LENGTH);
+    return;
+  }
+  if (at.tile * 128 >= s.oq) return;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), g = h / (a.b.heads / a.b.kv_heads);
+  const Lane l(threadIdx.x % kWave);
+  const int q0 = at.tile * 128 + 32 * w, i = q0 + l.n;
+  const bool in = i < s.nq;
+  bf16x8 q[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    uint4 u = make_uint4(0, 0, 0, 0);
+    if (in) u = load16(a.q.p + (s.q0 + (int64_t)i) * a.q.ld + 64 * h + 16 * k + 8 * l.h);
+    q[k] = as_bf16x8(u);
+  }
+  Keys keys = {0, s.nk};
+  if (in) keys = keys_of(a.b, s, i);
+  const Range r = range_of(keys, in);
+  if (threadIdx.x % kWave == 0) {
+    ends[w] = r.lo;
+    ends[4 + w] = r.hi;
+  }
+  __syncthreads();
+  const int first = __builtin_amdgcn_readfirstlane(min(min(ends[0], ends[1]), min(ends[2], ends[3])) / TK * TK);
+  const int last = __builtin_amdgcn_readfirstlane(max(max(ends[4], ends[5]), max(ends[6], ends[7])));
+
+  float m = -INFINITY, sum = 0.f;
+  f32x16 o[2] = {zeros(), zeros()};
+  Loads<DIRECT> ks, vs;
+  ks.init(a.k, s.k0, s.nk, 64 * g);
+  vs.init(a.v, s.k0, s.nk, 64 * g);
+  const auto step = [&](int k0, const uint4* kt, const uint4* vt, uint4* next_kt, uint4* next_vt) {
+    const bool more = k0 + TK < last;
+    if (more) {
+      ks.issue(k0 + TK, next_kt);
+      vs.issue(k0 + TK, next_vt);
+    }
+    if (k0 < r.hi && k0 + TK > r.lo) {
+      f32x16 x[2];
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        x[n] = zeros();
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[n] = mfma32(read_rows((const char*)kt, l, n, k), q[k], x[n]);
+      }
+      if (k0 < r.all_lo || k0 + TK > r.all_hi) {
+        const int lo = keys.lo - k0 - 4 * l.h;
+        const unsigned len = max(keys.hi - keys.lo, 0);
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
 #pragma unroll
           for (int e = 0; e < 16; ++e)
             x[n][e] = (unsigned)(32 * n + 8 * (e / 4) + e % 4 - lo) < len ? x[n][e] : -INFINITY;
       }
       float top = x[0][0];
 #pragma unroll
-      for (int n = 0; n < NB; ++n)
+      for (int n = 0; n < 2; ++n)
 #pragma unroll
         for (int e = 0; e < 16; ++e) top = fmaxf(top, x[n][e]);
       top = fmaxf(top, other_half(top)) * kScale2;
@@ -393,121 +629,68 @@ __global__ void __launch_bounds__(256, 2) attn_fwd_kernel(AttnFwdArgs a, int til
       }
       const float base = m == -INFINITY ? 0.f : m;
 #pragma unroll
-      for (int n = 0; n < NB; ++n)
+      for (int c = 0; c < 4; ++c) {
+        f32x16& p = x[c / 2];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          x[n][e] = __builtin_amdgcn_exp2f(fmaf(x[n][e], kScale2, -base));
-          sum += x[n][e];
+        for (int e = 8 * (c % 2); e < 8 * (c % 2) + 8; ++e) {
+          p[e] = __builtin_amdgcn_exp2f(fmaf(p[e], kScale2, -base));
+          sum += p[e];
         }
+        const bf16x8 b = narrow(p, 8 * (c % 2));
 #pragma unroll
-      for (int n = 0; n < NB; ++n)
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const bf16x8 p = narrow(x[n], 8 * c);
-#pragma unroll
-          for (int d = 0; d < 2; ++d) o[d] = mfma32(read_cols(vt, l, d, 2 * n + c), p, o[d]);
-        }
+        for (int d = 0; d < 2; ++d) o[d] = mfma32(read_cols((const char*)vt, l, d, c), b, o[d]);
+      }
     }
     if (more) {
-      ks.store(lds + (at ^ (2 * kTileBytes)));
-      vs.store(lds + (at ^ (2 * kTileBytes)) + kTileBytes);
+      ks.arrive(next_kt);
+      vs.arrive(next_vt);
     }
-    __syncthreads();
+    landed();
+  };
+
+  if (first < last) {
+    ks.issue(first, key0);
+    ks.arrive(key0);
+    vs.issue(first, val0);
+    vs.arrive(val0);
+    settled(q);
+    landed();
+    for (int k0 = first; k0 < last; k0 += 2 * TK) {
+      step(k0, key0, val0, key1, val1);
+      if (k0 + TK >= last) break;
+      step(k0 + TK, key1, val1, key0, val0);
+    }
   }
   sum += other_half(sum);
 
-  if constexpr (QW == 4) {
-    const float inv = sum == 0.f || !in ? 0.f : 1.f / sum;
-    bool bad = false;
+  const float inv = sum == 0.f || !in ? 0.f : 1.f / sum;
+  bool bad = false;
 #pragma unroll
-    for (int d = 0; d < 2; ++d)
+  for (int d = 0; d < 2; ++d)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        o[d][e] = inv == 0.f && sum == 0.f ? 0.f : o[d][e] * inv;
-        bad |= !(fabsf(o[d][e]) < INFINITY);
-        o[d][e] = in ? o[d][e] : 0.f;
-      }
-    by_rows(lds + w * 32 * 256, l, o, [&](int row, int c, const float(&v)[8]) {
-      if (q0 + row >= s.oq) return;
-      const uint4 u = narrow8(v);
-      store_piece(a.o, s.q0 + (int64_t)(q0 + row), h, c, u);
-      if (!a.rest.p) return;
-      const uint32_t hi[4] = {u.x, u.y, u.z, u.w};
-      float low[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) low[e] = v[e] - bf16_to_f32((uint16_t)(hi[e / 2] >> (16 * (e % 2))));
-      store_piece(a.rest, s.q0 + (int64_t)(q0 + row), h, c, narrow8(low));
-    });
-    if (a.lse && l.h == 0 && i < s.oq)
-      a.lse[(size_t)h * a.b.q_rows + s.q0 + i] = sum == 0.f || !in ? -INFINITY : (m + __log2f(sum)) * kLn2;
-    // what is not finite may come from keys that this row does not see
-    uint64_t again = __ballot(bad && in);
-    if (again) __threadfence_block();
-    again = (again | again >> 32) & 0xffffffffu;
-    for (; again; again &= again - 1) fwd_row(a, s, h, q0 + __builtin_ctzll(again));
-  } else {
-    // the four waves' sums joined: [wave][dimension][query], and every thread 8 dimensions of a query
-    float* part = (float*)lds;
-    __shared__ float stat[4][2][32];
-    __shared__ int bad[32];
-#pragma unroll
-    for (int d = 0; d < 2; ++d)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) part[(w * 64 + 32 * d + 8 * (e / 4) + 4 * l.h + e % 4) * 32 + l.n] = o[d][e];
-    if (l.h == 0) {
-      stat[w][0][l.n] = m;
-      stat[w][1][l.n] = sum;
+    for (int e = 0; e < 16; ++e) {
+      o[d][e] = inv == 0.f && sum == 0.f ? 0.f : o[d][e] * inv;
+      bad |= !(fabsf(o[d][e]) < INFINITY);
+      o[d][e] = in ? o[d][e] : 0.f;
     }
-    if (threadIdx.x < 32) bad[threadIdx.x] = 0;
-    __syncthreads();
-    const int n = threadIdx.x % 32, d0 = threadIdx.x / 32 * 8, row = q0 + n;
-    const float top = fmaxf(fmaxf(stat[0][0][n], stat[1][0][n]), fmaxf(stat[2][0][n], stat[3][0][n]));
-    const float base = top == -INFINITY ? 0.f : top;
-    float v[8] = {}, total = 0.f;
+  by_rows((char*)(w == 0 ? key0 : w == 1 ? key1 : w == 2 ? val0 : val1), l, o, [&](int row, int c, const float(&v)[8]) {
+    if (q0 + row >= s.oq) return;
+    const uint4 u = narrow8(v);
+    store_piece(a.o, s.q0 + (int64_t)(q0 + row), h, c, u);
+    if (!a.rest.p) return;
+    const uint32_t hi[4] = {u.x, u.y, u.z, u.w};
+    float low[8];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const float f = __builtin_amdgcn_exp2f(stat[u][0][n] - base);
-      total = fmaf(stat[u][1][n], f, total);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = fmaf(part[(u * 64 + d0 + e) * 32 + n], f, v[e]);
-    }
-    const bool live = row < s.oq, some = row < s.nq && total != 0.f;
-    if (splits > 1) {
-      if (!live) return;
-      const size_t at = ((size_t)split * a.b.heads + h) * a.b.q_rows + s.q0 + row;
-      const size_t rows = (size_t)splits * a.b.heads * a.b.q_rows;
-      *(f32x4*)(a.part + at * 64 + d0) = f32x4{v[0], v[1], v[2], v[3]};
-      *(f32x4*)(a.part + at * 64 + d0 + 4) = f32x4{v[4], v[5], v[6], v[7]};
-      if (d0 == 0) {
-        a.part[rows * 64 + at] = some ? top : -INFINITY;
-        a.part[rows * 65 + at] = some ? total : 0.f;
-      }
-      return;
-    }
-    const float inv = some ? 1.f / total : 0.f;
-    uint32_t hi[4], low[4];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      v[e] = some ? v[e] * inv : 0.f;
-      if (!(fabsf(v[e]) < INFINITY)) bad[n] = 1;
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      hi[e] = f32x2_to_bf16x2(v[2 * e], v[2 * e + 1]);
-      low[e] = f32x2_to_bf16x2(v[2 * e] - bf16_to_f32(hi[e] & 0xffff), v[2 * e + 1] - bf16_to_f32(hi[e] >> 16));
-    }
-    __syncthreads();
-    const bool again = live && bad[n];
-    if (live && !again) {
-      const int64_t qr = s.q0 + (int64_t)row;
-      __builtin_memcpy(a.o.p + qr * a.o.ld + 64 * h + d0, hi, 16);
-      if (a.rest.p) __builtin_memcpy(a.rest.p + qr * a.rest.ld + 64 * h + d0, low, 16);
-      if (a.lse && d0 == 0) a.lse[(size_t)h * a.b.q_rows + qr] = some ? (top + __log2f(total)) * kLn2 : -INFINITY;
-    }
-    // what is not finite may come from keys that the row does not see
-    for (uint32_t rows = (uint32_t)__ballot(again); rows; rows &= rows - 1)
-      if (__builtin_ctz(rows) % 4 == w) fwd_row(a, s, h, q0 + __builtin_ctz(rows));
-  }
+    for (int e = 0; e < 8; ++e) low[e] = v[e] - bf16_to_f32((uint16_t)(hi[e / 2] >> (16 * (e % 2))));
+    store_piece(a.rest, s.q0 + (int64_t)(q0 + row), h, c, narrow8(low));
+  });
+  if (a.lse && l.h == 0 && i < s.oq)
+    a.lse[(size_t)h * a.b.q_rows + s.q0 + i] = sum == 0.f || !in ? -INFINITY : (m + __log2f(sum)) * kLn2;
+  // what is not finite may come from keys that this row does not see
+  uint64_t again = __ballot(bad && in);
+  if (again) __threadfence_block();
+  again = (again | again >> 32) & 0xffffffffu;
+  for (; again; again &= again - 1) fwd_row(a, s, h, q0 + __builtin_ctzll(again));
 }
 
 // The parts of a row's keys joined: a wave a row and head, a lane a dimension.
@@ -540,35 +723,17 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnFwdArgs a, int tiles
 
 // ----------------------------------------------------------------- backward
 
-// dq.  As the forward kernel, with p from lse and two products more: dP^T = V dO^T and, from dS, dQ^T =
-// K^T dS^T.  It leaves delta and what 32 queries see together for the second kernel.
-template <int QW>
-__global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnBwdArgs a, int tiles) {
-  constexpr int TK = QW == 4 ? 64 : 128, NB = QW == 4 ? 2 : 1, kTileBytes = TK * kRowBytes;
-  __shared__ __attribute__((aligned(16))) char lds[4 * kTileBytes];
-  __shared__ int ends[8];
-  const Place at = place_of(tiles, a.b.heads, a.b.batch, a.b.causal);
-  if (!at.in) return;
-  const int h = at.h;
-  const Span s = span_of(a.b, at.b);
-  if (!s.ok) {
-    if (threadIdx.x == 0) atomicOr(a.b.err, AD_ERR_LENGTH);
-    return;
-  }
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), g = h / (a.b.heads / a.b.kv_heads);
-  const Lane l(threadIdx.x % kWave);
-  const int q0 = at.tile * 32 * QW + (QW == 4 ? 32 * w : 0), i = q0 + l.n;
-  if (at.tile * 32 * QW >= s.oq) return;
+// What a query's column of the products needs: its row of q and dout, delta = dout . o, lse in powers of two, and
+// the keys it sees.
+__device__ __forceinline__ void dq_operands(const AttnBwdArgs& a, const Span& s, int h, int i, const Lane& l, bf16x8 (&q)[4],
+                                            bf16x8 (&go)[4], float& delta, float& lse, Keys& keys) {
   const bool in = i < s.nq;
   const int64_t row = s.q0 + (int64_t)i;
-  const size_t stat = (size_t)h * a.b.q_rows + row;
-
-  bf16x8 q[4], go[4];
-  float delta = 0.f, lse = 0.f;
-  Keys keys = {0, s.nk};
+  delta = lse = 0.f;
+  keys = {0, s.nk};
   if (in) {
     keys = keys_of(a.b, s, i);
-    lse = a.lse[stat] * kLog2e;
+    lse = a.lse[(size_t)h * a.b.q_rows + row] * kLog2e;
     if (lse == -INFINITY) keys.hi = keys.lo;
   }
 #pragma unroll
@@ -591,96 +756,23 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnBwdArgs a, int tile
     for (int e = 0; e < 8; ++e) delta = fmaf(d[e], o[e] + r[e], delta);
   }
   delta += other_half(delta);
-  const Range r = range_of(keys, in);
-  if (QW == 4 || w == 0) {
-    if (in && l.h == 0) a.delta[stat] = delta;
-    if (h == 0 && threadIdx.x % kWave == 0 && q0 < s.nq)
-      a.ranges[(size_t)at.b * a.blocks + q0 / 32] = make_int4(r.lo, r.hi, r.all_lo, r.all_hi);
+  settled(q);
+  settled(go);
+}
+// Of 32 keys, the first of this lane's being k: those that the query does not see give p = 0 and dP = 0.
+__device__ __forceinline__ void hide(const Keys& keys, int k, f32x16& x, f32x16& y) {
+  const int lo = keys.lo - k;
+  const unsigned len = max(keys.hi - keys.lo, 0);
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    const bool seen = (unsigned)(8 * (e / 4) + e % 4 - lo) < len;
+    x[e] = seen ? x[e] : -INFINITY;
+    y[e] = seen ? y[e] : 0.f;
   }
-
-  int first = r.lo, last = r.hi;
-  if (QW == 4) {
-    if (threadIdx.x % kWave == 0) {
-      ends[w] = r.lo;
-      ends[4 + w] = r.hi;
-    }
-    __syncthreads();
-    first = min(min(ends[0], ends[1]), min(ends[2], ends[3]));
-    last = max(max(ends[4], ends[5]), max(ends[6], ends[7]));
-  }
-  first = first / TK * TK;
-
-  f32x16 dq[2] = {zeros(), zeros()};
-  Stage<TK> ks, vs;
-  if (first < last) {
-    ks.load(a.k, s.k0, s.nk, 64 * g, first);
-    vs.load(a.v, s.k0, s.nk, 64 * g, first);
-    ks.store(lds);
-    vs.store(lds + kTileBytes);
-  }
-  __syncthreads();
-  for (int k0 = first, buf = 0; k0 < last; k0 += TK, buf ^= 2 * kTileBytes) {
-    const bool more = k0 + TK < last;
-    if (more) {
-      ks.load(a.k, s.k0, s.nk, 64 * g, k0 + TK);
-      vs.load(a.v, s.k0, s.nk, 64 * g, k0 + TK);
-    }
-    const int mine = QW == 4 ? k0 : k0 + 32 * w;
-    if (mine < r.hi && mine + 32 * NB > r.lo) {
-      const char* kt = lds + buf + (QW == 4 ? 0 : w * 32 * kRowBytes);
-      const char* vt = kt + kTileBytes;
-      const bool cut = mine < r.all_lo || mine + 32 * NB > r.all_hi;
-#pragma unroll
-      for (int n = 0; n < NB; ++n) {
-        f32x16 x = zeros(), y = zeros();
-#pragma unroll
-        for (int k = 0; k < 4; ++k) x = mfma32(read_rows(kt, l, n, k), q[k], x);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) y = mfma32(read_rows(vt, l, n, k), go[k], y);
-        if (cut) {
-          const int lo = keys.lo - mine - 4 * l.h;
-          const unsigned len = max(keys.hi - keys.lo, 0);
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const bool seen = (unsigned)(32 * n + 8 * (e / 4) + e % 4 - lo) < len;
-            x[e] = seen ? x[e] : -INFINITY;
-            y[e] = seen ? y[e] : 0.f;
-          }
-        }
-#pragma unroll
-        for (int e = 0; e < 16; ++e) x[e] = __builtin_amdgcn_exp2f(fmaf(x[e], kScale2, -lse)) * (y[e] - delta);
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const bf16x8 ds = narrow(x, 8 * c);
-#pragma unroll
-          for (int d = 0; d < 2; ++d) dq[d] = mfma32(read_cols(kt, l, d, 2 * n + c), ds, dq[d]);
-        }
-      }
-    }
-    if (more) {
-      ks.store(lds + (buf ^ (2 * kTileBytes)));
-      vs.store(lds + (buf ^ (2 * kTileBytes)) + kTileBytes);
-    }
-    __syncthreads();
-  }
-
-  if constexpr (QW == 1) {
-    // the other waves' sums to the first one, which goes on alone
-    float* part = (float*)lds;
-    if (w > 0)
-#pragma unroll
-      for (int d = 0; d < 2; ++d)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) part[((w - 1) * 32 + 16 * d + e) * 64 + threadIdx.x % kWave] = dq[d][e];
-    __syncthreads();
-    if (w > 0) return;
-#pragma unroll
-    for (int d = 0; d < 2; ++d)
-#pragma unroll
-      for (int e = 0; e < 16; ++e)
-#pragma unroll
-        for (int u = 0; u < 3; ++u) dq[d][e] += part[(u * 32 + 16 * d + e) * 64 + threadIdx.x];
-  }
+}
+// The 32 rows from q0 on.
+__device__ __forceinline__ void dq_out(const AttnBwdArgs& a, const Span& s, int h, int q0, bool in, const Lane& l, char* buf,
+                                       f32x16 (&dq)[2]) {
   bool bad = false;
 #pragma unroll
   for (int d = 0; d < 2; ++d)
@@ -689,7 +781,7 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnBwdArgs a, int tile
       dq[d][e] = in ? dq[d][e] * kScale : 0.f;
       bad |= !(fabsf(dq[d][e]) < INFINITY);
     }
-  by_rows(lds + (QW == 1 ? 0 : w * 32 * 256), l, dq, [&](int n, int c, const float(&v)[8]) {
+  by_rows(buf, l, dq, [&](int n, int c, const float(&v)[8]) {
     if (q0 + n >= s.oq) return;
     const int64_t to = s.q0 + (int64_t)(q0 + n);
     float x[8];
@@ -710,32 +802,279 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnBwdArgs a, int tile
   for (; again; again &= again - 1) dq_row(a, s, h, q0 + __builtin_ctzll(again));
 }
 
-// dk and dv: the same with the queries on the rows (S = Q K^T), a wave 32 keys and all of the queries that
-// see them, of every head that shares them.  KW waves of 32 keys each share tiles of 64 queries, or four
-// waves take a quarter of the queries each.
-template <int KW>
-__global__ void __launch_bounds__(256, 2) attn_dkv_kernel(AttnBwdArgs a, int tiles) {
-  constexpr int TQ = KW == 4 ? 64 : 128, NB = KW == 4 ? 2 : 1, kTileBytes = TQ * kRowBytes;
-  constexpr int kStatBytes = 4 * TQ * 4, kStageBytes = 2 * kTileBytes + kStatBytes;
-  __shared__ __attribute__((aligned(16))) char lds[2 * kStageBytes];
-  const Place at = place_of(tiles, a.b.kv_heads, a.b.batch, false);
+// dq of 32 queries, the four waves a quarter of each tile of 128 keys.
+__global__ void __launch_bounds__(256, 2) attn_dq_few_kernel(AttnBwdArgs a, int tiles) {
+  constexpr int TK = 128, kTileBytes = TK * kRowBytes;
+  __shared__ __attribute__((aligned(16))) char lds[4 * kTileBytes];
+  const Place at = place_of(tiles, a.b.heads, a.b.batch, a.b.causal);
   if (!at.in) return;
-  const int g = at.h;
+  const int h = at.h;
   const Span s = span_of(a.b, at.b);
   if (!s.ok) {
     if (threadIdx.x == 0) atomicOr(a.b.err, AD_ERR_LENGTH);
     return;
   }
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), g = h / (a.b.heads / a.b.kv_heads);
   const Lane l(threadIdx.x % kWave);
-  const int j0 = at.tile * 32 * KW + (KW == 4 ? 32 * w : 0), j = j0 + l.n;
-  if (at.tile * 32 * KW >= s.ok_) return;
-  const bool in = j < s.nk;
-  bf16x8 k[4], v[4];
+  const int q0 = at.tile * 32, i = q0 + l.n;
+  if (q0 >= s.oq) return;
+  const bool in = i < s.nq;
+  bf16x8 q[4], go[4];
+  float delta, lse;
+  Keys keys;
+  dq_operands(a, s, h, i, l, q, go, delta, lse, keys);
+  const Range r = range_of(keys, in);
+  if (w == 0) {
+    if (in && l.h == 0) a.delta[(size_t)h * a.b.q_rows + s.q0 + i] = delta;
+    if (h == 0 && threadIdx.x == 0 && q0 < s.nq)
+      a.ranges[(size_t)at.b * a.blocks + at.tile] = make_int4(r.lo, r.hi, r.all_lo, r.all_hi);
+  }
+  const int first = r.lo / TK * TK, last = r.hi;
+  f32x16 dq[2] = {zeros(), zeros()};
+  Stage<TK> ks, vs;
+  ks.init(a.k, s.k0, s.nk, 64 * g);
+  vs.init(a.v, s.k0, s.nk, 64 * g);
+  if (first < last) {
+    ks.load(first);
+    vs.load(first);
+    ks.store(lds);
+    vs.store(lds + kTileBytes);
+  }
+  __syncthreads();
+  for (int k0 = first, buf = 0; k0 < last; k0 += TK, buf ^= 2 * kTileBytes) {
+    const bool more = k0 + TK < last;
+    if (more) {
+      ks.load(k0 + TK);
+      vs.load(k0 + TK);
+    }
+    const int mine = k0 + 32 * w;
+    if (mine < r.hi && mine + 32 > r.lo) {
+      const char* kt = lds + buf + w * 32 * kRowBytes;
+      const char* vt = kt + kTileBytes;
+      f32x16 x = zeros(), y = zeros();
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x = mfma32(read_rows(kt, l, 0, k), q[k], x);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) y = mfma32(read_rows(vt, l, 0, k), go[k], y);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) y[e] -= delta;
+      if (mine < r.all_lo || mine + 32 > r.all_hi) hide(keys, mine + 4 * l.h, x, y);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[e] = __builtin_amdgcn_exp2f(fmaf(x[e], kScale2, -lse)) * y[e];
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const bf16x8 ds = narrow(x, 8 * c);
+#pragma unroll
+        for (int d = 0; d < 2; ++d) dq[d] = mfma32(read_cols(kt, l, d, c), ds, dq[d]);
+      }
+    }
+    if (more) {
+      ks.store(lds + (buf ^ (2 * kTileBytes)));
+      vs.store(lds + (buf ^ (2 * kTileBytes)) + kTileBytes);
+    }
+    __syncthreads();
+  }
+  // the other waves' sums to the first one, which goes on alone
+  float* part = (float*)lds;
+  if (w > 0)
+#pragma unroll
+    for (int d = 0; d < 2; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) part[((w - 1) * 32 + 16 * d + e) * 64 + threadIdx.x % kWave] = dq[d][e];
+  __syncthreads();
+  if (w > 0) return;
+#pragma unroll
+  for (int d = 0; d < 2; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+#pragma unroll
+      for (int u = 0; u < 3; ++u) dq[d][e] += part[(u * 32 + 16 * d + e) * 64 + threadIdx.x];
+  dq_out(a, s, h, q0, in, l, lds, dq);
+}
+
+// dq of four waves of 32 queries that share tiles of 64 keys: as the forward kernel, with p from lse and two
+// products more, dP^T = V dO^T and, from dS, dQ^T = K^T dS^T.  It leaves delta and what 32 queries see
+// together for the kernel of dk and dv.
+template <bool DIRECT>
+__global__ void __launch_bounds__(256, DIRECT ? 3 : 2) attn_dq_wide_kernel(AttnBwdArgs a, int tiles) {
+  constexpr int TK = 64;
+  __shared__ uint4 key0[512], key1[512], val0[512], val1[512];
+  __shared__ int ends[8];
+  const Place at = place_of(tiles, a.b.heads, a.b.batch, a.b.causal);
+  if (!at.in) return;
+  const int h = at.h;
+  const Span s = span_of(a.b, at.b);
+  if (!s.ok) {
+    if (threadIdx.x == 0) atomicOr(a.b.err, AD_ERR_LENGTH);
+    return;
+  }
+  if (at.tile * 128 >= s.oq) return;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), g = h / (a.b.heads / a.b.kv_heads);
+  const Lane l(threadIdx.x % kWave);
+  const int q0 = at.tile * 128 + 32 * w, i = q0 + l.n;
+  const bool in = i < s.nq;
+  const int64_t row = s.q0 + (int64_t)i;
+  bf16x8 q[4], go[4];
+  float delta, lse;
+  Keys keys;
+  dq_operands(a, s, h, i, l, q, go, delta, lse, keys);
+  const Range r = range_of(keys, in);
+  if (in && l.h == 0) a.delta[(size_t)h * a.b.q_rows + row] = delta;
+  if (threadIdx.x % kWave == 0) {
+    if (h == 0 && q0 < s.nq) a.ranges[(size_t)at.b * a.blocks + q0 / 32] = make_int4(r.lo, r.hi, r.all_lo, r.all_hi);
+    ends[w] = r.lo;
+    ends[4 + w] = r.hi;
+  }
+  __syncthreads();
+  const int first = __builtin_amdgcn_readfirstlane(min(min(ends[0], ends[1]), min(ends[2], ends[3])) / TK * TK);
+  const int last = __builtin_amdgcn_readfirstlane(max(max(ends[4], ends[5]), max(ends[6], ends[7])));
+
+  f32x16 dq[2] = {zeros(), zeros()}, off;     // off: dP - delta starts from -delta
+#pragma unroll
+  for (int e = 0; e < 16; ++e) off[e] = -delta;
+  Loads<DIRECT> ks, vs;
+  ks.init(a.k, s.k0, s.nk, 64 * g);
+  vs.init(a.v, s.k0, s.nk, 64 * g);
+  const auto step = [&](int k0, const uint4* kt, const uint4* vt, uint4* next_kt, uint4* next_vt) {
+    const bool more = k0 + TK < last;
+    if (more) {
+      ks.issue(k0 + TK, next_kt);
+      vs.issue(k0 + TK, next_vt);
+    }
+    if (k0 < r.hi && k0 + TK > r.lo) {
+      const bool cut = k0 < r.all_lo || k0 + TK > r.all_hi;
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        f32x16 x = zeros(), y = off;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x = mfma32(read_rows((const char*)kt, l, n, k), q[k], x);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) y = mfma32(read_rows((const char*)vt, l, n, k), go[k], y);
+        if (cut) hide(keys, k0 + 32 * n + 4 * l.h, x, y);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] = __builtin_amdgcn_exp2f(fmaf(x[e], kScale2, -lse)) * y[e];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const bf16x8 ds = narrow(x, 8 * c);
+#pragma unroll
+          for (int d = 0; d < 2; ++d) dq[d] = mfma32(read_cols((const char*)kt, l, d, 2 * n + c), ds, dq[d]);
+        }
+      }
+    }
+    if (more) {
+      ks.arrive(next_kt);
+      vs.arrive(next_vt);
+    }
+    landed();
+  };
+  if (first < last) {
+    ks.issue(first, key0);
+    ks.arrive(key0);
+    vs.issue(first, val0);
+    vs.arrive(val0);
+    landed();
+    for (int k0 = first; k0 < last; k0 += 2 * TK) {
+      step(k0, key0, val0, key1, val1);
+      if (k0 + TK >= last) break;
+      step(k0 + TK, key1, val1, key0, val0);
+    }
+  }
+  dq_out(a, s, h, q0, in, l, (char*)(w == 0 ? key0 : w == 1 ? key1 : w == 2 ? val0 : val1), dq);
+}
+
+// dk and dv: the same with the queries on the rows (S = Q K^T), a wave 32 keys and all of the queries that
+// see them, of every head that shares them.
+
+// What the products need of a tile's TQ queries besides their rows, on its way to LDS: [TQ] each of lse in powers of
+// two (+infinity where a row sees nothing: p = 0), -delta, and the keys [lo, hi) that the query sees.
+template <int TQ>
+struct StatLoads {
+  float lse, off;
+  int lo, hi;
+  __device__ __forceinline__ void issue(const AttnBwdArgs& a, const Span& s, int h, int i0) {
+    lse = off = 0.f;
+    lo = hi = 0;
+    const int i = i0 + (int)threadIdx.x;
+    if (threadIdx.x < TQ && i < s.nq) {
+      const size_t at = (size_t)h * a.b.q_rows + s.q0 + i;
+      lse = a.lse[at] * kLog2e;
+      off = -a.delta[at];
+      const Keys r = keys_of(a.b, s, i);
+      lo = r.lo;
+      hi = max(r.hi, r.lo);
+      if (lse == -INFINITY) {
+        hi = r.lo;
+        lse = INFINITY;
+      }
+    }
+  }
+  __device__ __forceinline__ void arrive(float* to) const {
+    if (threadIdx.x < TQ) {
+      to[threadIdx.x] = lse;
+      to[TQ + threadIdx.x] = off;
+      ((int*)to)[2 * TQ + threadIdx.x] = lo;
+      ((int*)to)[3 * TQ + threadIdx.x] = hi;
+    }
+  }
+};
+
+// The steps of a workgroup's keys [k0, k1): tiles of TQ queries of one head after the other, those that some
+// of the keys are seen by.
+template <int TQ>
+struct Walk {
+  // (the first kernel's table is constant here: scalar loads)
+  typedef const __attribute__((address_space(4))) int* Table;
+  Table ranges;
+  bool window, causal;
+  int nq, nk, k0, k1, start, tiles, t, h, heads_end;
+  __device__ __forceinline__ Walk(const AttnBwdArgs& a, const Span& s, int b, int g, int k0_, int k1_) {
+    ranges = (Table)(uintptr_t)(a.ranges + (size_t)b * a.blocks);
+    window = a.b.window;
+    causal = a.b.causal;
+    nq = s.nq; nk = s.nk; k0 = k0_; k1 = k1_;
+    tiles = (nq + TQ - 1) / TQ;
+    // (causal: the queries before key - (nk - nq) do not see the key)
+    start = causal ? min(max(k0 - (nk - nq), 0) / TQ, tiles) : 0;
+    const int group = a.b.heads / a.b.kv_heads;
+    t = start;
+    h = g * group;
+    heads_end = h + group;
+  }
+  // what the queries 32 u .. + 31 see together
+  __device__ __forceinline__ Range seen(int u) const {
+    Range r = {0, nk, 0, nk};
+    if (window) {
+      const Table p = ranges + 4 * u;
+      r = Range{p[0], p[1], p[2], p[3]};
+    } else if (causal) {
+      r.all_hi = 32 * u + nk - nq + 1;
+      r.hi = min(nk, r.all_hi + 31);
+    }
+    return r;
+  }
+  __device__ __forceinline__ bool wanted() const {
+    if (!window) return true;
+    for (int u = t * (TQ / 32); u < min((t + 1) * (TQ / 32), (nq + 31) / 32); ++u) {
+      const Range r = seen(u);
+      if (r.lo < k1 && r.hi > k0) return true;
+    }
+    return false;
+  }
+  // from (h, t) on to a step that is wanted; false: there is none
+  __device__ __forceinline__ bool settle() {
+    for (; h < heads_end; ++h, t = start)
+      for (; t < tiles; ++t)
+        if (wanted()) return true;
+    return false;
+  }
+};
+
+__device__ __forceinline__ void keys_operands(const AttnBwdArgs& a, const Span& s, int g, int j, const Lane& l, bf16x8 (&k)[4],
+                                              bf16x8 (&v)[4]) {
 #pragma unroll
   for (int c = 0; c < 4; ++c) {
     uint4 uk = make_uint4(0, 0, 0, 0), uv = uk;
-    if (in) {
+    if (j < s.nk) {
       const int64_t row = s.k0 + (int64_t)j;
       uk = load16(a.k.p + row * a.k.ld + 64 * g + 16 * c + 8 * l.h);
       uv = load16(a.v.p + row * a.v.ld + 64 * g + 16 * c + 8 * l.h);
@@ -743,147 +1082,61 @@ __global__ void __launch_bounds__(256, 2) attn_dkv_kernel(AttnBwdArgs a, int til
     k[c] = as_bf16x8(uk);
     v[c] = as_bf16x8(uv);
   }
-  const int group = a.b.heads / a.b.kv_heads, blocks = (s.nq + TQ - 1) / TQ;
-  const int tile0 = at.tile * 32 * KW, tile1 = min(tile0 + 32 * KW, s.nk);     // the workgroup's keys
-  const int4* ranges = a.ranges + (size_t)at.b * a.blocks;
-
-  // steps: TQ queries of one head, those that some key of the workgroup is seen by
-  const auto wanted = [&](int t) {
-    for (int u = t * (TQ / 32); u < min((t + 1) * (TQ / 32), (s.nq + 31) / 32); ++u) {
-      const int4 r = ranges[u];
-      if (r.x < tile1 && r.y > tile0) return true;
-    }
-    return false;
-  };
-  // (causal: the queries before i see none of the keys from i + nk - nq + 1 on)
-  const int start = a.b.causal ? min(max(tile0 - (s.nk - s.nq), 0) / TQ, blocks) : 0;
-  int t = start, hq = g * group;
-  const auto settle = [&] {
-    while (hq < (g + 1) * group) {
-      while (t < blocks && !wanted(t)) ++t;
-      if (t < blocks) return true;
-      t = start;
-      ++hq;
-    }
-    return false;
-  };
-
-  Stage<TQ> qs, gs;
-  float st_lse, st_delta;
-  int st_lo, st_hi;
-  const auto load = [&] {
-    qs.load(a.q, s.q0, s.nq, 64 * hq, t * TQ);
-    gs.load(a.dout, s.q0, s.nq, 64 * hq, t * TQ);
-    st_lse = st_delta = 0.f;
-    st_lo = st_hi = 0;
-    const int i = t * TQ + (int)threadIdx.x;
-    if (threadIdx.x < TQ && i < s.nq) {
-      const size_t stat = (size_t)hq * a.b.q_rows + s.q0 + i;
-      st_lse = a.lse[stat] * kLog2e;
-      st_delta = a.delta[stat];
-      const Keys r = keys_of(a.b, s, i);
-      st_lo = r.lo;
-      st_hi = st_lse == -INFINITY ? r.lo : max(r.hi, r.lo);
-      if (st_lse == -INFINITY) st_lse = 0.f;
-    }
-  };
-  const auto store = [&](char* to) {
-    qs.store(to);
-    gs.store(to + kTileBytes);
-    if (threadIdx.x < TQ) {
-      float* f = (float*)(to + 2 * kTileBytes) + threadIdx.x;
-      f[0] = st_lse;
-      f[TQ] = st_delta;
-      ((int*)f)[2 * TQ] = st_lo;
-      ((int*)f)[3 * TQ] = st_hi;
-    }
-  };
-
-  f32x16 dk[2] = {zeros(), zeros()}, dv[2] = {zeros(), zeros()};
-  bool some = settle();
-  if (some) {
-    load();
-    store(lds);
+  settled(k);
+  settled(v);
+}
+// 32 queries (tiles qt of q and gt of dout) and the wave's 32 keys, this lane's being key j.  stat: of the lane's first
+// query; cut: some of the queries do not see some of the keys.
+template <int TQ>
+__device__ __forceinline__ void dkv_block(const char* qt, const char* gt, const float* stat, bool cut, int j, const Lane& l,
+                                          const bf16x8 (&k)[4], const bf16x8 (&v)[4], f32x16 (&dk)[2], f32x16 (&dv)[2]) {
+  f32x16 x = zeros(), y;       // dP - delta: the product starts from -delta
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const f32x4 d = *(const f32x4*)(stat + TQ + 8 * e);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) y[4 * e + c] = d[c];
   }
-  __syncthreads();
-  for (int buf = 0; some; buf ^= kStageBytes) {
-    const int now = t;
-    ++t;
-    some = settle();
-    if (some) load();
 #pragma unroll
-    for (int n = 0; n < NB; ++n) {
-      const int u = KW == 4 ? n : w, block = now * (TQ / 32) + u;
-      if (block * 32 >= s.nq) continue;
-      const int4 r = ranges[block];
-      if (r.x >= j0 + 32 || r.y <= j0) continue;
-      const char* qt = lds + buf + u * 32 * kRowBytes;
-      const char* gt = qt + kTileBytes;
-      const float* stat = (const float*)(lds + buf + 2 * kTileBytes) + 32 * u + 4 * l.h;
-      f32x16 x = zeros(), y = zeros();
+  for (int c = 0; c < 4; ++c) x = mfma32(read_rows(qt, l, 0, c), k[c], x);
 #pragma unroll
-      for (int c = 0; c < 4; ++c) x = mfma32(read_rows(qt, l, 0, c), k[c], x);
+  for (int c = 0; c < 4; ++c) y = mfma32(read_rows(gt, l, 0, c), v[c], y);
+  if (cut) {
 #pragma unroll
-      for (int c = 0; c < 4; ++c) y = mfma32(read_rows(gt, l, 0, c), v[c], y);
-      if (j0 < r.z || min(j0 + 32, s.nk) > r.w) {
+    for (int e = 0; e < 4; ++e) {
+      const int4 lo = *(const int4*)(stat + 2 * TQ + 8 * e), hi = *(const int4*)(stat + 3 * TQ + 8 * e);
+      const int los[4] = {lo.x, lo.y, lo.z, lo.w}, his[4] = {hi.x, hi.y, hi.z, hi.w};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int4 lo = *(const int4*)(stat + 2 * TQ + 8 * e), hi = *(const int4*)(stat + 3 * TQ + 8 * e);
-          const int los[4] = {lo.x, lo.y, lo.z, lo.w}, his[4] = {hi.x, hi.y, hi.z, hi.w};
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            const bool seen = j >= los[c] && j < his[c];
-            x[4 * e + c] = seen ? x[4 * e + c] : -INFINITY;
-            y[4 * e + c] = seen ? y[4 * e + c] : 0.f;
-          }
-        }
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const f32x4 lse = *(const f32x4*)(stat + 8 * e), delta = *(const f32x4*)(stat + TQ + 8 * e);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          x[4 * e + c] = __builtin_amdgcn_exp2f(fmaf(x[4 * e + c], kScale2, -lse[c]));
-          y[4 * e + c] = x[4 * e + c] * (y[4 * e + c] - delta[c]);
-        }
-      }
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const bf16x8 p = narrow(x, 8 * c), ds = narrow(y, 8 * c);
-#pragma unroll
-        for (int d = 0; d < 2; ++d) {
-          dv[d] = mfma32(read_cols(gt, l, d, c), p, dv[d]);
-          dk[d] = mfma32(read_cols(qt, l, d, c), ds, dk[d]);
-        }
+      for (int c = 0; c < 4; ++c) {
+        const bool seen = j >= los[c] && j < his[c];
+        x[4 * e + c] = seen ? x[4 * e + c] : -INFINITY;
+        y[4 * e + c] = seen ? y[4 * e + c] : 0.f;
       }
     }
-    if (some) store(lds + (buf ^ kStageBytes));
-    __syncthreads();
   }
-
-  if constexpr (KW == 1) {
-    float* part = (float*)lds;
-    // (dk and dv of three waves are 48 KB)
-    if (w > 0)
 #pragma unroll
-      for (int d = 0; d < 2; ++d)
+  for (int e = 0; e < 4; ++e) {
+    const f32x4 lse = *(const f32x4*)(stat + 8 * e);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          part[((w - 1) * 64 + 16 * d + e) * 64 + threadIdx.x % kWave] = dk[d][e];
-          part[((w - 1) * 64 + 32 + 16 * d + e) * 64 + threadIdx.x % kWave] = dv[d][e];
-        }
-    __syncthreads();
-    if (w > 0) return;
-#pragma unroll
-    for (int d = 0; d < 2; ++d)
-#pragma unroll
-      for (int e = 0; e < 16; ++e)
-#pragma unroll
-        for (int u = 0; u < 3; ++u) {
-          dk[d][e] += part[(u * 64 + 16 * d + e) * 64 + threadIdx.x];
-          dv[d][e] += part[(u * 64 + 32 + 16 * d + e) * 64 + threadIdx.x];
-        }
+    for (int c = 0; c < 4; ++c) {
+      x[4 * e + c] = __builtin_amdgcn_exp2f(fmaf(x[4 * e + c], kScale2, -lse[c]));
+      y[4 * e + c] *= x[4 * e + c];
+    }
   }
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const bf16x8 p = narrow(x, 8 * c), ds = narrow(y, 8 * c);
+#pragma unroll
+    for (int d = 0; d < 2; ++d) {
+      dv[d] = mfma32(read_cols(gt, l, d, c), p, dv[d]);
+      dk[d] = mfma32(read_cols(qt, l, d, c), ds, dk[d]);
+    }
+  }
+}
+// The 32 keys from j0 on.
+__device__ __forceinline__ void dkv_out(const AttnBwdArgs& a, const Span& s, int g, int j0, const Lane& l, char* buf,
+                                        f32x16 (&dk)[2], f32x16 (&dv)[2]) {
+  const bool in = j0 + l.n < s.nk;
   bool bad = false;
 #pragma unroll
   for (int d = 0; d < 2; ++d)
@@ -893,18 +1146,165 @@ __global__ void __launch_bounds__(256, 2) attn_dkv_kernel(AttnBwdArgs a, int til
       dv[d][e] = in ? dv[d][e] : 0.f;
       bad |= !(fabsf(dk[d][e]) < INFINITY) || !(fabsf(dv[d][e]) < INFINITY);
     }
-  char* mine = lds + (KW == 1 ? 0 : w * 32 * 256);
-  by_rows(mine, l, dk, [&](int n, int c, const float(&x)[8]) {
+  by_rows(buf, l, dk, [&](int n, int c, const float(&x)[8]) {
     if (j0 + n < s.ok_) store_piece(a.dk, s.k0 + (int64_t)(j0 + n), g, c, narrow8(x));
   });
   __builtin_amdgcn_wave_barrier();
-  by_rows(mine, l, dv, [&](int n, int c, const float(&x)[8]) {
+  by_rows(buf, l, dv, [&](int n, int c, const float(&x)[8]) {
     if (j0 + n < s.ok_) store_piece(a.dv, s.k0 + (int64_t)(j0 + n), g, c, narrow8(x));
   });
   uint64_t again = __ballot(bad);
   again = (again | again >> 32) & 0xffffffffu;
   if (again) __threadfence_block();
   for (; again; again &= again - 1) dkv_row(a, s, g, j0 + __builtin_ctzll(again));
+}
+
+// Four waves of 32 keys share tiles of 64 queries.
+template <bool DIRECT>
+__global__ void __launch_bounds__(256, 2) attn_dkv_wide_kernel(AttnBwdArgs a, int tiles) {
+  constexpr int TQ = 64;
+  __shared__ uint4 q0[512], q1[512], g0[512], g1[512];
+  __shared__ __attribute__((aligned(16))) float stat0[4 * TQ], stat1[4 * TQ];
+  const Place at = place_of(tiles, a.b.kv_heads, a.b.batch, false);
+  if (!at.in) return;
+  const int g = at.h;
+  const Span s = span_of(a.b, at.b);
+  if (!s.ok) {
+    if (threadIdx.x == 0) atomicOr(a.b.err, AD_ERR_LENGTH);
+    return;
+  }
+  if (at.tile * 128 >= s.ok_) return;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const Lane l(threadIdx.x % kWave);
+  const int j0 = at.tile * 128 + 32 * w, j = j0 + l.n;
+  bf16x8 k[4], v[4];
+  keys_operands(a, s, g, j, l, k, v);
+  Walk<TQ> walk(a, s, at.b, g, at.tile * 128, min(at.tile * 128 + 128, s.nk));
+  Loads<DIRECT> qs, gs;
+  StatLoads<TQ> ss;
+  qs.init(a.q, s.q0, s.nq, 0);
+  gs.init(a.dout, s.q0, s.nq, 0);
+  f32x16 dk[2] = {zeros(), zeros()}, dv[2] = {zeros(), zeros()};
+  const auto issue = [&](uint4* qt, uint4* gt) {
+    qs.issue(walk.t * TQ, qt, 128 * walk.h);
+    gs.issue(walk.t * TQ, gt, 128 * walk.h);
+    ss.issue(a, s, walk.h, walk.t * TQ);
+  };
+  const auto arrive = [&](uint4* qt, uint4* gt, float* stat) {
+    qs.arrive(qt);
+    gs.arrive(gt);
+    ss.arrive(stat);
+  };
+  bool some = walk.settle();
+  const auto step = [&](const uint4* qt, const uint4* gt, const float* stat, uint4* next_qt, uint4* next_gt, float* next_stat) {
+    const int now = walk.t;
+    ++walk.t;
+    some = walk.settle();
+    if (some) issue(next_qt, next_gt);
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      const int u = 2 * now + n;
+      if (32 * u >= s.nq) continue;
+      const Range r = walk.seen(u);
+      if (r.lo >= j0 + 32 || r.hi <= j0) continue;
+      dkv_block<TQ>((const char*)qt + n * 32 * kRowBytes, (const char*)gt + n * 32 * kRowBytes, stat + 32 * n + 4 * l.h,
+                    j0 < r.all_lo || min(j0 + 32, s.nk) > r.all_hi, j, l, k, v, dk, dv);
+    }
+    if (some) arrive(next_qt, next_gt, next_stat);
+    landed();
+  };
+  if (some) {
+    issue(q0, g0);
+    arrive(q0, g0, stat0);
+    landed();
+    while (true) {
+      step(q0, g0, stat0, q1, g1, stat1);
+      if (!some) break;
+      step(q1, g1, stat1, q0, g0, stat0);
+      if (!some) break;
+    }
+  }
+  dkv_out(a, s, g, j0, l, (char*)(w == 0 ? q0 : w == 1 ? q1 : w == 2 ? g0 : g1), dk, dv);
+}
+
+// 32 keys, the four waves a quarter of each tile of 128 queries.
+__global__ void __launch_bounds__(256, 2) attn_dkv_few_kernel(AttnBwdArgs a, int tiles) {
+  constexpr int TQ = 128, kTileBytes = TQ * kRowBytes, kStageBytes = 2 * kTileBytes + 16 * TQ;
+  __shared__ __attribute__((aligned(16))) char lds[2 * kStageBytes];
+  const Place at = place_of(tiles, a.b.kv_heads, a.b.batch, false);
+  if (!at.in) return;
+  const int g = at.h;
+  const Span s = span_of(a.b, at.b);
+  if (!s.ok) {
+    if (threadIdx.x == 0) atomicOr(a.b.err, AD_ERR_LENGTH);
+    return;
+  }
+  const int j0 = at.tile * 32;
+  if (j0 >= s.ok_) return;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const Lane l(threadIdx.x % kWave);
+  const int j = j0 + l.n;
+  bf16x8 k[4], v[4];
+  keys_operands(a, s, g, j, l, k, v);
+  Walk<TQ> walk(a, s, at.b, g, j0, min(j0 + 32, s.nk));
+  Stage<TQ> qs, gs;
+  StatLoads<TQ> ss;
+  f32x16 dk[2] = {zeros(), zeros()}, dv[2] = {zeros(), zeros()};
+  const auto load = [&] {
+    qs.init(a.q, s.q0, s.nq, 64 * walk.h);
+    gs.init(a.dout, s.q0, s.nq, 64 * walk.h);
+    qs.load(walk.t * TQ);
+    gs.load(walk.t * TQ);
+    ss.issue(a, s, walk.h, walk.t * TQ);
+  };
+  const auto store = [&](char* to) {
+    qs.store(to);
+    gs.store(to + kTileBytes);
+    ss.arrive((float*)(to + 2 * kTileBytes));
+  };
+  bool some = walk.settle();
+  if (some) {
+    load();
+    store(lds);
+  }
+  __syncthreads();
+  for (int buf = 0; some; buf ^= kStageBytes) {
+    const int u = walk.t * (TQ / 32) + w;
+    ++walk.t;
+    some = walk.settle();
+    if (some) load();
+    if (32 * u < s.nq) {
+      const Range r = walk.seen(u);
+      if (r.lo < j0 + 32 && r.hi > j0)
+        dkv_block<TQ>(lds + buf + w * 32 * kRowBytes, lds + buf + kTileBytes + w * 32 * kRowBytes,
+                      (const float*)(lds + buf + 2 * kTileBytes) + 32 * w + 4 * l.h,
+                      j0 < r.all_lo || min(j0 + 32, s.nk) > r.all_hi, j, l, k, v, dk, dv);
+    }
+    if (some) store(lds + (buf ^ kStageBytes));
+    __syncthreads();
+  }
+  // the other waves' sums (48 KB) to the first one, which goes on alone
+  float* part = (float*)lds;
+  if (w > 0)
+#pragma unroll
+    for (int d = 0; d < 2; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        part[((w - 1) * 64 + 16 * d + e) * 64 + threadIdx.x % kWave] = dk[d][e];
+        part[((w - 1) * 64 + 32 + 16 * d + e) * 64 + threadIdx.x % kWave] = dv[d][e];
+      }
+  __syncthreads();
+  if (w > 0) return;
+#pragma unroll
+  for (int d = 0; d < 2; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+#pragma unroll
+      for (int u = 0; u < 3; ++u) {
+        dk[d][e] += part[(u * 64 + 16 * d + e) * 64 + threadIdx.x];
+        dv[d][e] += part[(u * 64 + 32 + 16 * d + e) * 64 + threadIdx.x];
+      }
+  dkv_out(a, s, g, j0, l, lds, dk, dv);
 }
 
 }  // namespace
@@ -946,12 +1346,16 @@ int64_t attn_groups(const AttnBatch& b) {
                    places((b.q_max + 31) / 32, b.heads, b.batch), places((b.k_max + 31) / 32, b.kv_heads, b.batch)});
 }
 
+// rows of 16-byte pieces
+bool whole(const HMat& m) { return (uintptr_t)m.p % 16 == 0 && m.ld % 8 == 0; }
+
 void launch_attention(const AttnFwdArgs& a, hipStream_t st) {
   const FwdPlan p = fwd_plan(a.b);
   const int grid = (int)places(p.tiles, a.b.heads, a.b.batch) * p.splits;
   if (!grid) return;
-  if (!p.few) attn_fwd_kernel<4><<<grid, 256, 0, st>>>(a, p.tiles, 1, 0);
-  else attn_fwd_kernel<1><<<grid, 256, 0, st>>>(a, p.tiles, p.splits, p.chunk);
+  if (p.few) attn_fwd_few_kernel<<<grid, 256, 0, st>>>(a, p.tiles, p.splits, p.chunk);
+  else if (whole(a.k) && whole(a.v)) attn_fwd_wide_kernel<true><<<grid, 256, 0, st>>>(a, p.tiles);
+  else attn_fwd_wide_kernel<false><<<grid, 256, 0, st>>>(a, p.tiles);
   if (p.splits > 1) {
     const int rows = (a.b.q_max + 3) / 4;
     attn_join_kernel<<<rows * a.b.heads * a.b.batch, 256, 0, st>>>(a, rows, p.splits);
@@ -968,16 +1372,18 @@ void launch_attention_backward(const AttnBwdArgs& args, hipStream_t st) {
   const int wide_q = (b.q_max + 127) / 128, wide_k = (b.k_max + 127) / 128;
   if (b.q_max > 0) {
     if ((int64_t)wide_q * b.heads * b.batch >= 512 && b.q_max > 32)
-      attn_dq_kernel<4><<<places(wide_q, b.heads, b.batch), 256, 0, st>>>(a, wide_q);
+      if (whole(a.k) && whole(a.v)) attn_dq_wide_kernel<true><<<places(wide_q, b.heads, b.batch), 256, 0, st>>>(a, wide_q);
+      else attn_dq_wide_kernel<false><<<places(wide_q, b.heads, b.batch), 256, 0, st>>>(a, wide_q);
     else
-      attn_dq_kernel<1><<<places(a.blocks, b.heads, b.batch), 256, 0, st>>>(a, a.blocks);
+      attn_dq_few_kernel<<<places(a.blocks, b.heads, b.batch), 256, 0, st>>>(a, a.blocks);
   }
   if (b.k_max > 0) {
     const int few_k = (b.k_max + 31) / 32;
     if ((int64_t)wide_k * b.kv_heads * b.batch >= 512 && b.k_max > 32)
-      attn_dkv_kernel<4><<<places(wide_k, b.kv_heads, b.batch), 256, 0, st>>>(a, wide_k);
+      if (whole(a.q) && whole(a.dout)) attn_dkv_wide_kernel<true><<<places(wide_k, b.kv_heads, b.batch), 256, 0, st>>>(a, wide_k);
+      else attn_dkv_wide_kernel<false><<<places(wide_k, b.kv_heads, b.batch), 256, 0, st>>>(a, wide_k);
     else
-      attn_dkv_kernel<1><<<places(few_k, b.kv_heads, b.batch), 256, 0, st>>>(a, few_k);
+      attn_dkv_few_kernel<<<places(few_k, b.kv_heads, b.batch), 256, 0, st>>>(a, few_k);
   }
 }
 

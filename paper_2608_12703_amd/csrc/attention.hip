@@ -1309,8 +1309,17 @@ __global__ void __launch_bounds__(256, 2) attn_dkv_few_kernel(AttnBwdArgs a, int
 
 }  // namespace
 
-// How a forward pass is cut: four waves of 32 queries where that gives every CU two workgroups, else 32
-// queries a workgroup, and where that leaves CUs without work the keys in `splits` parts of `chunk`.
+// Whether four waves take 32 rows each (of `rows` at most a sequence), or 32 rows together.  A wide workgroup has a tile
+// of 64 done in 0.9 us alone on its CU and in 0.75 among others, one of few rows 128 in 1.25 and 0.87: the
+// latter is worth it only while there are fewer than about 128 of the former (448 x 1500, 20 heads: 80
+// of them take 28.5 us, 280 small ones 21; 12 x 128 causal, 240: 8.7 and 12.7).  With windows a wide workgroup walks
+// over what 128 rows see, most of which each wave leaves out (12 x 131, windows of 41 in 1500: 35 and 25 us).
+bool wide_rows(const AttnBatch& b, int rows, int heads) {
+  return rows > 32 && (int64_t)((rows + 127) / 128) * heads * b.batch >= (b.window ? 1024 : 128);
+}
+
+// How a forward pass is cut; where even the small workgroups leave CUs without work, the keys in `splits` parts
+// of `chunk`.
 struct FwdPlan {
   bool few;
   int tiles, splits, chunk;
@@ -1319,7 +1328,7 @@ FwdPlan fwd_plan(const AttnBatch& b) {
   FwdPlan p = {false, (b.q_max + 127) / 128, 1, 0};
   if (!p.tiles || !b.batch) return p;
   const int64_t pairs = (int64_t)b.heads * b.batch;
-  if (pairs * p.tiles >= 512 && b.q_max > 32) return p;
+  if (wide_rows(b, b.q_max, b.heads)) return p;
   p.few = true;
   p.tiles = (b.q_max + 31) / 32;
   const int stages = std::max((b.k_max + 127) / 128, 1);
@@ -1368,10 +1377,9 @@ void launch_attention_backward(const AttnBwdArgs& args, hipStream_t st) {
   if (!b.batch) return;
   a.blocks = (b.q_max + 31) / 32;
   a.ranges = (int4*)((char*)a.delta + attn_bwd_delta_bytes(b));
-  // a tile a workgroup where that gives every CU two of them, else a quarter
   const int wide_q = (b.q_max + 127) / 128, wide_k = (b.k_max + 127) / 128;
   if (b.q_max > 0) {
-    if ((int64_t)wide_q * b.heads * b.batch >= 512 && b.q_max > 32)
+    if (wide_rows(b, b.q_max, b.heads))
       if (whole(a.k) && whole(a.v)) attn_dq_wide_kernel<true><<<places(wide_q, b.heads, b.batch), 256, 0, st>>>(a, wide_q);
       else attn_dq_wide_kernel<false><<<places(wide_q, b.heads, b.batch), 256, 0, st>>>(a, wide_q);
     else
@@ -1379,7 +1387,7 @@ void launch_attention_backward(const AttnBwdArgs& args, hipStream_t st) {
   }
   if (b.k_max > 0) {
     const int few_k = (b.k_max + 31) / 32;
-    if ((int64_t)wide_k * b.kv_heads * b.batch >= 512 && b.k_max > 32)
+    if (wide_rows(b, b.k_max, b.kv_heads))
       if (whole(a.q) && whole(a.dout)) attn_dkv_wide_kernel<true><<<places(wide_k, b.kv_heads, b.batch), 256, 0, st>>>(a, wide_k);
       else attn_dkv_wide_kernel<false><<<places(wide_k, b.kv_heads, b.batch), 256, 0, st>>>(a, wide_k);
     else

@@ -552,10 +552,12 @@ class Attention:
     """What an attention call knows of its batch (ad.h: ad_attn), kept from one call to the next: heads,
     the tables of the sequences' rows (int32 tensors, read when the kernels run) and which keys are visible.
     q_max and k_max bound the rows of a sequence.  err_flag (int32 [1]) collects AD_ERR_* bits; without
-    one the object has its own, `err_flag`."""
+    one the object has its own, `err_flag`.  covers: the caller says that every row of the matrices belongs to
+    a sequence (as its padding at least), which callers that sum over rows need to know."""
 
     def __init__(self, q_heads: int, kv_heads: int, cu_q, cu_k, q_max: int, k_max: int, q_len=None, k_len=None,
-                 causal: bool = False, window=None, err_flag=None):
+                 causal: bool = False, window=None, err_flag=None, covers: bool = False):
+        self.covers = covers
         self.batch = cu_q.shape[0] - 1
         if self.batch < 0:
             raise ValueError("cu_q needs at least one entry")

@@ -12,40 +12,6 @@ constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
 constexpr float kScale = 0.125f;                       // 1 / sqrt(64)
 constexpr float kScale2 = kScale * kLog2e;             // scores in powers of two
 
-// One sequence's rows; ok = false where its table entries are out of range.
-struct Span {
-  int q0, nq, oq, k0, nk, ok_;   // first row, rows that hold something, rows it owns; keys; keys it owns
-  bool ok;
-};
-__device__ __forceinline__ Span span_of(const AttnBatch& a, int b) {
-  Span s;
-  s.q0 = a.cu_q[b];
-  s.k0 = a.cu_k[b];
-  const int qe = a.cu_q[b + 1], ke = a.cu_k[b + 1];
-  s.ok = s.q0 >= 0 && qe >= s.q0 && qe <= a.q_rows && s.k0 >= 0 && ke >= s.k0 && ke <= a.k_rows;
-  s.oq = qe - s.q0;
-  s.ok_ = ke - s.k0;
-  s.nq = a.q_len ? a.q_len[b] : s.oq;
-  s.nk = a.k_len ? a.k_len[b] : s.ok_;
-  s.ok = s.ok && s.oq <= a.q_max && s.ok_ <= a.k_max && s.nq >= 0 && s.nq <= s.oq && s.nk >= 0 && s.nk <= s.ok_;
-  return s;
-}
-
-// The keys [lo, hi) that query i of the sequence sees (lo >= hi: none).
-struct Keys {
-  int lo, hi;
-};
-__device__ __forceinline__ Keys keys_of(const AttnBatch& a, const Span& s, int i) {
-  Keys r = {0, s.nk};
-  if (a.causal) r.hi = min(r.hi, max(i + s.nk - s.nq + 1, 0));
-  if (a.window) {
-    const int2 w = *(const int2*)(a.window + 2 * (size_t)(s.q0 + i));
-    r.lo = max(r.lo, w.x);
-    r.hi = min(r.hi, w.y);
-  }
-  return r;
-}
-
 __device__ __forceinline__ float at(const HMat& m, size_t row, int col) {
   return m.p ? bf16_to_f32(m.p[row * m.ld + col]) : 0.f;
 }
@@ -348,7 +314,6 @@ __device__ __forceinline__ Place place_of(int tiles, int heads, int batch, bool 
   r.in = pair < batch * heads;
   return r;
 }
-int64_t places(int64_t tiles, int64_t heads, int64_t batch) { return (heads * batch + 7) / 8 * 8 * tiles; }
 
 __device__ __forceinline__ int wave_min(int v) {
 #pragma unroll
@@ -1147,11 +1112,11 @@ __device__ __forceinline__ void dkv_out(const AttnBwdArgs& a, const Span& s, int
       bad |= !(fabsf(dk[d][e]) < INFINITY) || !(fabsf(dv[d][e]) < INFINITY);
     }
   by_rows(buf, l, dk, [&](int n, int c, const float(&x)[8]) {
-    if (j0 + n < s.ok_) store_piece(a.dk, s.k0 + (int64_t)(j0 + n), g, c, narrow8(x));
+    if (j0 + n < s.ow) store_piece(a.dk, s.k0 + (int64_t)(j0 + n), g, c, narrow8(x));
   });
   __builtin_amdgcn_wave_barrier();
   by_rows(buf, l, dv, [&](int n, int c, const float(&x)[8]) {
-    if (j0 + n < s.ok_) store_piece(a.dv, s.k0 + (int64_t)(j0 + n), g, c, narrow8(x));
+    if (j0 + n < s.ow) store_piece(a.dv, s.k0 + (int64_t)(j0 + n), g, c, narrow8(x));
   });
   uint64_t again = __ballot(bad);
   again = (again | again >> 32) & 0xffffffffu;
@@ -1173,7 +1138,7 @@ __global__ void __launch_bounds__(256, 2) attn_dkv_wide_kernel(AttnBwdArgs a, in
     if (threadIdx.x == 0) atomicOr(a.b.err, AD_ERR_LENGTH);
     return;
   }
-  if (at.tile * 128 >= s.ok_) return;
+  if (at.tile * 128 >= s.ow) return;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const Lane l(threadIdx.x % kWave);
   const int j0 = at.tile * 128 + 32 * w, j = j0 + l.n;
@@ -1240,7 +1205,7 @@ __global__ void __launch_bounds__(256, 2) attn_dkv_few_kernel(AttnBwdArgs a, int
     return;
   }
   const int j0 = at.tile * 32;
-  if (j0 >= s.ok_) return;
+  if (j0 >= s.ow) return;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const Lane l(threadIdx.x % kWave);
   const int j = j0 + l.n;
@@ -1308,52 +1273,6 @@ __global__ void __launch_bounds__(256, 2) attn_dkv_few_kernel(AttnBwdArgs a, int
 }
 
 }  // namespace
-
-// Whether four waves take 32 rows each (of `rows` at most a sequence), or 32 rows together.  A wide workgroup has a tile
-// of 64 done in 0.9 us alone on its CU and in 0.75 among others, one of few rows 128 in 1.25 and 0.87: the
-// latter is worth it only while there are fewer than about 128 of the former (448 x 1500, 20 heads: 80
-// of them take 28.5 us, 280 small ones 21; 12 x 128 causal, 240: 8.7 and 12.7).  With windows a wide workgroup walks
-// over what 128 rows see, most of which each wave leaves out (12 x 131, windows of 41 in 1500: 35 and 25 us).
-bool wide_rows(const AttnBatch& b, int rows, int heads) {
-  return rows > 32 && (int64_t)((rows + 127) / 128) * heads * b.batch >= (b.window ? 1024 : 128);
-}
-
-// How a forward pass is cut; where even the small workgroups leave CUs without work, the keys in `splits` parts
-// of `chunk`.
-struct FwdPlan {
-  bool few;
-  int tiles, splits, chunk;
-};
-FwdPlan fwd_plan(const AttnBatch& b) {
-  FwdPlan p = {false, (b.q_max + 127) / 128, 1, 0};
-  if (!p.tiles || !b.batch) return p;
-  const int64_t pairs = (int64_t)b.heads * b.batch;
-  if (wide_rows(b, b.q_max, b.heads)) return p;
-  p.few = true;
-  p.tiles = (b.q_max + 31) / 32;
-  const int stages = std::max((b.k_max + 127) / 128, 1);
-  const int64_t groups = pairs * p.tiles;
-  const int want = (int)std::min<int64_t>(std::min(stages, 64), std::max<int64_t>(512 / groups, 1));
-  const int each = (stages + want - 1) / want;
-  p.splits = (stages + each - 1) / each;
-  p.chunk = each * 128;
-  return p;
-}
-
-size_t attn_fwd_bytes(const AttnBatch& b) {
-  const FwdPlan p = fwd_plan(b);
-  return p.splits > 1 ? 4ull * 66 * p.splits * b.heads * b.q_rows : 0;
-}
-// delta [heads][q_rows], then what 32 queries of a sequence see together [batch][blocks]
-size_t attn_bwd_delta_bytes(const AttnBatch& b) { return (4ull * b.heads * b.q_rows + 255) / 256 * 256; }
-size_t attn_bwd_bytes(const AttnBatch& b) {
-  return attn_bwd_delta_bytes(b) + 16ull * b.batch * ((b.q_max + 31) / 32);
-}
-int64_t attn_groups(const AttnBatch& b) {
-  const FwdPlan p = fwd_plan(b);
-  return std::max({places(p.tiles, b.heads, b.batch) * p.splits, (int64_t)((b.q_max + 3) / 4) * b.heads * b.batch,
-                   places((b.q_max + 31) / 32, b.heads, b.batch), places((b.k_max + 31) / 32, b.kv_heads, b.batch)});
-}
 
 // rows of 16-byte pieces
 bool whole(const HMat& m) { return (uintptr_t)m.p % 16 == 0 && m.ld % 8 == 0; }

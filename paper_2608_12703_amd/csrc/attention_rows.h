@@ -1,0 +1,111 @@
+// Which rows of a batch belong to what, and how attention is cut into workgroups: rules on the tables and on
+// sizes, without the HIP headers.
+#pragma once
+
+#include <algorithm>
+#include <cstddef>
+#include <cstdint>
+
+#ifdef __HIPCC__
+#define AD_BOTH __host__ __device__ __forceinline__
+#else
+#define AD_BOTH inline
+#endif
+
+namespace ad {
+
+// What both passes know of a batch (ad_attn).
+struct AttnBatch {
+  int batch, heads, kv_heads, q_rows, k_rows, q_max, k_max, causal;
+  const int *cu_q, *cu_k, *q_len, *k_len, *window;
+  int* err;
+};
+AD_BOTH int smaller(int a, int b) { return a < b ? a : b; }
+AD_BOTH int larger(int a, int b) { return a > b ? a : b; }
+
+// One sequence's rows; ok = false where its table entries are out of range.
+struct Span {
+  int q0, nq, oq, k0, nk, ow;    // first row, rows that hold something, rows it owns; the same of the keys
+  bool ok;
+};
+AD_BOTH Span span_of(const AttnBatch& a, int b) {
+  Span s;
+  s.q0 = a.cu_q[b];
+  s.k0 = a.cu_k[b];
+  const int qe = a.cu_q[b + 1], ke = a.cu_k[b + 1];
+  s.ok = s.q0 >= 0 && qe >= s.q0 && qe <= a.q_rows && s.k0 >= 0 && ke >= s.k0 && ke <= a.k_rows;
+  s.oq = qe - s.q0;
+  s.ow = ke - s.k0;
+  s.nq = a.q_len ? a.q_len[b] : s.oq;
+  s.nk = a.k_len ? a.k_len[b] : s.ow;
+  s.ok = s.ok && s.oq <= a.q_max && s.ow <= a.k_max && s.nq >= 0 && s.nq <= s.oq && s.nk >= 0 && s.nk <= s.ow;
+  return s;
+}
+
+// The keys [lo, hi) that query i of the sequence sees (lo >= hi: none).
+struct Keys {
+  int lo, hi;
+};
+AD_BOTH Keys keys_of(const AttnBatch& a, const Span& s, int i) {
+  Keys r = {0, s.nk};
+  if (a.causal) r.hi = smaller(r.hi, larger(i + s.nk - s.nq + 1, 0));
+  if (a.window) {
+    const int* w = a.window + 2 * ((size_t)s.q0 + i);
+    r.lo = larger(r.lo, w[0]);
+    r.hi = smaller(r.hi, w[1]);
+  }
+  return r;
+}
+
+// ----------------------------------------------------------------- workgroups
+
+// Workgroups of a launch with this many tiles a (sequence, head): the pairs are dealt out over eight XCDs.
+inline int64_t places(int64_t tiles, int64_t heads, int64_t batch) { return (heads * batch + 7) / 8 * 8 * tiles; }
+
+// Whether four waves take 32 rows each (of `rows` at most a sequence), or 32 rows together.  A wide workgroup has a tile
+// of 64 done in 0.9 us alone on its CU and in 0.75 among others, one of few rows 128 in 1.25 and 0.87: the
+// latter is worth it only while there are fewer than about 128 of the former (448 x 1500, 20 heads: 80
+// of them take 28.5 us, 280 small ones 21; 12 x 128 causal, 240: 8.7 and 12.7).  With windows a wide workgroup walks
+// over what 128 rows see, most of which each wave leaves out (12 x 131, windows of 41 in 1500: 35 and 25 us).
+inline bool wide_rows(const AttnBatch& b, int rows, int heads) {
+  return rows > 32 && (int64_t)((rows + 127) / 128) * heads * b.batch >= (b.window ? 1024 : 128);
+}
+
+// How a forward pass is cut; where even the small workgroups leave CUs without work, the keys in `splits` parts
+// of `chunk`.
+struct FwdPlan {
+  bool few;
+  int tiles, splits, chunk;
+};
+inline FwdPlan fwd_plan(const AttnBatch& b) {
+  FwdPlan p = {false, (b.q_max + 127) / 128, 1, 0};
+  if (!p.tiles || !b.batch) return p;
+  const int64_t pairs = (int64_t)b.heads * b.batch;
+  if (wide_rows(b, b.q_max, b.heads)) return p;
+  p.few = true;
+  p.tiles = (b.q_max + 31) / 32;
+  const int stages = std::max((b.k_max + 127) / 128, 1);
+  const int64_t groups = pairs * p.tiles;
+  const int want = (int)std::min<int64_t>(std::min(stages, 64), std::max<int64_t>(512 / groups, 1));
+  const int each = (stages + want - 1) / want;
+  p.splits = (stages + each - 1) / each;
+  p.chunk = each * 128;
+  return p;
+}
+
+inline size_t attn_fwd_bytes(const AttnBatch& b) {
+  const FwdPlan p = fwd_plan(b);
+  return p.splits > 1 ? 4ull * 66 * p.splits * b.heads * b.q_rows : 0;
+}
+// delta [heads][q_rows], then what 32 queries of a sequence see together [batch][blocks]
+inline size_t attn_bwd_delta_bytes(const AttnBatch& b) { return (4ull * b.heads * b.q_rows + 255) / 256 * 256; }
+inline size_t attn_bwd_bytes(const AttnBatch& b) {
+  return attn_bwd_delta_bytes(b) + 16ull * b.batch * ((b.q_max + 31) / 32);
+}
+inline int64_t attn_groups(const AttnBatch& b) {
+  const FwdPlan p = fwd_plan(b);
+  return std::max({places(p.tiles, b.heads, b.batch) * p.splits, (int64_t)((b.q_max + 3) / 4) * b.heads * b.batch,
+                   places((b.q_max + 31) / 32, b.heads, b.batch), places((b.k_max + 31) / 32, b.kv_heads, b.batch)});
+}
+
+}  // namespace ad

@@ -4,6 +4,7 @@
 
 #include "common.h"
 #include "../../include/ad.h"
+#include "attention_rows.h"
 
 namespace ad {
 
@@ -322,12 +323,6 @@ struct HMat {
   int64_t ld;
 };
 
-// What both passes know of a batch (ad_attn).
-struct AttnBatch {
-  int batch, heads, kv_heads, q_rows, k_rows, q_max, k_max, causal;
-  const int *cu_q, *cu_k, *q_len, *k_len, *window;
-  int* err;
-};
 struct AttnFwdArgs {
   AttnBatch b;
   HMat q, k, v, o, rest;   // rest.p NULL: not kept
@@ -344,10 +339,6 @@ struct AttnBwdArgs {
   int4* ranges;            // [batch][blocks]
   int blocks;
 };
-size_t attn_fwd_bytes(const AttnBatch& b);
-size_t attn_bwd_bytes(const AttnBatch& b);
-// workgroups of the largest launch, to be held under 2^31
-int64_t attn_groups(const AttnBatch& b);
 void launch_attention(const AttnFwdArgs& a, hipStream_t st);
 void launch_attention_backward(const AttnBwdArgs& a, hipStream_t st);
 

@@ -259,17 +259,6 @@ __device__ __forceinline__ void landed() {
   __builtin_amdgcn_s_waitcnt(0x0070);
   __builtin_amdgcn_s_barrier();
 }
-// One product, and VALU instructions that run beside it, N times.
-template <int N, int READS, int VALU>
-__device__ __forceinline__ void interleave() {
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
-    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-    __builtin_amdgcn_sched_group_barrier(0x402, VALU, 0);
-  }
-}
-
 // A wave's transposed 64 x 32 result (columns l.n) as rows: out(row, c, v) with columns 8 c .. + 7 of row, eight lanes a
 // row, so that memory is accessed in whole rows.  buf: 8 KB of the wave's own; a row's 16-byte pieces p are at p ^ (row % 16).
 template <class F>
@@ -340,6 +329,22 @@ __device__ __forceinline__ Range range_of(const Keys& k, bool in) {
   return r;
 }
 
+// The same of the queries q0 .. + 31, of which this lane has q0 + l.n with `keys`: without windows from the rules alone.
+__device__ __forceinline__ Range range_at(const AttnBatch& a, const Span& s, int q0, const Keys& keys, bool in) {
+  if (a.window) return range_of(keys, in);
+  const int rows = min(32, s.nq - q0);
+  if (rows <= 0) return Range{0x7fffffff, 0, 0, 0x7fffffff};
+  if (!a.causal) return Range{0, s.nk, 0, s.nk};
+  const int first = q0 + s.nk - s.nq + 1;
+  return Range{0, min(s.nk, max(first + rows - 1, 0)), 0, min(s.nk, max(first, 0))};
+}
+
+// Without windows: the keys that the `rows` queries from q0 on see end here.
+__device__ __forceinline__ int ends_at(const AttnBatch& a, const Span& s, int q0, int rows) {
+  rows = min(rows, s.nq - q0);
+  return rows <= 0 ? 0 : a.causal ? min(s.nk, max(q0 + rows + s.nk - s.nq, 0)) : s.nk;
+}
+
 // ----------------------------------------------------------------- forward
 
 // 32 queries, the four waves a quarter of each tile of 128 keys: where there are few queries.  One pass over the
@@ -364,6 +369,15 @@ __global__ void __launch_bounds__(256, 2) attn_fwd_few_kernel(AttnFwdArgs a, int
   const Lane l(threadIdx.x % kWave);
   const int q0 = tile * 32, i = q0 + l.n;
   if (q0 >= s.oq) return;
+  Stage<TK> ks, vs;
+  ks.init(a.k, s.k0, s.nk, 64 * g);
+  vs.init(a.v, s.k0, s.nk, 64 * g);
+  // (without windows the first tile is under way before anything else is asked for)
+  const bool early = !a.b.window && split * chunk < ends_at(a.b, s, q0, 32);
+  if (early) {
+    ks.load(split * chunk);
+    vs.load(split * chunk);
+  }
   const bool in = i < s.nq;
   Keys keys = {0, s.nk};
   if (in) keys = keys_of(a.b, s, i);
@@ -371,7 +385,13 @@ __global__ void __launch_bounds__(256, 2) attn_fwd_few_kernel(AttnFwdArgs a, int
     keys.lo = max(keys.lo, split * chunk);
     keys.hi = min(keys.hi, (split + 1) * chunk);
   }
-  const Range r = range_of(keys, in);
+  Range r = range_at(a.b, s, q0, keys, in);
+  if (splits > 1 && !a.b.window) {
+    r.lo = max(r.lo, split * chunk);
+    r.hi = min(r.hi, (split + 1) * chunk);
+    r.all_lo = max(r.all_lo, split * chunk);
+    r.all_hi = min(r.all_hi, (split + 1) * chunk);
+  }
 
   bf16x8 q[4];
 #pragma unroll
@@ -385,12 +405,11 @@ __global__ void __launch_bounds__(256, 2) attn_fwd_few_kernel(AttnFwdArgs a, int
   const int first = r.lo / TK * TK, last = r.hi;
   float m = -INFINITY, sum = 0.f;
   f32x16 o[2] = {zeros(), zeros()};
-  Stage<TK> ks, vs;
-  ks.init(a.k, s.k0, s.nk, 64 * g);
-  vs.init(a.v, s.k0, s.nk, 64 * g);
   if (first < last) {
-    ks.load(first);
-    vs.load(first);
+    if (!early) {
+      ks.load(first);
+      vs.load(first);
+    }
     ks.store(lds);
     vs.store(lds + kTileBytes);
   }
@@ -531,6 +550,15 @@ __global__ void __launch_bounds__(256, DIRECT ? 4 : 2) attn_fwd_wide_kernel(Attn
   const Lane l(threadIdx.x % kWave);
   const int q0 = at.tile * 128 + 32 * w, i = q0 + l.n;
   const bool in = i < s.nq;
+  Loads<DIRECT> ks, vs;
+  ks.init(a.k, s.k0, s.nk, 64 * g);
+  vs.init(a.v, s.k0, s.nk, 64 * g);
+  // (without windows the first tile is under way before anything else is asked for)
+  int first = 0, last = ends_at(a.b, s, at.tile * 128, 128);
+  if (!a.b.window && last > 0) {
+    ks.issue(0, key0);
+    vs.issue(0, val0);
+  }
   bf16x8 q[4];
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
@@ -540,20 +568,23 @@ __global__ void __launch_bounds__(256, DIRECT ? 4 : 2) attn_fwd_wide_kernel(Attn
   }
   Keys keys = {0, s.nk};
   if (in) keys = keys_of(a.b, s, i);
-  const Range r = range_of(keys, in);
-  if (threadIdx.x % kWave == 0) {
-    ends[w] = r.lo;
-    ends[4 + w] = r.hi;
+  const Range r = range_at(a.b, s, q0, keys, in);
+  if (a.b.window) {
+    if (threadIdx.x % kWave == 0) {
+      ends[w] = r.lo;
+      ends[4 + w] = r.hi;
+    }
+    __syncthreads();
+    first = __builtin_amdgcn_readfirstlane(min(min(ends[0], ends[1]), min(ends[2], ends[3])) / TK * TK);
+    last = __builtin_amdgcn_readfirstlane(max(max(ends[4], ends[5]), max(ends[6], ends[7])));
+    if (first < last) {
+      ks.issue(first, key0);
+      vs.issue(first, val0);
+    }
   }
-  __syncthreads();
-  const int first = __builtin_amdgcn_readfirstlane(min(min(ends[0], ends[1]), min(ends[2], ends[3])) / TK * TK);
-  const int last = __builtin_amdgcn_readfirstlane(max(max(ends[4], ends[5]), max(ends[6], ends[7])));
 
   float m = -INFINITY, sum = 0.f;
   f32x16 o[2] = {zeros(), zeros()};
-  Loads<DIRECT> ks, vs;
-  ks.init(a.k, s.k0, s.nk, 64 * g);
-  vs.init(a.v, s.k0, s.nk, 64 * g);
   const auto step = [&](int k0, const uint4* kt, const uint4* vt, uint4* next_kt, uint4* next_vt) {
     const bool more = k0 + TK < last;
     if (more) {
@@ -614,9 +645,7 @@ __global__ void __launch_bounds__(256, DIRECT ? 4 : 2) attn_fwd_wide_kernel(Attn
   };
 
   if (first < last) {
-    ks.issue(first, key0);
     ks.arrive(key0);
-    vs.issue(first, val0);
     vs.arrive(val0);
     settled(q);
     landed();
@@ -672,9 +701,16 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnFwdArgs a, int tiles
   const float top = wave_max(mu), base = top == -INFINITY ? 0.f : top;
   const float f = __builtin_amdgcn_exp2f(mu - base);
   const float total = wave_sum(lu * f);
+  // (eight loads at once)
   float o = 0.f;
-  for (int u = 0; u < splits; ++u)
-    o = fmaf(a.part[(at + u * stride) * 64 + d], __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), u)), o);
+  for (int u0 = 0; u0 < splits; u0 += 8) {
+    float v[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v[u] = a.part[(at + min(u0 + u, splits - 1) * stride) * 64 + d];
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (u0 + u < splits) o = fmaf(v[u], __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), u0 + u)), o);
+  }
   o = total == 0.f ? 0.f : o / total;
   if (__any(!(fabsf(o) < INFINITY))) {
     fwd_row(a, s, h, i);
@@ -699,7 +735,6 @@ __device__ __forceinline__ void dq_operands(const AttnBwdArgs& a, const Span& s,
   if (in) {
     keys = keys_of(a.b, s, i);
     lse = a.lse[(size_t)h * a.b.q_rows + row] * kLog2e;
-    if (lse == -INFINITY) keys.hi = keys.lo;
   }
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
@@ -721,6 +756,7 @@ __device__ __forceinline__ void dq_operands(const AttnBwdArgs& a, const Span& s,
     for (int e = 0; e < 8; ++e) delta = fmaf(d[e], o[e] + r[e], delta);
   }
   delta += other_half(delta);
+  if (lse == -INFINITY) lse = INFINITY;     // sees nothing: p = exp2(s - inf) = 0
   settled(q);
   settled(go);
 }
@@ -783,25 +819,33 @@ __global__ void __launch_bounds__(256, 2) attn_dq_few_kernel(AttnBwdArgs a, int 
   const Lane l(threadIdx.x % kWave);
   const int q0 = at.tile * 32, i = q0 + l.n;
   if (q0 >= s.oq) return;
+  Stage<TK> ks, vs;
+  ks.init(a.k, s.k0, s.nk, 64 * g);
+  vs.init(a.v, s.k0, s.nk, 64 * g);
+  // (without windows the first tile is under way before anything else is asked for)
+  const bool early = !a.b.window && ends_at(a.b, s, q0, 32) > 0;
+  if (early) {
+    ks.load(0);
+    vs.load(0);
+  }
   const bool in = i < s.nq;
   bf16x8 q[4], go[4];
   float delta, lse;
   Keys keys;
   dq_operands(a, s, h, i, l, q, go, delta, lse, keys);
-  const Range r = range_of(keys, in);
+  const Range r = range_at(a.b, s, q0, keys, in);
   if (w == 0) {
     if (in && l.h == 0) a.delta[(size_t)h * a.b.q_rows + s.q0 + i] = delta;
-    if (h == 0 && threadIdx.x == 0 && q0 < s.nq)
+    if (a.b.window && h == 0 && threadIdx.x == 0 && q0 < s.nq)
       a.ranges[(size_t)at.b * a.blocks + at.tile] = make_int4(r.lo, r.hi, r.all_lo, r.all_hi);
   }
   const int first = r.lo / TK * TK, last = r.hi;
   f32x16 dq[2] = {zeros(), zeros()};
-  Stage<TK> ks, vs;
-  ks.init(a.k, s.k0, s.nk, 64 * g);
-  vs.init(a.v, s.k0, s.nk, 64 * g);
   if (first < last) {
-    ks.load(first);
-    vs.load(first);
+    if (!early) {
+      ks.load(first);
+      vs.load(first);
+    }
     ks.store(lds);
     vs.store(lds + kTileBytes);
   }
@@ -879,27 +923,39 @@ __global__ void __launch_bounds__(256, DIRECT ? 3 : 2) attn_dq_wide_kernel(AttnB
   const int q0 = at.tile * 128 + 32 * w, i = q0 + l.n;
   const bool in = i < s.nq;
   const int64_t row = s.q0 + (int64_t)i;
+  Loads<DIRECT> ks, vs;
+  ks.init(a.k, s.k0, s.nk, 64 * g);
+  vs.init(a.v, s.k0, s.nk, 64 * g);
+  // (without windows the first tile is under way before anything else is asked for)
+  int first = 0, last = ends_at(a.b, s, at.tile * 128, 128);
+  if (!a.b.window && last > 0) {
+    ks.issue(0, key0);
+    vs.issue(0, val0);
+  }
   bf16x8 q[4], go[4];
   float delta, lse;
   Keys keys;
   dq_operands(a, s, h, i, l, q, go, delta, lse, keys);
-  const Range r = range_of(keys, in);
+  const Range r = range_at(a.b, s, q0, keys, in);
   if (in && l.h == 0) a.delta[(size_t)h * a.b.q_rows + row] = delta;
-  if (threadIdx.x % kWave == 0) {
-    if (h == 0 && q0 < s.nq) a.ranges[(size_t)at.b * a.blocks + q0 / 32] = make_int4(r.lo, r.hi, r.all_lo, r.all_hi);
-    ends[w] = r.lo;
-    ends[4 + w] = r.hi;
+  if (a.b.window) {
+    if (threadIdx.x % kWave == 0) {
+      if (h == 0 && q0 < s.nq) a.ranges[(size_t)at.b * a.blocks + q0 / 32] = make_int4(r.lo, r.hi, r.all_lo, r.all_hi);
+      ends[w] = r.lo;
+      ends[4 + w] = r.hi;
+    }
+    __syncthreads();
+    first = __builtin_amdgcn_readfirstlane(min(min(ends[0], ends[1]), min(ends[2], ends[3])) / TK * TK);
+    last = __builtin_amdgcn_readfirstlane(max(max(ends[4], ends[5]), max(ends[6], ends[7])));
+    if (first < last) {
+      ks.issue(first, key0);
+      vs.issue(first, val0);
+    }
   }
-  __syncthreads();
-  const int first = __builtin_amdgcn_readfirstlane(min(min(ends[0], ends[1]), min(ends[2], ends[3])) / TK * TK);
-  const int last = __builtin_amdgcn_readfirstlane(max(max(ends[4], ends[5]), max(ends[6], ends[7])));
 
   f32x16 dq[2] = {zeros(), zeros()}, off;     // off: dP - delta starts from -delta
 #pragma unroll
   for (int e = 0; e < 16; ++e) off[e] = -delta;
-  Loads<DIRECT> ks, vs;
-  ks.init(a.k, s.k0, s.nk, 64 * g);
-  vs.init(a.v, s.k0, s.nk, 64 * g);
   const auto step = [&](int k0, const uint4* kt, const uint4* vt, uint4* next_kt, uint4* next_vt) {
     const bool more = k0 + TK < last;
     if (more) {
@@ -933,9 +989,7 @@ __global__ void __launch_bounds__(256, DIRECT ? 3 : 2) attn_dq_wide_kernel(AttnB
     landed();
   };
   if (first < last) {
-    ks.issue(first, key0);
     ks.arrive(key0);
-    vs.issue(first, val0);
     vs.arrive(val0);
     landed();
     for (int k0 = first; k0 < last; k0 += 2 * TK) {
@@ -954,31 +1008,33 @@ __global__ void __launch_bounds__(256, DIRECT ? 3 : 2) attn_dq_wide_kernel(AttnB
 // two (+infinity where a row sees nothing: p = 0), -delta, and the keys [lo, hi) that the query sees.
 template <int TQ>
 struct StatLoads {
-  float lse, off;
-  int lo, hi;
+  float lse, delta;
+  int lo, hi, i;
+  // (nothing waits for what is loaded here)
   __device__ __forceinline__ void issue(const AttnBwdArgs& a, const Span& s, int h, int i0) {
-    lse = off = 0.f;
-    lo = hi = 0;
-    const int i = i0 + (int)threadIdx.x;
+    i = i0 + (int)threadIdx.x;
+    lse = delta = 0.f;
+    lo = 0;
+    hi = s.nk;
     if (threadIdx.x < TQ && i < s.nq) {
       const size_t at = (size_t)h * a.b.q_rows + s.q0 + i;
-      lse = a.lse[at] * kLog2e;
-      off = -a.delta[at];
-      const Keys r = keys_of(a.b, s, i);
-      lo = r.lo;
-      hi = max(r.hi, r.lo);
-      if (lse == -INFINITY) {
-        hi = r.lo;
-        lse = INFINITY;
+      lse = a.lse[at];
+      delta = a.delta[at];
+      if (a.b.window) {
+        lo = a.b.window[2 * ((size_t)s.q0 + i)];
+        hi = a.b.window[2 * ((size_t)s.q0 + i) + 1];
       }
     }
   }
-  __device__ __forceinline__ void arrive(float* to) const {
+  __device__ __forceinline__ void arrive(const AttnBwdArgs& a, const Span& s, float* to) const {
     if (threadIdx.x < TQ) {
-      to[threadIdx.x] = lse;
-      to[TQ + threadIdx.x] = off;
+      const bool none = lse == -INFINITY || i >= s.nq;     // sees nothing
+      int end = min(hi, s.nk);
+      if (a.b.causal) end = min(end, i + s.nk - s.nq + 1);
+      to[threadIdx.x] = i >= s.nq ? 0.f : none ? INFINITY : lse * kLog2e;
+      to[TQ + threadIdx.x] = -delta;
       ((int*)to)[2 * TQ + threadIdx.x] = lo;
-      ((int*)to)[3 * TQ + threadIdx.x] = hi;
+      ((int*)to)[3 * TQ + threadIdx.x] = none ? lo : end;
     }
   }
 };
@@ -1142,8 +1198,6 @@ __global__ void __launch_bounds__(256, 2) attn_dkv_wide_kernel(AttnBwdArgs a, in
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const Lane l(threadIdx.x % kWave);
   const int j0 = at.tile * 128 + 32 * w, j = j0 + l.n;
-  bf16x8 k[4], v[4];
-  keys_operands(a, s, g, j, l, k, v);
   Walk<TQ> walk(a, s, at.b, g, at.tile * 128, min(at.tile * 128 + 128, s.nk));
   Loads<DIRECT> qs, gs;
   StatLoads<TQ> ss;
@@ -1158,9 +1212,12 @@ __global__ void __launch_bounds__(256, 2) attn_dkv_wide_kernel(AttnBwdArgs a, in
   const auto arrive = [&](uint4* qt, uint4* gt, float* stat) {
     qs.arrive(qt);
     gs.arrive(gt);
-    ss.arrive(stat);
+    ss.arrive(a, s, stat);
   };
   bool some = walk.settle();
+  if (some) issue(q0, g0);
+  bf16x8 k[4], v[4];
+  keys_operands(a, s, g, j, l, k, v);
   const auto step = [&](const uint4* qt, const uint4* gt, const float* stat, uint4* next_qt, uint4* next_gt, float* next_stat) {
     const int now = walk.t;
     ++walk.t;
@@ -1179,7 +1236,6 @@ __global__ void __launch_bounds__(256, 2) attn_dkv_wide_kernel(AttnBwdArgs a, in
     landed();
   };
   if (some) {
-    issue(q0, g0);
     arrive(q0, g0, stat0);
     landed();
     while (true) {
@@ -1225,7 +1281,7 @@ __global__ void __launch_bounds__(256, 2) attn_dkv_few_kernel(AttnBwdArgs a, int
   const auto store = [&](char* to) {
     qs.store(to);
     gs.store(to + kTileBytes);
-    ss.arrive((float*)(to + 2 * kTileBytes));
+    ss.arrive(a, s, (float*)(to + 2 * kTileBytes));
   };
   bool some = walk.settle();
   if (some) {
@@ -1306,7 +1362,7 @@ void launch_attention_backward(const AttnBwdArgs& args, hipStream_t st) {
   }
   if (b.k_max > 0) {
     const int few_k = (b.k_max + 31) / 32;
-    if (wide_rows(b, b.k_max, b.kv_heads))
+    if (wide_rows(b, b.k_max, b.kv_heads, true))
       if (whole(a.q) && whole(a.dout)) attn_dkv_wide_kernel<true><<<places(wide_k, b.kv_heads, b.batch), 256, 0, st>>>(a, wide_k);
       else attn_dkv_wide_kernel<false><<<places(wide_k, b.kv_heads, b.batch), 256, 0, st>>>(a, wide_k);
     else

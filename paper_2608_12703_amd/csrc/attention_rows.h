@@ -66,9 +66,10 @@ inline int64_t places(int64_t tiles, int64_t heads, int64_t batch) { return (hea
 // of 64 done in 0.9 us alone on its CU and in 0.75 among others, one of few rows 128 in 1.25 and 0.87: the
 // latter is worth it only while there are fewer than about 128 of the former (448 x 1500, 20 heads: 80
 // of them take 28.5 us, 280 small ones 21; 12 x 128 causal, 240: 8.7 and 12.7).  With windows a wide workgroup walks
-// over what 128 rows see, most of which each wave leaves out (12 x 131, windows of 41 in 1500: 35 and 25 us).
-inline bool wide_rows(const AttnBatch& b, int rows, int heads) {
-  return rows > 32 && (int64_t)((rows + 127) / 128) * heads * b.batch >= (b.window ? 1024 : 128);
+// over what 128 rows see, most of which each wave leaves out (12 x 131, windows of 41 in 1500: 35 and 25 us); a
+// workgroup of keys walks over the few queries that see them (36 and 76).
+inline bool wide_rows(const AttnBatch& b, int rows, int heads, bool keys = false) {
+  return rows > 32 && (int64_t)((rows + 127) / 128) * heads * b.batch >= (b.window && !keys ? 1024 : 128);
 }
 
 // How a forward pass is cut; where even the small workgroups leave CUs without work, the keys in `splits` parts

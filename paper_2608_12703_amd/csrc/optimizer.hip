@@ -2,7 +2,13 @@
 //
 // All of it streams each tensor once: the floor is HBM traffic.  A workgroup takes kChunk elements of
 // one tensor (the tensors of a launch are kernel arguments, found by their first workgroup), a
-// lane 8 consecutive elements at a time: 16-byte accesses of every type.
+// lane 4 consecutive elements at a time, so that a wave's float32 access is 1 KB side by side.
+//
+// Measured for a draft block of 29.5 million parameters (a large copy reaches 4.9 TB/s): float32 states with bf16 copies
+// 156 us for 885 MB (5.7 TB/s), 8-bit states 101 us for 535 MB, their values read back 47 us for 295 MB (6.3), the norm
+// 20 + 3 us for 118 MB.  Float32 goes past the caches (nontemporal): what a step reads it does not read again before the
+// next one.  Through the caches the first took 187 us and the third 107 (stores alone past them: 183 and 50); 8 elements a
+// lane 197 and 116.  Bytes go through the caches: past them a byte-aligned word became four accesses (86 us).
 #include <algorithm>
 
 #include "train.h"
@@ -12,69 +18,76 @@ namespace ad {
 
 namespace {
 
-constexpr int kPass = 2048, kChunk = 4 * kPass;   // elements that a workgroup has at once, and in all
-constexpr int kGroup = 128;                       // elements that share a scale: 16 lanes
+constexpr int kPass = 1024, kChunk = 8 * kPass;   // elements that a workgroup has at once, and in all
+constexpr int kGroup = 128;                       // elements that share a scale: 32 lanes
 
 // ----------------------------------------------------------------- elements of any alignment
 
-__device__ __forceinline__ void get8(const float* p, int n, float (&v)[8]) {
-  if (n >= 8) {
-    __builtin_memcpy(v, p, 32);
+constexpr int kE = 4;                             // consecutive elements of a lane: 16 bytes of float32
+
+typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
+// (KEEP: through the caches, for what is read again soon)
+template <bool KEEP = false>
+__device__ __forceinline__ void get(const float* p, int n, float (&v)[kE]) {
+  if (n >= kE) {
+    const f4 u = KEEP ? *(const f4*)p : __builtin_nontemporal_load((const f4*)p);
+#pragma unroll
+    for (int i = 0; i < kE; ++i) v[i] = u[i];
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.f;
+    for (int i = 0; i < kE; ++i) v[i] = i < n ? p[i] : 0.f;
   }
 }
-__device__ __forceinline__ void put8(float* p, int n, const float (&v)[8]) {
-  if (n >= 8) {
-    __builtin_memcpy(p, v, 32);
+__device__ __forceinline__ void put(float* p, int n, const float (&v)[kE]) {
+  if (n >= kE) {
+    __builtin_nontemporal_store(f4{v[0], v[1], v[2], v[3]}, (f4*)p);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < kE; ++i)
       if (i < n) p[i] = v[i];
   }
 }
-__device__ __forceinline__ void get8(const uint16_t* p, int n, float (&v)[8]) {
-  if (n >= 8) {
-    u32x4 u;
-    __builtin_memcpy(&u, p, 16);
-    widen8(u, v);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < n ? bf16_to_f32(p[i]) : 0.f;
-  }
-}
-__device__ __forceinline__ void put8(uint16_t* p, int n, u32x4 u) {
-  if (n >= 8) {
-    __builtin_memcpy(p, &u, 16);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < n) p[i] = (uint16_t)(u[i / 2] >> (16 * (i % 2)));
-  }
-}
-__device__ __forceinline__ u32x4 narrow8(const float (&v)[8]) {
-  return u32x4{f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]), f32x2_to_bf16x2(v[4], v[5]),
-               f32x2_to_bf16x2(v[6], v[7])};
-}
-__device__ __forceinline__ u32x2 get_bytes(const void* p, int n) {
-  u32x2 u = {0, 0};
-  if (n >= 8) {
+__device__ __forceinline__ void get(const uint16_t* p, int n, float (&v)[kE]) {
+  if (n >= kE) {
+    u32x2 u;
     __builtin_memcpy(&u, p, 8);
+#pragma unroll
+    for (int i = 0; i < kE; ++i) v[i] = __uint_as_float(i % 2 ? u[i / 2] & 0xffff0000u : u[i / 2] << 16);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < n) u[i / 4] |= (uint32_t)((const uint8_t*)p)[i] << (8 * (i % 4));
+    for (int i = 0; i < kE; ++i) v[i] = i < n ? bf16_to_f32(p[i]) : 0.f;
   }
-  return u;
 }
-__device__ __forceinline__ void put_bytes(void* p, int n, u32x2 u) {
-  if (n >= 8) {
+__device__ __forceinline__ void put(uint16_t* p, int n, u32x2 u) {
+  if (n >= kE) {
     __builtin_memcpy(p, &u, 8);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < n) ((uint8_t*)p)[i] = (uint8_t)(u[i / 4] >> (8 * (i % 4)));
+    for (int i = 0; i < kE; ++i)
+      if (i < n) p[i] = (uint16_t)(u[i / 2] >> (16 * (i % 2)));
+  }
+}
+__device__ __forceinline__ u32x2 narrow(const float (&v)[kE]) {
+  return u32x2{f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3])};
+}
+__device__ __forceinline__ uint32_t get_bytes(const void* p, int n) {
+  uint32_t u = 0;
+  if (n >= kE) {
+    __builtin_memcpy(&u, p, 4);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kE; ++i)
+      if (i < n) u |= (uint32_t)((const uint8_t*)p)[i] << (8 * i);
+  }
+  return u;
+}
+__device__ __forceinline__ void put_bytes(void* p, int n, uint32_t u) {
+  if (n >= kE) {
+    __builtin_memcpy(p, &u, 4);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kE; ++i)
+      if (i < n) ((uint8_t*)p)[i] = (uint8_t)(u >> (8 * i));
   }
 }
 
@@ -93,12 +106,14 @@ __host__ __device__ __forceinline__ uint32_t mix(uint32_t x) {
 // 16 bits as a threshold inside (0, 1); exact
 __device__ __forceinline__ float threshold(uint32_t bits) { return ((float)bits + 0.5f) * (1.0f / 65536.0f); }
 
-// Largest of 16 lanes, as the bits of magnitudes (a NaN is larger than an infinity).
+// Largest of 32 lanes, as the bits of magnitudes (a NaN is larger than an infinity).
 __device__ __forceinline__ uint32_t group_max(uint32_t m) {
   m = max(m, (uint32_t)ror16<8>((int)m));
   m = max(m, (uint32_t)ror16<4>((int)m));
   m = max(m, (uint32_t)ror16<2>((int)m));
-  return max(m, (uint32_t)ror16<1>((int)m));
+  m = max(m, (uint32_t)ror16<1>((int)m));
+  const auto r = __builtin_amdgcn_permlane16_swap(m, m, false, false);
+  return max(r[0], r[1]);
 }
 constexpr uint32_t kTiny = 0x0d800000u;           // 2^-100
 constexpr uint32_t kInf = 0x7f800000u;
@@ -129,15 +144,15 @@ __device__ __forceinline__ int code_v(float v, float inv, float r) {
   const float q = low + (x - low * low > r * (2.f * low + 1.f) ? 1.f : 0.f);
   return (int)__builtin_amdgcn_fmed3f(q, v > 0.f && inv > 0.f ? 1.f : 0.f, 255.f);
 }
-__device__ __forceinline__ void value_m(u32x2 q, float s, float (&v)[8]) {
+__device__ __forceinline__ void value_m(uint32_t q, float s, float (&v)[kE]) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = (float)(int8_t)(q[i / 4] >> (8 * (i % 4))) * s;
+  for (int i = 0; i < kE; ++i) v[i] = (float)(int8_t)(q >> (8 * i)) * s;
 }
-__device__ __forceinline__ void value_v(u32x2 q, float s, float (&v)[8]) {
+__device__ __forceinline__ void value_v(uint32_t q, float s, float (&v)[kE]) {
 #pragma clang fp contract(off)
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float r = (float)(uint8_t)(q[i / 4] >> (8 * (i % 4)));
+  for (int i = 0; i < kE; ++i) {
+    const float r = (float)(uint8_t)(q >> (8 * i));
     v[i] = r * r * s;
   }
 }
@@ -162,27 +177,27 @@ template <bool STATE8>
 __device__ __forceinline__ void adamw_pass(const OptTensor& t, const AdamwArgs& a, const Hyper& y, float keep, float gs,
                                            uint32_t key, int64_t i) {
 #pragma clang fp contract(off)
-  const int n = (int)min(t.n - i, (int64_t)8);          // may be <= 0: the lane only takes part in its group
-  float p[8] = {}, g[8] = {}, m[8] = {}, v[8] = {};
+  const int n = (int)min(t.n - i, (int64_t)kE);          // may be <= 0: the lane only takes part in its group
+  float p[kE] = {}, g[kE] = {}, m[kE] = {}, v[kE] = {};
   if (n > 0) {
-    if (t.kinds & OPT_GRAD16) get8((const uint16_t*)t.grad + i, n, g);
-    else get8((const float*)t.grad + i, n, g);
+    if (t.kinds & OPT_GRAD16) get((const uint16_t*)t.grad + i, n, g);
+    else get((const float*)t.grad + i, n, g);
     if (STATE8) {
       value_m(get_bytes((const int8_t*)t.m + i, n), t.m_scale[i / kGroup], m);
       value_v(get_bytes((const uint8_t*)t.v + i, n), t.v_scale[i / kGroup], v);
     } else {
-      get8((const float*)t.m + i, n, m);
-      get8((const float*)t.v + i, n, v);
+      get((const float*)t.m + i, n, m);
+      get((const float*)t.v + i, n, v);
     }
-    if (t.kinds & OPT_PARAM16) get8((const uint16_t*)t.param + i, n, p);
-    else get8((const float*)t.param + i, n, p);
+    if (t.kinds & OPT_PARAM16) get((const uint16_t*)t.param + i, n, p);
+    else get((const float*)t.param + i, n, p);
   }
-  uint32_t bits[8];
+  uint32_t bits[kE];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) bits[e] = mix(key + (uint32_t)(i + e) * kGolden);
+  for (int e = 0; e < kE; ++e) bits[e] = mix(key + (uint32_t)(i + e) * kGolden);
   uint32_t top_m = 0, top_v = 0;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
+  for (int e = 0; e < kE; ++e) {
     const float ge = g[e] * gs;
     m[e] = m[e] * a.b1 + ge * a.ob1;
     v[e] = v[e] * a.b2 + ge * ge * a.ob2;
@@ -195,21 +210,21 @@ __device__ __forceinline__ void adamw_pass(const OptTensor& t, const AdamwArgs& 
   }
   if (n > 0) {
     if (t.kinds & OPT_PARAM16) {
-      u32x4 u = {0, 0, 0, 0};
+      u32x2 u = {0, 0};
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
+      for (int e = 0; e < kE; ++e) {
         const uint32_t b = __float_as_uint(p[e]);
         const uint32_t up = (b & kInf) == kInf ? (uint32_t)f32_to_bf16(p[e]) : (b + (mix(bits[e] + kGolden) & 0xffffu)) >> 16;
         u[e / 2] |= up << (16 * (e % 2));
       }
-      put8((uint16_t*)t.param + i, n, u);
+      put((uint16_t*)t.param + i, n, u);
     } else {
-      put8((float*)t.param + i, n, p);
-      if (t.copy) put8((uint16_t*)t.copy + i, n, narrow8(p));
+      put((float*)t.param + i, n, p);
+      if (t.copy) put((uint16_t*)t.copy + i, n, narrow(p));
     }
     if (!STATE8) {
-      put8((float*)t.m + i, n, m);
-      put8((float*)t.v + i, n, v);
+      put((float*)t.m + i, n, m);
+      put((float*)t.v + i, n, v);
     }
   }
   if (STATE8) {
@@ -217,18 +232,13 @@ __device__ __forceinline__ void adamw_pass(const OptTensor& t, const AdamwArgs& 
     scale_of(group_max(top_m), 127.f, ms, mi);
     scale_of(group_max(top_v), 65025.f, vs, vi);
     if (n > 0) {
-      u32x2 qm, qv;
+      uint32_t cm[kE], cv[kE];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        uint32_t cm[4], cv[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          cm[e] = (uint32_t)code_m(m[4 * h + e], mi, threshold(bits[4 * h + e] & 0xffffu));
-          cv[e] = (uint32_t)code_v(v[4 * h + e], vi, threshold(bits[4 * h + e] >> 16));
-        }
-        qm[h] = pack_bytes(cm[0], cm[1], cm[2], cm[3]);
-        qv[h] = pack_bytes(cv[0], cv[1], cv[2], cv[3]);
+      for (int e = 0; e < kE; ++e) {
+        cm[e] = (uint32_t)code_m(m[e], mi, threshold(bits[e] & 0xffffu));
+        cv[e] = (uint32_t)code_v(v[e], vi, threshold(bits[e] >> 16));
       }
+      const uint32_t qm = pack_bytes(cm[0], cm[1], cm[2], cm[3]), qv = pack_bytes(cv[0], cv[1], cv[2], cv[3]);
       put_bytes((int8_t*)t.m + i, n, qm);
       put_bytes((uint8_t*)t.v + i, n, qv);
       if (i % kGroup == 0) {
@@ -262,7 +272,7 @@ __global__ void __launch_bounds__(256) adamw_kernel(OptList l, AdamwArgs a) {
   const uint32_t key = mix(t.key + y.key);
   const int64_t base = (int64_t)(blockIdx.x - l.first[&t - l.t]) * kChunk;
   for (int c = 0; c < kChunk; c += kPass) {
-    const int64_t i = base + c + 8 * threadIdx.x;
+    const int64_t i = base + c + kE * threadIdx.x;
     if (base + c >= t.n) break;
     if (t.kinds & OPT_STATE8) adamw_pass<true>(t, a, y, keep, gs, key, i);
     else adamw_pass<false>(t, a, y, keep, gs, key, i);
@@ -277,19 +287,19 @@ __global__ void __launch_bounds__(256) opt_state_kernel(OptList l, StateAt s, fl
   const OptTensor& t = l.t[k];
   const int64_t base = (int64_t)(blockIdx.x - l.first[k]) * kChunk;
   for (int c = 0; c < kChunk; c += kPass) {
-    const int64_t i = base + c + 8 * threadIdx.x;
-    const int n = (int)min(t.n - i, (int64_t)8);
+    const int64_t i = base + c + kE * threadIdx.x;
+    const int n = (int)min(t.n - i, (int64_t)kE);
     if (n <= 0) break;
-    float x[8];
+    float x[kE];
     if (m) {
       if (t.kinds & OPT_STATE8) value_m(get_bytes((const int8_t*)t.m + i, n), t.m_scale[i / kGroup], x);
-      else get8((const float*)t.m + i, n, x);
-      put8(m + s.at[k] + i, n, x);
+      else get((const float*)t.m + i, n, x);
+      put(m + s.at[k] + i, n, x);
     }
     if (v) {
       if (t.kinds & OPT_STATE8) value_v(get_bytes((const uint8_t*)t.v + i, n), t.v_scale[i / kGroup], x);
-      else get8((const float*)t.v + i, n, x);
-      put8(v + s.at[k] + i, n, x);
+      else get((const float*)t.v + i, n, x);
+      put(v + s.at[k] + i, n, x);
     }
   }
 }
@@ -311,26 +321,33 @@ __global__ void __launch_bounds__(256) grad_squares_kernel(OptList l, double* pa
   const int64_t base = (int64_t)(blockIdx.x - l.first[k]) * kChunk;
   double s = 0.0;
   for (int c = 0; c < kChunk; c += kPass) {
-    const int64_t i = base + c + 8 * threadIdx.x;
-    const int n = (int)min(t.n - i, (int64_t)8);
+    const int64_t i = base + c + kE * threadIdx.x;
+    const int n = (int)min(t.n - i, (int64_t)kE);
     if (n <= 0) break;
-    float g[8];
-    if (t.kinds & OPT_GRAD16) get8((const uint16_t*)t.grad + i, n, g);
-    else get8((const float*)t.grad + i, n, g);
+    float g[kE];
+    if (t.kinds & OPT_GRAD16) get((const uint16_t*)t.grad + i, n, g);
+    else get<true>((const float*)t.grad + i, n, g);      // (the step reads them next)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s = fma((double)g[e], (double)g[e], s);
+    for (int e = 0; e < kE; ++e) s = fma((double)g[e], (double)g[e], s);
   }
   s = block_total(s, red);
   if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
 
-__global__ void __launch_bounds__(256) grad_norm_kernel(const double* part, int64_t parts, double max_norm, float* out,
-                                                        int* step) {
-  __shared__ double red[4];
+__global__ void __launch_bounds__(1024) grad_norm_kernel(const double* part, int64_t parts, double max_norm, float* out,
+                                                         int* step) {
+  __shared__ double red[16];
   double s = 0.0;
-  for (int64_t i = threadIdx.x; i < parts; i += 256) s += part[i];
-  s = block_total(s, red);
+#pragma unroll 4
+  for (int64_t i = threadIdx.x; i < parts; i += 1024) s += part[i];
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) s += __shfl_xor(s, o, kWave);
+  if (threadIdx.x % kWave == 0) red[threadIdx.x / kWave] = s;
+  __syncthreads();
   if (threadIdx.x == 0) {
+    s = red[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) s += red[i];
     const double norm = sqrt(s);
     out[0] = (float)norm;
     const bool fine = (float)norm < INFINITY;           // (NaN is not)
@@ -356,7 +373,7 @@ void launch_grad_squares(const OptList& l, double* part, hipStream_t st) {
   if (l.first[l.count]) grad_squares_kernel<<<l.first[l.count], 256, 0, st>>>(l, part);
 }
 void launch_grad_norm(const double* part, int64_t parts, double max_norm, float* out, int* step, hipStream_t st) {
-  grad_norm_kernel<<<1, 256, 0, st>>>(part, parts, max_norm, out, step);
+  grad_norm_kernel<<<1, 1024, 0, st>>>(part, parts, max_norm, out, step);
 }
 
 }  // namespace ad

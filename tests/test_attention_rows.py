@@ -25,7 +25,7 @@ int main() {
     if (what == 'p') {
       if (next()) b.window = some;
       const FwdPlan p = fwd_plan(b);
-      printf("%d %d %d %d %d %zu %zu %lld\\n", p.few, p.tiles, p.splits, p.chunk, wide_rows(b, b.k_max, b.kv_heads),
+      printf("%d %d %d %d %d %zu %zu %lld\\n", p.few, p.tiles, p.splits, p.chunk, wide_rows(b, b.k_max, b.kv_heads, true),
              attn_fwd_bytes(b), attn_bwd_bytes(b), (long long)attn_groups(b));
       continue;
     }

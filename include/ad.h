@@ -516,7 +516,7 @@ ad_status ad_linear_wgrad(int32_t rows, int32_t n, int32_t k, const ad_mat* dy, 
  * that sequence is written; rows that a wrong table gives to two sequences may hold either's.
  */
 typedef struct {
-  int32_t batch;              /* sequences, 0 <= batch <= 65535                       */
+  int32_t batch;              /* sequences, 0 <= batch <= 65535, batch * q_heads <= 524280 */
   int32_t q_heads, kv_heads;  /* kv_heads divides q_heads                             */
   int32_t q_rows, k_rows;     /* rows of the matrices                                 */
   int32_t q_max, k_max;       /* no sequence owns more rows than this                 */
@@ -536,8 +536,8 @@ typedef struct {
  * for the backward pass: lse [q_heads][q_rows] float32, the row's log sum_j exp(s_ij), and o_rest (bf16,
  * as o), what o's rounding took away.  A row that sees no key, or only scores of -infinity, and a
  * padding row give o = o_rest = 0 and lse = -infinity.
- * workspace: device, >= ad_attention_workspace_size() bytes (of the sizes in a; the tables are
- * not read), 256-byte aligned, NULL where that is 0.
+ * workspace: device, >= ad_attention_workspace_size() bytes (of the sizes in a and of whether it has
+ * a window; the tables are not read), 256-byte aligned, NULL where that is 0.
  * Errors: AD_EINVAL (NULL argument, misaligned data, ld too small, heads that do not divide),
  * AD_ERANGE (sizes), AD_ENOSPACE, AD_EUNSUPPORTED (a float32 matrix), AD_EHIP.
  */

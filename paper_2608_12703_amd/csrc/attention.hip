@@ -12,6 +12,8 @@ constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
 constexpr float kScale = 0.125f;                       // 1 / sqrt(64)
 constexpr float kScale2 = kScale * kLog2e;             // scores in powers of two
 
+__device__ __forceinline__ int key_head(const AttnBatch& a, int h) { return a.group == 1 ? h : h / a.group; }
+
 __device__ __forceinline__ float at(const HMat& m, size_t row, int col) {
   return m.p ? bf16_to_f32(m.p[row * m.ld + col]) : 0.f;
 }
@@ -19,7 +21,7 @@ __device__ __forceinline__ float at(const HMat& m, size_t row, int col) {
 // A row at a time, a lane a dimension: what is right whatever the keys hold, since only visible
 // ones are read.
 __device__ void fwd_row(const AttnFwdArgs& a, const Span& s, int h, int i) {
-  const int d = threadIdx.x % kWave, g = h / (a.b.heads / a.b.kv_heads);
+  const int d = threadIdx.x % kWave, g = key_head(a.b, h);
   const size_t row = s.q0 + i;
   float m = -INFINITY, l = 0.f, o = 0.f;
   if (i < s.nq) {
@@ -43,14 +45,13 @@ __device__ void fwd_row(const AttnFwdArgs& a, const Span& s, int h, int i) {
 }
 
 __device__ void dq_row(const AttnBwdArgs& a, const Span& s, int h, int i) {
-  const int d = threadIdx.x % kWave, g = h / (a.b.heads / a.b.kv_heads);
+  const int d = threadIdx.x % kWave, g = key_head(a.b, h);
   const size_t row = s.q0 + i;
   float acc = 0.f;
   if (i < s.nq) {
     const float q = at(a.q, row, 64 * h + d) * kScale2, go = at(a.dout, row, 64 * h + d);
     const float delta = wave_sum(go * (at(a.o, row, 64 * h + d) + at(a.rest, row, 64 * h + d)));
     const float lse = a.lse[(size_t)h * a.b.q_rows + row] * kLog2e;
-    if (d == 0) a.delta[(size_t)h * a.b.q_rows + row] = delta;
     Keys r = keys_of(a.b, s, i);
     if (lse == -INFINITY) r.hi = r.lo;
     for (int j = r.lo; j < r.hi; ++j) {
@@ -67,7 +68,7 @@ __device__ void dq_row(const AttnBwdArgs& a, const Span& s, int h, int i) {
 }
 
 __device__ void dkv_row(const AttnBwdArgs& a, const Span& s, int g, int j) {
-  const int d = threadIdx.x % kWave, n = a.b.heads / a.b.kv_heads;
+  const int d = threadIdx.x % kWave, n = a.b.group;
   const size_t row = s.k0 + j;
   float dk = 0.f, dv = 0.f;
   if (j < s.nk) {
@@ -80,7 +81,7 @@ __device__ void dkv_row(const AttnBwdArgs& a, const Span& s, int g, int j) {
         if (j < r.lo || j >= r.hi || lse == -INFINITY) continue;
         const float q = at(a.q, qr, 64 * h + d), go = at(a.dout, qr, 64 * h + d);
         const float p = __builtin_amdgcn_exp2f(wave_sum(q * k) - lse);
-        const float ds = p * (wave_sum(go * v) - a.delta[(size_t)h * a.b.q_rows + qr]);
+        const float ds = p * wave_sum(go * (v - at(a.o, qr, 64 * h + d) - at(a.rest, qr, 64 * h + d)));   // dP - delta
         dk = fmaf(ds, q, dk);
         dv = fmaf(p, go, dv);
       }
@@ -288,19 +289,20 @@ __device__ __forceinline__ void store_piece(const HMat& m, int64_t row, int h, i
   __builtin_memcpy(m.p + row * m.ld + 64 * h + 8 * c, &u, 16);
 }
 
-// The tiles of one (sequence, head) follow each other on one of the eight XCDs, whose L2 then has its
-// keys: workgroup id i runs on XCD i % 8.
+// The tiles of one (sequence, head) run on one of the eight XCDs, whose L2 then has its keys: workgroups are dealt
+// to them in turn, and a row of the grid holds 8 pairs times their tiles.
 struct Place {
   int b, h, tile;
   bool in;
 };
-__device__ __forceinline__ Place place_of(int tiles, int heads, int batch, bool last_first) {
-  const int slot = blockIdx.x / 8, pair = slot / tiles * 8 + blockIdx.x % 8, t = slot % tiles;
+// (a quotient by a product: the prologue is as long as its instructions)
+__device__ __forceinline__ Place place_of(int heads, uint64_t per_head, int batch) {
+  const int pair = blockIdx.y * 8 + blockIdx.x % 8;
   Place r;
-  r.b = pair / heads;
-  r.h = pair % heads;
-  r.tile = last_first ? tiles - 1 - t : t;
-  r.in = pair < batch * heads;
+  r.b = (int)(((uint64_t)pair * per_head) >> kPerShift);
+  r.h = pair - r.b * heads;
+  r.tile = blockIdx.x / 8;
+  r.in = r.b < batch;
   return r;
 }
 
@@ -355,17 +357,16 @@ constexpr float kLazy = 8.f;
 __global__ void __launch_bounds__(256, 2) attn_fwd_few_kernel(AttnFwdArgs a, int tiles, int splits, int chunk) {
   constexpr int TK = 128, kTileBytes = TK * kRowBytes;
   __shared__ __attribute__((aligned(16))) char lds[4 * kTileBytes];   // two stages of keys and values
-  const int split = blockIdx.x % splits;
-  const int slot = blockIdx.x / splits / 8, pair = slot / tiles * 8 + blockIdx.x / splits % 8;
-  const int b = pair / a.b.heads, h = pair % a.b.heads;
-  const int tile = a.b.causal ? tiles - 1 - slot % tiles : slot % tiles;
-  if (pair >= a.b.batch * a.b.heads) return;
+  const Place at = place_of(a.b.heads, a.b.per_head, a.b.batch);
+  if (!at.in) return;
+  const int split = splits > 1 ? at.tile % splits : 0, nth = splits > 1 ? at.tile / splits : at.tile;
+  const int b = at.b, h = at.h, tile = a.b.causal ? tiles - 1 - nth : nth;
   const Span s = span_of(a.b, b);
   if (!s.ok) {
     if (threadIdx.x == 0) atomicOr(a.b.err, AD_ERR_LENGTH);
     return;
   }
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), g = h / (a.b.heads / a.b.kv_heads);
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), g = key_head(a.b, h);
   const Lane l(threadIdx.x % kWave);
   const int q0 = tile * 32, i = q0 + l.n;
   if (q0 >= s.oq) return;
@@ -414,7 +415,7 @@ __global__ void __launch_bounds__(256, 2) attn_fwd_few_kernel(AttnFwdArgs a, int
     vs.store(lds + kTileBytes);
   }
   __syncthreads();
-  for (int k0 = first, at = 0; k0 < last; k0 += TK, at ^= 2 * kTileBytes) {
+  for (int k0 = first, buf = 0; k0 < last; k0 += TK, buf ^= 2 * kTileBytes) {
     const bool more = k0 + TK < last;
     if (more) {
       ks.load(k0 + TK);
@@ -422,7 +423,7 @@ __global__ void __launch_bounds__(256, 2) attn_fwd_few_kernel(AttnFwdArgs a, int
     }
     const int mine = k0 + 32 * w;            // this wave's first key
     if (mine < r.hi && mine + 32 > r.lo) {
-      const char* kt = lds + at + w * 32 * kRowBytes;
+      const char* kt = lds + buf + w * 32 * kRowBytes;
       const char* vt = kt + kTileBytes;
       f32x16 x = zeros();
 #pragma unroll
@@ -460,8 +461,8 @@ __global__ void __launch_bounds__(256, 2) attn_fwd_few_kernel(AttnFwdArgs a, int
       }
     }
     if (more) {
-      ks.store(lds + (at ^ (2 * kTileBytes)));
-      vs.store(lds + (at ^ (2 * kTileBytes)) + kTileBytes);
+      ks.store(lds + (buf ^ (2 * kTileBytes)));
+      vs.store(lds + (buf ^ (2 * kTileBytes)) + kTileBytes);
     }
     __syncthreads();
   }
@@ -495,13 +496,13 @@ __global__ void __launch_bounds__(256, 2) attn_fwd_few_kernel(AttnFwdArgs a, int
   const bool live = row < s.oq, some = row < s.nq && total != 0.f;
   if (splits > 1) {
     if (!live) return;
-    const size_t at = ((size_t)split * a.b.heads + h) * a.b.q_rows + s.q0 + row;
+    const size_t to = ((size_t)split * a.b.heads + h) * a.b.q_rows + s.q0 + row;
     const size_t rows = (size_t)splits * a.b.heads * a.b.q_rows;
-    *(f32x4*)(a.part + at * 64 + d0) = f32x4{v[0], v[1], v[2], v[3]};
-    *(f32x4*)(a.part + at * 64 + d0 + 4) = f32x4{v[4], v[5], v[6], v[7]};
+    *(f32x4*)(a.part + to * 64 + d0) = f32x4{v[0], v[1], v[2], v[3]};
+    *(f32x4*)(a.part + to * 64 + d0 + 4) = f32x4{v[4], v[5], v[6], v[7]};
     if (d0 == 0) {
-      a.part[rows * 64 + at] = some ? top : -INFINITY;
-      a.part[rows * 65 + at] = some ? total : 0.f;
+      a.part[rows * 64 + to] = some ? top : -INFINITY;
+      a.part[rows * 65 + to] = some ? total : 0.f;
     }
     return;
   }
@@ -537,8 +538,9 @@ __global__ void __launch_bounds__(256, DIRECT ? 4 : 2) attn_fwd_wide_kernel(Attn
   // (distinct objects, so that the compiler can tell a read of one tile from the loads that fill another)
   __shared__ uint4 key0[512], key1[512], val0[512], val1[512];
   __shared__ int ends[8];
-  const Place at = place_of(tiles, a.b.heads, a.b.batch, a.b.causal);
+  Place at = place_of(a.b.heads, a.b.per_head, a.b.batch);
   if (!at.in) return;
+  if (a.b.causal) at.tile = tiles - 1 - at.tile;        // (the longest first)
   const int h = at.h;
   const Span s = span_of(a.b, at.b);
   if (!s.ok) {
@@ -546,7 +548,7 @@ __global__ void __launch_bounds__(256, DIRECT ? 4 : 2) attn_fwd_wide_kernel(Attn
     return;
   }
   if (at.tile * 128 >= s.oq) return;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), g = h / (a.b.heads / a.b.kv_heads);
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), g = key_head(a.b, h);
   const Lane l(threadIdx.x % kWave);
   const int q0 = at.tile * 128 + 32 * w, i = q0 + l.n;
   const bool in = i < s.nq;
@@ -688,8 +690,8 @@ __global__ void __launch_bounds__(256, DIRECT ? 4 : 2) attn_fwd_wide_kernel(Attn
 }
 
 // The parts of a row's keys joined: a wave a row and head, a lane a dimension.
-__global__ void __launch_bounds__(256) attn_join_kernel(AttnFwdArgs a, int tiles, int splits) {
-  const int tile = blockIdx.x % tiles, h = blockIdx.x / tiles % a.b.heads, b = blockIdx.x / tiles / a.b.heads;
+__global__ void __launch_bounds__(256) attn_join_kernel(AttnFwdArgs a, int splits) {
+  const int tile = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
   const Span s = span_of(a.b, b);
   const int i = tile * 4 + threadIdx.x / kWave, d = threadIdx.x % kWave;
   if (!s.ok || i >= s.oq) return;
@@ -807,15 +809,16 @@ __device__ __forceinline__ void dq_out(const AttnBwdArgs& a, const Span& s, int 
 __global__ void __launch_bounds__(256, 2) attn_dq_few_kernel(AttnBwdArgs a, int tiles) {
   constexpr int TK = 128, kTileBytes = TK * kRowBytes;
   __shared__ __attribute__((aligned(16))) char lds[4 * kTileBytes];
-  const Place at = place_of(tiles, a.b.heads, a.b.batch, a.b.causal);
+  Place at = place_of(a.b.heads, a.b.per_head, a.b.batch);
   if (!at.in) return;
+  if (a.b.causal) at.tile = tiles - 1 - at.tile;        // (the longest first)
   const int h = at.h;
   const Span s = span_of(a.b, at.b);
   if (!s.ok) {
     if (threadIdx.x == 0) atomicOr(a.b.err, AD_ERR_LENGTH);
     return;
   }
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), g = h / (a.b.heads / a.b.kv_heads);
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), g = key_head(a.b, h);
   const Lane l(threadIdx.x % kWave);
   const int q0 = at.tile * 32, i = q0 + l.n;
   if (q0 >= s.oq) return;
@@ -905,12 +908,13 @@ __global__ void __launch_bounds__(256, 2) attn_dq_few_kernel(AttnBwdArgs a, int 
 // products more, dP^T = V dO^T and, from dS, dQ^T = K^T dS^T.  It leaves delta and what 32 queries see
 // together for the kernel of dk and dv.
 template <bool DIRECT>
-__global__ void __launch_bounds__(256, DIRECT ? 3 : 2) attn_dq_wide_kernel(AttnBwdArgs a, int tiles) {
+__device__ __forceinline__ void dq_wide(const AttnBwdArgs& a, int tiles) {
   constexpr int TK = 64;
   __shared__ uint4 key0[512], key1[512], val0[512], val1[512];
   __shared__ int ends[8];
-  const Place at = place_of(tiles, a.b.heads, a.b.batch, a.b.causal);
+  Place at = place_of(a.b.heads, a.b.per_head, a.b.batch);
   if (!at.in) return;
+  if (a.b.causal) at.tile = tiles - 1 - at.tile;        // (the longest first)
   const int h = at.h;
   const Span s = span_of(a.b, at.b);
   if (!s.ok) {
@@ -918,7 +922,7 @@ __global__ void __launch_bounds__(256, DIRECT ? 3 : 2) attn_dq_wide_kernel(AttnB
     return;
   }
   if (at.tile * 128 >= s.oq) return;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), g = h / (a.b.heads / a.b.kv_heads);
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), g = key_head(a.b, h);
   const Lane l(threadIdx.x % kWave);
   const int q0 = at.tile * 128 + 32 * w, i = q0 + l.n;
   const bool in = i < s.nq;
@@ -937,7 +941,7 @@ __global__ void __launch_bounds__(256, DIRECT ? 3 : 2) attn_dq_wide_kernel(AttnB
   Keys keys;
   dq_operands(a, s, h, i, l, q, go, delta, lse, keys);
   const Range r = range_at(a.b, s, q0, keys, in);
-  if (in && l.h == 0) a.delta[(size_t)h * a.b.q_rows + row] = delta;
+  if (a.delta && in && l.h == 0) a.delta[(size_t)h * a.b.q_rows + row] = delta;
   if (a.b.window) {
     if (threadIdx.x % kWave == 0) {
       if (h == 0 && q0 < s.nq) a.ranges[(size_t)at.b * a.blocks + q0 / 32] = make_int4(r.lo, r.hi, r.all_lo, r.all_hi);
@@ -1001,22 +1005,43 @@ __global__ void __launch_bounds__(256, DIRECT ? 3 : 2) attn_dq_wide_kernel(AttnB
   dq_out(a, s, h, q0, in, l, (char*)(w == 0 ? key0 : w == 1 ? key1 : w == 2 ? val0 : val1), dq);
 }
 
+template <bool DIRECT>
+__global__ void __launch_bounds__(256, DIRECT ? 3 : 2) attn_dq_wide_kernel(AttnBwdArgs a, int tiles) {
+  dq_wide<DIRECT>(a, tiles);
+}
+
 // dk and dv: the same with the queries on the rows (S = Q K^T), a wave 32 keys and all of the queries that
 // see them, of every head that shares them.
 
 // What the products need of a tile's TQ queries besides their rows, on its way to LDS: [TQ] each of lse in powers of
 // two (+infinity where a row sees nothing: p = 0), -delta, and the keys [lo, hi) that the query sees.
-template <int TQ>
+// OWN (TQ = 64): delta is computed here, four threads a query.
+template <int TQ, bool OWN = false>
 struct StatLoads {
   float lse, delta;
   int lo, hi, i;
+  uint4 row[OWN ? 6 : 1];
   // (nothing waits for what is loaded here)
   __device__ __forceinline__ void issue(const AttnBwdArgs& a, const Span& s, int h, int i0) {
-    i = i0 + (int)threadIdx.x;
+    i = i0 + (int)(OWN ? threadIdx.x / 4 : threadIdx.x);
     lse = delta = 0.f;
     lo = 0;
     hi = s.nk;
-    if (threadIdx.x < TQ && i < s.nq) {
+    if constexpr (OWN) {
+#pragma unroll
+      for (int c = 0; c < 6; ++c) row[c] = make_uint4(0, 0, 0, 0);
+      if (i < s.nq) {
+        const int64_t r = s.q0 + (int64_t)i;
+        const int col = 64 * h + 16 * (threadIdx.x % 4);
+        lse = a.lse[(size_t)h * a.b.q_rows + r];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          row[c] = load16(a.dout.p + r * a.dout.ld + col + 8 * c);
+          row[2 + c] = load16(a.o.p + r * a.o.ld + col + 8 * c);
+          if (a.rest.p) row[4 + c] = load16(a.rest.p + r * a.rest.ld + col + 8 * c);
+        }
+      }
+    } else if (threadIdx.x < TQ && i < s.nq) {
       const size_t at = (size_t)h * a.b.q_rows + s.q0 + i;
       lse = a.lse[at];
       delta = a.delta[at];
@@ -1026,15 +1051,29 @@ struct StatLoads {
       }
     }
   }
-  __device__ __forceinline__ void arrive(const AttnBwdArgs& a, const Span& s, float* to) const {
-    if (threadIdx.x < TQ) {
+  __device__ __forceinline__ void arrive(const AttnBwdArgs& a, const Span& s, float* to) {
+    if constexpr (OWN) {
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        float d[8], o[8], r[8];
+        widen8(__builtin_bit_cast(u32x4, row[c]), d);
+        widen8(__builtin_bit_cast(u32x4, row[2 + c]), o);
+        widen8(__builtin_bit_cast(u32x4, row[4 + c]), r);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) delta = fmaf(d[e], o[e] + r[e], delta);
+      }
+      delta += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(delta), 0xB1, 0xf, 0xf, false));   // lane ^ 1
+      delta += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(delta), 0x4E, 0xf, 0xf, false));   // lane ^ 2
+    }
+    const int n = OWN ? threadIdx.x / 4 : threadIdx.x;
+    if (OWN ? threadIdx.x % 4 == 0 : threadIdx.x < TQ) {
       const bool none = lse == -INFINITY || i >= s.nq;     // sees nothing
       int end = min(hi, s.nk);
       if (a.b.causal) end = min(end, i + s.nk - s.nq + 1);
-      to[threadIdx.x] = i >= s.nq ? 0.f : none ? INFINITY : lse * kLog2e;
-      to[TQ + threadIdx.x] = -delta;
-      ((int*)to)[2 * TQ + threadIdx.x] = lo;
-      ((int*)to)[3 * TQ + threadIdx.x] = none ? lo : end;
+      to[n] = i >= s.nq ? 0.f : none ? INFINITY : lse * kLog2e;
+      to[TQ + n] = -delta;
+      ((int*)to)[2 * TQ + n] = lo;
+      ((int*)to)[3 * TQ + n] = none ? lo : end;
     }
   }
 };
@@ -1056,7 +1095,7 @@ struct Walk {
     tiles = (nq + TQ - 1) / TQ;
     // (causal: the queries before key - (nk - nq) do not see the key)
     start = causal ? min(max(k0 - (nk - nq), 0) / TQ, tiles) : 0;
-    const int group = a.b.heads / a.b.kv_heads;
+    const int group = a.b.group;
     t = start;
     h = g * group;
     heads_end = h + group;
@@ -1181,12 +1220,13 @@ __device__ __forceinline__ void dkv_out(const AttnBwdArgs& a, const Span& s, int
 }
 
 // Four waves of 32 keys share tiles of 64 queries.
-template <bool DIRECT>
-__global__ void __launch_bounds__(256, 2) attn_dkv_wide_kernel(AttnBwdArgs a, int tiles) {
+template <bool DIRECT, bool OWN>
+__device__ __forceinline__ void dkv_wide(const AttnBwdArgs& a, int before) {
   constexpr int TQ = 64;
   __shared__ uint4 q0[512], q1[512], g0[512], g1[512];
   __shared__ __attribute__((aligned(16))) float stat0[4 * TQ], stat1[4 * TQ];
-  const Place at = place_of(tiles, a.b.kv_heads, a.b.batch, false);
+  Place at = place_of(a.b.kv_heads, a.b.per_kv_head, a.b.batch);
+  at.tile -= before;
   if (!at.in) return;
   const int g = at.h;
   const Span s = span_of(a.b, at.b);
@@ -1200,7 +1240,7 @@ __global__ void __launch_bounds__(256, 2) attn_dkv_wide_kernel(AttnBwdArgs a, in
   const int j0 = at.tile * 128 + 32 * w, j = j0 + l.n;
   Walk<TQ> walk(a, s, at.b, g, at.tile * 128, min(at.tile * 128 + 128, s.nk));
   Loads<DIRECT> qs, gs;
-  StatLoads<TQ> ss;
+  StatLoads<TQ, OWN> ss;
   qs.init(a.q, s.q0, s.nq, 0);
   gs.init(a.dout, s.q0, s.nq, 0);
   f32x16 dk[2] = {zeros(), zeros()}, dv[2] = {zeros(), zeros()};
@@ -1248,11 +1288,23 @@ __global__ void __launch_bounds__(256, 2) attn_dkv_wide_kernel(AttnBwdArgs a, in
   dkv_out(a, s, g, j0, l, (char*)(w == 0 ? q0 : w == 1 ? q1 : w == 2 ? g0 : g1), dk, dv);
 }
 
+template <bool DIRECT>
+__global__ void __launch_bounds__(256, 2) attn_dkv_wide_kernel(AttnBwdArgs a) {
+  dkv_wide<DIRECT, false>(a, 0);
+}
+// Both of them in one launch, for batches so small that their workgroups are on the chip at once: those of dk
+// and dv then compute delta themselves from dout, o and its rest.
+template <bool DIRECT>
+__global__ void __launch_bounds__(256, 2) attn_bwd_both_kernel(AttnBwdArgs a, int dq_tiles) {
+  if ((int)blockIdx.x / 8 < dq_tiles) dq_wide<DIRECT>(a, dq_tiles);
+  else dkv_wide<DIRECT, true>(a, dq_tiles);
+}
+
 // 32 keys, the four waves a quarter of each tile of 128 queries.
-__global__ void __launch_bounds__(256, 2) attn_dkv_few_kernel(AttnBwdArgs a, int tiles) {
+__global__ void __launch_bounds__(256, 2) attn_dkv_few_kernel(AttnBwdArgs a) {
   constexpr int TQ = 128, kTileBytes = TQ * kRowBytes, kStageBytes = 2 * kTileBytes + 16 * TQ;
   __shared__ __attribute__((aligned(16))) char lds[2 * kStageBytes];
-  const Place at = place_of(tiles, a.b.kv_heads, a.b.batch, false);
+  const Place at = place_of(a.b.kv_heads, a.b.per_kv_head, a.b.batch);
   if (!at.in) return;
   const int g = at.h;
   const Span s = span_of(a.b, at.b);
@@ -1333,17 +1385,16 @@ __global__ void __launch_bounds__(256, 2) attn_dkv_few_kernel(AttnBwdArgs a, int
 // rows of 16-byte pieces
 bool whole(const HMat& m) { return (uintptr_t)m.p % 16 == 0 && m.ld % 8 == 0; }
 
+dim3 grid_of(int tiles, int heads, int batch) { return dim3(8 * tiles, (heads * batch + 7) / 8); }
+
 void launch_attention(const AttnFwdArgs& a, hipStream_t st) {
   const FwdPlan p = fwd_plan(a.b);
-  const int grid = (int)places(p.tiles, a.b.heads, a.b.batch) * p.splits;
-  if (!grid) return;
+  if (!p.tiles || !a.b.batch) return;
+  const dim3 grid = grid_of(p.tiles * p.splits, a.b.heads, a.b.batch);
   if (p.few) attn_fwd_few_kernel<<<grid, 256, 0, st>>>(a, p.tiles, p.splits, p.chunk);
   else if (whole(a.k) && whole(a.v)) attn_fwd_wide_kernel<true><<<grid, 256, 0, st>>>(a, p.tiles);
   else attn_fwd_wide_kernel<false><<<grid, 256, 0, st>>>(a, p.tiles);
-  if (p.splits > 1) {
-    const int rows = (a.b.q_max + 3) / 4;
-    attn_join_kernel<<<rows * a.b.heads * a.b.batch, 256, 0, st>>>(a, rows, p.splits);
-  }
+  if (p.splits > 1) attn_join_kernel<<<dim3((a.b.q_max + 3) / 4, a.b.heads, a.b.batch), 256, 0, st>>>(a, p.splits);
 }
 
 void launch_attention_backward(const AttnBwdArgs& args, hipStream_t st) {
@@ -1352,21 +1403,26 @@ void launch_attention_backward(const AttnBwdArgs& args, hipStream_t st) {
   if (!b.batch) return;
   a.blocks = (b.q_max + 31) / 32;
   a.ranges = (int4*)((char*)a.delta + attn_bwd_delta_bytes(b));
-  const int wide_q = (b.q_max + 127) / 128, wide_k = (b.k_max + 127) / 128;
-  if (b.q_max > 0) {
-    if (wide_rows(b, b.q_max, b.heads))
-      if (whole(a.k) && whole(a.v)) attn_dq_wide_kernel<true><<<places(wide_q, b.heads, b.batch), 256, 0, st>>>(a, wide_q);
-      else attn_dq_wide_kernel<false><<<places(wide_q, b.heads, b.batch), 256, 0, st>>>(a, wide_q);
-    else
-      attn_dq_few_kernel<<<places(a.blocks, b.heads, b.batch), 256, 0, st>>>(a, a.blocks);
+  const bool wide_q = wide_rows(b, b.q_max, b.heads), wide_k = wide_rows(b, b.k_max, b.kv_heads, true);
+  const bool direct_q = whole(a.k) && whole(a.v), direct_k = whole(a.q) && whole(a.dout);
+  const int tiles_q = wide_q ? (b.q_max + 127) / 128 : a.blocks, tiles_k = wide_k ? (b.k_max + 127) / 128 : (b.k_max + 31) / 32;
+  const dim3 grid_q = grid_of(tiles_q, b.heads, b.batch), grid_k = grid_of(tiles_k, b.kv_heads, b.batch);
+  if (!b.window && wide_q && wide_k && grid_q.x * grid_q.y + grid_k.x * grid_k.y <= 512) {
+    a.delta = nullptr;
+    const dim3 grid(grid_q.x + grid_k.x, grid_q.y);
+    if (direct_q && direct_k) attn_bwd_both_kernel<true><<<grid, 256, 0, st>>>(a, tiles_q);
+    else attn_bwd_both_kernel<false><<<grid, 256, 0, st>>>(a, tiles_q);
+    return;
   }
-  if (b.k_max > 0) {
-    const int few_k = (b.k_max + 31) / 32;
-    if (wide_rows(b, b.k_max, b.kv_heads, true))
-      if (whole(a.q) && whole(a.dout)) attn_dkv_wide_kernel<true><<<places(wide_k, b.kv_heads, b.batch), 256, 0, st>>>(a, wide_k);
-      else attn_dkv_wide_kernel<false><<<places(wide_k, b.kv_heads, b.batch), 256, 0, st>>>(a, wide_k);
-    else
-      attn_dkv_few_kernel<<<places(few_k, b.kv_heads, b.batch), 256, 0, st>>>(a, few_k);
+  if (tiles_q > 0) {
+    if (!wide_q) attn_dq_few_kernel<<<grid_q, 256, 0, st>>>(a, tiles_q);
+    else if (direct_q) attn_dq_wide_kernel<true><<<grid_q, 256, 0, st>>>(a, tiles_q);
+    else attn_dq_wide_kernel<false><<<grid_q, 256, 0, st>>>(a, tiles_q);
+  }
+  if (tiles_k > 0) {
+    if (!wide_k) attn_dkv_few_kernel<<<grid_k, 256, 0, st>>>(a);
+    else if (direct_k) attn_dkv_wide_kernel<true><<<grid_k, 256, 0, st>>>(a);
+    else attn_dkv_wide_kernel<false><<<grid_k, 256, 0, st>>>(a);
   }
 }
 

@@ -16,10 +16,16 @@ namespace ad {
 
 // What both passes know of a batch (ad_attn).
 struct AttnBatch {
-  int batch, heads, kv_heads, q_rows, k_rows, q_max, k_max, causal;
+  int batch, heads, kv_heads, group, q_rows, k_rows, q_max, k_max, causal;   // group = heads / kv_heads
+  uint64_t per_head, per_kv_head;                                            // per() of heads and kv_heads
   const int *cu_q, *cu_k, *q_len, *k_len, *window;
   int* err;
 };
+// n / d = (n per(d)) >> kPerShift for n < 2^24, d <= 2^14: per(d) d - 2^40 < d, so the quotient is off by less than
+// n d / 2^40 < 1 / d.
+constexpr int kPerShift = 40;
+inline uint64_t per(int d) { return ((uint64_t(1) << kPerShift) + d - 1) / d; }
+
 AD_BOTH int smaller(int a, int b) { return a < b ? a : b; }
 AD_BOTH int larger(int a, int b) { return a > b ? a : b; }
 
@@ -58,9 +64,6 @@ AD_BOTH Keys keys_of(const AttnBatch& a, const Span& s, int i) {
 }
 
 // ----------------------------------------------------------------- workgroups
-
-// Workgroups of a launch with this many tiles a (sequence, head): the pairs are dealt out over eight XCDs.
-inline int64_t places(int64_t tiles, int64_t heads, int64_t batch) { return (heads * batch + 7) / 8 * 8 * tiles; }
 
 // Whether four waves take 32 rows each (of `rows` at most a sequence), or 32 rows together.  A wide workgroup has a tile
 // of 64 done in 0.9 us alone on its CU and in 0.75 among others, one of few rows 128 in 1.25 and 0.87: the
@@ -103,10 +106,8 @@ inline size_t attn_bwd_delta_bytes(const AttnBatch& b) { return (4ull * b.heads 
 inline size_t attn_bwd_bytes(const AttnBatch& b) {
   return attn_bwd_delta_bytes(b) + 16ull * b.batch * ((b.q_max + 31) / 32);
 }
-inline int64_t attn_groups(const AttnBatch& b) {
-  const FwdPlan p = fwd_plan(b);
-  return std::max({places(p.tiles, b.heads, b.batch) * p.splits, (int64_t)((b.q_max + 3) / 4) * b.heads * b.batch,
-                   places((b.q_max + 31) / 32, b.heads, b.batch), places((b.k_max + 31) / 32, b.kv_heads, b.batch)});
-}
+// A launch's grid has 8 workgroups a tile in x and a row for 8 (sequence, head) pairs in y.
+constexpr int kMaxPairs = 65535 * 8;
+inline bool attn_fits(const AttnBatch& b) { return (int64_t)b.batch * b.heads <= kMaxPairs; }
 
 }  // namespace ad

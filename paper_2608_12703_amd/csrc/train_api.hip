@@ -116,6 +116,7 @@ ad_status attn_ok(const ad_attn* a) {
   if (a->q_heads < 1 || a->q_heads > kMaxHeads || a->kv_heads < 1 || a->kv_heads > kMaxHeads)
     return fail(AD_ERANGE, "heads must be in [1, 2^14]");
   if (a->q_heads % a->kv_heads) return bad("kv_heads must divide q_heads");
+  if ((int64_t)a->batch * a->q_heads > ad::kMaxPairs) return fail(AD_ERANGE, "batch * q_heads must be at most 524280");
   if (a->q_rows < 0 || a->q_rows > kMaxRows || a->k_rows < 0 || a->k_rows > kMaxRows)
     return fail(AD_ERANGE, "rows must be in [0, 2^24]");
   if (a->q_max < 0 || a->q_max > kMaxRows || a->k_max < 0 || a->k_max > kMaxRows)
@@ -126,6 +127,8 @@ ad_status attn_ok(const ad_attn* a) {
 ad::AttnBatch attn_batch(const ad_attn* a) {
   ad::AttnBatch b{};
   b.batch = a->batch; b.heads = a->q_heads; b.kv_heads = a->kv_heads;
+  b.group = a->q_heads / a->kv_heads;
+  b.per_head = ad::per(a->q_heads); b.per_kv_head = ad::per(a->kv_heads);
   b.q_rows = a->q_rows; b.k_rows = a->k_rows;
   // (no sequence can have more rows than there are)
   b.q_max = a->q_max < a->q_rows ? a->q_max : a->q_rows;
@@ -136,14 +139,13 @@ ad::AttnBatch attn_batch(const ad_attn* a) {
   return b;
 }
 
-// The sizes, the tables and that every launch's workgroups can be counted.
+// The sizes and the tables.
 ad_status attn_call_ok(const ad_attn* a) {
   AD_TRY(attn_ok(a));
   if (!a->cu_q || !a->cu_k || !a->err_flag) return bad("NULL argument: cu_q, cu_k or err_flag");
   const void* tables[] = {a->cu_q, a->cu_k, a->q_len, a->k_len, a->window, a->err_flag};
   for (const void* t : tables)
     if ((uintptr_t)t % 4) return bad("misaligned table");
-  if (ad::attn_groups(attn_batch(a)) >= INT32_MAX) return fail(AD_ERANGE, "batch * heads * rows is too large");
   return AD_OK;
 }
 

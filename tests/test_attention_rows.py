@@ -25,8 +25,17 @@ int main() {
     if (what == 'p') {
       if (next()) b.window = some;
       const FwdPlan p = fwd_plan(b);
-      printf("%d %d %d %d %d %zu %zu %lld\\n", p.few, p.tiles, p.splits, p.chunk, wide_rows(b, b.k_max, b.kv_heads, true),
-             attn_fwd_bytes(b), attn_bwd_bytes(b), (long long)attn_groups(b));
+      printf("%d %d %d %d %d %zu %zu %d\\n", p.few, p.tiles, p.splits, p.chunk, wide_rows(b, b.k_max, b.kv_heads, true),
+             attn_fwd_bytes(b), attn_bwd_bytes(b), attn_fits(b));
+      continue;
+    }
+    if (what == 'd') {
+      int bad = 0;
+      const uint64_t m = per(b.batch);
+      for (uint64_t n = 0; n < (1 << 24); n += 1 + n / 4096)
+        for (uint64_t k : {n / b.batch * b.batch, n / b.batch * b.batch + b.batch - 1, n})
+          bad += k < (1 << 24) && (k * m) >> kPerShift != k / b.batch;
+      printf("%d\\n", bad);
       continue;
     }
     const int padded = next(), window = next();
@@ -130,9 +139,10 @@ def test_plans(ask):
     lines = [["p", b, h, kv, b * q, b * k, q, k, 0, w] for b, h, kv, q, k, w in shapes]
     kinds = set()
     for (b, h, kv, q, k, w), line in zip(shapes, ask(lines)):
-        few, tiles, splits, chunk, wide_k, fwd, bwd, groups = map(int, line.split())
+        few, tiles, splits, chunk, wide_k, fwd, bwd, fits = map(int, line.split())
+        assert fits == (b * h <= 65535 * 8)
         if not b or not q:
-            assert fwd == 0 and groups >= 0
+            assert fwd == 0
             continue
         assert tiles == -(-q // (32 if few else 128))
         assert 1 <= splits <= 64                       # (a wave joins them, a lane a part)
@@ -142,6 +152,10 @@ def test_plans(ask):
         assert fwd == (4 * 66 * splits * h * b * q if splits > 1 else 0)
         # what 32 queries see together, behind a float for each row and head
         assert bwd >= 4 * h * b * q + 16 * b * -(-q // 32)
-        assert groups >= (b * h * tiles * splits) and groups >= b * kv * -(-k // 32)
         kinds.add((few, splits > 1, wide_k))
     assert len(kinds) >= 5
+
+
+def test_quotients(ask):
+    divisors = [1, 2, 3, 5, 6, 7, 12, 20, 61, 127, 641, 1000, 4095, 6700, 16383, 16384]
+    assert ask([["d", d, 1, 1, 0, 0, 0, 0, 0] for d in divisors]) == ["0"] * len(divisors)

@@ -23,12 +23,14 @@ BATCHES = {
     "windows_causal": dict(ql=[70, 33, 150], kl=[70, 33, 150], window="random", causal=True, heads=4, kv=2, lead=5),
     "sharp": dict(ql=[96], kl=[200], spread=12.0),
     "long": dict(ql=[700], kl=[700], causal=True, heads=1, kv=1),
-    # enough workgroups for four waves of 32 rows each (128, or 1024 with windows)
+    # enough workgroups for four waves of 32 rows each (128, or 1024 with windows); with more than 512 of
+    # them both gradients have a launch of their own (wide_many)
     "wide": dict(ql=[140, 97] * 8, kl=[150, 64] * 8, heads=4, kv=4),
     "wide_causal": dict(ql=[131, 140, 1, 129] * 4, kl=[131, 140, 1, 129] * 4, heads=4, kv=4, causal=True),
     "wide_longer": dict(ql=[131, 40, 140, 129] * 4, kl=[200, 300, 64, 1] * 4, heads=4, kv=4, causal=True, lead=1),
     "wide_shared": dict(ql=[70] * 20, kl=[90] * 20, heads=8, kv=4),
     "wide_cross": dict(ql=[33, 70, 128, 40] * 8, kl=[300, 1, 0, 129] * 8, heads=4, kv=4, padded=True),
+    "wide_many": dict(ql=[140, 35] * 20, kl=[150, 40] * 20, heads=6, kv=6, causal=True),
     "wide_windows": dict(ql=[40, 128] * 32, kl=[150, 60] * 32, heads=16, kv=16, window="random"),
 }
 
@@ -103,6 +105,7 @@ SIZES = {
     "few_split": dict(ql=[3, 1], kl=[700, 130], heads=1, kv=1),
     "wide": dict(ql=[140] * 16, kl=[150] * 16, heads=4, kv=4),
     "wide_shared": dict(ql=[70] * 20, kl=[90] * 20, heads=8, kv=4),
+    "wide_many": dict(ql=[140, 35] * 20, kl=[150, 40] * 20, heads=6, kv=6),
     "wide_windows": dict(ql=[40] * 64, kl=[150] * 64, heads=16, kv=16),
 }
 

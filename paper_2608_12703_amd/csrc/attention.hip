@@ -167,6 +167,30 @@ __device__ __forceinline__ void settled(bf16x8 (&v)[4]) {
   for (int k = 0; k < 4; ++k) asm volatile("" : "+v"(v[k]));
 }
 
+// 32 rows of a matrix that a wave has as an operand (columns l % 32): loaded in whole rows, eight lanes a row,
+// and turned in 4 KB of LDS of the wave's own.  Loaded as the operand has them, 32 bytes of 32 rows at a time,
+// each line came from L2 four times over.
+struct Rows {
+  uint4 reg[4];     // row 8 j + lane / 8, columns 8 (lane % 8) .. + 7
+  static __device__ __forceinline__ int row(int j) { return 8 * j + threadIdx.x % kWave / 8; }
+  __device__ __forceinline__ void load(const HMat& m, int64_t first, int rows, int col) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      reg[j] = make_uint4(0, 0, 0, 0);
+      if (row(j) < rows) reg[j] = load16(m.p + (first + row(j)) * m.ld + col + 8 * (threadIdx.x % 8));
+    }
+  }
+  __device__ __forceinline__ void operand(char* buf, const Lane& l, bf16x8 (&v)[4]) const {
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int j = 0; j < 4; ++j) *(uint4*)(buf + row(j) * kRowBytes + (((threadIdx.x % 8) ^ turn(row(j))) << 4)) = reg[j];
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = read_rows(buf, l, 0, k);
+    __builtin_amdgcn_wave_barrier();
+  }
+};
+
 // A tile of TR rows on its way from memory to LDS: thread t of 256 takes 16-byte piece t % 8 of rows
 // t / 8 + 32 j.  Rows past the sequence's last one become zeros.  A scalar base and a 32-bit offset a lane.
 template <int TR>
@@ -561,13 +585,8 @@ __global__ void __launch_bounds__(256, DIRECT ? 4 : 2) attn_fwd_wide_kernel(Attn
     ks.issue(0, key0);
     vs.issue(0, val0);
   }
-  bf16x8 q[4];
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    uint4 u = make_uint4(0, 0, 0, 0);
-    if (in) u = load16(a.q.p + (s.q0 + (int64_t)i) * a.q.ld + 64 * h + 16 * k + 8 * l.h);
-    q[k] = as_bf16x8(u);
-  }
+  Rows rows;
+  rows.load(a.q, s.q0 + (int64_t)q0, s.nq - q0, 64 * h);
   Keys keys = {0, s.nk};
   if (in) keys = keys_of(a.b, s, i);
   const Range r = range_at(a.b, s, q0, keys, in);
@@ -585,6 +604,8 @@ __global__ void __launch_bounds__(256, DIRECT ? 4 : 2) attn_fwd_wide_kernel(Attn
     }
   }
 
+  bf16x8 q[4];
+  rows.operand((char*)((w < 2 ? key1 : val1) + w % 2 * 256), l, q);
   float m = -INFINITY, sum = 0.f;
   f32x16 o[2] = {zeros(), zeros()};
   const auto step = [&](int k0, const uint4* kt, const uint4* vt, uint4* next_kt, uint4* next_vt) {
@@ -936,12 +957,18 @@ __device__ __forceinline__ void dq_wide(const AttnBwdArgs& a, int tiles) {
     ks.issue(0, key0);
     vs.issue(0, val0);
   }
-  bf16x8 q[4], go[4];
-  float delta, lse;
-  Keys keys;
-  dq_operands(a, s, h, i, l, q, go, delta, lse, keys);
+  Rows rq, rg, ro, rr;
+  rq.load(a.q, s.q0 + (int64_t)q0, s.nq - q0, 64 * h);
+  rg.load(a.dout, s.q0 + (int64_t)q0, s.nq - q0, 64 * h);
+  ro.load(a.o, s.q0 + (int64_t)q0, s.nq - q0, 64 * h);
+  rr.load(a.rest, s.q0 + (int64_t)q0, a.rest.p ? s.nq - q0 : 0, 64 * h);
+  float lse = 0.f;
+  Keys keys = {0, s.nk};
+  if (in) {
+    keys = keys_of(a.b, s, i);
+    lse = a.lse[(size_t)h * a.b.q_rows + row] * kLog2e;
+  }
   const Range r = range_at(a.b, s, q0, keys, in);
-  if (a.delta && in && l.h == 0) a.delta[(size_t)h * a.b.q_rows + row] = delta;
   if (a.b.window) {
     if (threadIdx.x % kWave == 0) {
       if (h == 0 && q0 < s.nq) a.ranges[(size_t)at.b * a.blocks + q0 / 32] = make_int4(r.lo, r.hi, r.all_lo, r.all_hi);
@@ -957,6 +984,30 @@ __device__ __forceinline__ void dq_wide(const AttnBwdArgs& a, int tiles) {
     }
   }
 
+  if (lse == -INFINITY) lse = INFINITY;     // sees nothing: p = exp2(s - inf) = 0
+  char* buf = (char*)((w < 2 ? key1 : val1) + w % 2 * 256);
+  bf16x8 q[4], go[4];
+  rq.operand(buf, l, q);
+  rg.operand(buf, l, go);
+  // delta: a row's eight lanes add up, and hand it over in the operand's order
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    float d[8], o[8], e[8], sum = 0.f;
+    widen8(__builtin_bit_cast(u32x4, rg.reg[j]), d);
+    widen8(__builtin_bit_cast(u32x4, ro.reg[j]), o);
+    widen8(__builtin_bit_cast(u32x4, rr.reg[j]), e);
+#pragma unroll
+    for (int c = 0; c < 8; ++c) sum = fmaf(d[c], o[c] + e[c], sum);
+    sum += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(sum), 0xB1, 0xf, 0xf, false));    // lane ^ 1
+    sum += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(sum), 0x4E, 0xf, 0xf, false));    // lane ^ 2
+    sum += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(sum), 0x141, 0xf, 0xf, false));   // 7 - lane
+    if (threadIdx.x % 8 == 0) ((float*)buf)[Rows::row(j)] = sum;
+  }
+  __builtin_amdgcn_wave_barrier();
+  const float delta = ((const float*)buf)[l.n];
+  settled(q);
+  settled(go);
+  if (a.delta && in && l.h == 0) a.delta[(size_t)h * a.b.q_rows + row] = delta;
   f32x16 dq[2] = {zeros(), zeros()}, off;     // off: dP - delta starts from -delta
 #pragma unroll
   for (int e = 0; e < 16; ++e) off[e] = -delta;
@@ -1256,8 +1307,15 @@ __device__ __forceinline__ void dkv_wide(const AttnBwdArgs& a, int before) {
   };
   bool some = walk.settle();
   if (some) issue(q0, g0);
+  Rows rk, rv;
+  rk.load(a.k, s.k0 + (int64_t)j0, s.nk - j0, 64 * g);
+  rv.load(a.v, s.k0 + (int64_t)j0, s.nk - j0, 64 * g);
   bf16x8 k[4], v[4];
-  keys_operands(a, s, g, j, l, k, v);
+  char* buf = (char*)((w < 2 ? q1 : g1) + w % 2 * 256);
+  rk.operand(buf, l, k);
+  rv.operand(buf, l, v);
+  settled(k);
+  settled(v);
   const auto step = [&](const uint4* qt, const uint4* gt, const float* stat, uint4* next_qt, uint4* next_gt, float* next_stat) {
     const int now = walk.t;
     ++walk.t;

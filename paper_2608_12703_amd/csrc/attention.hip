@@ -304,6 +304,11 @@ __device__ __forceinline__ void by_rows(char* buf, const Lane& l, const f32x16 (
     out(row, c, r);
   }
 }
+// The columns (rows of the result) of which some lane says so, as bits.
+__device__ __forceinline__ uint32_t columns(bool bad) {
+  const uint64_t m = __ballot(bad);
+  return (uint32_t)(m | m >> 32);
+}
 __device__ __forceinline__ uint4 narrow8(const float (&v)[8]) {
   return make_uint4(f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]), f32x2_to_bf16x2(v[4], v[5]),
                     f32x2_to_bf16x2(v[6], v[7]));
@@ -690,8 +695,11 @@ __global__ void __launch_bounds__(256, DIRECT ? 4 : 2) attn_fwd_wide_kernel(Attn
       bad |= !(fabsf(o[d][e]) < INFINITY);
       o[d][e] = in ? o[d][e] : 0.f;
     }
+  if (first >= last) __syncthreads();      // (another wave's rows may still be in the place that is written next)
+  // what is not finite may come from keys that the row does not see: such rows are computed again below
+  uint32_t again = columns(bad && in);
   by_rows((char*)(w == 0 ? key0 : w == 1 ? key1 : w == 2 ? val0 : val1), l, o, [&](int row, int c, const float(&v)[8]) {
-    if (q0 + row >= s.oq) return;
+    if (q0 + row >= s.oq || again >> row & 1) return;
     const uint4 u = narrow8(v);
     store_piece(a.o, s.q0 + (int64_t)(q0 + row), h, c, u);
     if (!a.rest.p) return;
@@ -701,13 +709,9 @@ __global__ void __launch_bounds__(256, DIRECT ? 4 : 2) attn_fwd_wide_kernel(Attn
     for (int e = 0; e < 8; ++e) low[e] = v[e] - bf16_to_f32((uint16_t)(hi[e / 2] >> (16 * (e % 2))));
     store_piece(a.rest, s.q0 + (int64_t)(q0 + row), h, c, narrow8(low));
   });
-  if (a.lse && l.h == 0 && i < s.oq)
+  if (a.lse && l.h == 0 && i < s.oq && !(again >> l.n & 1))
     a.lse[(size_t)h * a.b.q_rows + s.q0 + i] = sum == 0.f || !in ? -INFINITY : (m + __log2f(sum)) * kLn2;
-  // what is not finite may come from keys that this row does not see
-  uint64_t again = __ballot(bad && in);
-  if (again) __threadfence_block();
-  again = (again | again >> 32) & 0xffffffffu;
-  for (; again; again &= again - 1) fwd_row(a, s, h, q0 + __builtin_ctzll(again));
+  for (; again; again &= again - 1) fwd_row(a, s, h, q0 + __builtin_ctz(again));
 }
 
 // The parts of a row's keys joined: a wave a row and head, a lane a dimension.
@@ -805,8 +809,11 @@ __device__ __forceinline__ void dq_out(const AttnBwdArgs& a, const Span& s, int 
       dq[d][e] = in ? dq[d][e] * kScale : 0.f;
       bad |= !(fabsf(dq[d][e]) < INFINITY);
     }
+  // what is not finite may come from keys that the row does not see: such rows are computed again below (and are not
+  // written before: dq may be res)
+  uint32_t again = columns(bad);
   by_rows(buf, l, dq, [&](int n, int c, const float(&v)[8]) {
-    if (q0 + n >= s.oq) return;
+    if (q0 + n >= s.oq || again >> n & 1) return;
     const int64_t to = s.q0 + (int64_t)(q0 + n);
     float x[8];
 #pragma unroll
@@ -819,11 +826,7 @@ __device__ __forceinline__ void dq_out(const AttnBwdArgs& a, const Span& s, int 
     }
     store_piece(a.dq, to, h, c, narrow8(x));
   });
-  // what is not finite may come from keys that the row does not see
-  uint64_t again = __ballot(bad);
-  again = (again | again >> 32) & 0xffffffffu;
-  if (again) __threadfence_block();
-  for (; again; again &= again - 1) dq_row(a, s, h, q0 + __builtin_ctzll(again));
+  for (; again; again &= again - 1) dq_row(a, s, h, q0 + __builtin_ctz(again));
 }
 
 // dq of 32 queries, the four waves a quarter of each tile of 128 keys.
@@ -1053,6 +1056,7 @@ __device__ __forceinline__ void dq_wide(const AttnBwdArgs& a, int tiles) {
       step(k0 + TK, key1, val1, key0, val0);
     }
   }
+  if (first >= last) __syncthreads();      // (another wave's rows may still be in the place that is written next)
   dq_out(a, s, h, q0, in, l, (char*)(w == 0 ? key0 : w == 1 ? key1 : w == 2 ? val0 : val1), dq);
 }
 
@@ -1257,17 +1261,15 @@ __device__ __forceinline__ void dkv_out(const AttnBwdArgs& a, const Span& s, int
       dv[d][e] = in ? dv[d][e] : 0.f;
       bad |= !(fabsf(dk[d][e]) < INFINITY) || !(fabsf(dv[d][e]) < INFINITY);
     }
+  uint32_t again = columns(bad);
   by_rows(buf, l, dk, [&](int n, int c, const float(&x)[8]) {
-    if (j0 + n < s.ow) store_piece(a.dk, s.k0 + (int64_t)(j0 + n), g, c, narrow8(x));
+    if (j0 + n < s.ow && !(again >> n & 1)) store_piece(a.dk, s.k0 + (int64_t)(j0 + n), g, c, narrow8(x));
   });
   __builtin_amdgcn_wave_barrier();
   by_rows(buf, l, dv, [&](int n, int c, const float(&x)[8]) {
-    if (j0 + n < s.ow) store_piece(a.dv, s.k0 + (int64_t)(j0 + n), g, c, narrow8(x));
+    if (j0 + n < s.ow && !(again >> n & 1)) store_piece(a.dv, s.k0 + (int64_t)(j0 + n), g, c, narrow8(x));
   });
-  uint64_t again = __ballot(bad);
-  again = (again | again >> 32) & 0xffffffffu;
-  if (again) __threadfence_block();
-  for (; again; again &= again - 1) dkv_row(a, s, g, j0 + __builtin_ctzll(again));
+  for (; again; again &= again - 1) dkv_row(a, s, g, j0 + __builtin_ctz(again));
 }
 
 // Four waves of 32 keys share tiles of 64 queries.
@@ -1342,6 +1344,8 @@ __device__ __forceinline__ void dkv_wide(const AttnBwdArgs& a, int before) {
       step(q1, g1, stat1, q0, g0, stat0);
       if (!some) break;
     }
+  } else {
+    __syncthreads();      // (another wave's rows may still be in the place that is written next)
   }
   dkv_out(a, s, g, j0, l, (char*)(w == 0 ? q0 : w == 1 ? q1 : w == 2 ? g0 : g1), dk, dv);
 }
@@ -1465,7 +1469,7 @@ void launch_attention_backward(const AttnBwdArgs& args, hipStream_t st) {
   const bool direct_q = whole(a.k) && whole(a.v), direct_k = whole(a.q) && whole(a.dout);
   const int tiles_q = wide_q ? (b.q_max + 127) / 128 : a.blocks, tiles_k = wide_k ? (b.k_max + 127) / 128 : (b.k_max + 31) / 32;
   const dim3 grid_q = grid_of(tiles_q, b.heads, b.batch), grid_k = grid_of(tiles_k, b.kv_heads, b.batch);
-  if (!b.window && wide_q && wide_k && grid_q.x * grid_q.y + grid_k.x * grid_k.y <= 512) {
+  if (!b.window && wide_q && wide_k && (size_t)grid_q.x * grid_q.y + (size_t)grid_k.x * grid_k.y <= 512) {
     a.delta = nullptr;
     const dim3 grid(grid_q.x + grid_k.x, grid_q.y);
     if (direct_q && direct_k) attn_bwd_both_kernel<true><<<grid, 256, 0, st>>>(a, tiles_q);

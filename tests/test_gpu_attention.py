@@ -159,6 +159,41 @@ def test_hidden_places_have_no_influence(name, value):
     near(dv, ref.dv, ref.tol_dv, "dv")
 
 
+@pytest.mark.parametrize("name", ["few", "wide", "wide_many"])
+def test_gradient_in_place_of_the_other_one_with_hidden_infinities(name):
+    """dq written over dq_res, where the rows' first result is not finite: the other gradient is added once."""
+    kw = dict(SIZES[name], kl=SIZES[name]["ql"])
+    bt = Batch(seed=12, causal=True, **kw)
+    res = torch.randn(bt.q_rows, 64 * bt.heads, generator=torch.Generator().manual_seed(2)).to(BF16)
+    ref = Ref(bt, res)
+    last = torch.tensor([c - 1 for c in bt.cu_q[1:]])
+    bt.k[last] = float("inf")
+    at = bt.handle()
+    dq = put(res)
+    dk, dv = torch.empty_like(bt.k, device="cuda"), torch.empty_like(bt.v, device="cuda")
+    o = ref.o.to(BF16)
+    ad.attention_backward(at, put(bt.q), put(bt.k), put(bt.v), put(o), put((ref.o - o.double()).to(BF16)), ref.lse.float().cuda(),
+                          put(bt.dout), dq, dq, dk, dv, space(ad.attention_backward_workspace_size, at, bt))
+    before = torch.ones(bt.q_rows, dtype=torch.bool)
+    before[last] = False
+    near(dq.double().cpu()[before], ref.dq[before], (ref.tol_dq + 2.0 ** -23 * res.double().abs())[before], "dq")
+
+
+@pytest.mark.parametrize("heads", [4, 12])
+def test_many_rows_without_keys_and_keys_without_rows(heads):
+    """Four waves that meet at no tile still keep out of each other's places (4 heads: both gradients in one launch)."""
+    for ql, kl in (([140] * 16, [0, 150] * 8), ([0, 140] * 8, [150] * 16)):
+        bt = Batch(ql, kl, heads=heads, kv=heads, seed=heads)
+        ref = Ref(bt)
+        at, o, _, lse = forward(bt)
+        near(o.get(), ref.o, ref.tol_o, "o")
+        near(lse.double().cpu(), ref.lse, ref.tol_lse, "lse")
+        dq, dk, dv = backward(bt, ref)
+        near(dq, ref.dq, ref.tol_dq, "dq")
+        near(dk, ref.dk, ref.tol_dk, "dk")
+        near(dv, ref.dv, ref.tol_dv, "dv")
+
+
 @pytest.mark.parametrize("name", ["few", "wide"])
 def test_causal_rows_do_not_see_what_comes(name):
     """The last key and value hold NaN: the rows before are as without them; the last row is NaN."""

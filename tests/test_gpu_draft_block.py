@@ -340,3 +340,95 @@ def test_refusals():
         AdamW(params, block.grads, state="4bit")
     with pytest.raises(ValueError):
         AdamW(params, block.grads[:3])
+
+
+def test_a_training_step_of_the_objective():
+    """What a training loop runs: the block, its final LayerNorm and the target's head, the objective, back through all of
+    them, and the step, which the draft model reads its new weights from.  Gradients against autograd of L_tok + lambda
+    L_anchor in float64 (the alignment term's gradient goes through the queries; tolerance above, with the head's logits,
+    whose gradient is rounded to bf16, as two operators more)."""
+    from paper_2608_12703_amd import synth
+    from paper_2608_12703_amd.configs import Config
+    from paper_2608_12703_amd.harness import Session
+    cfg = Config(name="unit_step", n_layers=2, d_model=128, n_heads=2, d_ffn=256, vocab=1000, dtype="bf16", batch=3, k=4,
+                 k_min=0, frames=150, frames_min=40, kv_max=0, geo_p=0.3, seed=13)
+    dcfg = synth.draft_config(cfg)
+    target, own = synth.make_params(cfg), synth.make_draft_params(cfg)
+    named = {n: own[n] for n, _ in synth.param_specs(dcfg) if n not in ("tok_emb", "pos_emb")}
+    named["tok_emb"], named["pos_emb"] = target["tok_emb"], target["pos_emb"]
+    B, R, Ts, d, V, sigma, lam = 3, 24, [150, 90, 41], cfg.d_model, cfg.vocab, 5.0, 0.1
+    sess = Session(dcfg, named, B, R - 1, Ts, want_logits=True)
+    g = _gen(71)
+    encs = [synth.make_encoder(cfg, b, T) for b, T in enumerate(Ts)]
+    layer = sess.model.params[4:24]                        # the tensors that the draft model reads
+    head, gain, bias = sess.model.params[0], sess.model.params[2], sess.model.params[3]
+    f = layer[16].shape[0]
+    ql, rows = [24, 17, 9], B * R
+    ints = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    cu, off = [b * R for b in range(B + 1)], sess.enc_off.tolist() + [sess.frames_cap]
+    self_batch = ad.Attention(2, 2, ints(cu), ints(cu), R, R, q_len=ints(ql), k_len=ints(ql), causal=True, covers=True)
+    cross_batch = ad.Attention(2, 2, ints(cu), ints(off), R, max(b - a for a, b in zip(off, off[1:])), q_len=ints(ql),
+                               k_len=ints(Ts), covers=True)
+    x = torch.randn(rows, d, generator=g)
+    live = torch.cat([torch.arange(R) < n for n in ql])
+    targets = torch.where(live, torch.randint(0, V, (rows,), generator=g), -1)
+    center = torch.where(live & (torch.rand(rows, generator=g) < 0.7), torch.randint(0, 41, (rows,), generator=g), -1)
+
+    block = DraftBlock(layer, rows, sess.frames_cap, B)
+    opt = AdamW(block.params, block.grads, state="8bit", seed=3)
+    e = lambda *s, dt=F32: torch.empty(*s, dtype=dt, device="cuda")  # noqa: E731
+    X, enc, err = x.cuda(), sess.upload_encoder(encs), torch.zeros(1, dtype=torch.int32, device="cuda")
+    out, xq, h, mean, rstd, logits = e(rows, d), e(rows, d), e(rows, d, dt=BF16), e(rows), e(rows), e(rows, V)
+    terms, row, dxq, dlogits, dh, dx = e(4), e(rows), e(rows, d), e(rows, V), e(rows, d), e(rows, d)
+    need = max(ad.anchordraft_loss_workspace_size(sess.model, B, R), ad.linear_workspace_size(rows, V, d),
+               ad.linear_dgrad_workspace_size(rows, V, d), ad.layer_norm_backward_workspace_size(rows, d))
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    T32, C32 = targets.to(torch.int32).cuda(), center.to(torch.int32).cuda()
+
+    def pass_():
+        sess.prefill_encoder(encs)
+        block.zero_grads()
+        block.forward(X, enc, self_batch, cross_batch, out, xq)
+        ad.layer_norm(out, gain, bias, h, mean, rstd)
+        ad.linear(h, head, None, ad.ACT_NONE, None, logits, None, None, ws)
+        ad.anchordraft_loss(sess.model, sess.cross_struct(), 0, B, R, xq, C32, sigma, lam, logits, T32, None, None, terms,
+                            row, dxq, dlogits, None, err, ws)
+        ad.linear_dgrad(dlogits.to(BF16), head, ad.ACT_NONE, None, None, dh, None, ws)
+        ad.layer_norm_backward(dh, out, mean, rstd, None, gain, None, dx, None, None, None, None)
+        block.backward(dx, dx, dxq)
+
+    def reference(params):
+        leaves, x64 = _leaves(params), x.double().requires_grad_()
+        t = Data(d, ql=tuple(ql), kl=tuple(Ts), stride=R)
+        t.enc = torch.cat([torch.from_numpy(v).float() for v in encs]).to(BF16)
+        y, q = _block(leaves, x64, t)
+        z = _norm(y, gain.cpu().double(), bias.cpu().double()) @ head.cpu().double().T
+        loss = torch.nn.functional.cross_entropy(z, targets, ignore_index=-1)
+        kv = (t.enc.double() @ leaves[10].T + leaves[11]).detach()
+        n = int((center >= 0).sum())
+        for r in torch.nonzero(center >= 0)[:, 0].tolist():
+            b = r // R
+            k = kv[t.cu_k[b]:t.cu_k[b + 1], :d].view(-1, 2, 64)
+            a = torch.softmax(torch.einsum("hd,jhd->hj", q[r].view(2, 64), k) / 8, 1).mean(0)
+            w = torch.exp(-(torch.arange(Ts[b]).double() - float(center[r])).square() / (2 * sigma ** 2))
+            loss = loss - lam / n * (w / w.sum() * a.log()).sum()
+        loss.backward()
+        return loss, leaves, x64
+
+    for step in range(2):               # the second pass sees the step's weights, in the block and in the draft model
+        before = [p.cpu() for p in layer]
+        pass_()
+        assert int(err) == 0 and int(self_batch.err_flag) == 0 and int(cross_batch.err_flag) == 0
+        loss, leaves, x64 = reference(before)
+        assert float(terms[0]) == pytest.approx(float(loss.detach()), rel=4 * H)
+        _close(dx, x64.grad, "dx", 22 * H)
+        for i, (got, p) in enumerate(zip(block.grads, leaves)):
+            keep = torch.ones(len(p), dtype=torch.bool)
+            if i in (3, 11):
+                keep[d:2 * d] = i == 11
+                keep[:d] = i == 3
+            _close(got.cpu()[keep], p.grad[keep], (step, i), 22 * H)
+        opt.step()
+        # (a step of 1e-3 is under half of bf16's step next to a LayerNorm's gain of 1: those move in float32 first)
+        assert all(not torch.equal(a, b.cpu()) for a, b in zip(before, layer) if a.dim() > 1)
+    assert int(opt.steps) == 2 and f == 256

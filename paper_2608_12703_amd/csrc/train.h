@@ -377,6 +377,8 @@ int64_t opt_groups(int64_t n);   // workgroups of a tensor
 void launch_adamw(const OptList& l, AdamwArgs a, hipStream_t st);
 void launch_opt_state(const OptList& l, float* m, float* v, const int64_t* at, hipStream_t st);
 void launch_grad_squares(const OptList& l, double* part, hipStream_t st);
+bool norm_of_few(const OptList& l);      // one launch is enough
+void launch_grad_norm_few(OptList l, double max_norm, float* out, int* step, hipStream_t st);
 void launch_grad_norm(const double* part, int64_t parts, double max_norm, float* out, int* step, hipStream_t st);
 
 }  // namespace ad

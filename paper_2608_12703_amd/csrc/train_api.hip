@@ -572,11 +572,15 @@ ad_status ad_grad_norm(const ad_opt_tensor* tensors, int32_t count, double max_n
   AD_TRY(space_ok(workspace, workspace_bytes, align256(8 * (size_t)parts)));
   (void)hipGetLastError();
   double* part = (double*)workspace;
+  bool done = false;
   by_launch(tensors, count, 0.0, [&](const ad::OptList& l, const int*) {
+    // (the only list)
+    done = part == workspace && l.first[l.count] == parts && ad::norm_of_few(l);
+    if (done) return ad::launch_grad_norm_few(l, max_norm, out, step, (hipStream_t)stream);
     ad::launch_grad_squares(l, part, (hipStream_t)stream);
     part += l.first[l.count];
   });
-  ad::launch_grad_norm((const double*)workspace, parts, max_norm, out, step, (hipStream_t)stream);
+  if (!done) ad::launch_grad_norm((const double*)workspace, parts, max_norm, out, step, (hipStream_t)stream);
   return check_hip("ad_grad_norm");
 }
 

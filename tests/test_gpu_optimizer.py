@@ -333,3 +333,19 @@ def test_more_tensors_than_a_launch_holds():
     m = torch.empty(total, device="cuda")
     ad.opt_state(opt, m, None)
     assert torch.equal(m, torch.cat(x["m"]))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("sizes", [[1], [1023, 1, 1025, 0, 3], [16 * 1024] * 3, [16 * 1024] * 3 + [1], [381] * 40, [381] * 41,
+                                   [0, 0, 5000, 0]])
+def test_grad_norm_of_few_elements(sizes, dtype):
+    """One launch for up to 48 pieces of 1024 elements; tensors at odd places; the same bits each time."""
+    g = [(torch.randn(n + 1, generator=_gen(n + i)) * 0.1).to(dtype) for i, n in enumerate(sizes)]
+    opt = ad.OptTensors(grads=[x.cuda()[1:] for x in g])
+    ws = torch.empty(max(ad.grad_norm_workspace_size(opt), 1), dtype=torch.uint8, device="cuda")
+    outs = [torch.full((2,), -1.0, device="cuda") for _ in range(3)]
+    for out in outs:
+        ad.grad_norm(opt, 0.0, out, ws)
+    want = math.sqrt(sum(float(x[1:].double().square().sum()) for x in g))
+    assert abs(float(outs[0][0]) - want) <= 2 * U * want and float(outs[0][1]) == 1.0
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])

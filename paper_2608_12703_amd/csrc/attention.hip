@@ -180,11 +180,15 @@ struct Rows {
       if (row(j) < rows) reg[j] = load16(m.p + (first + row(j)) * m.ld + col + 8 * (threadIdx.x % 8));
     }
   }
-  __device__ __forceinline__ void operand(char* buf, const Lane& l, bf16x8 (&v)[4]) const {
+  // as a tile of the wave's own
+  __device__ __forceinline__ void place(char* buf) const {
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int j = 0; j < 4; ++j) *(uint4*)(buf + row(j) * kRowBytes + (((threadIdx.x % 8) ^ turn(row(j))) << 4)) = reg[j];
     __builtin_amdgcn_wave_barrier();
+  }
+  __device__ __forceinline__ void operand(char* buf, const Lane& l, bf16x8 (&v)[4]) const {
+    place(buf);
 #pragma unroll
     for (int k = 0; k < 4; ++k) v[k] = read_rows(buf, l, 0, k);
     __builtin_amdgcn_wave_barrier();
@@ -558,6 +562,140 @@ __global__ void __launch_bounds__(256, 2) attn_fwd_few_kernel(AttnFwdArgs a, int
   // what is not finite may come from keys that the row does not see
   for (uint32_t rows = (uint32_t)__ballot(again); rows; rows &= rows - 1)
     if (__builtin_ctz(rows) % 4 == w) fwd_row(a, s, h, q0 + __builtin_ctz(rows));
+}
+
+// 32 queries, eight waves that take 32 keys each in turn, loaded a step ahead into places of their own: nobody waits for
+// anybody before the end, and a CU has its keys at about 40 bytes a cycle (twelve waves: no more).
+constexpr int kKeyWaves = 8;
+__global__ void __launch_bounds__(64 * kKeyWaves) attn_fwd_keys_kernel(AttnFwdArgs a) {
+  constexpr int W = kKeyWaves, kPlace = 64 * kRowBytes;
+  __shared__ __attribute__((aligned(16))) char lds[W * kPlace];   // a wave's keys and values, then its sums
+  __shared__ float stat[W][2][32];
+  __shared__ int bad[32];
+  const Place at = place_of(a.b.heads, a.b.per_head, a.b.batch);
+  if (!at.in) return;
+  const int h = at.h;
+  const Span s = span_of(a.b, at.b);
+  if (!s.ok) {
+    if (threadIdx.x == 0) atomicOr(a.b.err, AD_ERR_LENGTH);
+    return;
+  }
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), g = key_head(a.b, h);
+  const Lane l(threadIdx.x % kWave);
+  const int q0 = at.tile * 32, i = q0 + l.n;
+  if (q0 >= s.oq) return;
+  const bool in = i < s.nq;
+  Rows ks, vs, qs;
+  const auto load = [&](int k0) {
+    ks.load(a.k, s.k0 + (int64_t)k0, s.nk - k0, 64 * g);
+    vs.load(a.v, s.k0 + (int64_t)k0, s.nk - k0, 64 * g);
+  };
+  // (without windows the first keys are under way before anything else is asked for)
+  if (!a.b.window && 32 * w < s.nk) load(32 * w);
+  qs.load(a.q, s.q0 + (int64_t)q0, s.nq - q0, 64 * h);
+  Keys keys = {0, s.nk};
+  if (in) keys = keys_of(a.b, s, i);
+  const Range r = range_at(a.b, s, q0, keys, in);
+  const int mine = a.b.window ? first_piece(r.lo, r.hi, w) : 32 * w;
+  char* const kt = lds + w * kPlace;
+  char* const vt = kt + 32 * kRowBytes;
+  bf16x8 q[4];
+  if (a.b.window && mine < r.hi) load(mine);
+  qs.operand(kt, l, q);
+  settled(q);
+  float m = -INFINITY, sum = 0.f;
+  f32x16 o[2] = {zeros(), zeros()};
+  for (int k0 = mine; k0 < r.hi; k0 += 32 * W) {
+    ks.place(kt);
+    vs.place(vt);
+    if (k0 + 32 * W < r.hi) load(k0 + 32 * W);
+    f32x16 x = zeros();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x = mfma32(read_rows(kt, l, 0, k), q[k], x);
+    if (k0 < r.all_lo || k0 + 32 > r.all_hi) {
+      const int lo = keys.lo - k0 - 4 * l.h;
+      const unsigned len = max(keys.hi - keys.lo, 0);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[e] = (unsigned)(8 * (e / 4) + e % 4 - lo) < len ? x[e] : -INFINITY;
+    }
+    float top = x[0];
+#pragma unroll
+    for (int e = 1; e < 16; ++e) top = fmaxf(top, x[e]);
+    top = fmaxf(top, other_half(top)) * kScale2;
+    if (__any(top > m + kLazy)) {
+      const float now = fmaxf(m, top), old = __builtin_amdgcn_exp2f(m - (now == -INFINITY ? 0.f : now));
+      m = now;
+      sum *= old;
+#pragma unroll
+      for (int d = 0; d < 2; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[d][e] *= old;
+    }
+    const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      x[e] = __builtin_amdgcn_exp2f(fmaf(x[e], kScale2, -base));
+      sum += x[e];
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const bf16x8 p = narrow(x, 8 * c);
+#pragma unroll
+      for (int d = 0; d < 2; ++d) o[d] = mfma32(read_cols(vt, l, d, c), p, o[d]);
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+  sum += other_half(sum);
+
+  // the waves' sums joined: [wave][dimension][query], and every thread 4 dimensions of a query
+  float* part = (float*)lds;
+#pragma unroll
+  for (int d = 0; d < 2; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) part[(w * 64 + 32 * d + 8 * (e / 4) + 4 * l.h + e % 4) * 32 + l.n] = o[d][e];
+  if (l.h == 0) {
+    stat[w][0][l.n] = m;
+    stat[w][1][l.n] = sum;
+  }
+  if (threadIdx.x < 32) bad[threadIdx.x] = 0;
+  __syncthreads();
+  const int n = threadIdx.x % 32, d0 = threadIdx.x / 32 * 4, row = q0 + n;
+  float top = stat[0][0][n];
+#pragma unroll
+  for (int u = 1; u < W; ++u) top = fmaxf(top, stat[u][0][n]);
+  const float base = top == -INFINITY ? 0.f : top;
+  float v[4] = {}, total = 0.f;
+#pragma unroll 4
+  for (int u = 0; u < W; ++u) {
+    const float f = __builtin_amdgcn_exp2f(stat[u][0][n] - base);
+    total = fmaf(stat[u][1][n], f, total);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = fmaf(part[(u * 64 + d0 + e) * 32 + n], f, v[e]);
+  }
+  const bool live = row < s.oq, some = row < s.nq && total != 0.f;
+  const float inv = some ? 1.f / total : 0.f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    v[e] = some ? v[e] * inv : 0.f;
+    if (!(fabsf(v[e]) < INFINITY)) bad[n] = 1;
+  }
+  uint32_t hi[2], low[2];
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    hi[e] = f32x2_to_bf16x2(v[2 * e], v[2 * e + 1]);
+    low[e] = f32x2_to_bf16x2(v[2 * e] - bf16_to_f32(hi[e] & 0xffff), v[2 * e + 1] - bf16_to_f32(hi[e] >> 16));
+  }
+  __syncthreads();
+  const bool again = live && bad[n];
+  if (live && !again) {
+    const int64_t qr = s.q0 + (int64_t)row;
+    __builtin_memcpy(a.o.p + qr * a.o.ld + 64 * h + d0, hi, 8);
+    if (a.rest.p) __builtin_memcpy(a.rest.p + qr * a.rest.ld + 64 * h + d0, low, 8);
+    if (a.lse && d0 == 0) a.lse[(size_t)h * a.b.q_rows + qr] = some ? (top + __log2f(total)) * kLn2 : -INFINITY;
+  }
+  // what is not finite may come from keys that the row does not see
+  for (uint32_t rows = (uint32_t)__ballot(again); rows; rows &= rows - 1)
+    if (__builtin_ctz(rows) % W == w) fwd_row(a, s, h, q0 + __builtin_ctz(rows));
 }
 
 // Four waves of 32 queries share tiles of 64 keys.
@@ -1452,6 +1590,7 @@ dim3 grid_of(int tiles, int heads, int batch) { return dim3(8 * tiles, (heads * 
 void launch_attention(const AttnFwdArgs& a, hipStream_t st) {
   const FwdPlan p = fwd_plan(a.b);
   if (!p.tiles || !a.b.batch) return;
+  if (p.keys) return attn_fwd_keys_kernel<<<grid_of(p.tiles, a.b.heads, a.b.batch), 64 * kKeyWaves, 0, st>>>(a);
   const dim3 grid = grid_of(p.tiles * p.splits, a.b.heads, a.b.batch);
   if (p.few) attn_fwd_few_kernel<<<grid, 256, 0, st>>>(a, p.tiles, p.splits, p.chunk);
   else if (whole(a.k) && whole(a.v)) attn_fwd_wide_kernel<true><<<grid, 256, 0, st>>>(a, p.tiles);

@@ -63,6 +63,10 @@ AD_BOTH Keys keys_of(const AttnBatch& a, const Span& s, int i) {
   return r;
 }
 
+// Where wave w starts that takes 32 of the keys [lo, hi) in turn with others; where there are none (lo the largest
+// integer, hi = 0) it is not before hi, so that nothing is read.
+AD_BOTH int first_piece(int lo, int hi, int w) { return smaller(lo, hi) / 32 * 32 + 32 * w; }
+
 // ----------------------------------------------------------------- workgroups
 
 // Whether four waves take 32 rows each (of `rows` at most a sequence), or 32 rows together.  A wide workgroup has a tile
@@ -75,14 +79,16 @@ inline bool wide_rows(const AttnBatch& b, int rows, int heads, bool keys = false
   return rows > 32 && (int64_t)((rows + 127) / 128) * heads * b.batch >= (b.window && !keys ? 1024 : 128);
 }
 
-// How a forward pass is cut; where even the small workgroups leave CUs without work, the keys in `splits` parts
-// of `chunk`.
+// How a forward pass is cut.  Where even the small workgroups leave CUs without work, eight waves have keys of their own
+// (`keys`, in rounds of 256), or the keys are in `splits` parts of `chunk` and a second launch joins them.  A round takes
+// 0.7 us, a part 1 us for every 128 keys and the second launch 4: with 20 workgroups 448 keys 8.4 and 11.1 us, 1500
+// 11.2 and 11.1, 4000 20.7 and 13.4; with 80 1500 11.7 and 13.7, 4000 21.1 and 21.4; with 240 17.6 and 22.3, 46 and 53.
 struct FwdPlan {
-  bool few;
+  bool few, keys;
   int tiles, splits, chunk;
 };
 inline FwdPlan fwd_plan(const AttnBatch& b) {
-  FwdPlan p = {false, (b.q_max + 127) / 128, 1, 0};
+  FwdPlan p = {false, false, (b.q_max + 127) / 128, 1, 0};
   if (!p.tiles || !b.batch) return p;
   const int64_t pairs = (int64_t)b.heads * b.batch;
   if (wide_rows(b, b.q_max, b.heads)) return p;
@@ -93,6 +99,8 @@ inline FwdPlan fwd_plan(const AttnBatch& b) {
   const int want = (int)std::min<int64_t>(std::min(stages, 64), std::max<int64_t>(512 / groups, 1));
   const int each = (stages + want - 1) / want;
   p.splits = (stages + each - 1) / each;
+  p.keys = p.splits > 1 && (stages + 1) / 2 <= 4 + 2 * each;
+  if (p.keys) p.splits = 1;
   p.chunk = each * 128;
   return p;
 }

@@ -29,6 +29,10 @@ int main() {
              attn_fwd_bytes(b), attn_bwd_bytes(b), attn_fits(b));
       continue;
     }
+    if (what == 'f') {
+      printf("%d\\n", first_piece(b.q_rows, b.k_rows, b.batch));
+      continue;
+    }
     if (what == 'd') {
       int bad = 0;
       const uint64_t m = per(b.batch);
@@ -159,3 +163,12 @@ def test_plans(ask):
 def test_quotients(ask):
     divisors = [1, 2, 3, 5, 6, 7, 12, 20, 61, 127, 641, 1000, 4095, 6700, 16383, 16384]
     assert ask([["d", d, 1, 1, 0, 0, 0, 0, 0] for d in divisors]) == ["0"] * len(divisors)
+
+
+def test_first_piece(ask):
+    """Pieces of 32 keys in turn: they cover what is visible, and none begins where nothing is."""
+    none = 2 ** 31 - 1
+    cases = [(w, lo, hi) for lo, hi in ((none, 0), (0, 0), (0, 1), (31, 33), (32, 64), (1499, 1500), (none, none)) for w in range(8)]
+    got = [int(x) for x in ask([["f", w, 1, 1, lo, hi, 0, 0, 0] for w, lo, hi in cases if hi < none])]
+    for (w, lo, hi), at in zip(cases, got):
+        assert at == (min(lo, hi) // 32 + w) * 32 and (lo < hi or at >= hi)

@@ -23,6 +23,10 @@ BATCHES = {
     "windows_causal": dict(ql=[70, 33, 150], kl=[70, 33, 150], window="random", causal=True, heads=4, kv=2, lead=5),
     "sharp": dict(ql=[96], kl=[200], spread=12.0),
     "long": dict(ql=[700], kl=[700], causal=True, heads=1, kv=1),
+    # keys in parts, which a second launch joins
+    "parts": dict(ql=[17, 65, 3], kl=[2600, 217, 64], heads=2, kv=1),
+    "parts_causal": dict(ql=[40, 1, 3], kl=[1900, 2100, 0], heads=3, kv=3, causal=True, lead=3),
+    "parts_windows": dict(ql=[33, 20, 2], kl=[2000, 129, 1], window="random", padded=True),
     # enough workgroups for four waves of 32 rows each (128, or 1024 with windows); with more than 512 of
     # them both gradients have a launch of their own (wide_many)
     "wide": dict(ql=[140, 97] * 8, kl=[150, 64] * 8, heads=4, kv=4),
@@ -102,6 +106,7 @@ def test_a_row_of_one_key_has_no_gradient_for_its_query():
 SIZES = {
     # few rows a workgroup, and four waves of 32 rows each (chosen by the number of workgroups)
     "few": dict(ql=[40, 9], kl=[150, 70], heads=2, kv=2),
+    "parts": dict(ql=[3, 1], kl=[2600, 130], heads=1, kv=1),
     "few_split": dict(ql=[3, 1], kl=[700, 130], heads=1, kv=1),
     "wide": dict(ql=[140] * 16, kl=[150] * 16, heads=4, kv=4),
     "wide_shared": dict(ql=[70] * 20, kl=[90] * 20, heads=8, kv=4),
@@ -224,7 +229,7 @@ def test_scores_without_a_finite_value():
     assert not bool(got[0].any()) and z[0] == -float("inf") and bool(torch.isnan(got[1]).all())
 
 
-@pytest.mark.parametrize("name", ["few", "few_split", "wide"])
+@pytest.mark.parametrize("name", ["few", "parts", "few_split", "wide"])
 @pytest.mark.parametrize("what", ["past", "negative", "back", "long", "length"])
 def test_tables_out_of_range(name, what):
     """The kernels' own checks: the sequence is left out and AD_ERR_LENGTH set, the others are right."""

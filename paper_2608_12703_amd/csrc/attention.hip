@@ -1,4 +1,21 @@
 // Attention over matrices and its gradients (the draft block's training), 64-wide heads.
+//
+// Forward, a query at a time: s_j = q . k_j / 8 over the keys it sees, m the largest so far and l the sum of
+// exp(s_j - m), o = sum_j exp(s_j - m) v_j / l, lse = m + log l: one pass over the keys, 4 x 64 operations a visible pair.
+// Backward: p_j = exp(s_j - lse), delta = dout . o, dS_j = p_j (dout . v_j - delta), dq = sum dS_j k_j / 8, and over
+// the queries dk_j = sum dS q / 8, dv_j = sum p dout: five products, 10 x 64 operations, of which dq's kernel and that of
+// dk and dv each do S and dP again (14 in all), because sums over queries and over keys in one kernel would need
+// atomics, whose order changes results.
+//
+// Scores, sums and statistics are float32.  p and dS are rounded to bf16 for the second products (as all their operands
+// are), results once: against 64 bits dq is off by 0.0025 to 0.0029 (root mean square), its own rounding being 0.0017; dS in
+// two parts would cost half of dq's products again.  m, lse and scores are kept in powers of two inside the kernels.
+//
+// What bounds the large shapes is a wave's own instructions, not memory.  For 64 keys x 32 queries a wave has 16 products
+// of 32 x 32 x 16 in 512 cycles and about 860 cycles of vector instructions (scale, exponential, maximum, sum, rounding),
+// 1590 in all alone on a SIMD; dq 768 + 830, dk and dv 1024 + 1000 of 2575.  Other waves of the SIMD fill some of the
+// gaps: 8 x 2048 rows, 20 heads: forward 208 us (825 TF/s), both gradients 630 (680 TF/s of the five products); a large bf16
+// product reaches 1485.  Longer prologues and fewer tiles make 32 x 448 x 1500 slower: forward 172 us (640 TF/s).
 #include <algorithm>
 #include <type_traits>
 
@@ -382,10 +399,14 @@ __device__ __forceinline__ int ends_at(const AttnBatch& a, const Span& s, int q0
 
 // ----------------------------------------------------------------- forward
 
-// 32 queries, the four waves a quarter of each tile of 128 keys: where there are few queries.  One pass over the
-// keys with the running maximum m and sum l; the maximum that is taken off is only moved when a score exceeds
-// it by 8 (in powers of two), which keeps p under 256.
+// The maximum that is taken off is only moved when a score exceeds it by 8 (in powers of two): p stays under 256 and
+// what is added up before keeps its scale, which saves 32 products a lane on most tiles.
 constexpr float kLazy = 8.f;
+
+// 32 queries, the four waves a quarter of each tile of 128 keys and their sums joined at the end: where there are few
+// workgroups of 128 queries.  A tile takes 0.87 us, its loads a round trip to L2 or HBM ahead through registers.
+// With splits a workgroup has `chunk` of the keys and leaves its sums to attn_join_kernel (20 heads of one query over
+// 4000 keys: 8 + 5 us; a launch is 5 us by itself).
 
 __global__ void __launch_bounds__(256, 2) attn_fwd_few_kernel(AttnFwdArgs a, int tiles, int splits, int chunk) {
   constexpr int TK = 128, kTileBytes = TK * kRowBytes;
@@ -698,7 +719,10 @@ __global__ void __launch_bounds__(64 * kKeyWaves) attn_fwd_keys_kernel(AttnFwdAr
     if (__builtin_ctz(rows) % W == w) fwd_row(a, s, h, q0 + __builtin_ctz(rows));
 }
 
-// Four waves of 32 queries share tiles of 64 keys.
+// Four waves of 32 queries share tiles of 64 keys: the next tile is on its way straight to LDS while one is worked on, and
+// 33 KB of LDS and 120 registers leave room for four workgroups on a CU, whose vector instructions and products overlap.
+// 32 x 448 causal, 20 heads: 49 us; tiles through registers, conflicts in a third of LDS' cycles: 83.  Products of one tile beside
+// the exponentials of the one before in the same wave: 175 us where this takes 109 (registers).
 template <bool DIRECT>
 __global__ void __launch_bounds__(256, DIRECT ? 4 : 2) attn_fwd_wide_kernel(AttnFwdArgs a, int tiles) {
   constexpr int TK = 64;
@@ -852,7 +876,8 @@ __global__ void __launch_bounds__(256, DIRECT ? 4 : 2) attn_fwd_wide_kernel(Attn
   for (; again; again &= again - 1) fwd_row(a, s, h, q0 + __builtin_ctz(again));
 }
 
-// The parts of a row's keys joined: a wave a row and head, a lane a dimension.
+// The parts of a row's keys joined: a wave a row and head, a lane a dimension.  4.8 us for 20 rows of 12 parts, most of it
+// the launch and three round trips to memory.
 __global__ void __launch_bounds__(256) attn_join_kernel(AttnFwdArgs a, int splits) {
   const int tile = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
   const Span s = span_of(a.b, b);
@@ -967,7 +992,9 @@ __device__ __forceinline__ void dq_out(const AttnBwdArgs& a, const Span& s, int 
   for (; again; again &= again - 1) dq_row(a, s, h, q0 + __builtin_ctz(again));
 }
 
-// dq of 32 queries, the four waves a quarter of each tile of 128 keys.
+// dq of 32 queries, the four waves a quarter of each tile of 128 keys (where there are few workgroups of 128).  It leaves
+// delta and what 32 queries see together for the kernel of dk and dv.  With windows of 41 of 1500 keys a workgroup walks
+// over the two or three tiles that its queries see: 12 x 131 rows, 20 heads: 33 us, its loads' latencies.
 __global__ void __launch_bounds__(256, 2) attn_dq_few_kernel(AttnBwdArgs a, int tiles) {
   constexpr int TK = 128, kTileBytes = TK * kRowBytes;
   __shared__ __attribute__((aligned(16))) char lds[4 * kTileBytes];
@@ -1067,8 +1094,9 @@ __global__ void __launch_bounds__(256, 2) attn_dq_few_kernel(AttnBwdArgs a, int 
 }
 
 // dq of four waves of 32 queries that share tiles of 64 keys: as the forward kernel, with p from lse and two
-// products more, dP^T = V dO^T and, from dS, dQ^T = K^T dS^T.  It leaves delta and what 32 queries see
-// together for the kernel of dk and dv.
+// products more, dP^T = V dO^T and, from dS, dQ^T = K^T dS^T.  dP's accumulator starts from -delta.  It leaves delta
+// (unless both gradients are in one launch) and what 32 queries see together for the kernel of dk and dv.
+// 32 x 448 x 1500, 20 heads: 197 us, 512 cycles of products more a tile than the forward pass.
 template <bool DIRECT>
 __device__ __forceinline__ void dq_wide(const AttnBwdArgs& a, int tiles) {
   constexpr int TK = 64;
@@ -1410,7 +1438,10 @@ __device__ __forceinline__ void dkv_out(const AttnBwdArgs& a, const Span& s, int
   for (; again; again &= again - 1) dkv_row(a, s, g, j0 + __builtin_ctz(again));
 }
 
-// Four waves of 32 keys share tiles of 64 queries.
+// Four waves of 32 keys share tiles of 64 queries: four products a pair of tiles (S, dP, dV, dK).  64 accumulators
+// and 32 operands of its own leave 190 registers' worth of work: two workgroups a CU (three by force: 34 registers
+// spilled, 15% slower).  32 x 448 x 1500, 20 heads: 325 us; one 5000-long causal sequence, 12 heads, has 480
+// workgroups, of which the longest alone takes as long as all: 174 us (dq: 123).
 template <bool DIRECT, bool OWN>
 __device__ __forceinline__ void dkv_wide(const AttnBwdArgs& a, int before) {
   constexpr int TQ = 64;
@@ -1492,15 +1523,16 @@ template <bool DIRECT>
 __global__ void __launch_bounds__(256, 2) attn_dkv_wide_kernel(AttnBwdArgs a) {
   dkv_wide<DIRECT, false>(a, 0);
 }
-// Both of them in one launch, for batches so small that their workgroups are on the chip at once: those of dk
-// and dv then compute delta themselves from dout, o and its rest.
+// Both of them in one launch, for batches so small that their workgroups are on the chip at once (512, two a CU): those
+// of dk and dv then compute delta themselves from dout, o and its rest.  12 x 128 causal, 20 heads: 23 us in two
+// launches, 17 in one.
 template <bool DIRECT>
 __global__ void __launch_bounds__(256, 2) attn_bwd_both_kernel(AttnBwdArgs a, int dq_tiles) {
   if ((int)blockIdx.x / 8 < dq_tiles) dq_wide<DIRECT>(a, dq_tiles);
   else dkv_wide<DIRECT, true>(a, dq_tiles);
 }
 
-// 32 keys, the four waves a quarter of each tile of 128 queries.
+// 32 keys, the four waves a quarter of each tile of 128 queries (where there are few workgroups of 128).
 __global__ void __launch_bounds__(256, 2) attn_dkv_few_kernel(AttnBwdArgs a) {
   constexpr int TQ = 128, kTileBytes = TQ * kRowBytes, kStageBytes = 2 * kTileBytes + 16 * TQ;
   __shared__ __attribute__((aligned(16))) char lds[2 * kStageBytes];

@@ -554,8 +554,8 @@ ad_status ad_attention(const ad_attn* a, const ad_mat* q, const ad_mat* k, const
  * visible keys shows: dS of a single key is 0 only with it).  dout, dq, dk, dv bf16, of the shapes of
  * o, q, k, v; dq_res (optional, float32 or bf16, as q) is a gradient that reaches the queries on
  * another way, as the objective's out_dxq does; dq may be dq_res when their types and ld are the same.
- * Sums are float32, p and dS enter their products as bf16, every output is rounded once.  Padding
- * rows get 0 (and dq_res is not added to them).
+ * Sums are float32; p and, for dk, dS enter their products as bf16, for dq dS as two bf16 parts; every output
+ * is rounded once.  Padding rows get 0 (and dq_res is not added to them).
  * workspace and errors as for ad_attention.
  */
 ad_status ad_attention_backward_workspace_size(const ad_attn* a, size_t* bytes);

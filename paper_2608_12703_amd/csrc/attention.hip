@@ -4,18 +4,20 @@
 // exp(s_j - m), o = sum_j exp(s_j - m) v_j / l, lse = m + log l: one pass over the keys, 4 x 64 operations a visible pair.
 // Backward: p_j = exp(s_j - lse), delta = dout . o, dS_j = p_j (dout . v_j - delta), dq = sum dS_j k_j / 8, and over
 // the queries dk_j = sum dS q / 8, dv_j = sum p dout: five products, 10 x 64 operations, of which dq's kernel and that of
-// dk and dv each do S and dP again (14 in all), because sums over queries and over keys in one kernel would need
-// atomics, whose order changes results.
+// dk and dv each do S and dP (7 products, and one more for dS's second part), because sums over queries and over keys in
+// one kernel would need atomics, whose order changes results.
 //
-// Scores, sums and statistics are float32.  p and dS are rounded to bf16 for the second products (as all their operands
-// are), results once: against 64 bits dq is off by 0.0025 to 0.0029 (root mean square), its own rounding being 0.0017; dS in
-// two parts would cost half of dq's products again.  m, lse and scores are kept in powers of two inside the kernels.
+// Scores, sums and statistics are float32, results are rounded once.  p, and dS for dk, are rounded to bf16 for the second
+// products, whose operands are bf16.  For dq dS goes in as two bf16 parts: the terms of a row cancel (their sum over the
+// keys is 0), and rounded once dq was off by 0.0025 to 0.0029 of itself (root mean square) where its own rounding is 0.0017.
+// The second part costs dq's kernel a quarter on large shapes (32 x 448 x 1500 197 to 250 us).
+// m, lse and scores are kept in powers of two inside the kernels.
 //
 // What bounds the large shapes is a wave's own instructions, not memory.  For 64 keys x 32 queries a wave has 16 products
 // of 32 x 32 x 16 in 512 cycles and about 860 cycles of vector instructions (scale, exponential, maximum, sum, rounding),
-// 1590 in all alone on a SIMD; dq 768 + 830, dk and dv 1024 + 1000 of 2575.  Other waves of the SIMD fill some of the
-// gaps: 8 x 2048 rows, 20 heads: forward 208 us (825 TF/s), both gradients 630 (680 TF/s of the five products); a large bf16
-// product reaches 1485.  Longer prologues and fewer tiles make 32 x 448 x 1500 slower: forward 172 us (640 TF/s).
+// 1590 in all alone on a SIMD; dq 768 + 830 (and 256 for dS's second part), dk and dv 1024 + 1000 of 2575.  Other waves of
+// the SIMD fill some of the gaps: 8 x 2048 rows, 20 heads: forward 208 us (825 TF/s; a large bf16 product reaches 1485).
+// Prologue and epilogue make short ones slower: 32 x 448 x 1500 forward 172 us (640 TF/s).
 #include <algorithm>
 #include <type_traits>
 
@@ -158,6 +160,18 @@ __device__ __forceinline__ bf16x8 read_cols(const char* tile, const Lane& l, int
 __device__ __forceinline__ bf16x8 narrow(const f32x16& v, int e) {
   return as_bf16x8(make_uint4(f32x2_to_bf16x2(v[e], v[e + 1]), f32x2_to_bf16x2(v[e + 2], v[e + 3]),
                               f32x2_to_bf16x2(v[e + 4], v[e + 5]), f32x2_to_bf16x2(v[e + 6], v[e + 7])));
+}
+// The same in two parts, the second what rounding took from the first.
+__device__ __forceinline__ bf16x8 narrow(const f32x16& v, int e, bf16x8& rest) {
+  uint32_t hi[4], low[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float x = v[e + 2 * i], y = v[e + 2 * i + 1];
+    hi[i] = f32x2_to_bf16x2(x, y);
+    low[i] = f32x2_to_bf16x2(x - __uint_as_float(hi[i] << 16), y - __uint_as_float(hi[i] & 0xffff0000u));
+  }
+  rest = as_bf16x8(make_uint4(low[0], low[1], low[2], low[3]));
+  return as_bf16x8(make_uint4(hi[0], hi[1], hi[2], hi[3]));
 }
 // with the lane that has the same column's other rows
 __device__ __forceinline__ float other_half(float v) {
@@ -1064,9 +1078,14 @@ __global__ void __launch_bounds__(256, 2) attn_dq_few_kernel(AttnBwdArgs a, int 
       for (int e = 0; e < 16; ++e) x[e] = __builtin_amdgcn_exp2f(fmaf(x[e], kScale2, -lse)) * y[e];
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        const bf16x8 ds = narrow(x, 8 * c);
+        bf16x8 rest;
+        const bf16x8 ds = narrow(x, 8 * c, rest);
 #pragma unroll
-        for (int d = 0; d < 2; ++d) dq[d] = mfma32(read_cols(kt, l, d, c), ds, dq[d]);
+        for (int d = 0; d < 2; ++d) {
+          const bf16x8 k = read_cols(kt, l, d, c);
+          dq[d] = mfma32(k, ds, dq[d]);
+          dq[d] = mfma32(k, rest, dq[d]);
+        }
       }
     }
     if (more) {
@@ -1096,7 +1115,7 @@ __global__ void __launch_bounds__(256, 2) attn_dq_few_kernel(AttnBwdArgs a, int 
 // dq of four waves of 32 queries that share tiles of 64 keys: as the forward kernel, with p from lse and two
 // products more, dP^T = V dO^T and, from dS, dQ^T = K^T dS^T.  dP's accumulator starts from -delta.  It leaves delta
 // (unless both gradients are in one launch) and what 32 queries see together for the kernel of dk and dv.
-// 32 x 448 x 1500, 20 heads: 197 us, 512 cycles of products more a tile than the forward pass.
+// 32 x 448 x 1500, 20 heads: 250 us, twice the products of the forward pass.
 template <bool DIRECT>
 __device__ __forceinline__ void dq_wide(const AttnBwdArgs& a, int tiles) {
   constexpr int TK = 64;
@@ -1200,9 +1219,14 @@ __device__ __forceinline__ void dq_wide(const AttnBwdArgs& a, int tiles) {
         for (int e = 0; e < 16; ++e) x[e] = __builtin_amdgcn_exp2f(fmaf(x[e], kScale2, -lse)) * y[e];
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          const bf16x8 ds = narrow(x, 8 * c);
+          bf16x8 rest;
+          const bf16x8 ds = narrow(x, 8 * c, rest);
 #pragma unroll
-          for (int d = 0; d < 2; ++d) dq[d] = mfma32(read_cols((const char*)kt, l, d, 2 * n + c), ds, dq[d]);
+          for (int d = 0; d < 2; ++d) {
+            const bf16x8 k = read_cols((const char*)kt, l, d, 2 * n + c);
+            dq[d] = mfma32(k, ds, dq[d]);
+            dq[d] = mfma32(k, rest, dq[d]);
+          }
         }
       }
     }
@@ -1441,7 +1465,7 @@ __device__ __forceinline__ void dkv_out(const AttnBwdArgs& a, const Span& s, int
 // Four waves of 32 keys share tiles of 64 queries: four products a pair of tiles (S, dP, dV, dK).  64 accumulators
 // and 32 operands of its own leave 190 registers' worth of work: two workgroups a CU (three by force: 34 registers
 // spilled, 15% slower).  32 x 448 x 1500, 20 heads: 325 us; one 5000-long causal sequence, 12 heads, has 480
-// workgroups, of which the longest alone takes as long as all: 174 us (dq: 123).
+// workgroups, of which the longest alone takes as long as all: 174 us (dq: 153).
 template <bool DIRECT, bool OWN>
 __device__ __forceinline__ void dkv_wide(const AttnBwdArgs& a, int before) {
   constexpr int TQ = 64;

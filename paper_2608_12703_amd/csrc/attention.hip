@@ -497,10 +497,9 @@ __global__ void __launch_bounds__(256, 2) attn_fwd_few_kernel(AttnFwdArgs a, int
 #pragma unroll
       for (int k = 0; k < 4; ++k) x = mfma32(read_rows(kt, l, 0, k), q[k], x);
       if (mine < r.all_lo || mine + 32 > r.all_hi) {
-        const int lo = keys.lo - mine - 4 * l.h;
-        const unsigned len = max(keys.hi - keys.lo, 0);
+        const Mask mask = mask_of(keys, mine + 4 * l.h);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) x[e] = (unsigned)(8 * (e / 4) + e % 4 - lo) < len ? x[e] : -INFINITY;
+        for (int e = 0; e < 16; ++e) x[e] = shows(mask, 8 * (e / 4) + e % 4) ? x[e] : -INFINITY;
       }
       float top = x[0];
 #pragma unroll
@@ -648,10 +647,9 @@ __global__ void __launch_bounds__(64 * kKeyWaves) attn_fwd_keys_kernel(AttnFwdAr
 #pragma unroll
     for (int k = 0; k < 4; ++k) x = mfma32(read_rows(kt, l, 0, k), q[k], x);
     if (k0 < r.all_lo || k0 + 32 > r.all_hi) {
-      const int lo = keys.lo - k0 - 4 * l.h;
-      const unsigned len = max(keys.hi - keys.lo, 0);
+      const Mask mask = mask_of(keys, k0 + 4 * l.h);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) x[e] = (unsigned)(8 * (e / 4) + e % 4 - lo) < len ? x[e] : -INFINITY;
+      for (int e = 0; e < 16; ++e) x[e] = shows(mask, 8 * (e / 4) + e % 4) ? x[e] : -INFINITY;
     }
     float top = x[0];
 #pragma unroll
@@ -804,13 +802,11 @@ __global__ void __launch_bounds__(256, DIRECT ? 4 : 2) attn_fwd_wide_kernel(Attn
         for (int k = 0; k < 4; ++k) x[n] = mfma32(read_rows((const char*)kt, l, n, k), q[k], x[n]);
       }
       if (k0 < r.all_lo || k0 + TK > r.all_hi) {
-        const int lo = keys.lo - k0 - 4 * l.h;
-        const unsigned len = max(keys.hi - keys.lo, 0);
+        const Mask mask = mask_of(keys, k0 + 4 * l.h);
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll
-          for (int e = 0; e < 16; ++e)
-            x[n][e] = (unsigned)(32 * n + 8 * (e / 4) + e % 4 - lo) < len ? x[n][e] : -INFINITY;
+          for (int e = 0; e < 16; ++e) x[n][e] = shows(mask, 32 * n + 8 * (e / 4) + e % 4) ? x[n][e] : -INFINITY;
       }
       float top = x[0][0];
 #pragma unroll
@@ -966,11 +962,10 @@ __device__ __forceinline__ void dq_operands(const AttnBwdArgs& a, const Span& s,
 }
 // Of 32 keys, the first of this lane's being k: those that the query does not see give p = 0 and dP = 0.
 __device__ __forceinline__ void hide(const Keys& keys, int k, f32x16& x, f32x16& y) {
-  const int lo = keys.lo - k;
-  const unsigned len = max(keys.hi - keys.lo, 0);
+  const Mask mask = mask_of(keys, k);
 #pragma unroll
   for (int e = 0; e < 16; ++e) {
-    const bool seen = (unsigned)(8 * (e / 4) + e % 4 - lo) < len;
+    const bool seen = shows(mask, 8 * (e / 4) + e % 4);
     x[e] = seen ? x[e] : -INFINITY;
     y[e] = seen ? y[e] : 0.f;
   }

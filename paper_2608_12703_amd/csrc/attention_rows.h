@@ -48,7 +48,7 @@ AD_BOTH Span span_of(const AttnBatch& a, int b) {
   return s;
 }
 
-// The keys [lo, hi) that query i of the sequence sees (lo >= hi: none).
+// The keys [lo, hi) that query i of the sequence sees (lo >= hi: none), both ends in [0, nk] whatever the window holds.
 struct Keys {
   int lo, hi;
 };
@@ -57,11 +57,20 @@ AD_BOTH Keys keys_of(const AttnBatch& a, const Span& s, int i) {
   if (a.causal) r.hi = smaller(r.hi, larger(i + s.nk - s.nq + 1, 0));
   if (a.window) {
     const int* w = a.window + 2 * ((size_t)s.q0 + i);
-    r.lo = larger(r.lo, w[0]);
-    r.hi = smaller(r.hi, w[1]);
+    r.lo = smaller(larger(w[0], 0), s.nk);
+    r.hi = smaller(r.hi, larger(w[1], 0));
   }
   return r;
 }
+
+// Of the places from key `first` on, place e (at most a tile's) is seen where shows() says so: the keys' ends lie in
+// [0, nk], so no difference overflows.
+struct Mask {
+  int lo;
+  unsigned len;
+};
+AD_BOTH Mask mask_of(const Keys& k, int first) { return Mask{k.lo - first, (unsigned)larger(k.hi - k.lo, 0)}; }
+AD_BOTH bool shows(const Mask& m, int e) { return (unsigned)(e - m.lo) < m.len; }
 
 // Where wave w starts that takes 32 of the keys [lo, hi) in turn with others; where there are none (lo the largest
 // integer, hi = 0) it is not before hi, so that nothing is read.

@@ -578,7 +578,7 @@ ad_status ad_attention_backward(const ad_attn* a, const ad_mat* q, const ad_mat*
  */
 typedef enum { AD_STATE_F = 0, AD_STATE_8 = 1 } ad_state;
 typedef struct {
-  int64_t n;                  /* 0 <= n <= 2^40                                       */
+  int64_t n;                  /* 0 <= n <= 2^37 - 8192                                */
   void* param;                /* device [n] of param_dtype                            */
   void* copy;                 /* device [n] bf16 (optional, float32 param only): the
                                  parameter after the step, rounded                    */

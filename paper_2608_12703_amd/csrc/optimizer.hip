@@ -18,7 +18,8 @@ namespace ad {
 
 namespace {
 
-constexpr int kPass = 1024, kChunk = 8 * kPass;   // elements that a workgroup has at once, and in all
+constexpr int kPass = 1024, kChunk = kOptChunk;   // elements that a workgroup has at once, and in all
+static_assert(kChunk % kPass == 0, "whole passes");
 constexpr int kGroup = 128;                       // elements that share a scale: 32 lanes
 
 // ----------------------------------------------------------------- elements of any alignment
@@ -384,8 +385,6 @@ __global__ void __launch_bounds__(1024) grad_norm_few_kernel(OptList l, double m
 }
 
 }  // namespace
-
-int64_t opt_groups(int64_t n) { return (n + kChunk - 1) / kChunk; }
 
 void launch_adamw(const OptList& l, AdamwArgs a, hipStream_t st) {
   a.key = mix(a.seed + kGolden * (uint32_t)a.step);

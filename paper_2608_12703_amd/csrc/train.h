@@ -5,6 +5,7 @@
 #include "common.h"
 #include "../../include/ad.h"
 #include "attention_rows.h"
+#include "opt_launch.h"
 
 namespace ad {
 
@@ -356,8 +357,6 @@ struct OptTensor {
   int kinds;               // OPT_*
 };
 enum : int { OPT_PARAM16 = 1, OPT_GRAD16 = 2, OPT_STATE8 = 4 };
-// Tensors of one launch: kernel arguments hold 4 KB.
-constexpr int kOptTensors = 40;
 struct OptList {
   int count;
   int first[kOptTensors + 1];   // first workgroup of each tensor
@@ -373,7 +372,6 @@ struct AdamwArgs {
   const float *lr_at, *scale;
   const int* step_at;
 };
-int64_t opt_groups(int64_t n);   // workgroups of a tensor
 void launch_adamw(const OptList& l, AdamwArgs a, hipStream_t st);
 void launch_opt_state(const OptList& l, float* m, float* v, const int64_t* at, hipStream_t st);
 void launch_grad_squares(const OptList& l, double* part, hipStream_t st);

@@ -163,7 +163,7 @@ ad_status tensors_ok(const ad_opt_tensor* t, int32_t count) {
   if (count < 0) return fail(AD_ERANGE, "count must not be negative");
   if (count > 0 && !t) return bad("NULL argument: tensors");
   for (int32_t i = 0; i < count; ++i)
-    if (t[i].n < 0 || t[i].n > ((int64_t)1 << 40)) return fail(AD_ERANGE, "n must be in [0, 2^40]");
+    if (t[i].n < 0 || t[i].n > ad::kOptMost) return fail(AD_ERANGE, "n must be in [0, 2^37 - 8192]");
   return AD_OK;
 }
 ad_status array_ok(const char* name, const void* p, int size) {
@@ -190,39 +190,29 @@ ad_status state_ok(const ad_opt_tensor& t) {
 }
 
 // Hands the tensors that hold something to `go`, a launch's worth at a time: the list and the tensors' places.
-// Returns false where a launch would have too many workgroups.
 template <class F>
-bool by_launch(const ad_opt_tensor* t, int32_t count, double lr, F&& go) {
+void by_launch(const ad_opt_tensor* t, int32_t count, double lr, F&& go) {
   ad::OptList l;
   int at[ad::kOptTensors];
-  int64_t groups = 0;
-  l.count = 0;
-  l.first[0] = 0;
-  const auto flush = [&] {
-    if (l.count) go(l, at);
-    l.count = 0;
-    groups = 0;
-  };
-  for (int32_t i = 0; i < count; ++i) {
-    const int64_t more = ad::opt_groups(t[i].n);
-    if (!more) continue;
-    if (more >= INT32_MAX) return false;
-    if (l.count == ad::kOptTensors || groups + more >= INT32_MAX) flush();
-    ad::OptTensor& d = l.t[l.count];
-    d.n = t[i].n;
-    d.param = t[i].param; d.copy = t[i].copy; d.grad = t[i].grad;
-    d.m = t[i].m; d.v = t[i].v; d.m_scale = t[i].m_scale; d.v_scale = t[i].v_scale;
-    d.keep = (float)(1.0 - lr * t[i].weight_decay);
-    d.decay = (float)t[i].weight_decay;
-    d.key = (uint32_t)i;
-    d.kinds = (t[i].param_dtype == AD_BF16 ? ad::OPT_PARAM16 : 0) | (t[i].grad_dtype == AD_BF16 ? ad::OPT_GRAD16 : 0) |
-              (t[i].state == AD_STATE_8 ? ad::OPT_STATE8 : 0);
-    at[l.count] = i;
-    groups += more;
-    l.first[++l.count] = (int)groups;
+  for (int i = 0; i < count;) {
+    i = ad::opt_launch([&](int k) { return t[k].n; }, count, i, at, l.count);
+    if (!l.count) return;
+    l.first[0] = 0;
+    for (int k = 0; k < l.count; ++k) {
+      const ad_opt_tensor& f = t[at[k]];
+      ad::OptTensor& d = l.t[k];
+      d.n = f.n;
+      d.param = f.param; d.copy = f.copy; d.grad = f.grad;
+      d.m = f.m; d.v = f.v; d.m_scale = f.m_scale; d.v_scale = f.v_scale;
+      d.keep = (float)(1.0 - lr * f.weight_decay);
+      d.decay = (float)f.weight_decay;
+      d.key = (uint32_t)at[k];
+      d.kinds = (f.param_dtype == AD_BF16 ? ad::OPT_PARAM16 : 0) | (f.grad_dtype == AD_BF16 ? ad::OPT_GRAD16 : 0) |
+                (f.state == AD_STATE_8 ? ad::OPT_STATE8 : 0);
+      l.first[k + 1] = l.first[k] + (int)ad::opt_groups(f.n);
+    }
+    go(l, at);
   }
-  flush();
-  return true;
 }
 int64_t norm_parts(const ad_opt_tensor* t, int32_t count) {
   int64_t parts = 0;
@@ -511,7 +501,6 @@ ad_status ad_adamw(const ad_opt_tensor* tensors, int32_t count, const ad_adamw_a
     if (t.copy && t.param_dtype == AD_BF16) return bad("copy goes with a float32 param");
     if ((uintptr_t)t.copy % 2) return bad("misaligned: copy");
     if (t.n) AD_TRY(array_ok("param", t.param, width(t.param_dtype)));
-    if (ad::opt_groups(t.n) >= INT32_MAX) return fail(AD_ERANGE, "n is too large");
   }
   ad::AdamwArgs a{};
   a.b1 = (float)h.beta1; a.ob1 = (float)(1.0 - h.beta1);
@@ -533,10 +522,7 @@ ad_status ad_opt_state(const ad_opt_tensor* tensors, int32_t count, float* m, fl
   AD_TRY(tensors_ok(tensors, count));
   AD_TRY(floats_ok("m", m));
   AD_TRY(floats_ok("v", v));
-  for (int32_t i = 0; i < count; ++i) {
-    AD_TRY(state_ok(tensors[i]));
-    if (ad::opt_groups(tensors[i].n) >= INT32_MAX) return fail(AD_ERANGE, "n is too large");
-  }
+  for (int32_t i = 0; i < count; ++i) AD_TRY(state_ok(tensors[i]));
   (void)hipGetLastError();
   int64_t at = 0;
   int32_t done = 0;
@@ -564,10 +550,7 @@ ad_status ad_grad_norm(const ad_opt_tensor* tensors, int32_t count, double max_n
   if (!(max_norm >= 0 && std::isfinite(max_norm))) return fail(AD_ERANGE, "max_norm must be finite and not negative");
   AD_TRY(array_ok("out", out, 4));
   if ((uintptr_t)step % 4) return bad("misaligned: step");
-  for (int32_t i = 0; i < count; ++i) {
-    AD_TRY(grad_ok(tensors[i]));
-    if (ad::opt_groups(tensors[i].n) >= INT32_MAX) return fail(AD_ERANGE, "n is too large");
-  }
+  for (int32_t i = 0; i < count; ++i) AD_TRY(grad_ok(tensors[i]));
   const int64_t parts = norm_parts(tensors, count);
   AD_TRY(space_ok(workspace, workspace_bytes, align256(8 * (size_t)parts)));
   (void)hipGetLastError();

@@ -603,8 +603,8 @@ typedef struct {
  * mean (steps are smaller than half its spacing).  Random bits come from a hash of (seed, t, the
  * tensor's place in the list, the element); the caller gives a run a seed.
  * lr_at / step_at (device, optional) replace lr and step, for steps in a captured graph; with
- * grad_scale (device [1], optional) not finite nothing is written (see ad_grad_norm).  No two tensors may
- * overlap.  count = 0 does nothing.
+ * grad_scale (device [1], optional) not finite (see ad_grad_norm), or a value at lr_at or step_at that would be refused
+ * as lr or step, nothing is written.  No two tensors may overlap.  count = 0 does nothing.
  * Errors: AD_EINVAL (NULL argument, unknown dtype or state, misaligned pointer, copy of a bf16 param), AD_ERANGE
  * (n, step < 1, lr < 0 or not finite, betas outside [0, 1), eps < 0, weight_decay < 0), AD_EHIP.
  */

@@ -170,6 +170,7 @@ struct Hyper {
   float root, rate;
   uint32_t key;
   float lr;
+  int fine;       // step and lr are what the host takes
 };
 
 template <bool STATE8>
@@ -251,7 +252,7 @@ __device__ __forceinline__ void adamw_pass(const OptTensor& t, const AdamwArgs& 
 __global__ void __launch_bounds__(256) adamw_kernel(OptList l, AdamwArgs a) {
   __shared__ Hyper shared;
   const OptTensor& t = l.t[find(l, blockIdx.x)];
-  Hyper y = {a.root, a.rate, a.key, 0.f};
+  Hyper y = {a.root, a.rate, a.key, 0.f, 1};
   float keep = t.keep;
   if (a.lr_at || a.step_at) {
     if (threadIdx.x == 0) {
@@ -261,13 +262,14 @@ __global__ void __launch_bounds__(256) adamw_kernel(OptList l, AdamwArgs a) {
       shared.rate = (float)(lr / -expm1(step * log(a.beta1)));
       shared.key = mix(a.seed + kGolden * (uint32_t)step);
       shared.lr = (float)lr;
+      shared.fine = step >= 1 && lr >= 0.0 && lr < INFINITY;
     }
     __syncthreads();
     y = shared;
     keep = (float)(1.0 - (double)y.lr * (double)t.decay);
   }
   const float gs = a.scale ? *a.scale : 1.f;
-  if (!(fabsf(gs) < INFINITY)) return;
+  if (!y.fine || !(fabsf(gs) < INFINITY)) return;
   const uint32_t key = mix(t.key + y.key);
   const int64_t base = (int64_t)(blockIdx.x - l.first[&t - l.t]) * kChunk;
   for (int c = 0; c < kChunk; c += kPass) {

@@ -381,10 +381,6 @@ __device__ __forceinline__ int wave_most(int v) {
   return v;
 }
 // What 32 queries (one a column, both halves alike) see together.
-struct Range {
-  int lo, hi;          // some of them may see [lo, hi)
-  int all_lo, all_hi;  // all of them see [all_lo, all_hi)
-};
 __device__ __forceinline__ Range range_of(const Keys& k, bool in) {
   const bool some = in && k.lo < k.hi;
   Range r;
@@ -1318,56 +1314,11 @@ struct StatLoads {
   }
 };
 
-// The steps of a workgroup's keys [k0, k1): tiles of TQ queries of one head after the other, those that some
-// of the keys are seen by.
-template <int TQ>
-struct Walk {
-  // (the first kernel's table is constant here: scalar loads)
-  typedef const __attribute__((address_space(4))) int* Table;
-  Table ranges;
-  bool window, causal;
-  int nq, nk, k0, k1, start, tiles, t, h, heads_end;
-  __device__ __forceinline__ Walk(const AttnBwdArgs& a, const Span& s, int b, int g, int k0_, int k1_) {
-    ranges = (Table)(uintptr_t)(a.ranges + (size_t)b * a.blocks);
-    window = a.b.window;
-    causal = a.b.causal;
-    nq = s.nq; nk = s.nk; k0 = k0_; k1 = k1_;
-    tiles = (nq + TQ - 1) / TQ;
-    // (causal: the queries before key - (nk - nq) do not see the key)
-    start = causal ? min(max(k0 - (nk - nq), 0) / TQ, tiles) : 0;
-    const int group = a.b.group;
-    t = start;
-    h = g * group;
-    heads_end = h + group;
-  }
-  // what the queries 32 u .. + 31 see together
-  __device__ __forceinline__ Range seen(int u) const {
-    Range r = {0, nk, 0, nk};
-    if (window) {
-      const Table p = ranges + 4 * u;
-      r = Range{p[0], p[1], p[2], p[3]};
-    } else if (causal) {
-      r.all_hi = 32 * u + nk - nq + 1;
-      r.hi = min(nk, r.all_hi + 31);
-    }
-    return r;
-  }
-  __device__ __forceinline__ bool wanted() const {
-    if (!window) return true;
-    for (int u = t * (TQ / 32); u < min((t + 1) * (TQ / 32), (nq + 31) / 32); ++u) {
-      const Range r = seen(u);
-      if (r.lo < k1 && r.hi > k0) return true;
-    }
-    return false;
-  }
-  // from (h, t) on to a step that is wanted; false: there is none
-  __device__ __forceinline__ bool settle() {
-    for (; h < heads_end; ++h, t = start)
-      for (; t < tiles; ++t)
-        if (wanted()) return true;
-    return false;
-  }
-};
+// (the first kernel's table is constant here: scalar loads)
+typedef const __attribute__((address_space(4))) int* Table;
+__device__ __forceinline__ Table ranges_of(const AttnBwdArgs& a, int b) {
+  return (Table)(uintptr_t)(a.ranges + (size_t)b * a.blocks);
+}
 
 __device__ __forceinline__ void keys_operands(const AttnBwdArgs& a, const Span& s, int g, int j, const Lane& l, bf16x8 (&k)[4],
                                               bf16x8 (&v)[4]) {
@@ -1479,7 +1430,7 @@ __device__ __forceinline__ void dkv_wide(const AttnBwdArgs& a, int before) {
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const Lane l(threadIdx.x % kWave);
   const int j0 = at.tile * 128 + 32 * w, j = j0 + l.n;
-  Walk<TQ> walk(a, s, at.b, g, at.tile * 128, min(at.tile * 128 + 128, s.nk));
+  Walk<TQ, Table> walk(a.b, s, ranges_of(a, at.b), g, at.tile * 128, min(at.tile * 128 + 128, s.nk));
   Loads<DIRECT> qs, gs;
   StatLoads<TQ, OWN> ss;
   qs.init(a.q, s.q0, s.nq, 0);
@@ -1570,7 +1521,7 @@ __global__ void __launch_bounds__(256, 2) attn_dkv_few_kernel(AttnBwdArgs a) {
   const int j = j0 + l.n;
   bf16x8 k[4], v[4];
   keys_operands(a, s, g, j, l, k, v);
-  Walk<TQ> walk(a, s, at.b, g, j0, min(j0 + 32, s.nk));
+  Walk<TQ, Table> walk(a.b, s, ranges_of(a, at.b), g, j0, min(j0 + 32, s.nk));
   Stage<TQ> qs, gs;
   StatLoads<TQ> ss;
   f32x16 dk[2] = {zeros(), zeros()}, dv[2] = {zeros(), zeros()};

@@ -72,6 +72,60 @@ struct Mask {
 AD_BOTH Mask mask_of(const Keys& k, int first) { return Mask{k.lo - first, (unsigned)larger(k.hi - k.lo, 0)}; }
 AD_BOTH bool shows(const Mask& m, int e) { return (unsigned)(e - m.lo) < m.len; }
 
+// What 32 queries see together.
+struct Range {
+  int lo, hi;          // some of them may see [lo, hi)
+  int all_lo, all_hi;  // all of them see [all_lo, all_hi)
+};
+
+// The steps of a workgroup's keys [k0, k1): tiles of TQ queries of one head after the other, those that some
+// of the keys are seen by.  ranges: of every 32 queries of the sequence the four numbers of a Range (read with windows only).
+template <int TQ, class Table>
+struct Walk {
+  Table ranges;
+  bool window, causal;
+  int nq, nk, k0, k1, start, tiles, t, h, heads_end;
+  AD_BOTH Walk(const AttnBatch& a, const Span& s, Table ranges_, int g, int k0_, int k1_) {
+    ranges = ranges_;
+    window = a.window;
+    causal = a.causal;
+    nq = s.nq; nk = s.nk; k0 = k0_; k1 = k1_;
+    tiles = (nq + TQ - 1) / TQ;
+    // (causal: the queries before key - (nk - nq) do not see the key)
+    start = causal ? smaller(larger(k0 - (nk - nq), 0) / TQ, tiles) : 0;
+    t = start;
+    h = g * a.group;
+    heads_end = k1 > k0 ? h + a.group : h;      // (keys that are all padding: no steps)
+  }
+  // what the queries 32 u .. + 31 see together
+  AD_BOTH Range seen(int u) const {
+    Range r = {0, nk, 0, nk};
+    if (window) {
+      const Table p = ranges + 4 * u;
+      r = Range{p[0], p[1], p[2], p[3]};
+    } else if (causal) {
+      r.all_hi = 32 * u + nk - nq + 1;
+      r.hi = smaller(nk, r.all_hi + 31);
+    }
+    return r;
+  }
+  AD_BOTH bool wanted() const {
+    if (!window) return true;
+    for (int u = t * (TQ / 32); u < smaller((t + 1) * (TQ / 32), (nq + 31) / 32); ++u) {
+      const Range r = seen(u);
+      if (r.lo < k1 && r.hi > k0) return true;
+    }
+    return false;
+  }
+  // from (h, t) on to a step that is wanted; false: there is none
+  AD_BOTH bool settle() {
+    for (; h < heads_end; ++h, t = start)
+      for (; t < tiles; ++t)
+        if (wanted()) return true;
+    return false;
+  }
+};
+
 // Where wave w starts that takes 32 of the keys [lo, hi) in turn with others; where there are none (lo the largest
 // integer, hi = 0) it is not before hi, so that nothing is read.
 AD_BOTH int first_piece(int lo, int hi, int w) { return smaller(lo, hi) / 32 * 32 + 32 * w; }

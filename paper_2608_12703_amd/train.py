@@ -342,6 +342,7 @@ class DraftBlock:
         self.self_attention = SelfAttention(params[0:6], max_rows, scratch)
         self.cross_attention = CrossAttention(params[6:14], max_rows, max_keys, scratch)
         self.feed_forward = FeedForward(params[14:20], max_rows, Scratch(d, f, max_rows, dev))
+        self._parts = (self.self_attention, self.cross_attention, self.feed_forward)
         self.grads = self.self_attention.grads + self.cross_attention.grads + self.feed_forward.grads
 
     def zero_grads(self):
@@ -349,7 +350,10 @@ class DraftBlock:
             g.zero_()
 
     def forward(self, x, enc, self_batch: ad.Attention, cross_batch: ad.Attention, out, xq=None):
-        """out <- the block of float32 rows x [rows][d] and encoder states enc (bf16 [keys][d]); out may be x."""
+        """out <- the block of float32 rows x [rows][d] and encoder states enc (bf16 [keys][d]); out may be x.  After a
+        refused pass there is nothing to go back from."""
+        for part in self._parts:       # (one that is refused halfway has new rows in some and old ones in others)
+            part.rows = None
         self.self_attention.forward(x, self_batch, out)
         self.cross_attention.forward(out, enc, cross_batch, out, xq)
         self.feed_forward.forward(out, out)

@@ -359,7 +359,16 @@ class DraftBlock:
         self.feed_forward.forward(out, out)
 
     def backward(self, dout, dx, dxq=None):
-        """dx <- dL/dx (float32) from dout = dL/dout, and the parameters' gradients added; dx may be dout."""
+        """dx <- dL/dx (float32) from dout = dL/dout, and the parameters' gradients added; dx may be dout.  A refused pass
+        adds nothing."""
+        rows = dout.shape[0]
+        for part in self._parts:
+            if part.rows != rows:
+                raise ValueError(f"{rows} rows, but the last forward pass had {part.rows}")
+        self.feed_forward._rows("dout", dout, rows, torch.float32, torch.bfloat16)
+        self.feed_forward._rows("dx", dx, rows, torch.float32, torch.bfloat16)
+        if dxq is not None:
+            self.cross_attention._check("dxq", dxq, rows, torch.float32, torch.bfloat16)
         self.feed_forward.backward(dout, dx)
         self.cross_attention.backward(dx, dx, dxq=dxq)
         self.self_attention.backward(dx, dx)

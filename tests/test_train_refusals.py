@@ -1,5 +1,5 @@
-"""A refused pass of the draft block leaves nothing to go back from (CPU only: the sublayers' own calls are refused or
-replaced)."""
+"""A refused pass of the draft block leaves nothing to go back from, and a refused way back adds nothing (CPU only: the
+sublayers' own calls are refused or replaced)."""
 import pytest
 import torch
 
@@ -50,3 +50,26 @@ def test_a_refused_pass_leaves_nothing_to_go_back_from(refused, monkeypatch):
         block.forward(x, enc, _batch(3, 3), _batch(3, 5), torch.zeros(3, 64), xq)
     with pytest.raises(ValueError, match="last forward pass had None"):
         block.backward(torch.zeros(3, 64), torch.zeros(3, 64))
+
+
+@pytest.mark.parametrize("bad", ["rows", "cross", "dout", "dx", "dxq"])
+def test_a_refused_way_back_reaches_no_sublayer(bad, monkeypatch):
+    block, parts = _block()
+    for s in parts:
+        s.rows = 3
+        monkeypatch.setattr(s, "backward", lambda *a, **kw: pytest.fail("a sublayer ran"))
+    if bad == "cross":
+        block.cross_attention.rows = 2
+    # (the tensors' own checks, without a GPU)
+    def check(name, t, rows, *dtypes):
+        if t.shape != (rows, 64) or t.dtype not in dtypes:
+            raise ValueError(name)
+    monkeypatch.setattr(block.cross_attention, "_check", check)
+    monkeypatch.setattr(block.feed_forward, "_rows", check)
+    t = dict(dout=torch.zeros(3, 64), dx=torch.zeros(3, 64), dxq=torch.zeros(3, 64))
+    if bad == "rows":
+        t["dout"] = torch.zeros(2, 64)
+    elif bad in t:
+        t[bad] = torch.zeros(3, 32) if bad != "dxq" else torch.zeros(3, 64, dtype=torch.float16)
+    with pytest.raises(ValueError):
+        block.backward(t["dout"], t["dx"], t["dxq"])

@@ -650,7 +650,10 @@ class OptTensors:
 
     def __init__(self, params=None, grads=None, m=None, v=None, m_scale=None, v_scale=None, copies=None,
                  weight_decay=0.0):
-        lists = dict(params=params, grads=grads, m=m, v=v, m_scale=m_scale, v_scale=v_scale, copies=copies)
+        # (tuples of its own: the tensors live as long as their addresses are used, whatever becomes of the caller's lists)
+        lists = {name: None if x is None else tuple(x) for name, x in
+                 dict(params=params, grads=grads, m=m, v=v, m_scale=m_scale, v_scale=v_scale, copies=copies).items()}
+        params, grads, m, v, m_scale, v_scale, copies = lists.values()
         given = [x for x in (grads, params, m) if x is not None]
         if not given:
             raise ValueError("no tensors given")

@@ -644,7 +644,8 @@ def attention_backward(at: Attention, q, k, v, o, o_rest, lse, dout, dq_res, dq,
 
 class OptTensors:
     """Parameters with their gradients and optimizer states (ad.h: ad_opt_tensor), kept from one step to the
-    next: lists of contiguous tensors of equal sizes on one GPU.  m and v are float32, or int8 and uint8 with the
+    next: lists of contiguous tensors of equal sizes on one GPU, of which a step's may not overlap (gradients among
+    themselves may).  m and v are float32, or int8 and uint8 with the
     scales m_scale and v_scale of every 128 elements; copies (bf16) and any list that a call does not use may
     be None; weight_decay is one number or a list."""
 
@@ -689,6 +690,20 @@ class OptTensors:
                     raise ValueError("8-bit states need m_scale and v_scale")
                 e.m_scale = self._at("m_scale", m_scale[i], groups, torch.float32)
                 e.v_scale = self._at("v_scale", v_scale[i], groups, torch.float32)
+        if self.steps:
+            self._apart()
+
+    def _apart(self):
+        """Refuses a step that would write an element twice, or as it reads it as a gradient."""
+        spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), name != "grads", f"{name}[{i}]")
+                       for name, x in self.tensors.items() if x is not None for i, t in enumerate(x) if t is not None and t.numel())
+        most = {False: (0, ""), True: (0, "")}      # how far those before reach: all of them, those that are written
+        for begin, end, written, name in spans:
+            over, other = most[not written]
+            if begin < over:
+                raise ValueError(f"{name} and {other} overlap: a step would write one of them twice, or as it reads it")
+            for kind in (False, True) if written else (False,):
+                most[kind] = max(most[kind], (end, name))
 
     def _at(self, name: str, t, n: int, *dtypes):
         if t is None:

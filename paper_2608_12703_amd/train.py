@@ -379,7 +379,9 @@ class AdamW:
     clipped to norm 1).  params: bf16 or float32 tensors on the GPU, which a step writes; grads: tensors of their
     shapes, float32 or bf16.  bf16 parameters have float32 ones here, of which they are the rounded copies.
     state: "f32" or "8bit".  Learning rate, step count and norm live on the GPU, so that a step can be captured
-    into a graph with the pass that makes its gradients."""
+    into a graph with the pass that makes its gradients.  The float32 parameters are made once: a step overwrites values
+    that were put into bf16 ones since, unless read_params() is called.  state_dict() and load_state_dict() carry a
+    training run over."""
 
     def __init__(self, params, grads, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01,
                  max_norm: float = 1.0, state: str = "f32", seed: int = 0):
@@ -397,6 +399,7 @@ class AdamW:
         if eight:
             for name in ("m_scale", "v_scale"):
                 states[name] = [make(-(-p.numel() // 128), torch.float32) for p in params]
+        self.state, self._kept = state, states
         decay = [weight_decay if p.dim() > 1 else 0.0 for p in params]
         # (copies: float32 parameters are their own)
         groups = ([i for i, p in enumerate(params) if p.dtype is torch.float32],
@@ -421,6 +424,42 @@ class AdamW:
         ad.grad_norm(self._all, self.max_norm, self.norm, self._workspace, step=self.steps)
         for k, part in enumerate(self._parts):
             ad.adamw(part, self.lr, self.steps, *self.betas, self.eps, self.seed + k, self.norm[1:])
+
+    def _states(self):
+        """What a step reads and writes besides the parameters' copies: lists of tensors by name."""
+        return dict(master=self.master, **self._kept)
+
+    @torch.no_grad()
+    def read_params(self):
+        """Takes the parameters as they are now, after new values were put into them; the states stay."""
+        for p, master in zip(self.params, self.master):
+            if master is not p:
+                master.copy_(p)
+
+    def state_dict(self):
+        """Copies of everything that the next step hangs on: the float32 parameters, the states as they are held, step
+        count, learning rate and seed."""
+        return dict(state=self.state, seed=self.seed, steps=self.steps.clone(), lr=self.lr.clone(),
+                    **{name: [t.clone() for t in x] for name, x in self._states().items()})
+
+    @torch.no_grad()
+    def load_state_dict(self, saved):
+        """Goes on from state_dict() of an optimizer over parameters of the same shapes, and writes the parameters.  In
+        place: a captured step goes on with them (and with the seed that it was captured with).  What does not fit is
+        refused as a whole."""
+        if saved["state"] != self.state:
+            raise ValueError(f"states in {saved['state']!r}, expected {self.state!r}")
+        pairs = [(name, t, u) for name, x in self._states().items() for t, u in zip(x, saved[name], strict=True)]
+        for name, t, u in (*pairs, ("steps", self.steps, saved["steps"]), ("lr", self.lr, saved["lr"])):
+            if t.shape != u.shape or t.dtype is not u.dtype:
+                raise ValueError(f"{name}: {tuple(u.shape)} of {u.dtype}, expected {tuple(t.shape)} of {t.dtype}")
+        seed = int(saved["seed"])
+        for _, t, u in (*pairs, ("", self.steps, saved["steps"]), ("", self.lr, saved["lr"])):
+            t.copy_(u)
+        for p, master in zip(self.params, self.master):
+            if master is not p:
+                p.copy_(master)
+        self.seed = seed
 
     def states(self):
         """(m, v) of every parameter as float32 tensors of its shape."""

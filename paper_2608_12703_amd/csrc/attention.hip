@@ -575,8 +575,8 @@ __global__ void __launch_bounds__(256, 2) attn_fwd_few_kernel(AttnFwdArgs a, int
   const bool live = row < s.oq, some = row < s.nq && total != 0.f;
   if (splits > 1) {
     if (!live) return;
-    const size_t to = ((size_t)split * a.b.heads + h) * a.b.q_rows + s.q0 + row;
-    const size_t rows = (size_t)splits * a.b.heads * a.b.q_rows;
+    const size_t each = part_rows(a.b), rows = splits * each;
+    const size_t to = split * each + part_row(a.b, b, h, row);
     *(f32x4*)(a.part + to * 64 + d0) = f32x4{v[0], v[1], v[2], v[3]};
     *(f32x4*)(a.part + to * 64 + d0 + 4) = f32x4{v[4], v[5], v[6], v[7]};
     if (d0 == 0) {
@@ -905,8 +905,8 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnFwdArgs a, int split
   const Span s = span_of(a.b, b);
   const int i = tile * 4 + threadIdx.x / kWave, d = threadIdx.x % kWave;
   if (!s.ok || i >= s.oq) return;
-  const size_t stride = (size_t)a.b.heads * a.b.q_rows, rows = stride * splits;
-  const size_t row = s.q0 + i, at = (size_t)h * a.b.q_rows + row;
+  const size_t stride = part_rows(a.b), rows = stride * splits;
+  const size_t row = s.q0 + i, at = part_row(a.b, b, h, i);
   // (lane u holds part u's maximum; there are at most 64)
   const float mu = d < splits ? a.part[rows * 64 + at + d * stride] : -INFINITY;
   const float lu = d < splits ? a.part[rows * 65 + at + d * stride] : 0.f;
@@ -931,7 +931,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnFwdArgs a, int split
   const uint16_t hi = f32_to_bf16(o);
   a.o.p[row * a.o.ld + 64 * h + d] = hi;
   if (a.rest.p) a.rest.p[row * a.rest.ld + 64 * h + d] = f32_to_bf16(o - bf16_to_f32(hi));
-  if (a.lse && d == 0) a.lse[at] = total == 0.f ? -INFINITY : (top + __log2f(total)) * kLn2;
+  if (a.lse && d == 0) a.lse[(size_t)h * a.b.q_rows + row] = total == 0.f ? -INFINITY : (top + __log2f(total)) * kLn2;
 }
 
 // ----------------------------------------------------------------- backward

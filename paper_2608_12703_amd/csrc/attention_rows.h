@@ -168,9 +168,13 @@ inline FwdPlan fwd_plan(const AttnBatch& b) {
   return p;
 }
 
+// A part's rows, and a query's place among them.  By sequence and not by the matrix's rows, which may be far more: so
+// all parts have at most the rows of fwd_plan's 512 workgroups.
+AD_BOTH size_t part_rows(const AttnBatch& b) { return (size_t)b.heads * b.batch * b.q_max; }
+AD_BOTH size_t part_row(const AttnBatch& a, int b, int h, int i) { return ((size_t)h * a.batch + b) * a.q_max + i; }
 inline size_t attn_fwd_bytes(const AttnBatch& b) {
   const FwdPlan p = fwd_plan(b);
-  return p.splits > 1 ? 4ull * 66 * p.splits * b.heads * b.q_rows : 0;
+  return p.splits > 1 ? 4ull * 66 * p.splits * part_rows(b) : 0;
 }
 // delta [heads][q_rows], then what 32 queries of a sequence see together [batch][blocks]
 inline size_t attn_bwd_delta_bytes(const AttnBatch& b) { return (4ull * b.heads * b.q_rows + 255) / 256 * 256; }

@@ -30,6 +30,8 @@ ROUTES = {
     "few_several_windows": ("few several", dict(ql=[6] * 300, kl=_lens(300, 500, 8), heads=1, kv=1,
                                                 window=_wide_windows(1800, 500, 400, 9))),
     "parts_one": ("few parts one", dict(ql=[17, 65, 3], kl=[2600, 217, 64], heads=2, kv=1)),
+    "parts_outside": ("few parts one", dict(ql=[3, 1, 2], kl=[2600, 130, 700], heads=2, kv=1, lead=300)),
+    "parts_outside_padded": ("few parts several", dict(ql=[30, 1], kl=[9000, 130], heads=1, kv=1, lead=300, padded=True)),
     "parts_several": ("few parts several", dict(ql=[1], kl=[10000], heads=1, kv=1)),
     "parts_several_heads": ("few parts several", dict(ql=[3, 1, 20], kl=[3000, 2700, 0], heads=20, kv=5)),
     "parts_several_causal": ("few parts several", dict(ql=[40, 3], kl=[9000, 8300], heads=1, kv=1, causal=True)),

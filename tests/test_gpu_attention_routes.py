@@ -4,7 +4,7 @@ import functools
 
 import pytest
 
-from attention_common import Batch, Ref, backward, forward, near
+from attention_common import GUARD, Batch, Ref, backward, forward, near
 from attention_routes import ROUTES
 
 pytestmark = pytest.mark.gpu
@@ -24,7 +24,8 @@ def test_ways_through_attention(name, pad, shift):
     got, low = o.get(), rest.get()
     near(got, ref.o, ref.tol_o, "o")
     near(lse.double().cpu(), ref.lse, ref.tol_lse, "lse")
-    assert bool((low.abs() <= got.abs() * 2.0 ** -8).all()) and int(at.err_flag) == 0
+    inside = ref.o != GUARD
+    assert bool((low.abs() <= got.abs() * 2.0 ** -8)[inside].all()) and bool((low == GUARD)[~inside].all()) and int(at.err_flag) == 0
     dq, dk, dv = backward(bt, ref, pad, shift)
     near(dq, ref.dq, ref.tol_dq, "dq")
     near(dk, ref.dk, ref.tol_dk, "dk")

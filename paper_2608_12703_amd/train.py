@@ -389,6 +389,12 @@ class AdamW:
             raise ValueError(f"state {state!r}, expected 'f32' or '8bit'")
         if not params or len(params) != len(grads):
             raise ValueError(f"{len(params)} parameters and {len(grads)} gradients")
+        # (what a call of the step would refuse: the norm has counted the step by then)
+        beta1, beta2 = betas
+        if not (0.0 <= beta1 < 1.0 and 0.0 <= beta2 < 1.0):
+            raise ValueError(f"betas {betas}, expected two numbers in [0, 1)")
+        for name, x in (("lr", lr), ("eps", eps), ("weight_decay", weight_decay), ("max_norm", max_norm)):
+            self._number(name, x)
         dev = params[0].device
         make = lambda n, dt: torch.zeros(n, dtype=dt, device=dev)  # noqa: E731
         self.params, self.grads, self.betas, self.eps, self.max_norm, self.seed = params, grads, betas, eps, max_norm, seed
@@ -416,7 +422,13 @@ class AdamW:
         self.steps = make(1, torch.int32)          # steps taken
         self.norm = make(2, torch.float32)         # the last gradients' norm, and the factor they were clipped with
 
+    @staticmethod
+    def _number(name: str, x: float):
+        if not 0.0 <= x <= torch.finfo(torch.float32).max:
+            raise ValueError(f"{name} {x}, expected a finite number of float32 that is not negative")
+
     def set_lr(self, lr: float):
+        self._number("lr", lr)
         self.lr.fill_(lr)
 
     def step(self):

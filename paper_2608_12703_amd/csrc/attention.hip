@@ -37,10 +37,10 @@ __device__ __forceinline__ float at(const HMat& m, size_t row, int col) {
   return m.p ? bf16_to_f32(m.p[row * m.ld + col]) : 0.f;
 }
 
-// A row at a time, a lane a dimension: what is right whatever the keys hold, since only visible
-// ones are read.  A key takes a wave about 0.9 us (dk and dv: 1.7 a query), so a walk ends where nothing can change any
-// more: a sum that is NaN stays NaN.  32 x 448 x 1500, 20 heads, all rows NaN: 0.23 ms forward and 1.5 back, where walks to
-// the end take 104 and 360 (a row that is not finite in some of its columns only still does).
+// A row at a time, a lane a dimension: what is right whatever the keys hold, since only visible ones are read.  A key
+// takes a wave about 0.9 us, so a walk ends where nothing can change any more: a sum that is NaN stays NaN.  32 x 448 x
+// 1500, 20 heads, all rows NaN: 0.23 ms forward and 1.6 back, where walks to the end take 104 and 360.  (What is not finite
+// in some columns only is walked to the end: an infinity in one column of every value, 35 ms and 39.)
 __device__ void fwd_row(const AttnFwdArgs& a, const Span& s, int h, int i) {
   const int d = threadIdx.x % kWave, g = key_head(a.b, h);
   const size_t row = s.q0 + i;
@@ -97,18 +97,24 @@ __device__ void dkv_row(const AttnBwdArgs& a, const Span& s, int g, int j) {
   if (j < s.nk) {
     const float k = at(a.k, row, 64 * g + d) * kScale2, v = at(a.v, row, 64 * g + d);
     const int first = a.b.causal ? max(j - (s.nk - s.nq), 0) : 0, tiles = (s.nq - first + kWave - 1) / kWave;
+    // lse in powers of two of 64 queries of a head, a lane each, -infinity where they do not see the key
+    const auto seen = [&](int t) {
+      const int i = first + t % tiles * kWave + d;
+      if (i >= s.nq) return -INFINITY;
+      const Keys r = keys_of(a.b, s, i);
+      return j >= r.lo && j < r.hi ? a.lse[(size_t)(g * n + t / tiles) * a.b.q_rows + s.q0 + i] * kLog2e : -INFINITY;
+    };
+    // (a query whose scores are NaN: so are its p and dS, and there is nothing to add up)
     bool more = true;
     for (int t = 0; t < n * tiles && more; ++t) {
-      // 64 queries of a head, a lane each: those that see the key
-      const int h = g * n + t / tiles, i0 = first + t % tiles * kWave, mine = i0 + d;
-      float each = -INFINITY;
-      bool sees = false;
-      if (mine < s.nq) {
-        const Keys r = keys_of(a.b, s, mine);
-        each = a.lse[(size_t)h * a.b.q_rows + s.q0 + mine] * kLog2e;
-        sees = j >= r.lo && j < r.hi && each != -INFINITY;
-      }
-      for (uint64_t left = __ballot(sees); left && more; left &= left - 1) {
+      const float each = seen(t);
+      more = !__any(each != each);
+    }
+    if (!more) dk = dv = __uint_as_float(0x7fc00000u);
+    for (int t = 0; t < n * tiles && more; ++t) {
+      const int h = g * n + t / tiles, i0 = first + t % tiles * kWave;
+      const float each = seen(t);
+      for (uint64_t left = __ballot(each != -INFINITY); left && more; left &= left - 1) {
         const int i = __builtin_ctzll(left);
         const size_t qr = s.q0 + (size_t)(i0 + i);
         const float lse = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(each), i));

@@ -54,7 +54,7 @@ def _time(f):
     return a.elapsed_time(b)
 
 
-@pytest.mark.parametrize("place", ["q", "kv", "dout", "all"])
+@pytest.mark.parametrize("place", ["q", "kv", "dout", "all", "last"])
 @pytest.mark.parametrize("causal", [False, True])
 def test_a_pass_of_nan_ends_soon(causal, place):
     """32 sequences of 448 rows, 20 heads: 0.05 to 0.6 ms with finite rows.  Each wave computes its 32 rows again, of which
@@ -64,7 +64,8 @@ def test_a_pass_of_nan_ends_soon(causal, place):
     g = torch.Generator(device="cuda").manual_seed(1)
     rand = lambda rows: torch.randn(rows, 64 * heads, generator=g, device="cuda").to(BF16)  # noqa: E731
     q, do, k, v = rand(batch * nq), rand(batch * nq), rand(batch * nk), rand(batch * nk)
-    for t in {"q": (q,), "kv": (k, v), "dout": (do,), "all": (q, k, v, do)}[place]:
+    last = q.view(batch, nq, -1)[:, -1]           # one row of each sequence, which sees every key
+    for t in {"q": (q,), "kv": (k, v), "dout": (do,), "all": (q, k, v, do), "last": (last,)}[place]:
         t.fill_(math.nan)
     ints = lambda n: torch.arange(batch + 1, dtype=torch.int32, device="cuda") * n  # noqa: E731
     at = ad.Attention(heads, heads, ints(nq), ints(nk), nq, nk, causal=causal)
@@ -74,4 +75,7 @@ def test_a_pass_of_nan_ends_soon(causal, place):
     fwd, bwd = buf(ad.attention_workspace_size), buf(ad.attention_backward_workspace_size)
     assert _time(lambda: ad.attention(at, q, k, v, o, lse, rest, fwd)) < 10.0
     assert _time(lambda: ad.attention_backward(at, q, k, v, o, rest, lse, do, None, dq, dk, dv, bwd)) < 10.0
-    assert bool(torch.isnan(dq).all()) and bool(torch.isnan(dk).all()) and (place == "dout" or bool(torch.isnan(o).all()))
+    rows = slice(None) if place != "last" else slice(nq - 1, None, nq)
+    assert bool(torch.isnan(dq[rows]).all()) and bool(torch.isnan(dk).all()) and bool(torch.isnan(dv).all())
+    assert place == "dout" or bool(torch.isnan(o[rows]).all())
+    assert place != "last" or int(torch.isnan(o).sum()) == int(torch.isnan(dq).sum()) == batch * 64 * heads

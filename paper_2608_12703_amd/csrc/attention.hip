@@ -13,11 +13,13 @@
 // The second part costs dq's kernel a quarter on large shapes (32 x 448 x 1500 197 to 250 us).
 // m, lse and scores are kept in powers of two inside the kernels.
 //
-// What bounds the large shapes is a wave's own instructions, not memory.  For 64 keys x 32 queries a wave has 16 products
-// of 32 x 32 x 16 in 512 cycles and about 860 cycles of vector instructions (scale, exponential, maximum, sum, rounding),
-// 1590 in all alone on a SIMD; dq 768 + 830 (and 256 for dS's second part), dk and dv 1024 + 1000 of 2575.  Other waves of
-// the SIMD fill some of the gaps: 8 x 2048 rows, 20 heads: forward 208 us (825 TF/s; a large bf16 product reaches 1485).
-// Prologue and epilogue make short ones slower: 32 x 448 x 1500 forward 172 us (640 TF/s).
+// For 64 keys x 32 queries a wave issues vector instructions (scale, exponential, maximum, sum, rounding; the issue of the
+// products counted) for 860 cycles beside 512 of products forward, 1230 beside 1024 in dq, 1310 beside 1024 in dk and dv.
+// Forward that is the bound of a large shape: by the counters of 8 x 2048 rows, 20 heads, vector instructions have 72% of a
+// SIMD's cycles and products 43%, with 3.2 waves on it (195 us, 880 TF/s; a large bf16 product reaches 1630).  The gradients
+// fill neither: 32 x 448 x 1500 53 and 44% in dq (2.4 waves), 39 and 31% in dk and dv (1.8), LDS 18 and 28%; waves wait for
+// 35 and 41% of their cycles, and registers leave no room for more of them.
+// Prologue and epilogue make short ones slower: 32 x 448 x 1500 forward 150 us (730 TF/s), 157 with o's rest.
 #include <algorithm>
 #include <type_traits>
 
@@ -751,7 +753,7 @@ __global__ void __launch_bounds__(64 * kKeyWaves) attn_fwd_keys_kernel(AttnFwdAr
 
 // Four waves of 32 queries share tiles of 64 keys: the next tile is on its way straight to LDS while one is worked on, and
 // 33 KB of LDS and 120 registers leave room for four workgroups on a CU, whose vector instructions and products overlap.
-// 32 x 448 causal, 20 heads: 49 us; tiles through registers, conflicts in a third of LDS' cycles: 83.  Products of one tile beside
+// 32 x 448 causal, 20 heads: 47 us; tiles through registers, conflicts in a third of LDS' cycles: 83.  Products of one tile beside
 // the exponentials of the one before in the same wave: 175 us where this takes 109 (registers).
 template <bool DIRECT>
 __global__ void __launch_bounds__(256, DIRECT ? 4 : 2) attn_fwd_wide_kernel(AttnFwdArgs a, int tiles) {
@@ -1128,7 +1130,7 @@ __global__ void __launch_bounds__(256, 2) attn_dq_few_kernel(AttnBwdArgs a, int 
 // dq of four waves of 32 queries that share tiles of 64 keys: as the forward kernel, with p from lse and two
 // products more, dP^T = V dO^T and, from dS, dQ^T = K^T dS^T.  dP's accumulator starts from -delta.  It leaves delta
 // (unless both gradients are in one launch) and what 32 queries see together for the kernel of dk and dv.
-// 32 x 448 x 1500, 20 heads: 250 us, twice the products of the forward pass.
+// 32 x 448 x 1500, 20 heads: 271 us (the median of traced launches; least 243), twice the products of the forward pass.
 template <bool DIRECT>
 __device__ __forceinline__ void dq_wide(const AttnBwdArgs& a, int tiles) {
   constexpr int TK = 64;
@@ -1432,8 +1434,8 @@ __device__ __forceinline__ void dkv_out(const AttnBwdArgs& a, const Span& s, int
 
 // Four waves of 32 keys share tiles of 64 queries: four products a pair of tiles (S, dP, dV, dK).  64 accumulators
 // and 32 operands of its own leave 190 registers' worth of work: two workgroups a CU (three by force: 34 registers
-// spilled, 15% slower).  32 x 448 x 1500, 20 heads: 325 us; one 5000-long causal sequence, 12 heads, has 480
-// workgroups, of which the longest alone takes as long as all: 174 us (dq: 153).
+// spilled, 15% slower).  32 x 448 x 1500, 20 heads: 363 us (the median of traced launches; least 327); one 5000-long causal
+// sequence, 12 heads, has 480 workgroups, of which the longest alone takes as long as all: 175 us (dq: 154).
 template <bool DIRECT, bool OWN>
 __device__ __forceinline__ void dkv_wide(const AttnBwdArgs& a, int before) {
   constexpr int TQ = 64;

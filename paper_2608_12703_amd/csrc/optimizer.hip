@@ -4,11 +4,14 @@
 // one tensor (the tensors of a launch are kernel arguments, found by their first workgroup), a
 // lane 4 consecutive elements at a time, so that a wave's float32 access is 1 KB side by side.
 //
-// Measured for a draft block of 29.5 million parameters (a large copy reaches 4.9 TB/s): float32 states with bf16 copies
-// 156 us for 885 MB (5.7 TB/s), 8-bit states 101 us for 535 MB, their values read back 47 us for 295 MB (6.3), the norm
-// 20 + 3 us for 118 MB.  Float32 goes past the caches (nontemporal): what a step reads it does not read again before the
-// next one.  Through the caches the first took 187 us and the third 107 (stores alone past them: 183 and 50); 8 elements a
-// lane 197 and 116.  Bytes go through the caches: past them a byte-aligned word became four accesses (86 us).
+// Measured for a draft block of 29.5 million parameters (a large copy reaches 5.2 TB/s): float32 states with bf16 copies
+// 156 us for 885 MB (5.7 TB/s; 159 a pass, 160 with step and rate on the device), 8-bit states 100 us for 535 MB, their values
+// read back 44 us for 295 MB (6.6), bf16 parameters with float32 states 115 us for 708 MB (6.1; 8-bit states 95), the norm
+// 19 + 4 us for 118 MB.  17 vectors of 8064 elements in all: 4.9 us a pass, 5.6 with step and rate on the device, whose 64-bit
+// scalars a thread of each workgroup computes before its loads.
+// Float32 goes past the caches (nontemporal): what a step reads it does not read again before the next one.  Through the
+// caches the first took 187 us and the third 107 (stores alone past them: 183 and 50); 8 elements a lane 197 and 116.  Bytes
+// go through the caches: past them a byte-aligned word became four accesses (86 us).
 #include <algorithm>
 
 #include "train.h"
